@@ -61,7 +61,7 @@ extern "C" {
 
 typedef enum {
   STAMP_OK = 0,
-  STAMP_ERR_INVALID_ARG = 1, /* null pointer, non-positive size, bad enum value            */
+  STAMP_ERR_INVALID_ARG = 1, /* null or misaligned pointer, bad size or enum value         */
   STAMP_ERR_UNSUPPORTED = 2, /* valid request outside the shape / transform rules above    */
   STAMP_ERR_WORKSPACE = 3,   /* ws is null, misaligned or smaller than required            */
   STAMP_ERR_CUDA = 4,        /* a CUDA runtime / driver call failed (launch, tensor map)   */
@@ -252,6 +252,60 @@ int stamp_linear_fused_host(const stamp_config* cfg, const void* X_host, int x_d
                             const float* w_scale, const float* bias, int B, int L, int K, int N, void* Y_host,
                             int y_dtype, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- block-scaled 8-bit floating point layers: tokens that stand alone ----------------------------------
+ *
+ * The sequence transform needs a run of consecutive tokens.  A decode step has single tokens, and an expert layer has
+ * each expert's tokens scattered over the sequence: there is no run to transform.  For them a quantizer that looks at
+ * one token at a time: e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest value 448) with one power-of-two
+ * scale per block of 128 input features, stored as its biased exponent (e8m0: byte b stands for 2^(b - 127), 255 for
+ * NaN).  No counterpart in the paper.
+ *
+ *   scale = 2^e, e the smallest integer >= -126 with max |x| / 2^e <= 448 over the block (a block of zeros: 1)
+ *   code  = x / scale rounded to nearest even.  A block that holds an infinity or a NaN gets scale NaN and NaN codes.
+ *
+ * Activations have a scale per token and block; weights one per block of 128 output channels x 128 features.  With
+ * b(k) = k / 128 (the last block may be short):
+ *
+ *   Y[m, n] = sum_k x[m, k] w[n, k] * x_scale[m, b(k)] * w_scale[n / 128, b(k)]  (+ bias[n]),
+ *   products and sums in fp32 on the tensor cores, rounded once to the output type.
+ *
+ * All tensors are dense and row-major except where a row distance is given.  K (features) is a multiple of 16, N and
+ * the number of rows are any; no workspace.  Zero rows are valid: nothing is launched.  X, code and weight buffers
+ * start on 16-byte boundaries (STAMP_ERR_INVALID_ARG otherwise).
+ */
+
+/* Activations [T, K] -> codes and scales of M rows.
+ *   X      rows of K features, ldx elements from one to the next (ldx >= K; rows start on 16-byte boundaries)   in
+ *   rows   [M] int32: output row m is row rows[m] of X -- the dispatch of tokens to experts, in the same pass.
+ *          NULL: output row m is row m (M <= T).  An index outside [0, T) gives a row of zeros and is reported by
+ *          stamp_last_device_status() as STAMP_ERR_INVALID_ARG                                                  in
+ *   codes  [M, K] e4m3, scale [M, ceil(K / 128)] e8m0                                                           out */
+int stamp_fp8_quantize(const void* X, int x_dtype, long long ldx, const int32_t* rows, int T, int M, int K, void* codes,
+                       void* scale, void* stream);
+
+/* Between the two products of a gated layer: h[m, f] = g / (1 + exp(-g)) * u in fp32, g = X[m, f], u = X[m, F + f],
+ * quantized without being stored.  X [M, 2 F], rows ldx elements apart; codes [M, F], scale [M, ceil(F / 128)]. */
+int stamp_fp8_gated_quantize(const void* X, int x_dtype, long long ldx, int M, int F, void* codes, void* scale,
+                             void* stream);
+
+/* Weights (offline): W [E, N, K] -> codes [E, N, K], scale [E, ceil(N / 128), ceil(K / 128)].  E = 1 for one layer. */
+int stamp_fp8_quantize_weights(const void* W, int w_dtype, int E, int N, int K, void* codes, void* scale, void* stream);
+
+/* The product with one weight matrix.  x [M, K], x_scale [M, ceil(K / 128)], w [N, K], w_scale, bias [N] float or
+ * NULL: as above; Y [M, N] y_dtype (STAMP_F32 or STAMP_BF16). */
+int stamp_fp8_linear(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int M,
+                     int N, int K, void* Y, int y_dtype, void* stream);
+
+/* The product grouped by expert: row m of expert e's run offsets[e] <= m < offsets[e + 1] is multiplied with w[e].
+ *   offsets  [E + 1] int32 on the device, 0 = offsets[0] <= offsets[1] <= ... <= offsets[E] <= M; runs may be empty and
+ *            of any length; rows from offsets[E] on belong to nobody and are not written.  Offsets that break the
+ *            order write nothing and are reported by stamp_last_device_status() as STAMP_ERR_INVALID_ARG    in
+ *   w        [E, N, K], w_scale [E, ceil(N / 128), ceil(K / 128)], bias [E, N] float or NULL; 1 <= E <= 1024   in
+ *   Y        [M, N]                                                                                         out */
+int stamp_fp8_linear_grouped(const void* x, const void* x_scale, const int32_t* offsets, const void* w,
+                             const void* w_scale, const float* bias, int M, int E, int N, int K, void* Y, int y_dtype,
+                             void* stream);
+
 /* ---- parity / debug exports: the intermediate stages, judged separately against the oracle ---- */
 
 /* T = L X in fp32, logical token order.  T [B, L, K] float out. */
@@ -289,8 +343,9 @@ int stamp_debug_fused_operand(const stamp_config* cfg, const void* X, int x_dtyp
                               void* stream);
 
 /* Synchronizes `stream`, then reads and clears the device status word of the current device.
- * *status is STAMP_OK or STAMP_ERR_TIMEOUT (a bounded wait inside a kernel expired; outputs of
- * the calls since the last read are then invalid). */
+ * *status is STAMP_OK, STAMP_ERR_TIMEOUT (a bounded wait inside a kernel expired; outputs of
+ * the calls since the last read are then invalid) or STAMP_ERR_INVALID_ARG (row indices or expert
+ * offsets on the device were out of range: stamp_fp8_quantize, stamp_fp8_linear_grouped). */
 int stamp_last_device_status(void* stream, int* status);
 
 /* Measurement hook: while both events are non-NULL, every tensor-core GEMM launched by the

@@ -26,7 +26,12 @@ EXPORTS = (
     "stamp_last_launch_count", "stamp_status_string", "stamp_inverse_noalloc", "stamp_debug_fused_operand",
     "stamp_measure_i8_mma_issue", "stamp_debug_expire_wait",
     "stamp_dequantize", "stamp_prepare_weights_both",
+    "stamp_fp8_quantize", "stamp_fp8_gated_quantize", "stamp_fp8_quantize_weights", "stamp_fp8_linear",
+    "stamp_fp8_linear_grouped",
 )
+
+FP8_BLOCK = 128                      # features per scale of the block-scaled 8-bit floating point layers
+FP8_CODES, FP8_SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
 class StampConfig(ctypes.Structure):
@@ -65,6 +70,12 @@ def lib() -> ctypes.CDLL:
         _lib.stamp_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
             getattr(_lib, name)
+        p, i, n = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong
+        _lib.stamp_fp8_quantize.argtypes = (p, i, n, p, i, i, i, p, p, p)
+        _lib.stamp_fp8_gated_quantize.argtypes = (p, i, n, i, i, p, p, p)
+        _lib.stamp_fp8_quantize_weights.argtypes = (p, i, i, i, i, p, p, p)
+        _lib.stamp_fp8_linear.argtypes = (p, p, p, p, p, i, i, i, p, i, p)
+        _lib.stamp_fp8_linear_grouped.argtypes = (p, p, p, p, p, p, i, i, i, i, p, i, p)
     return _lib
 
 
@@ -212,6 +223,104 @@ def stamp_linear_fused(cfg: StampConfig, X: torch.Tensor, w: torch.Tensor, w_for
     _check(lib().stamp_linear_fused(ctypes.byref(cfg), _ptr(X), _dtype_code(X), _ptr(w), int(w_format),
                                     _ptr(w_scale), _ptr(bias), B, L, K, N, _ptr(Y), _dtype_code(Y), wp, wb,
                                     _stream()), "stamp_linear_fused")
+    return Y
+
+
+def _fp8_blocks(n: int) -> int:
+    return (n + FP8_BLOCK - 1) // FP8_BLOCK
+
+
+def _fp8_arg(t: torch.Tensor, what: str, shape, dtype) -> int:
+    """Address of a dense CUDA tensor of this shape and type."""
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous CUDA tensor of shape {tuple(shape)} and type {dtype}, "
+                         f"got {tuple(t.shape)}, {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _fp8_rows(X: torch.Tensor) -> int:
+    """Distance of two rows of a CUDA matrix whose rows are dense (a slice of columns of a wider one is fine)."""
+    if X.dim() != 2 or not X.is_cuda or (X.shape[1] > 1 and X.stride(1) != 1):
+        raise ValueError("expected a two-dimensional CUDA tensor with dense rows")
+    return X.stride(0) if X.shape[0] > 1 else X.shape[1]
+
+
+def _fp8_outputs(M: int, K: int, codes, scale, device):
+    shape, blocks = (M, K), (M, _fp8_blocks(K))
+    codes = torch.empty(shape, dtype=FP8_CODES, device=device) if codes is None else codes
+    scale = torch.empty(blocks, dtype=FP8_SCALE, device=device) if scale is None else scale
+    return codes, _fp8_arg(codes, "codes", shape, FP8_CODES), scale, _fp8_arg(scale, "scale", blocks, FP8_SCALE)
+
+
+def stamp_fp8_quantize(X: torch.Tensor, rows: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
+                       scale: Optional[torch.Tensor] = None):
+    """[T, K] activations -> (codes [M, K], scale [M, ceil(K / 128)]); rows [M] int32: which row of X each output row is
+    (M = T and every row itself without it).  codes, scale: buffers to write instead of new ones."""
+    ld = _fp8_rows(X)
+    T, K = X.shape
+    M = T if rows is None else rows.numel()
+    codes, cp, scale, sp = _fp8_outputs(M, K, codes, scale, X.device)
+    rp = None if rows is None else _fp8_arg(rows, "rows", (M,), torch.int32)
+    _check(lib().stamp_fp8_quantize(X.data_ptr(), _dtype_code(X), ld, rp, T, M, K, cp, sp,
+                                    torch.cuda.current_stream().cuda_stream), "stamp_fp8_quantize")
+    return codes, scale
+
+
+def stamp_fp8_gated_quantize(X: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """[M, 2 F] gates and ups -> (codes [M, F], scale [M, ceil(F / 128)]) of silu(gate) * up."""
+    ld = _fp8_rows(X)
+    M, F = X.shape[0], X.shape[1] // 2
+    if X.shape[1] != 2 * F:
+        raise ValueError("expected as many gates as ups")
+    codes, cp, scale, sp = _fp8_outputs(M, F, codes, scale, X.device)
+    _check(lib().stamp_fp8_gated_quantize(X.data_ptr(), _dtype_code(X), ld, M, F, cp, sp,
+                                          torch.cuda.current_stream().cuda_stream), "stamp_fp8_gated_quantize")
+    return codes, scale
+
+
+def stamp_fp8_quantize_weights(W: torch.Tensor):
+    """[N, K] or, for experts, [E, N, K] weights -> codes of that shape and scale [(E,) ceil(N / 128), ceil(K / 128)]."""
+    if W.dim() not in (2, 3):
+        raise ValueError("expected a matrix, or one for each expert")
+    E, (N, K) = W.shape[0] if W.dim() == 3 else 1, W.shape[-2:]
+    codes = torch.empty(W.shape, dtype=FP8_CODES, device=W.device)
+    scale = torch.empty((*W.shape[:-2], _fp8_blocks(N), _fp8_blocks(K)), dtype=FP8_SCALE, device=W.device)
+    _check(lib().stamp_fp8_quantize_weights(_ptr(W), _dtype_code(W), E, N, K, _ptr(codes), _ptr(scale), _stream()),
+           "stamp_fp8_quantize_weights")
+    return codes, scale
+
+
+def stamp_fp8_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                     bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Codes [M, K] times weight codes [N, K] -> [M, N]; bias [N] float32."""
+    M, K = x.shape
+    N = w.shape[0]
+    Y = torch.empty((M, N), dtype=out_dtype, device=x.device) if out is None else out
+    _check(lib().stamp_fp8_linear(
+        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, _fp8_blocks(K)), FP8_SCALE),
+        _fp8_arg(w, "w", (N, K), FP8_CODES), _fp8_arg(w_scale, "w_scale", (_fp8_blocks(N), _fp8_blocks(K)), FP8_SCALE),
+        None if bias is None else _fp8_arg(bias, "bias", (N,), torch.float32), M, N, K,
+        _fp8_arg(Y, "out", (M, N), Y.dtype), _dtype_code(Y), torch.cuda.current_stream().cuda_stream), "stamp_fp8_linear")
+    return Y
+
+
+def stamp_fp8_linear_grouped(x: torch.Tensor, x_scale: torch.Tensor, offsets: torch.Tensor, w: torch.Tensor,
+                             w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Codes [M, K] in expert order times the weight codes [E, N, K] of each row's expert -> [M, N].  offsets [E + 1]
+    int32 on the device: expert e's rows are offsets[e] .. offsets[e + 1] - 1; rows from offsets[E] on are not written.
+    bias [E, N] float32."""
+    M, K = x.shape
+    E, N = w.shape[0], w.shape[1]
+    Y = torch.empty((M, N), dtype=out_dtype, device=x.device) if out is None else out
+    _check(lib().stamp_fp8_linear_grouped(
+        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, _fp8_blocks(K)), FP8_SCALE),
+        _fp8_arg(offsets, "offsets", (E + 1,), torch.int32), _fp8_arg(w, "w", (E, N, K), FP8_CODES),
+        _fp8_arg(w_scale, "w_scale", (E, _fp8_blocks(N), _fp8_blocks(K)), FP8_SCALE),
+        None if bias is None else _fp8_arg(bias, "bias", (E, N), torch.float32), M, E, N, K,
+        _fp8_arg(Y, "out", (M, N), Y.dtype), _dtype_code(Y), torch.cuda.current_stream().cuda_stream),
+        "stamp_fp8_linear_grouped")
     return Y
 
 

@@ -10,6 +10,8 @@
 #include "k_dct.cuh"
 #include "k_dct_tc.cuh"
 #include "k_debug.cuh"
+#include "k_fp8_gemm.cuh"
+#include "k_fp8_quant.cuh"
 #include "k_gemm.cuh"
 #include "k_haar2d.cuh"
 #include "k_generic.cuh"
@@ -1237,6 +1239,49 @@ static int fused_quantize_tiled(const Problem& pb, const CqChoice& cc, const voi
   return run_quantize_haar(pb, cc, X, x_dtype, a8, nullptr, nullptr, x_scale, nullptr, base, wl, st, &tl);
 }
 
+// ------------------------------------------------------------------------------------------
+// Block-scaled 8-bit floating point layers
+// ------------------------------------------------------------------------------------------
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename TIn, bool GATED>
+static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale,
+                            cudaStream_t st) {
+  const long ks = (K + FP8_BLOCK - 1) / FP8_BLOCK;
+  const long groups = M * ks;
+  if (groups > (1L << 31)) return STAMP_ERR_UNSUPPORTED;   // the kernel counts blocks in 32 bits
+  const long ctas = (groups + FP8Q_THREADS / 8 - 1) / (FP8Q_THREADS / 8);
+  const long most = 8L * sm_count();   // the threads that fit the machine; the rest by striding
+  if (launch_pdl(k_fp8_quant<TIn, GATED>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(FP8Q_THREADS), 0, st,
+                 static_cast<const TIn*>(X), ld, rows, T, K, (unsigned)ks, (unsigned)groups, static_cast<uint8_t*>(codes),
+                 static_cast<uint8_t*>(scale)) != cudaSuccess) {
+    cudaGetLastError();
+    return STAMP_ERR_CUDA;
+  }
+  STAMP_CHECK_LAUNCH();
+  return STAMP_OK;
+}
+
+static int run_fp8_gemm(const Fp8GemmParams& p, int y_dtype, cudaStream_t st) {
+  const dim3 grid((unsigned)((p.N + 31) / 32), (unsigned)(p.M < 8 * 4096 ? (p.M + 7) / 8 : 4096));
+  if (y_dtype == STAMP_BF16)
+    k_fp8_product<__nv_bfloat16><<<grid, 256, 0, st>>>(p);
+  else
+    k_fp8_product<float><<<grid, 256, 0, st>>>(p);
+  STAMP_CHECK_LAUNCH();
+  return STAMP_OK;
+}
+
+// Arguments common to both products.
+static int check_fp8_product(const Fp8GemmParams& p, int y_dtype) {
+  if (p.M < 0 || p.E <= 0 || p.N <= 0 || p.K <= 0 || !dtype_ok(y_dtype)) return STAMP_ERR_INVALID_ARG;
+  if (p.K % 16 != 0 || p.E > FP8_MAX_EXPERTS || (long)p.E * p.N > (1L << 31) - 512 || p.M > (1 << 30)) return STAMP_ERR_UNSUPPORTED;
+  if (!p.w || !p.w_scale || !aligned16(p.w)) return STAMP_ERR_INVALID_ARG;
+  if (p.M > 0 && (!p.x || !p.x_scale || !p.y || !aligned16(p.x))) return STAMP_ERR_INVALID_ARG;
+  if (p.M > 0 && (reinterpret_cast<uintptr_t>(p.y) & (y_dtype == STAMP_BF16 ? 1 : 3)) != 0) return STAMP_ERR_INVALID_ARG;
+  return STAMP_OK;
+}
+
 }  // namespace stamp
 
 // ============================================================================================
@@ -1707,6 +1752,87 @@ int stamp_debug_expire_wait(long long limit_cycles, void* stream) {
   k_expire_wait<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(limit_cycles);
   STAMP_CHECK_LAUNCH();
   return STAMP_OK;
+}
+
+int stamp_fp8_quantize(const void* X, int x_dtype, long long ldx, const int32_t* rows, int T, int M, int K, void* codes,
+                       void* scale, void* stream) {
+  t_launches = 0;
+  if (T < 0 || M < 0 || K <= 0 || ldx < K || !dtype_ok(x_dtype)) return STAMP_ERR_INVALID_ARG;
+  if (!rows && M > T) return STAMP_ERR_INVALID_ARG;
+  if (K % 16 != 0) return STAMP_ERR_UNSUPPORTED;
+  if (M == 0) return STAMP_OK;
+  if (!X || !codes || !scale || !aligned16(X) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
+  if (ldx % (x_dtype == STAMP_BF16 ? 8 : 4) != 0) return STAMP_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (x_dtype == STAMP_BF16) return launch_fp8_quant<__nv_bfloat16, false>(X, ldx, rows, T, M, K, codes, scale, st);
+  return launch_fp8_quant<float, false>(X, ldx, rows, T, M, K, codes, scale, st);
+}
+
+int stamp_fp8_gated_quantize(const void* X, int x_dtype, long long ldx, int M, int F, void* codes, void* scale,
+                             void* stream) {
+  t_launches = 0;
+  if (M < 0 || F <= 0 || ldx < 2LL * F || !dtype_ok(x_dtype)) return STAMP_ERR_INVALID_ARG;
+  if (F % 16 != 0) return STAMP_ERR_UNSUPPORTED;
+  if (M == 0) return STAMP_OK;
+  if (!X || !codes || !scale || !aligned16(X) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
+  if (ldx % (x_dtype == STAMP_BF16 ? 8 : 4) != 0) return STAMP_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (x_dtype == STAMP_BF16) return launch_fp8_quant<__nv_bfloat16, true>(X, ldx, nullptr, M, M, F, codes, scale, st);
+  return launch_fp8_quant<float, true>(X, ldx, nullptr, M, M, F, codes, scale, st);
+}
+
+int stamp_fp8_quantize_weights(const void* W, int w_dtype, int E, int N, int K, void* codes, void* scale, void* stream) {
+  t_launches = 0;
+  if (!W || !codes || !scale || E <= 0 || N <= 0 || K <= 0 || !dtype_ok(w_dtype)) return STAMP_ERR_INVALID_ARG;
+  const long nb = ((long)N + FP8_BLOCK - 1) / FP8_BLOCK;
+  if (K % 16 != 0 || nb > 65535 || E > 65535) return STAMP_ERR_UNSUPPORTED;
+  if (!aligned16(W) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
+  const dim3 grid((unsigned)((K + FP8_BLOCK - 1) / FP8_BLOCK), (unsigned)nb, (unsigned)E);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (w_dtype == STAMP_BF16)
+    k_fp8_quant_weights<__nv_bfloat16><<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(W), N, K,
+                                                             static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale));
+  else
+    k_fp8_quant_weights<float><<<grid, 256, 0, st>>>(static_cast<const float*>(W), N, K, static_cast<uint8_t*>(codes),
+                                                     static_cast<uint8_t*>(scale));
+  STAMP_CHECK_LAUNCH();
+  return STAMP_OK;
+}
+
+static Fp8GemmParams fp8_params(const void* x, const void* x_scale, const int32_t* offsets, const void* w, const void* w_scale,
+                                const float* bias, int M, int E, int N, int K, void* Y) {
+  Fp8GemmParams p{};
+  p.x = static_cast<const uint8_t*>(x);
+  p.x_scale = static_cast<const uint8_t*>(x_scale);
+  p.offsets = offsets;
+  p.w = static_cast<const uint8_t*>(w);
+  p.w_scale = static_cast<const uint8_t*>(w_scale);
+  p.bias = bias;
+  p.y = Y;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  p.E = E;
+  p.ks = (int)(((long)K + FP8_BLOCK - 1) / FP8_BLOCK);
+  return p;
+}
+
+int stamp_fp8_linear(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int M,
+                     int N, int K, void* Y, int y_dtype, void* stream) {
+  t_launches = 0;
+  const Fp8GemmParams p = fp8_params(x, x_scale, nullptr, w, w_scale, bias, M, 1, N, K, Y);
+  if (int rc = check_fp8_product(p, y_dtype)) return rc;
+  return M == 0 ? STAMP_OK : run_fp8_gemm(p, y_dtype, static_cast<cudaStream_t>(stream));
+}
+
+int stamp_fp8_linear_grouped(const void* x, const void* x_scale, const int32_t* offsets, const void* w,
+                             const void* w_scale, const float* bias, int M, int E, int N, int K, void* Y, int y_dtype,
+                             void* stream) {
+  t_launches = 0;
+  const Fp8GemmParams p = fp8_params(x, x_scale, offsets, w, w_scale, bias, M, E, N, K, Y);
+  if (int rc = check_fp8_product(p, y_dtype)) return rc;
+  if (!offsets) return STAMP_ERR_INVALID_ARG;
+  return M == 0 ? STAMP_OK : run_fp8_gemm(p, y_dtype, static_cast<cudaStream_t>(stream));
 }
 
 int stamp_last_launch_count(void) { return t_launches; }
