@@ -1,10 +1,30 @@
-// Product of block-scaled e4m3 codes, with one weight matrix or with the weights of one expert per run of rows:
+// Product of block-scaled e4m3 codes on the 5th-generation tensor cores, with one weight matrix or with the weights of
+// one expert per run of rows:
 //   y[m, n] = sum_b sx[m, b] sw[n / 128, b] sum_{k in b} x[m, k] w[n, k]  (+ bias[n])
-// Plain CUDA-core form: one thread per output, sixteen codes per load, a block's products summed in fp32 and scaled
-// once per block.
+//
+// The power-of-two scales go into the instruction (tcgen05.mma kind::mxf8f6f4.block_scale): the sum runs over all of K
+// in one fp32 accumulator and nothing has to be drained and scaled per block.  The instruction takes a scale for every 32
+// features; a block of 128 uses the same byte of the scale words for its four instructions, so 512 features need one
+// 32-bit word per row, four blocks' bytes.
+//
+// Operand roles as in k_gemm.cuh: 128 output channels are the MMA A operand (TMEM lanes), tokens the B operand
+// (columns).  The extent in tokens is a field of the instruction, in steps of 16: a tile with few rows -- a decode
+// step, the end of an expert's run -- costs what its rows cost, and no expert's rows have to be padded.
+//
+//   warp 0     TMA producer: 128-byte-swizzled K-major tiles of both operands into a ring of FP8G_STAGES
+//   warp 1     allocates TMEM; one elected thread copies the scale words to TMEM (tcgen05.cp) and issues the MMAs
+//   warp 2     scale producer: gathers the scale words of 512 features of the tile's tokens and channels into the
+//              order tcgen05.cp wants (row i of 32: rows i, i + 32, i + 64, i + 96), one step ahead of the MMAs
+//   warps 4-11 epilogue: drain the finished accumulator while the next tile fills the other
+// Every wait is bounded; when one expires the CTA raises the device status word, unwinds and frees its TMEM.
+//
+// PAIR = false: tiles of 128 channels x up to 128 tokens, one CTA each.  For few tiles the sum can be split over a
+// cluster of 2, 4 or 8 CTAs (parameter `split`; one tile per cluster): each leaves its partial tile in its own shared
+// memory, and each adds up a share of the tokens over all of them in rank order -- no atomics, a fixed order.
+// PAIR = true: CTA pairs (cta_group::2), tiles of 256 channels x up to 256 tokens.  Two accumulators of 256 columns and
+// the scales do not fit the 512 columns: the accumulators overlap in 32 columns, which the epilogue drains first; the
+// next tile starts when they are free.
 #pragma once
-#include <cuda_fp8.h>
-
 #include "common.cuh"
 #include "k_fp8_quant.cuh"
 #include "ptx.cuh"
@@ -12,6 +32,12 @@
 namespace stamp {
 
 constexpr int FP8_MAX_EXPERTS = 1024;
+constexpr int FP8G_BM = 128, FP8G_BK = 128, FP8G_STAGES = 6;
+constexpr int FP8G_X_ROWS = 128;                       // token rows a CTA stages at most
+constexpr int FP8G_X_SMALL = 16;                       // rows of the small token box: up to 64 rows are loaded with it
+constexpr int FP8G_EPI_WARPS = 8;
+constexpr int FP8G_THREADS = 128 + 32 * FP8G_EPI_WARPS;
+constexpr long long FP8G_WAIT_LIMIT = 4000000000LL;    // SM clocks (~2 s) before a wait gives up
 
 struct Fp8GemmParams {
   const uint8_t* x;        // [M, K]
@@ -22,61 +48,466 @@ struct Fp8GemmParams {
   const float* bias;       // [E, N] or nullptr
   void* y;                 // [M, N] float or bf16
   int M, N, K, E, ks;
+  int x_words;             // x_scale rows start on 4-byte boundaries
+  int split;               // CTAs that share a tile's sum (PAIR: 1)
+  int band;                // channel tiles per raster band
 };
 
-__device__ __forceinline__ float e8m0_value(uint8_t b) {
-  return b == 255 ? __uint_as_float(0x7FC00000u) : b == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(static_cast<uint32_t>(b) << 23);
+template <bool PAIR>
+struct Fp8Smem {
+  static constexpr int BN = PAIR ? 256 : 128;
+  static constexpr int W_BYTES = FP8G_BM * FP8G_BK;
+  static constexpr int STAGE_BYTES = W_BYTES + FP8G_X_ROWS * FP8G_BK;
+  static constexpr int SF_SLOT = 512 + BN * 4;         // scale words of 512 features: channels, then tokens
+  static constexpr int SF_OFFSET = FP8G_STAGES * STAGE_BYTES;
+  static constexpr int BAR_OFFSET = SF_OFFSET + 2 * SF_SLOT;
+  static constexpr int NUM_BARS = 2 * FP8G_STAGES + 8; // full, empty, sffull[2], sfempty[2], tfull[2], tempty[2]
+  static constexpr int TAB_OFFSET = BAR_OFFSET + NUM_BARS * 8 + 16;
+  static constexpr int DYN_BYTES = TAB_OFFSET + 2 * (FP8_MAX_EXPERTS + 1) * 4 + 1024;
+  // tensor memory: second accumulator, then the two buffers of scale columns (4 for channels, BN / 32 for tokens)
+  static constexpr int ACC1 = PAIR ? 224 : 128;
+  static constexpr int SF_COL = PAIR ? 480 : 256;
+  static constexpr int SF_COLS = 4 + BN / 32;
+};
+
+// One unit of work: up to BN rows of one expert's run times 128 (PAIR: 256) output channels.
+struct Fp8Tile {
+  int expert, ch_tile, row0, rows, n;   // n: rows rounded up to what an instruction takes
+};
+template <bool PAIR>
+__device__ __forceinline__ Fp8Tile fp8_tile(const Fp8GemmParams& p, const int* tile_start, const int* row_start, int experts, int tile,
+                                            int ch_tiles, int tok_tiles) {
+  // bands of `band` channel tiles; inside one, channel tiles vary fastest: CTAs running at the same time share token
+  // tiles, and the band's weights stay in L2 over an expert's token tiles
+  const int per_band = p.band * tok_tiles;
+  const int b = tile / per_band, rem = tile - b * per_band;
+  const int first = b * p.band, height = min(p.band, ch_tiles - first);
+  const int tt = rem / height;
+  Fp8Tile t;
+  t.ch_tile = first + (rem - tt * height);
+  int lo = 0, hi = experts;             // the expert whose tiles hold tt (empty runs have none)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (tile_start[mid] <= tt) lo = mid; else hi = mid;
+  }
+  t.expert = lo;
+  t.row0 = row_start[lo] + (tt - tile_start[lo]) * Fp8Smem<PAIR>::BN;
+  t.rows = min(Fp8Smem<PAIR>::BN, row_start[lo + 1] - t.row0);
+  constexpr int STEP = PAIR ? 32 : 16;
+  t.n = (t.rows + STEP - 1) / STEP * STEP;
+  return t;
 }
-__device__ __forceinline__ void e4m3x4_values(uint32_t u, float (&v)[4]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(u >> (16 * i)), __NV_E4M3);
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    v[2 * i] = f.x;
-    v[2 * i + 1] = f.y;
+
+// Two adjacent channels of one token.
+__device__ __forceinline__ void fp8_store2(float* y, float a, float b, bool both, bool vec) {
+  if (vec && both) {
+    *reinterpret_cast<float2*>(y) = make_float2(a, b);
+  } else {
+    y[0] = a;
+    if (both) y[1] = b;
+  }
+}
+__device__ __forceinline__ void fp8_store2(__nv_bfloat16* y, float a, float b, bool both, bool vec) {
+  if (vec && both) {
+    *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(a, b);
+  } else {
+    y[0] = __float2bfloat16_rn(a);
+    if (both) y[1] = __float2bfloat16_rn(b);
   }
 }
 
-template <typename TOut>
-__global__ void __launch_bounds__(256) k_fp8_product(Fp8GemmParams p) {
-  const int n = blockIdx.x * 32 + (threadIdx.x & 31);
-  for (long m = blockIdx.y * 8 + (threadIdx.x >> 5); m < p.M; m += gridDim.y * 8) {
-    int e = 0;
-    if (p.offsets) {
-      if (p.offsets[0] != 0 || m >= p.offsets[p.E]) continue;
-      int lo = 0, hi = p.E;   // the expert whose run holds row m
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.offsets[mid] <= m) lo = mid; else hi = mid;
-      }
-      e = lo;
+template <bool PAIR, typename TOut>
+__global__ void __launch_bounds__(FP8G_THREADS, 1)
+    k_fp8_gemm(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
+               const __grid_constant__ CUtensorMap tmap_x_small, Fp8GemmParams p) {
+  using SM = Fp8Smem<PAIR>;
+  constexpr int BN = SM::BN;
+  extern __shared__ uint8_t fp8g_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(fp8g_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + SM::BAR_OFFSET);
+  uint64_t* empty = full + FP8G_STAGES;
+  uint64_t* sffull = empty + FP8G_STAGES;
+  uint64_t* sfempty = sffull + 2;
+  uint64_t* tfull = sfempty + 2;
+  uint64_t* tempty = tfull + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  volatile uint32_t* abort_word = tmem_slot + 1;
+  int* tile_start = reinterpret_cast<int*>(smem + SM::TAB_OFFSET);
+  int* row_start = tile_start + FP8_MAX_EXPERTS + 1;
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const bool clustered = PAIR || p.split > 1;
+  const int rank = clustered ? static_cast<int>(ptx::cluster_ctarank()) : 0;
+  const int per_tile = PAIR ? 2 : p.split;             // CTAs of a tile
+  constexpr int CH_PER_TILE = PAIR ? 2 * FP8G_BM : FP8G_BM;
+  const int ch_tiles = (p.N + CH_PER_TILE - 1) / CH_PER_TILE;
+  // the part of K this CTA sums, in steps of 512 features (one scale word)
+  const int num_kb = (p.K + FP8G_BK - 1) / FP8G_BK;
+  const int steps = (num_kb + 3) / 4;
+  const int split_rank = PAIR ? 0 : rank;
+  const int step0 = steps * split_rank / p.split, step1 = steps * (split_rank + 1) / p.split;
+  const int kb0 = step0 * 4, kb1 = min(step1 * 4, num_kb);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < FP8G_STAGES; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
     }
-    if (n >= p.N) continue;
-    const uint4* xr = reinterpret_cast<const uint4*>(p.x + m * p.K);
-    const uint4* wr = reinterpret_cast<const uint4*>(p.w + (static_cast<long>(e) * p.N + n) * p.K);
-    const uint8_t* ws = p.w_scale + (static_cast<long>(e) * ((p.N + 127) / 128) + n / 128) * p.ks;
-    float y = 0.f;
-    for (int b = 0; b < p.ks; ++b) {
-      float part = 0.f;
-      for (int c = b * 8; c < min((b + 1) * 8, p.K / 16); ++c) {
-        const uint4 a = xr[c], w = wr[c];
-        const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, ww[4] = {w.x, w.y, w.z, w.w};
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(&sffull[a], PAIR ? 2 : 1);
+      ptx::mbar_init(&sfempty[a], 1);
+      ptx::mbar_init(&tfull[a], 1);
+      ptx::mbar_init(&tempty[a], PAIR ? 2 * FP8G_EPI_WARPS : FP8G_EPI_WARPS);
+    }
+    *abort_word = 0;
+    ptx::fence_mbar_init();
+    ptx::prefetch_tensormap(&tmap_w);
+    ptx::prefetch_tensormap(&tmap_x);
+    ptx::prefetch_tensormap(&tmap_x_small);
+  }
+  if (warp == 1) {
+    if constexpr (PAIR) {
+      ptx::tmem_alloc_pair(tmem_slot, 512);
+      ptx::tmem_relinquish_pair();
+    } else {
+      ptx::tmem_alloc(tmem_slot, 512);
+      ptx::tmem_relinquish();
+    }
+  }
+  ptx::grid_dependency_wait();   // codes, scales and offsets come from the kernels launched before
+  ptx::grid_launch_dependents();
+
+  // Where every expert's rows and tiles start.  Offsets that are out of order or past the rows: no tile at all.
+  bool bad = false;
+  if (p.offsets) {
+    for (int e = threadIdx.x; e <= p.E; e += FP8G_THREADS) {
+      const int o = __ldg(p.offsets + e);
+      row_start[e] = o;
+      bad |= o < 0 || o > p.M || (e == 0 ? o != 0 : o < __ldg(p.offsets + e - 1));
+    }
+  } else if (threadIdx.x == 0) {
+    row_start[0] = 0;
+    row_start[1] = p.M;
+  }
+  bad = __syncthreads_or(bad);
+  if (bad && threadIdx.x == 0) raise_device_status(STAMP_ERR_INVALID_ARG);
+  if (warp == 3) {
+    int sum = 0;
+    for (int e0 = 0; e0 < p.E; e0 += 32) {
+      const int e = e0 + lane;
+      int t = (e < p.E && !bad) ? (row_start[e + 1] - row_start[e] + BN - 1) / BN : 0;
+      const int own = t;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float av[4], wv[4];
-          e4m3x4_values(aw[i], av);
-          e4m3x4_values(ww[i], wv);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) part = fmaf(av[j], wv[j], part);
+      for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, t, d);
+        if (lane >= d) t += v;
+      }
+      if (e < p.E) tile_start[e] = sum + t - own;
+      sum += __shfl_sync(0xffffffffu, t, 31);
+    }
+    if (lane == 0) tile_start[p.E] = sum;
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (clustered) ptx::cluster_sync();   // all barriers of the cluster are initialised before anyone signals another's
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int tok_tiles = tile_start[p.E];
+  const int num_tiles = ch_tiles * tok_tiles;
+  const int tile0 = blockIdx.x / per_tile, tile_step = gridDim.x / per_tile;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer
+    if (ptx::elect_one()) {
+      int stage = 0;
+      uint32_t phase = 0, armed = 0, armed_parity = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+        const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+        const int mine = PAIR ? t.n / 2 : t.n;              // token rows this CTA stages
+        const int xrow = t.row0 + (PAIR ? rank * mine : 0);
+        const int wrow = t.expert * p.N + t.ch_tile * CH_PER_TILE + (PAIR ? rank * FP8G_BM : 0);
+        const bool small = mine <= 64;
+        const uint32_t bytes = SM::W_BYTES + (small ? mine : FP8G_X_ROWS) * FP8G_BK;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!ptx::mbar_wait_bounded(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT)) {
+            ok = false;
+            break;
+          }
+          uint8_t* ws = smem + stage * SM::STAGE_BYTES;
+          uint8_t* xs = ws + SM::W_BYTES;
+          if constexpr (PAIR) {
+            // all copies of the pair are counted on the even CTA's barrier
+            const uint32_t bar0 = ptx::mapa(ptx::smem_u32(&full[stage]), 0u);
+            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * bytes);
+            ptx::tma_load_2d_pair(ws, &tmap_w, bar0, kb * FP8G_BK, wrow);
+            if (small) {
+              for (int r = 0; r < mine; r += FP8G_X_SMALL)
+                ptx::tma_load_2d_pair(xs + r * FP8G_BK, &tmap_x_small, bar0, kb * FP8G_BK, xrow + r);
+            } else {
+              ptx::tma_load_2d_pair(xs, &tmap_x, bar0, kb * FP8G_BK, xrow);
+            }
+          } else {
+            ptx::mbar_arrive_expect_tx(&full[stage], bytes);
+            ptx::tma_load_2d(ws, &tmap_w, &full[stage], kb * FP8G_BK, wrow);
+            if (small) {
+              for (int r = 0; r < mine; r += FP8G_X_SMALL)
+                ptx::tma_load_2d(xs + r * FP8G_BK, &tmap_x_small, &full[stage], kb * FP8G_BK, xrow + r);
+            } else {
+              ptx::tma_load_2d(xs, &tmap_x, &full[stage], kb * FP8G_BK, xrow);
+            }
+          }
+          armed |= 1u << stage;
+          armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
+          if (++stage == FP8G_STAGES) {
+            stage = 0;
+            phase ^= 1u;
+          }
         }
       }
-      y = fmaf(part * e8m0_value(p.x_scale[m * p.ks + b]), e8m0_value(ws[b]), y);
+      if (!ok) {
+        *abort_word = 1;
+        raise_device_status(STAMP_ERR_TIMEOUT);
+        for (int s = 0; s < FP8G_STAGES; ++s)   // let the copies in flight land before the shared memory goes away
+          if (armed & (1u << s)) {
+            const long long t0 = clock64();
+            // (the odd CTA of a pair has no barrier of its own to watch: it just gives its copies the time)
+            while (((PAIR && rank != 0) || !ptx::mbar_try_wait(&full[s], (armed_parity >> s) & 1u)) && clock64() - t0 < 2000000LL) {
+            }
+          }
+      }
     }
-    if (p.bias) y += p.bias[static_cast<long>(e) * p.N + n];
-    if constexpr (sizeof(TOut) == 2)
-      static_cast<__nv_bfloat16*>(p.y)[m * p.N + n] = __float2bfloat16_rn(y);
-    else
-      static_cast<float*>(p.y)[m * p.N + n] = y;
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer (PAIR: the even CTA's, for both)
+    if ((!PAIR || rank == 0) && ptx::elect_one()) {
+      constexpr uint32_t idesc0 = ptx::make_mxf8_idesc(PAIR ? 2 * FP8G_BM : FP8G_BM);
+      int stage = 0, it = 0;
+      uint32_t phase = 0, scount = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++it) {
+        const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+        const int a = it & 1;
+        // PAIR: the columns shared with the previous tile's accumulator are drained (which implies that everything of
+        // the tile before it is); otherwise the tile that had this accumulator is
+        const bool free_acc = PAIR ? ptx::mbar_wait_bounded_cluster(&tempty[0], (it - 1) & 1, abort_word, FP8G_WAIT_LIMIT)
+                                   : ptx::mbar_wait_bounded(&tempty[a], ((it >> 1) & 1) ^ 1, abort_word, FP8G_WAIT_LIMIT);
+        if (!free_acc) {
+          ok = false;
+          break;
+        }
+        ptx::tc_fence_after();
+        const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(a * SM::ACC1);
+        for (int s = step0; s < step1 && ok; ++s, ++scount) {
+          // The scale words of this step.  Their slot was refilled only after the MMAs that used the slot's previous
+          // contents -- and the same tensor-memory columns -- had finished.
+          const uint32_t slot = scount & 1u;
+          const bool sf = PAIR ? ptx::mbar_wait_bounded_cluster(&sffull[slot], (scount >> 1) & 1u, abort_word, FP8G_WAIT_LIMIT)
+                               : ptx::mbar_wait_bounded(&sffull[slot], (scount >> 1) & 1u, abort_word, FP8G_WAIT_LIMIT);
+          if (!sf) {
+            ok = false;
+            break;
+          }
+          ptx::tc_fence_after();
+          const uint32_t sfs = ptx::smem_u32(smem + SM::SF_OFFSET + slot * SM::SF_SLOT);
+          const uint32_t sfa = tmem_base + SM::SF_COL + slot * SM::SF_COLS, sfb = sfa + 4;
+          ptx::tmem_copy_scales<PAIR>(sfa, ptx::make_rows16_desc(sfs));
+          for (int h = 0; h * 128 < t.n; ++h)
+            ptx::tmem_copy_scales<PAIR>(sfb + 4 * h, ptx::make_rows16_desc(sfs + 512 + 512 * h));
+          const int last = min(4 * s + 4, num_kb);
+          for (int kb = 4 * s; kb < last; ++kb) {
+            if (!ptx::mbar_wait_bounded(&full[stage], phase, abort_word, FP8G_WAIT_LIMIT)) {
+              ok = false;
+              break;
+            }
+            ptx::tc_fence_after();
+            const uint32_t wa = ptx::smem_u32(smem + stage * SM::STAGE_BYTES);
+            const uint32_t xa = wa + SM::W_BYTES;
+            const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, t.n, static_cast<uint32_t>(kb & 3));
+#pragma unroll
+            for (int k = 0; k < FP8G_BK / 32; ++k)
+              ptx::mma_mxf8_ss<PAIR>(tmem_d, ptx::make_kmajor_sw128_desc(wa + k * 32), ptx::make_kmajor_sw128_desc(xa + k * 32),
+                                     idesc, sfa, sfb, (kb > kb0 || k > 0) ? 1u : 0u);
+            if constexpr (PAIR) ptx::tc_commit_pair(&empty[stage], 3); else ptx::tc_commit(&empty[stage]);
+            if (++stage == FP8G_STAGES) {
+              stage = 0;
+              phase ^= 1u;
+            }
+          }
+          if (ok) {
+            if constexpr (PAIR) ptx::tc_commit_pair(&sfempty[slot], 3); else ptx::tc_commit(&sfempty[slot]);
+          }
+        }
+        if (ok) {
+          if constexpr (PAIR) ptx::tc_commit_pair(&tfull[a], 3); else ptx::tc_commit(&tfull[a]);
+        }
+      }
+      if (!ok) {
+        *abort_word = 1;
+        raise_device_status(STAMP_ERR_TIMEOUT);
+      }
+    }
+  } else if (warp == 2) {
+    // ------------------------------------------------------------------ scale producer
+    const uint32_t sffull_bar0 = PAIR ? ptx::mapa(ptx::smem_u32(&sffull[0]), 0u) : 0u;
+    const int ch_blocks = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
+    uint32_t scount = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+      const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+      // a CTA's 128 channels are one block of the weights' scales (a tile past the last channel takes the last block's)
+      const int cb = min(t.ch_tile * (CH_PER_TILE / FP8_BLOCK) + (PAIR ? rank : 0), ch_blocks - 1);
+      const uint8_t* wsc = p.w_scale + (static_cast<long>(t.expert) * ch_blocks + cb) * p.ks;
+      const uint8_t* xsc = p.x_scale + static_cast<long>(t.row0) * p.ks;
+      for (int s = step0; s < step1; ++s, ++scount) {
+        const int k = 4 * s, nk = min(4, p.ks - k);
+        uint32_t ww = 0x7F7F7F7Fu, xw[BN / 32];
+        for (int i = 0; i < nk; ++i) ww = (ww & ~(255u << (8 * i))) | (static_cast<uint32_t>(__ldg(wsc + k + i)) << (8 * i));
+#pragma unroll
+        for (int q = 0; q < BN / 32; ++q) {
+          const int r = q * 32 + lane;
+          xw[q] = 0x7F7F7F7Fu;      // rows past the run: any finite scale, their columns are not stored
+          if (r < t.rows) {
+            const uint8_t* ptr = xsc + static_cast<long>(r) * p.ks + k;
+            if (p.x_words) {
+              xw[q] = __ldg(reinterpret_cast<const uint32_t*>(ptr));
+            } else {
+              for (int i = 0; i < nk; ++i) xw[q] = (xw[q] & ~(255u << (8 * i))) | (static_cast<uint32_t>(__ldg(ptr + i)) << (8 * i));
+            }
+          }
+        }
+        const uint32_t slot = scount & 1u;
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&sfempty[slot], ((scount >> 1) & 1u) ^ 1u, abort_word, FP8G_WAIT_LIMIT))) {
+          ok = false;
+          break;
+        }
+        uint8_t* dst = smem + SM::SF_OFFSET + slot * SM::SF_SLOT + lane * 16;
+        *reinterpret_cast<uint4*>(dst) = make_uint4(ww, ww, ww, ww);
+#pragma unroll
+        for (int h = 0; h < BN / 128; ++h)
+          *reinterpret_cast<uint4*>(dst + 512 + 512 * h) = make_uint4(xw[4 * h], xw[4 * h + 1], xw[4 * h + 2], xw[4 * h + 3]);
+        ptx::fence_proxy_async_smem();   // tcgen05.cp reads them through the async proxy
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) ptx::mbar_arrive_cluster(sffull_bar0 + slot * 8u); else ptx::mbar_arrive(&sffull[slot]);
+        }
+      }
+    }
+    if (!ok) {
+      *abort_word = 1;
+      if (lane == 0) raise_device_status(STAMP_ERR_TIMEOUT);
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------------ epilogue warps
+    const int quarter = warp & 3;          // TMEM lanes this warp may touch
+    const int half = (warp - 4) >> 2;      // which half of the column chunks it takes
+    const int row = quarter * 32 + lane;
+    const uint32_t tempty_bar0 = PAIR ? ptx::mapa(ptx::smem_u32(&tempty[0]), 0u) : 0u;
+    const bool vec = (reinterpret_cast<uintptr_t>(p.y) & (2 * sizeof(TOut) - 1)) == 0 && (p.N & 1) == 0;
+    TOut* const y = static_cast<TOut*>(p.y);
+    int it = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++it) {
+      const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+      const int a = it & 1;
+      const int ch = (PAIR ? 2 * t.ch_tile + rank : t.ch_tile) * FP8G_BM + row;
+      float bias = 0.f;
+      if (p.bias && ch < p.N) bias = __ldg(p.bias + static_cast<long>(t.expert) * p.N + ch);
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
+        ok = false;
+        break;
+      }
+      ptx::tc_fence_after();
+      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(a * SM::ACC1);
+      const int chunks = (t.n + 31) / 32;
+      bool released = false;
+      auto release = [&]() {
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) ptx::mbar_arrive_cluster(tempty_bar0); else ptx::mbar_arrive(&tempty[a]);
+        }
+        released = true;
+      };
+      if (PAIR && half != 0) release();   // the shared columns are in the other warps' first chunk
+      for (int i = half; i < chunks; i += 2) {
+        // the chunk that overlaps the other accumulator first: the last of the first one, the first of the second
+        const int c = (PAIR && a == 0) ? chunks - 1 - i : i;
+        uint32_t r[32];
+        ptx::tmem_ld_32x32b_x32(taddr + 32 * c, r);
+        ptx::tmem_ld_wait();
+        if (PAIR ? i == 0 : i + 2 >= chunks) release();
+        if (!PAIR && p.split > 1) {
+          // this CTA's part of the sum, [token][channel], in the ring that nothing uses any more
+          float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) part[(32 * c + j) * FP8G_BM + row] = __uint_as_float(r[j]);
+          continue;
+        }
+        const int left = t.rows - 32 * c;
+        if constexpr (sizeof(TOut) == 4) {
+          if (ch < p.N) {
+            TOut* out = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j < left) out[static_cast<long>(j) * p.N] = __uint_as_float(r[j]) + bias;
+          }
+        } else {
+          // neighbouring lanes swap halves of a token pair: either then holds two adjacent channels of one token
+          const int odd = lane & 1;
+          const int ch2 = ch & ~1;
+          TOut* out = y + static_cast<long>(t.row0 + 32 * c + odd) * p.N + ch2;
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const float v0 = __uint_as_float(r[j]) + bias, v1 = __uint_as_float(r[j + 1]) + bias;
+            const float other = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 1);
+            if (j + odd < left && ch2 < p.N)
+              fp8_store2(out + static_cast<long>(j) * p.N, odd ? other : v0, odd ? v1 : other, ch2 + 1 < p.N, vec);
+          }
+        }
+      }
+      if (!released) release();
+    }
+    if (!ok) {
+      *abort_word = 1;
+      if (lane == 0) raise_device_status(STAMP_ERR_TIMEOUT);
+    }
+  }
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  // Nobody lets go of its shared and tensor memory while a CTA of the cluster may still signal into it.
+  if (clustered) ptx::cluster_sync();
+  if (!PAIR && p.split > 1) {
+    // every CTA adds up every split-th token of the tile over the cluster's partial sums, in rank order
+    if (tile0 < num_tiles && *abort_word == 0) {
+      const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile0, ch_tiles, tok_tiles);
+      const uint32_t part = ptx::smem_u32(smem);
+      const bool vec = (reinterpret_cast<uintptr_t>(p.y) & (2 * sizeof(TOut) - 1)) == 0 && (p.N & 1) == 0;
+      for (int i = threadIdx.x; i < (t.rows - rank + p.split - 1) / p.split * 64; i += FP8G_THREADS) {
+        const int tok = rank + (i >> 6) * p.split, c2 = 2 * (i & 63);
+        const int ch = t.ch_tile * FP8G_BM + c2;
+        float2 sum = make_float2(0.f, 0.f);
+        for (int s = 0; s < p.split; ++s) {
+          const float2 v = ptx::ld_dsmem_f2(ptx::mapa(part, static_cast<uint32_t>(s)) + (tok * FP8G_BM + c2) * 4);
+          sum.x += v.x;
+          sum.y += v.y;
+        }
+        if (ch < p.N) {
+          if (p.bias) {
+            const float* b = p.bias + static_cast<long>(t.expert) * p.N + ch;
+            sum.x += __ldg(b);
+            if (ch + 1 < p.N) sum.y += __ldg(b + 1);
+          }
+          fp8_store2(static_cast<TOut*>(p.y) + static_cast<long>(t.row0 + tok) * p.N + ch, sum.x, sum.y, ch + 1 < p.N, vec);
+        }
+      }
+    }
+    ptx::cluster_sync();
+  }
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    if constexpr (PAIR) ptx::tmem_dealloc_pair(tmem_base, 512); else ptx::tmem_dealloc(tmem_base, 512);
   }
 }
 

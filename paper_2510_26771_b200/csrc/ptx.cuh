@@ -311,6 +311,51 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
 
+// ---------------------------------------------------------------- block-scaled e4m3 (kind::mxf8f6f4)
+// Instruction descriptor without the N extent and the scale ids: e4m3 A and B, both K-major, fp32 D, e8m0 scales.
+__host__ __device__ constexpr uint32_t make_mxf8_idesc(int m) {
+  return (1u << 23)                          // scale format: e8m0
+         | (static_cast<uint32_t>(m >> 4) << 24);
+}
+// N extent, and which byte of the 32-bit scale words in tensor memory this instruction takes for A and for B.
+__device__ __forceinline__ uint32_t mxf8_idesc_with(uint32_t idesc, int n, uint32_t scale_id) {
+  return idesc | (static_cast<uint32_t>(n >> 3) << 17) | (scale_id << 4) | (scale_id << 29);
+}
+// D[tmem] (+)= (A[smem] * sA[tmem]) (B[smem] * sB[tmem]), one scale per row of A, per row of B and 32 features.
+template <bool PAIR>
+__device__ __forceinline__ void mma_mxf8_ss(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t tmem_sa,
+                                            uint32_t tmem_sb, uint32_t accumulate) {
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb)
+        : "memory");
+}
+// Shared-memory descriptor of 32 rows of 16 bytes that lie one after the other (groups of eight rows 128 bytes apart,
+// no swizzle): the source of tmem_copy_scales.  16-byte aligned.
+__device__ __forceinline__ uint64_t make_rows16_desc(uint32_t smem_addr_bytes) {
+  return static_cast<uint64_t>((smem_addr_bytes >> 4) & 0x3FFFu) | (static_cast<uint64_t>(128 >> 4) << 32) |
+         (static_cast<uint64_t>(1) << 46);
+}
+// 512 bytes from shared memory to four columns of tensor memory: row i goes to lane i of each of the four quarters.
+// Ordered before the tcgen05.mma that the same thread issues after it.
+template <bool PAIR>
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t sdesc) {
+  if constexpr (PAIR)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+
 // ---------------------------------------------------------------- programmatic dependent launch
 // Blocks until the grids this one depends on have completed and their writes are visible.  A no-op
 // for a launch without the programmatic-serialization attribute.  Everything before it (barrier
@@ -347,6 +392,11 @@ __device__ __forceinline__ void st_async_u32(uint32_t remote_addr, uint32_t valu
   asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(remote_addr),
                "r"(value), "r"(remote_bar)
                : "memory");
+}
+__device__ __forceinline__ float2 ld_dsmem_f2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+  return v;
 }
 __device__ __forceinline__ float4 ld_dsmem_f4(uint32_t addr) {
   float4 v;

@@ -1262,14 +1262,60 @@ static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int 
   return STAMP_OK;
 }
 
-static int run_fp8_gemm(const Fp8GemmParams& p, int y_dtype, cudaStream_t st) {
-  const dim3 grid((unsigned)((p.N + 31) / 32), (unsigned)(p.M < 8 * 4096 ? (p.M + 7) / 8 : 4096));
-  if (y_dtype == STAMP_BF16)
-    k_fp8_product<__nv_bfloat16><<<grid, 256, 0, st>>>(p);
-  else
-    k_fp8_product<float><<<grid, 256, 0, st>>>(p);
+template <bool PAIR, typename TOut>
+static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const CUtensorMap& txs, const Fp8GemmParams& p, long tiles,
+                           cudaStream_t st) {
+  auto kern = k_fp8_gemm<PAIR, TOut>;
+  constexpr int bytes = Fp8Smem<PAIR>::DYN_BYTES;
+  if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), bytes)) return rc;
+  const int per_tile = PAIR ? 2 : p.split;
+  const long slots = sm_count() / per_tile;
+  // persistent CTAs (pairs); a cluster that splits a sum takes one tile only
+  const long units = (p.split == 1 && tiles > slots) ? slots : tiles;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3((unsigned)(units * per_tile));
+  lc.blockDim = dim3(FP8G_THREADS);
+  lc.dynamicSmemBytes = bytes;
+  lc.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)per_tile;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = per_tile > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&lc, kern, tw, tx, txs, p) != cudaSuccess) {
+    cudaGetLastError();
+    return STAMP_ERR_CUDA;
+  }
   STAMP_CHECK_LAUNCH();
   return STAMP_OK;
+}
+
+static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
+  CUtensorMap tw, tx, txs;
+  if (int rc = make_tmap_i8(p.w, (long)p.E * p.N, p.K, FP8G_BM, &tw)) return rc;
+  if (int rc = make_tmap_i8(p.x, p.M, p.K, FP8G_X_ROWS, &tx)) return rc;
+  if (int rc = make_tmap_i8(p.x, p.M, p.K, FP8G_X_SMALL, &txs)) return rc;
+  p.x_words = (p.ks & 3) == 0 && (reinterpret_cast<uintptr_t>(p.x_scale) & 3) == 0;
+  p.split = 1;
+  p.band = 16;
+  // tiles at most: an expert's run ends in one part tile, and no more experts than rows have any
+  auto tiles_of = [&](int bn, int bch) {
+    const long tok = p.offsets ? (long)p.M / bn + (p.E < p.M ? p.E : p.M) : ((long)p.M + bn - 1) / bn;
+    return tok * ((p.N + bch - 1) / bch);
+  };
+  const long tiles = tiles_of(128, 128), pair_tiles = tiles_of(256, 256);
+  const bool pair = pair_tiles >= sm_count() / 2;
+  if (pair)
+    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16>(tw, tx, txs, p, pair_tiles, st)
+                                 : launch_fp8_gemm<true, float>(tw, tx, txs, p, pair_tiles, st);
+  const int steps = (p.ks + 3) / 4;
+  while (p.split < 8 && tiles * p.split * 2 <= sm_count() && p.split * 2 <= steps) p.split *= 2;
+  return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16>(tw, tx, txs, p, tiles, st)
+                               : launch_fp8_gemm<false, float>(tw, tx, txs, p, tiles, st);
 }
 
 // Arguments common to both products.

@@ -380,6 +380,17 @@ def test_rows_behind_the_last_run_stay_as_they_were(st):
     check_grouped(y, x, xs, offsets, w, ws)
 
 
+@pytest.mark.parametrize("bad", [[0, 5, 4, 9], [1, 2, 3, 9], [0, 2, 4, 10], [0, -1, 4, 9], [0, 2, 1 << 30, 9]])
+def test_offsets_out_of_order_write_nothing_and_are_reported(st, bad):
+    import torch
+    x, xs = codes_of(st, 9, 256, seed=1)
+    w, ws = weights_of(st, (3, 72, 256), seed=1)
+    y = torch.full((9, 72), 7.0, device="cuda")
+    st.stamp_fp8_linear_grouped(x, xs, torch.tensor(bad, dtype=torch.int32, device="cuda"), w, ws, out=y)
+    assert st.stamp_last_device_status() == 1 and st.stamp_last_device_status() == 0
+    assert bool((y == 7.0).all())
+
+
 def test_one_expert_equals_the_plain_product(st):
     import torch
     for M in (3, 200, 900):
