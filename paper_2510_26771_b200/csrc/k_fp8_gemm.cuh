@@ -13,8 +13,8 @@
 //
 //   warp 0     TMA producer: 128-byte-swizzled K-major tiles of both operands into a ring of FP8G_STAGES
 //   warp 1     allocates TMEM; one elected thread copies the scale words to TMEM (tcgen05.cp) and issues the MMAs
-//   warp 2     scale producer: gathers the scale words of 512 features of the tile's tokens and channels into the
-//              order tcgen05.cp wants (row i of 32: rows i, i + 32, i + 64, i + 96), one step ahead of the MMAs
+//   warps 2-3  scale producers: gather the scale words of 512 features of the tile's tokens and channels into the
+//              order tcgen05.cp wants (row i of 32: rows i, i + 32, i + 64, i + 96), up to FP8G_SF_SLOTS steps ahead
 //   warps 4-11 epilogue: drain the finished accumulator while the next tile fills the other
 // Every wait is bounded; when one expires the CTA raises the device status word, unwinds and frees its TMEM.
 //
@@ -35,6 +35,7 @@ constexpr int FP8_MAX_EXPERTS = 1024;
 constexpr int FP8G_BM = 128, FP8G_BK = 128, FP8G_STAGES = 6;
 constexpr int FP8G_X_ROWS = 128;                       // token rows a CTA stages at most
 constexpr int FP8G_X_SMALL = 16;                       // rows of the small token box: up to 64 rows are loaded with it
+constexpr int FP8G_SF_SLOTS = 4;                       // steps of 512 features whose scale words are staged
 constexpr int FP8G_EPI_WARPS = 8;
 constexpr int FP8G_THREADS = 128 + 32 * FP8G_EPI_WARPS;
 constexpr long long FP8G_WAIT_LIMIT = 4000000000LL;    // SM clocks (~2 s) before a wait gives up
@@ -60,8 +61,8 @@ struct Fp8Smem {
   static constexpr int STAGE_BYTES = W_BYTES + FP8G_X_ROWS * FP8G_BK;
   static constexpr int SF_SLOT = 512 + BN * 4;         // scale words of 512 features: channels, then tokens
   static constexpr int SF_OFFSET = FP8G_STAGES * STAGE_BYTES;
-  static constexpr int BAR_OFFSET = SF_OFFSET + 2 * SF_SLOT;
-  static constexpr int NUM_BARS = 2 * FP8G_STAGES + 8; // full, empty, sffull[2], sfempty[2], tfull[2], tempty[2]
+  static constexpr int BAR_OFFSET = SF_OFFSET + FP8G_SF_SLOTS * SF_SLOT;
+  static constexpr int NUM_BARS = 2 * FP8G_STAGES + 2 * FP8G_SF_SLOTS + 4; // full, empty, sffull, sfempty, tfull[2], tempty[2]
   static constexpr int TAB_OFFSET = BAR_OFFSET + NUM_BARS * 8 + 16;
   static constexpr int DYN_BYTES = TAB_OFFSET + 2 * (FP8_MAX_EXPERTS + 1) * 4 + 1024;
   // tensor memory: second accumulator, then the two buffers of scale columns (4 for channels, BN / 32 for tokens)
@@ -98,6 +99,15 @@ __device__ __forceinline__ Fp8Tile fp8_tile(const Fp8GemmParams& p, const int* t
   return t;
 }
 
+// The scale bytes of `n` (1..4) consecutive blocks as one word.  Where there is none -- blocks past K, rows past the
+// run, whose columns are not stored -- any finite scale does: 1.
+__device__ __forceinline__ uint32_t fp8_scale_word(const uint8_t* ptr, int n, bool live) {
+  uint32_t b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = (live && i < n) ? __ldg(ptr + i) : 0x7Fu;
+  return b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24);
+}
+
 // Two adjacent channels of one token.
 __device__ __forceinline__ void fp8_store2(float* y, float a, float b, bool both, bool vec) {
   if (vec && both) {
@@ -127,8 +137,8 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + SM::BAR_OFFSET);
   uint64_t* empty = full + FP8G_STAGES;
   uint64_t* sffull = empty + FP8G_STAGES;
-  uint64_t* sfempty = sffull + 2;
-  uint64_t* tfull = sfempty + 2;
+  uint64_t* sfempty = sffull + FP8G_SF_SLOTS;
+  uint64_t* tfull = sfempty + FP8G_SF_SLOTS;
   uint64_t* tempty = tfull + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
   volatile uint32_t* abort_word = tmem_slot + 1;
@@ -154,9 +164,11 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       ptx::mbar_init(&full[s], 1);
       ptx::mbar_init(&empty[s], 1);
     }
-    for (int a = 0; a < 2; ++a) {
+    for (int a = 0; a < FP8G_SF_SLOTS; ++a) {
       ptx::mbar_init(&sffull[a], PAIR ? 2 : 1);
       ptx::mbar_init(&sfempty[a], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
       ptx::mbar_init(&tempty[a], PAIR ? 2 * FP8G_EPI_WARPS : FP8G_EPI_WARPS);
     }
@@ -299,18 +311,21 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
         ptx::tc_fence_after();
         const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(a * SM::ACC1);
         for (int s = step0; s < step1 && ok; ++s, ++scount) {
-          // The scale words of this step.  Their slot was refilled only after the MMAs that used the slot's previous
-          // contents -- and the same tensor-memory columns -- had finished.
-          const uint32_t slot = scount & 1u;
-          const bool sf = PAIR ? ptx::mbar_wait_bounded_cluster(&sffull[slot], (scount >> 1) & 1u, abort_word, FP8G_WAIT_LIMIT)
-                               : ptx::mbar_wait_bounded(&sffull[slot], (scount >> 1) & 1u, abort_word, FP8G_WAIT_LIMIT);
+          // The scale words of this step, and their tensor-memory columns: two buffers, so the MMAs of the step before
+          // the last have to be through (they are, long before the last one's are: the queue stays filled).
+          const uint32_t slot = scount % FP8G_SF_SLOTS, before = scount - 2u;
+          const uint32_t parity = (scount / FP8G_SF_SLOTS) & 1u;
+          const bool sf = (PAIR ? ptx::mbar_wait_bounded_cluster(&sffull[slot], parity, abort_word, FP8G_WAIT_LIMIT)
+                                : ptx::mbar_wait_bounded(&sffull[slot], parity, abort_word, FP8G_WAIT_LIMIT)) &&
+                          (scount < 2u || ptx::mbar_wait_bounded(&sfempty[before % FP8G_SF_SLOTS], (before / FP8G_SF_SLOTS) & 1u,
+                                                                 abort_word, FP8G_WAIT_LIMIT));
           if (!sf) {
             ok = false;
             break;
           }
           ptx::tc_fence_after();
           const uint32_t sfs = ptx::smem_u32(smem + SM::SF_OFFSET + slot * SM::SF_SLOT);
-          const uint32_t sfa = tmem_base + SM::SF_COL + slot * SM::SF_COLS, sfb = sfa + 4;
+          const uint32_t sfa = tmem_base + SM::SF_COL + (scount & 1u) * SM::SF_COLS, sfb = sfa + 4;
           ptx::tmem_copy_scales<PAIR>(sfa, ptx::make_rows16_desc(sfs));
           for (int h = 0; h * 128 < t.n; ++h)
             ptx::tmem_copy_scales<PAIR>(sfb + 4 * h, ptx::make_rows16_desc(sfs + 512 + 512 * h));
@@ -347,8 +362,9 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
         raise_device_status(STAMP_ERR_TIMEOUT);
       }
     }
-  } else if (warp == 2) {
-    // ------------------------------------------------------------------ scale producer
+  } else if (warp < 4) {
+    // ------------------------------------------------------------------ scale producers: every other step each
+    const uint32_t odd_step = warp & 1;
     const uint32_t sffull_bar0 = PAIR ? ptx::mapa(ptx::smem_u32(&sffull[0]), 0u) : 0u;
     const int ch_blocks = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
     uint32_t scount = 0;
@@ -359,39 +375,64 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       const int cb = min(t.ch_tile * (CH_PER_TILE / FP8_BLOCK) + (PAIR ? rank : 0), ch_blocks - 1);
       const uint8_t* wsc = p.w_scale + (static_cast<long>(t.expert) * ch_blocks + cb) * p.ks;
       const uint8_t* xsc = p.x_scale + static_cast<long>(t.row0) * p.ks;
-      for (int s = step0; s < step1; ++s, ++scount) {
+      // Rows of scale bytes on word boundaries: one load per step.  Otherwise the two aligned words that hold the bytes,
+      // where both are sure to lie within the scales (four rows of this table before and after), or byte by byte.
+      const int mode = p.x_words ? 0 : (t.row0 >= 4 && t.row0 + t.rows + 4 <= p.M) ? 1 : 2;
+      // All loads of a step are issued before the first is used, and a step ahead of the words that are written.
+      uint32_t ww, xw[BN / 32];
+      auto load = [&](int s) {
         const int k = 4 * s, nk = min(4, p.ks - k);
-        uint32_t ww = 0x7F7F7F7Fu, xw[BN / 32];
-        for (int i = 0; i < nk; ++i) ww = (ww & ~(255u << (8 * i))) | (static_cast<uint32_t>(__ldg(wsc + k + i)) << (8 * i));
+        ww = fp8_scale_word(wsc + k, nk, true);
+        const uint8_t* at = xsc + static_cast<long>(lane) * p.ks + k;
+        const long step32 = 32L * p.ks;
+        if (mode == 0) {
 #pragma unroll
-        for (int q = 0; q < BN / 32; ++q) {
-          const int r = q * 32 + lane;
-          xw[q] = 0x7F7F7F7Fu;      // rows past the run: any finite scale, their columns are not stored
-          if (r < t.rows) {
-            const uint8_t* ptr = xsc + static_cast<long>(r) * p.ks + k;
-            if (p.x_words) {
-              xw[q] = __ldg(reinterpret_cast<const uint32_t*>(ptr));
-            } else {
-              for (int i = 0; i < nk; ++i) xw[q] = (xw[q] & ~(255u << (8 * i))) | (static_cast<uint32_t>(__ldg(ptr + i)) << (8 * i));
-            }
+          for (int q = 0; q < BN / 32; ++q, at += step32)
+            xw[q] = q * 32 + lane < t.rows ? __ldg(reinterpret_cast<const uint32_t*>(at)) : 0x7F7F7F7Fu;
+        } else if (mode == 1) {
+          uint32_t lo[BN / 32], hi[BN / 32];
+#pragma unroll
+          for (int q = 0; q < BN / 32; ++q) {
+            const uint32_t* word = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(at + q * step32) & ~uintptr_t(3));
+            const bool live = q * 32 + lane < t.rows;
+            lo[q] = live ? __ldg(word) : 0x7F7F7F7Fu;
+            hi[q] = live ? __ldg(word + 1) : 0x7F7F7F7Fu;
           }
+#pragma unroll
+          for (int q = 0; q < BN / 32; ++q)
+            xw[q] = __funnelshift_r(lo[q], hi[q], 8 * static_cast<uint32_t>(reinterpret_cast<uintptr_t>(at + q * step32) & 3));
+        } else {
+#pragma unroll
+          for (int q = 0; q < BN / 32; ++q, at += step32) xw[q] = fp8_scale_word(at, nk, q * 32 + lane < t.rows);
         }
-        const uint32_t slot = scount & 1u;
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&sfempty[slot], ((scount >> 1) & 1u) ^ 1u, abort_word, FP8G_WAIT_LIMIT))) {
+      };
+      int s = step0 + static_cast<int>((scount ^ odd_step) & 1u);
+      scount += s - step0;
+      if (s < step1) load(s);
+      for (; s < step1; s += 2, scount += 2) {
+        const uint32_t ww0 = ww;
+        uint32_t xw0[BN / 32];
+#pragma unroll
+        for (int q = 0; q < BN / 32; ++q) xw0[q] = xw[q];
+        if (s + 2 < step1) load(s + 2);
+        const uint32_t slot = scount % FP8G_SF_SLOTS;
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&sfempty[slot], ((scount / FP8G_SF_SLOTS) & 1u) ^ 1u, abort_word,
+                                                                   FP8G_WAIT_LIMIT))) {
           ok = false;
           break;
         }
         uint8_t* dst = smem + SM::SF_OFFSET + slot * SM::SF_SLOT + lane * 16;
-        *reinterpret_cast<uint4*>(dst) = make_uint4(ww, ww, ww, ww);
+        *reinterpret_cast<uint4*>(dst) = make_uint4(ww0, ww0, ww0, ww0);
 #pragma unroll
         for (int h = 0; h < BN / 128; ++h)
-          *reinterpret_cast<uint4*>(dst + 512 + 512 * h) = make_uint4(xw[4 * h], xw[4 * h + 1], xw[4 * h + 2], xw[4 * h + 3]);
+          *reinterpret_cast<uint4*>(dst + 512 + 512 * h) = make_uint4(xw0[4 * h], xw0[4 * h + 1], xw0[4 * h + 2], xw0[4 * h + 3]);
         ptx::fence_proxy_async_smem();   // tcgen05.cp reads them through the async proxy
         __syncwarp();
         if (lane == 0) {
           if constexpr (PAIR) ptx::mbar_arrive_cluster(sffull_bar0 + slot * 8u); else ptx::mbar_arrive(&sffull[slot]);
         }
       }
+      scount -= s - step1;   // steps of the tiles so far
     }
     if (!ok) {
       *abort_word = 1;
