@@ -226,8 +226,16 @@ def stamp_linear_fused(cfg: StampConfig, X: torch.Tensor, w: torch.Tensor, w_for
     return Y
 
 
+# The calls of the block-scaled layers are a few microseconds of device time for single tokens, so their marshalling is
+# kept short: argument types are declared once (lib()), addresses are passed as integers, new outputs are not checked.
+
 def _fp8_blocks(n: int) -> int:
     return (n + FP8_BLOCK - 1) // FP8_BLOCK
+
+
+def _fp8_stream(t: torch.Tensor) -> int:
+    """Handle of the current stream of the tensor's device (torch.cuda.current_stream() builds an object around it)."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def _fp8_arg(t: torch.Tensor, what: str, shape, dtype) -> int:
@@ -238,43 +246,53 @@ def _fp8_arg(t: torch.Tensor, what: str, shape, dtype) -> int:
     return t.data_ptr()
 
 
-def _fp8_rows(X: torch.Tensor) -> int:
-    """Distance of two rows of a CUDA matrix whose rows are dense (a slice of columns of a wider one is fine)."""
-    if X.dim() != 2 or not X.is_cuda or (X.shape[1] > 1 and X.stride(1) != 1):
-        raise ValueError("expected a two-dimensional CUDA tensor with dense rows")
-    return X.stride(0) if X.shape[0] > 1 else X.shape[1]
+def _fp8_rows(X: torch.Tensor):
+    """Rows, features, and the distance of two rows, of a CUDA matrix whose rows are dense (a slice of columns of a wider
+    one is fine)."""
+    if X.dim() != 2 or not X.is_cuda:
+        raise ValueError("expected a two-dimensional CUDA tensor")
+    rows, features = X.shape
+    ld, step = X.stride()
+    if step != 1 and features > 1:
+        raise ValueError("expected dense rows")
+    return rows, features, ld if rows > 1 else features
 
 
-def _fp8_outputs(M: int, K: int, codes, scale, device):
-    shape, blocks = (M, K), (M, _fp8_blocks(K))
-    codes = torch.empty(shape, dtype=FP8_CODES, device=device) if codes is None else codes
-    scale = torch.empty(blocks, dtype=FP8_SCALE, device=device) if scale is None else scale
-    return codes, _fp8_arg(codes, "codes", shape, FP8_CODES), scale, _fp8_arg(scale, "scale", blocks, FP8_SCALE)
+def _fp8_outputs(X: torch.Tensor, M: int, K: int, codes, scale):
+    """Codes and scales to write, and their addresses."""
+    if codes is None:
+        codes = X.new_empty((M, K), dtype=FP8_CODES)
+        cp = codes.data_ptr()
+    else:
+        cp = _fp8_arg(codes, "codes", (M, K), FP8_CODES)
+    if scale is None:
+        scale = X.new_empty((M, _fp8_blocks(K)), dtype=FP8_SCALE)
+        sp = scale.data_ptr()
+    else:
+        sp = _fp8_arg(scale, "scale", (M, _fp8_blocks(K)), FP8_SCALE)
+    return codes, cp, scale, sp
 
 
 def stamp_fp8_quantize(X: torch.Tensor, rows: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
                        scale: Optional[torch.Tensor] = None):
     """[T, K] activations -> (codes [M, K], scale [M, ceil(K / 128)]); rows [M] int32: which row of X each output row is
     (M = T and every row itself without it).  codes, scale: buffers to write instead of new ones."""
-    ld = _fp8_rows(X)
-    T, K = X.shape
+    T, K, ld = _fp8_rows(X)
     M = T if rows is None else rows.numel()
-    codes, cp, scale, sp = _fp8_outputs(M, K, codes, scale, X.device)
+    codes, cp, scale, sp = _fp8_outputs(X, M, K, codes, scale)
     rp = None if rows is None else _fp8_arg(rows, "rows", (M,), torch.int32)
-    _check(lib().stamp_fp8_quantize(X.data_ptr(), _dtype_code(X), ld, rp, T, M, K, cp, sp,
-                                    torch.cuda.current_stream().cuda_stream), "stamp_fp8_quantize")
+    _check(lib().stamp_fp8_quantize(X.data_ptr(), _dtype_code(X), ld, rp, T, M, K, cp, sp, _fp8_stream(X)), "stamp_fp8_quantize")
     return codes, scale
 
 
 def stamp_fp8_gated_quantize(X: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """[M, 2 F] gates and ups -> (codes [M, F], scale [M, ceil(F / 128)]) of silu(gate) * up."""
-    ld = _fp8_rows(X)
-    M, F = X.shape[0], X.shape[1] // 2
-    if X.shape[1] != 2 * F:
+    M, F2, ld = _fp8_rows(X)
+    F = F2 // 2
+    if F2 != 2 * F:
         raise ValueError("expected as many gates as ups")
-    codes, cp, scale, sp = _fp8_outputs(M, F, codes, scale, X.device)
-    _check(lib().stamp_fp8_gated_quantize(X.data_ptr(), _dtype_code(X), ld, M, F, cp, sp,
-                                          torch.cuda.current_stream().cuda_stream), "stamp_fp8_gated_quantize")
+    codes, cp, scale, sp = _fp8_outputs(X, M, F, codes, scale)
+    _check(lib().stamp_fp8_gated_quantize(X.data_ptr(), _dtype_code(X), ld, M, F, cp, sp, _fp8_stream(X)), "stamp_fp8_gated_quantize")
     return codes, scale
 
 
@@ -290,18 +308,27 @@ def stamp_fp8_quantize_weights(W: torch.Tensor):
     return codes, scale
 
 
+def _fp8_product_out(x: torch.Tensor, M: int, N: int, out_dtype, out):
+    """The output, its address and its type code."""
+    if out is None:
+        out = x.new_empty((M, N), dtype=out_dtype)
+        return out, out.data_ptr(), _dtype_code(out)
+    return out, _fp8_arg(out, "out", (M, N), out.dtype), _dtype_code(out)
+
+
 def stamp_fp8_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
                      bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Codes [M, K] times weight codes [N, K] -> [M, N]; bias [N] float32."""
     M, K = x.shape
     N = w.shape[0]
-    Y = torch.empty((M, N), dtype=out_dtype, device=x.device) if out is None else out
+    blocks = _fp8_blocks(K)
+    Y, yp, yd = _fp8_product_out(x, M, N, out_dtype, out)
     _check(lib().stamp_fp8_linear(
-        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, _fp8_blocks(K)), FP8_SCALE),
-        _fp8_arg(w, "w", (N, K), FP8_CODES), _fp8_arg(w_scale, "w_scale", (_fp8_blocks(N), _fp8_blocks(K)), FP8_SCALE),
-        None if bias is None else _fp8_arg(bias, "bias", (N,), torch.float32), M, N, K,
-        _fp8_arg(Y, "out", (M, N), Y.dtype), _dtype_code(Y), torch.cuda.current_stream().cuda_stream), "stamp_fp8_linear")
+        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, blocks), FP8_SCALE),
+        _fp8_arg(w, "w", (N, K), FP8_CODES), _fp8_arg(w_scale, "w_scale", (_fp8_blocks(N), blocks), FP8_SCALE),
+        None if bias is None else _fp8_arg(bias, "bias", (N,), torch.float32), M, N, K, yp, yd, _fp8_stream(x)),
+        "stamp_fp8_linear")
     return Y
 
 
@@ -313,13 +340,13 @@ def stamp_fp8_linear_grouped(x: torch.Tensor, x_scale: torch.Tensor, offsets: to
     bias [E, N] float32."""
     M, K = x.shape
     E, N = w.shape[0], w.shape[1]
-    Y = torch.empty((M, N), dtype=out_dtype, device=x.device) if out is None else out
+    blocks = _fp8_blocks(K)
+    Y, yp, yd = _fp8_product_out(x, M, N, out_dtype, out)
     _check(lib().stamp_fp8_linear_grouped(
-        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, _fp8_blocks(K)), FP8_SCALE),
+        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, blocks), FP8_SCALE),
         _fp8_arg(offsets, "offsets", (E + 1,), torch.int32), _fp8_arg(w, "w", (E, N, K), FP8_CODES),
-        _fp8_arg(w_scale, "w_scale", (E, _fp8_blocks(N), _fp8_blocks(K)), FP8_SCALE),
-        None if bias is None else _fp8_arg(bias, "bias", (E, N), torch.float32), M, E, N, K,
-        _fp8_arg(Y, "out", (M, N), Y.dtype), _dtype_code(Y), torch.cuda.current_stream().cuda_stream),
+        _fp8_arg(w_scale, "w_scale", (E, _fp8_blocks(N), blocks), FP8_SCALE),
+        None if bias is None else _fp8_arg(bias, "bias", (E, N), torch.float32), M, E, N, K, yp, yd, _fp8_stream(x)),
         "stamp_fp8_linear_grouped")
     return Y
 

@@ -32,10 +32,13 @@
 namespace stamp {
 
 constexpr int FP8_MAX_EXPERTS = 1024;
-constexpr int FP8G_BM = 128, FP8G_BK = 128, FP8G_STAGES = 6;
-constexpr int FP8G_X_ROWS = 128;                       // token rows a CTA stages at most
-constexpr int FP8G_X_SMALL = 16;                       // rows of the small token box: up to 64 rows are loaded with it
+constexpr int FP8G_BM = 128, FP8G_BK = 128;
+constexpr int FP8G_RING_BYTES = 208 * 1024;            // operand stages: 6 of 128 token rows ... 10 of 32
+constexpr int FP8G_MAX_STAGES = 10;
+constexpr int FP8G_ACC_COLS = 128;                     // tensor-memory columns of a tile of one CTA
+constexpr int FP8G_W_BYTES = FP8G_BM * FP8G_BK;
 constexpr int FP8G_SF_SLOTS = 4;                       // steps of 512 features whose scale words are staged
+constexpr int FP8G_TAIL_BOX = 32;
 constexpr int FP8G_EPI_WARPS = 8;
 constexpr int FP8G_THREADS = 128 + 32 * FP8G_EPI_WARPS;
 constexpr long long FP8G_WAIT_LIMIT = 4000000000LL;    // SM clocks (~2 s) before a wait gives up
@@ -50,24 +53,27 @@ struct Fp8GemmParams {
   void* y;                 // [M, N] float or bf16
   int M, N, K, E, ks;
   int x_words;             // x_scale rows start on 4-byte boundaries
+  int bn;                  // token rows of a tile: a multiple of 16, at most 128 (PAIR: 256)
+  int stages, stage_bytes; // operand ring: 128 channels and the token rows that one CTA stages (bn; PAIR: bn / 2)
+  int tail;                // tiles of up to this many staged rows (the ends of runs) are copied 32 rows at a time; 0: none
   int split;               // CTAs that share a tile's sum (PAIR: 1)
+  int chunk;               // steps of 512 features that one accumulator sums (fp32 output), else all of them
   int band;                // channel tiles per raster band
 };
 
 template <bool PAIR>
 struct Fp8Smem {
-  static constexpr int BN = PAIR ? 256 : 128;
-  static constexpr int W_BYTES = FP8G_BM * FP8G_BK;
-  static constexpr int STAGE_BYTES = W_BYTES + FP8G_X_ROWS * FP8G_BK;
+  static constexpr int BN = PAIR ? 256 : 128;          // token rows of the largest tile
   static constexpr int SF_SLOT = 512 + BN * 4;         // scale words of 512 features: channels, then tokens
-  static constexpr int SF_OFFSET = FP8G_STAGES * STAGE_BYTES;
+  static constexpr int SF_OFFSET = FP8G_RING_BYTES;
   static constexpr int BAR_OFFSET = SF_OFFSET + FP8G_SF_SLOTS * SF_SLOT;
-  static constexpr int NUM_BARS = 2 * FP8G_STAGES + 2 * FP8G_SF_SLOTS + 4; // full, empty, sffull, sfempty, tfull[2], tempty[2]
+  static constexpr int NUM_BARS = 2 * FP8G_MAX_STAGES + 2 * FP8G_SF_SLOTS + 4; // full, empty, sffull, sfempty, tfull[2], tempty[2]
   static constexpr int TAB_OFFSET = BAR_OFFSET + NUM_BARS * 8 + 16;
   static constexpr int DYN_BYTES = TAB_OFFSET + 2 * (FP8_MAX_EXPERTS + 1) * 4 + 1024;
+  static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one CTA");
   // tensor memory: second accumulator, then the two buffers of scale columns (4 for channels, BN / 32 for tokens)
-  static constexpr int ACC1 = PAIR ? 224 : 128;
-  static constexpr int SF_COL = PAIR ? 480 : 256;
+  static constexpr int ACC1 = PAIR ? 224 : FP8G_ACC_COLS;
+  static constexpr int SF_COL = PAIR ? 480 : 2 * FP8G_ACC_COLS;
   static constexpr int SF_COLS = 4 + BN / 32;
 };
 
@@ -75,27 +81,29 @@ struct Fp8Smem {
 struct Fp8Tile {
   int expert, ch_tile, row0, rows, n;   // n: rows rounded up to what an instruction takes
 };
-template <bool PAIR>
+// Bands of `band` channel tiles; inside one, channel tiles vary fastest: CTAs running at the same time share token tiles,
+// and the band's weights stay in L2 over an expert's token tiles.
+__device__ __forceinline__ void fp8_raster(int tile, int band, int ch_tiles, int tok_tiles, int& ch_tile, int& tok_tile) {
+  const int per_band = band * tok_tiles;
+  const int b = tile / per_band, rem = tile - b * per_band;
+  const int first = b * band, height = min(band, ch_tiles - first);
+  tok_tile = rem / height;
+  ch_tile = first + (rem - tok_tile * height);
+}
 __device__ __forceinline__ Fp8Tile fp8_tile(const Fp8GemmParams& p, const int* tile_start, const int* row_start, int experts, int tile,
                                             int ch_tiles, int tok_tiles) {
-  // bands of `band` channel tiles; inside one, channel tiles vary fastest: CTAs running at the same time share token
-  // tiles, and the band's weights stay in L2 over an expert's token tiles
-  const int per_band = p.band * tok_tiles;
-  const int b = tile / per_band, rem = tile - b * per_band;
-  const int first = b * p.band, height = min(p.band, ch_tiles - first);
-  const int tt = rem / height;
   Fp8Tile t;
-  t.ch_tile = first + (rem - tt * height);
+  int tt;
+  fp8_raster(tile, p.band, ch_tiles, tok_tiles, t.ch_tile, tt);
   int lo = 0, hi = experts;             // the expert whose tiles hold tt (empty runs have none)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (tile_start[mid] <= tt) lo = mid; else hi = mid;
   }
   t.expert = lo;
-  t.row0 = row_start[lo] + (tt - tile_start[lo]) * Fp8Smem<PAIR>::BN;
-  t.rows = min(Fp8Smem<PAIR>::BN, row_start[lo + 1] - t.row0);
-  constexpr int STEP = PAIR ? 32 : 16;
-  t.n = (t.rows + STEP - 1) / STEP * STEP;
+  t.row0 = row_start[lo] + (tt - tile_start[lo]) * p.bn;
+  t.rows = min(p.bn, row_start[lo + 1] - t.row0);
+  t.n = (t.rows + 15) & ~15;
   return t;
 }
 
@@ -129,14 +137,14 @@ __device__ __forceinline__ void fp8_store2(__nv_bfloat16* y, float a, float b, b
 template <bool PAIR, typename TOut>
 __global__ void __launch_bounds__(FP8G_THREADS, 1)
     k_fp8_gemm(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
-               const __grid_constant__ CUtensorMap tmap_x_small, Fp8GemmParams p) {
+               const __grid_constant__ CUtensorMap tmap_x_tail, Fp8GemmParams p) {
   using SM = Fp8Smem<PAIR>;
   constexpr int BN = SM::BN;
   extern __shared__ uint8_t fp8g_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(fp8g_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + SM::BAR_OFFSET);
-  uint64_t* empty = full + FP8G_STAGES;
-  uint64_t* sffull = empty + FP8G_STAGES;
+  uint64_t* empty = full + FP8G_MAX_STAGES;
+  uint64_t* sffull = empty + FP8G_MAX_STAGES;
   uint64_t* sfempty = sffull + FP8G_SF_SLOTS;
   uint64_t* tfull = sfempty + FP8G_SF_SLOTS;
   uint64_t* tempty = tfull + 2;
@@ -160,7 +168,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
   const int kb0 = step0 * 4, kb1 = min(step1 * 4, num_kb);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < FP8G_STAGES; ++s) {
+    for (int s = 0; s < FP8G_MAX_STAGES; ++s) {
       ptx::mbar_init(&full[s], 1);
       ptx::mbar_init(&empty[s], 1);
     }
@@ -176,7 +184,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&tmap_w);
     ptx::prefetch_tensormap(&tmap_x);
-    ptx::prefetch_tensormap(&tmap_x_small);
+    if (p.tail) ptx::prefetch_tensormap(&tmap_x_tail);
   }
   if (warp == 1) {
     if constexpr (PAIR) {
@@ -187,38 +195,38 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       ptx::tmem_relinquish();
     }
   }
-  ptx::grid_dependency_wait();   // codes, scales and offsets come from the kernels launched before
-  ptx::grid_launch_dependents();
-
   // Where every expert's rows and tiles start.  Offsets that are out of order or past the rows: no tile at all.
-  bool bad = false;
   if (p.offsets) {
+    ptx::grid_dependency_wait();
+    bool bad = false;
     for (int e = threadIdx.x; e <= p.E; e += FP8G_THREADS) {
       const int o = __ldg(p.offsets + e);
       row_start[e] = o;
       bad |= o < 0 || o > p.M || (e == 0 ? o != 0 : o < __ldg(p.offsets + e - 1));
     }
+    bad = __syncthreads_or(bad);
+    if (bad && threadIdx.x == 0) raise_device_status(STAMP_ERR_INVALID_ARG);
+    if (warp == 3) {
+      int sum = 0;
+      for (int e0 = 0; e0 < p.E; e0 += 32) {
+        const int e = e0 + lane;
+        int t = (e < p.E && !bad) ? (row_start[e + 1] - row_start[e] + p.bn - 1) / p.bn : 0;
+        const int own = t;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, t, d);
+          if (lane >= d) t += v;
+        }
+        if (e < p.E) tile_start[e] = sum + t - own;
+        sum += __shfl_sync(0xffffffffu, t, 31);
+      }
+      if (lane == 0) tile_start[p.E] = sum;
+    }
   } else if (threadIdx.x == 0) {
     row_start[0] = 0;
     row_start[1] = p.M;
-  }
-  bad = __syncthreads_or(bad);
-  if (bad && threadIdx.x == 0) raise_device_status(STAMP_ERR_INVALID_ARG);
-  if (warp == 3) {
-    int sum = 0;
-    for (int e0 = 0; e0 < p.E; e0 += 32) {
-      const int e = e0 + lane;
-      int t = (e < p.E && !bad) ? (row_start[e + 1] - row_start[e] + BN - 1) / BN : 0;
-      const int own = t;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, t, d);
-        if (lane >= d) t += v;
-      }
-      if (e < p.E) tile_start[e] = sum + t - own;
-      sum += __shfl_sync(0xffffffffu, t, 31);
-    }
-    if (lane == 0) tile_start[p.E] = sum;
+    tile_start[0] = 0;
+    tile_start[1] = (p.M + p.bn - 1) / p.bn;
   }
   ptx::tc_fence_before();
   __syncthreads();
@@ -228,6 +236,9 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
   const int tok_tiles = tile_start[p.E];
   const int num_tiles = ch_tiles * tok_tiles;
   const int tile0 = blockIdx.x / per_tile, tile_step = gridDim.x / per_tile;
+  // Everything above may overlap the kernels before this one; codes and scales come from them.
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
@@ -236,43 +247,37 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       uint32_t phase = 0, armed = 0, armed_parity = 0;
       bool ok = true;
       for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
-        const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
-        const int mine = PAIR ? t.n / 2 : t.n;              // token rows this CTA stages
+        const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+        const int mine = PAIR ? t.n / 2 : t.n;   // token rows this CTA stages (copies bring whole boxes: more, not used)
         const int xrow = t.row0 + (PAIR ? rank * mine : 0);
         const int wrow = t.expert * p.N + t.ch_tile * CH_PER_TILE + (PAIR ? rank * FP8G_BM : 0);
-        const bool small = mine <= 64;
-        const uint32_t bytes = SM::W_BYTES + (small ? mine : FP8G_X_ROWS) * FP8G_BK;
+        const int pieces = mine <= p.tail ? (mine + FP8G_TAIL_BOX - 1) / FP8G_TAIL_BOX : 0;
+        const uint32_t bytes = pieces ? FP8G_W_BYTES + pieces * (FP8G_TAIL_BOX * FP8G_BK) : p.stage_bytes;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!ptx::mbar_wait_bounded(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT)) {
             ok = false;
             break;
           }
-          uint8_t* ws = smem + stage * SM::STAGE_BYTES;
-          uint8_t* xs = ws + SM::W_BYTES;
+          uint8_t* ws = smem + stage * p.stage_bytes;
+          uint8_t* xs = ws + FP8G_W_BYTES;
           if constexpr (PAIR) {
             // all copies of the pair are counted on the even CTA's barrier
             const uint32_t bar0 = ptx::mapa(ptx::smem_u32(&full[stage]), 0u);
             if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * bytes);
             ptx::tma_load_2d_pair(ws, &tmap_w, bar0, kb * FP8G_BK, wrow);
-            if (small) {
-              for (int r = 0; r < mine; r += FP8G_X_SMALL)
-                ptx::tma_load_2d_pair(xs + r * FP8G_BK, &tmap_x_small, bar0, kb * FP8G_BK, xrow + r);
-            } else {
-              ptx::tma_load_2d_pair(xs, &tmap_x, bar0, kb * FP8G_BK, xrow);
-            }
+            if (pieces == 0) ptx::tma_load_2d_pair(xs, &tmap_x, bar0, kb * FP8G_BK, xrow);
+            for (int i = 0; i < pieces; ++i)
+              ptx::tma_load_2d_pair(xs + i * (FP8G_TAIL_BOX * FP8G_BK), &tmap_x_tail, bar0, kb * FP8G_BK, xrow + i * FP8G_TAIL_BOX);
           } else {
             ptx::mbar_arrive_expect_tx(&full[stage], bytes);
             ptx::tma_load_2d(ws, &tmap_w, &full[stage], kb * FP8G_BK, wrow);
-            if (small) {
-              for (int r = 0; r < mine; r += FP8G_X_SMALL)
-                ptx::tma_load_2d(xs + r * FP8G_BK, &tmap_x_small, &full[stage], kb * FP8G_BK, xrow + r);
-            } else {
-              ptx::tma_load_2d(xs, &tmap_x, &full[stage], kb * FP8G_BK, xrow);
-            }
+            if (pieces == 0) ptx::tma_load_2d(xs, &tmap_x, &full[stage], kb * FP8G_BK, xrow);
+            for (int i = 0; i < pieces; ++i)
+              ptx::tma_load_2d(xs + i * (FP8G_TAIL_BOX * FP8G_BK), &tmap_x_tail, &full[stage], kb * FP8G_BK, xrow + i * FP8G_TAIL_BOX);
           }
           armed |= 1u << stage;
           armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
-          if (++stage == FP8G_STAGES) {
+          if (++stage == p.stages) {
             stage = 0;
             phase ^= 1u;
           }
@@ -281,7 +286,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       if (!ok) {
         *abort_word = 1;
         raise_device_status(STAMP_ERR_TIMEOUT);
-        for (int s = 0; s < FP8G_STAGES; ++s)   // let the copies in flight land before the shared memory goes away
+        for (int s = 0; s < p.stages; ++s)   // let the copies in flight land before the shared memory goes away
           if (armed & (1u << s)) {
             const long long t0 = clock64();
             // (the odd CTA of a pair has no barrier of its own to watch: it just gives its copies the time)
@@ -297,38 +302,35 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       int stage = 0, it = 0;
       uint32_t phase = 0, scount = 0;
       bool ok = true;
-      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++it) {
-        const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
-        const int a = it & 1;
-        // PAIR: the columns shared with the previous tile's accumulator are drained (which implies that everything of
-        // the tile before it is); otherwise the tile that had this accumulator is
-        const bool free_acc = PAIR ? ptx::mbar_wait_bounded_cluster(&tempty[0], (it - 1) & 1, abort_word, FP8G_WAIT_LIMIT)
-                                   : ptx::mbar_wait_bounded(&tempty[a], ((it >> 1) & 1) ^ 1, abort_word, FP8G_WAIT_LIMIT);
-        if (!free_acc) {
-          ok = false;
-          break;
-        }
-        ptx::tc_fence_after();
-        const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(a * SM::ACC1);
+      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+        const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
         for (int s = step0; s < step1 && ok; ++s, ++scount) {
+          const int in_chunk = (s - step0) % p.chunk;   // steps that are in the accumulator already
+          const int a = it & 1;
           // The scale words of this step, and their tensor-memory columns: two buffers, so the MMAs of the step before
           // the last have to be through (they are, long before the last one's are: the queue stays filled).
           const uint32_t slot = scount % FP8G_SF_SLOTS, before = scount - 2u;
           const uint32_t parity = (scount / FP8G_SF_SLOTS) & 1u;
-          const bool sf = (PAIR ? ptx::mbar_wait_bounded_cluster(&sffull[slot], parity, abort_word, FP8G_WAIT_LIMIT)
-                                : ptx::mbar_wait_bounded(&sffull[slot], parity, abort_word, FP8G_WAIT_LIMIT)) &&
-                          (scount < 2u || ptx::mbar_wait_bounded(&sfempty[before % FP8G_SF_SLOTS], (before / FP8G_SF_SLOTS) & 1u,
-                                                                 abort_word, FP8G_WAIT_LIMIT));
-          if (!sf) {
-            ok = false;
-            break;
-          }
+          ok = (PAIR ? ptx::mbar_wait_bounded_cluster(&sffull[slot], parity, abort_word, FP8G_WAIT_LIMIT)
+                     : ptx::mbar_wait_bounded(&sffull[slot], parity, abort_word, FP8G_WAIT_LIMIT)) &&
+               (scount < 2u || ptx::mbar_wait_bounded(&sfempty[before % FP8G_SF_SLOTS], (before / FP8G_SF_SLOTS) & 1u, abort_word,
+                                                      FP8G_WAIT_LIMIT));
+          if (!ok) break;
           ptx::tc_fence_after();
           const uint32_t sfs = ptx::smem_u32(smem + SM::SF_OFFSET + slot * SM::SF_SLOT);
           const uint32_t sfa = tmem_base + SM::SF_COL + (scount & 1u) * SM::SF_COLS, sfb = sfa + 4;
           ptx::tmem_copy_scales<PAIR>(sfa, ptx::make_rows16_desc(sfs));
           for (int h = 0; h * 128 < t.n; ++h)
             ptx::tmem_copy_scales<PAIR>(sfb + 4 * h, ptx::make_rows16_desc(sfs + 512 + 512 * h));
+          if (in_chunk == 0) {
+            // PAIR: the columns shared with the previous accumulator are drained (which implies that everything of the
+            // one before it is); otherwise this accumulator's previous contents are
+            ok = PAIR ? ptx::mbar_wait_bounded(&tempty[0], (it - 1) & 1, abort_word, FP8G_WAIT_LIMIT)
+                      : ptx::mbar_wait_bounded(&tempty[a], ((it >> 1) & 1) ^ 1, abort_word, FP8G_WAIT_LIMIT);
+            if (!ok) break;
+            ptx::tc_fence_after();
+          }
+          const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(a * SM::ACC1);
           const int last = min(4 * s + 4, num_kb);
           for (int kb = 4 * s; kb < last; ++kb) {
             if (!ptx::mbar_wait_bounded(&full[stage], phase, abort_word, FP8G_WAIT_LIMIT)) {
@@ -336,25 +338,25 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
               break;
             }
             ptx::tc_fence_after();
-            const uint32_t wa = ptx::smem_u32(smem + stage * SM::STAGE_BYTES);
-            const uint32_t xa = wa + SM::W_BYTES;
+            const uint32_t wa = ptx::smem_u32(smem + stage * p.stage_bytes);
+            const uint32_t xa = wa + FP8G_W_BYTES;
             const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, t.n, static_cast<uint32_t>(kb & 3));
 #pragma unroll
             for (int k = 0; k < FP8G_BK / 32; ++k)
               ptx::mma_mxf8_ss<PAIR>(tmem_d, ptx::make_kmajor_sw128_desc(wa + k * 32), ptx::make_kmajor_sw128_desc(xa + k * 32),
-                                     idesc, sfa, sfb, (kb > kb0 || k > 0) ? 1u : 0u);
+                                     idesc, sfa, sfb, (in_chunk > 0 || kb > 4 * s || k > 0) ? 1u : 0u);
             if constexpr (PAIR) ptx::tc_commit_pair(&empty[stage], 3); else ptx::tc_commit(&empty[stage]);
-            if (++stage == FP8G_STAGES) {
+            if (++stage == p.stages) {
               stage = 0;
               phase ^= 1u;
             }
           }
-          if (ok) {
-            if constexpr (PAIR) ptx::tc_commit_pair(&sfempty[slot], 3); else ptx::tc_commit(&sfempty[slot]);
+          if (!ok) break;
+          if constexpr (PAIR) ptx::tc_commit_pair(&sfempty[slot], 3); else ptx::tc_commit(&sfempty[slot]);
+          if (in_chunk + 1 == p.chunk || s + 1 == step1) {
+            if constexpr (PAIR) ptx::tc_commit_pair(&tfull[a], 3); else ptx::tc_commit(&tfull[a]);
+            ++it;
           }
-        }
-        if (ok) {
-          if constexpr (PAIR) ptx::tc_commit_pair(&tfull[a], 3); else ptx::tc_commit(&tfull[a]);
         }
       }
       if (!ok) {
@@ -370,7 +372,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
     uint32_t scount = 0;
     bool ok = true;
     for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
-      const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+      const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
       // a CTA's 128 channels are one block of the weights' scales (a tile past the last channel takes the last block's)
       const int cb = min(t.ch_tile * (CH_PER_TILE / FP8_BLOCK) + (PAIR ? rank : 0), ch_blocks - 1);
       const uint8_t* wsc = p.w_scale + (static_cast<long>(t.expert) * ch_blocks + cb) * p.ks;
@@ -378,7 +380,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       // Rows of scale bytes on word boundaries: one load per step.  Otherwise the two aligned words that hold the bytes,
       // where both are sure to lie within the scales (four rows of this table before and after), or byte by byte.
       const int mode = p.x_words ? 0 : (t.row0 >= 4 && t.row0 + t.rows + 4 <= p.M) ? 1 : 2;
-      // All loads of a step are issued before the first is used, and a step ahead of the words that are written.
+      // All loads of a step are issued before the first is used; they are in flight while the step waits for its slot.
       uint32_t ww, xw[BN / 32];
       auto load = [&](int s) {
         const int k = 4 * s, nk = min(4, p.ks - k);
@@ -410,11 +412,6 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       scount += s - step0;
       if (s < step1) load(s);
       for (; s < step1; s += 2, scount += 2) {
-        const uint32_t ww0 = ww;
-        uint32_t xw0[BN / 32];
-#pragma unroll
-        for (int q = 0; q < BN / 32; ++q) xw0[q] = xw[q];
-        if (s + 2 < step1) load(s + 2);
         const uint32_t slot = scount % FP8G_SF_SLOTS;
         if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&sfempty[slot], ((scount / FP8G_SF_SLOTS) & 1u) ^ 1u, abort_word,
                                                                    FP8G_WAIT_LIMIT))) {
@@ -422,15 +419,17 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
           break;
         }
         uint8_t* dst = smem + SM::SF_OFFSET + slot * SM::SF_SLOT + lane * 16;
-        *reinterpret_cast<uint4*>(dst) = make_uint4(ww0, ww0, ww0, ww0);
+        *reinterpret_cast<uint4*>(dst) = make_uint4(ww, ww, ww, ww);
 #pragma unroll
         for (int h = 0; h < BN / 128; ++h)
-          *reinterpret_cast<uint4*>(dst + 512 + 512 * h) = make_uint4(xw0[4 * h], xw0[4 * h + 1], xw0[4 * h + 2], xw0[4 * h + 3]);
+          *reinterpret_cast<uint4*>(dst + 512 + 512 * h) = make_uint4(xw[4 * h], xw[4 * h + 1], xw[4 * h + 2], xw[4 * h + 3]);
         ptx::fence_proxy_async_smem();   // tcgen05.cp reads them through the async proxy
         __syncwarp();
         if (lane == 0) {
           if constexpr (PAIR) ptx::mbar_arrive_cluster(sffull_bar0 + slot * 8u); else ptx::mbar_arrive(&sffull[slot]);
         }
+        // (behind the arrival: with release semantics towards the cluster it would wait for loads in flight)
+        if (s + 2 < step1) load(s + 2);
       }
       scount -= s - step1;   // steps of the tiles so far
     }
@@ -448,66 +447,102 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
     TOut* const y = static_cast<TOut*>(p.y);
     int it = 0;
     bool ok = true;
-    for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++it) {
-      const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
-      const int a = it & 1;
+    for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+      const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
       const int ch = (PAIR ? 2 * t.ch_tile + rank : t.ch_tile) * FP8G_BM + row;
       float bias = 0.f;
       if (p.bias && ch < p.N) bias = __ldg(p.bias + static_cast<long>(t.expert) * p.N + ch);
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
-        ok = false;
-        break;
-      }
-      ptx::tc_fence_after();
-      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(a * SM::ACC1);
-      const int chunks = (t.n + 31) / 32;
-      bool released = false;
-      auto release = [&]() {
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (PAIR) ptx::mbar_arrive_cluster(tempty_bar0); else ptx::mbar_arrive(&tempty[a]);
+      for (int c0 = step0; c0 < step1; c0 += p.chunk, ++it) {
+        const int a = it & 1;
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
+          ok = false;
+          break;
         }
-        released = true;
-      };
-      if (PAIR && half != 0) release();   // the shared columns are in the other warps' first chunk
-      for (int i = half; i < chunks; i += 2) {
-        // the chunk that overlaps the other accumulator first: the last of the first one, the first of the second
-        const int c = (PAIR && a == 0) ? chunks - 1 - i : i;
-        uint32_t r[32];
-        ptx::tmem_ld_32x32b_x32(taddr + 32 * c, r);
-        ptx::tmem_ld_wait();
-        if (PAIR ? i == 0 : i + 2 >= chunks) release();
-        if (!PAIR && p.split > 1) {
-          // this CTA's part of the sum, [token][channel], in the ring that nothing uses any more
-          float* part = reinterpret_cast<float*>(smem);
+        ptx::tc_fence_after();
+        const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(a * SM::ACC1);
+        const int chunks = (t.n + 31) / 32;
+        bool released = false;
+        auto release = [&]() {
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR) ptx::mbar_arrive_cluster_relaxed(tempty_bar0); else ptx::mbar_arrive(&tempty[a]);
+          }
+          released = true;
+        };
+        if (PAIR && half != 0) release();   // the shared columns are in the other warps' first chunk
+        for (int i = half; i < chunks; i += 2) {
+          // the chunk that overlaps the other accumulator first: the last of the first one, the first of the second
+          const int c = (PAIR && a == 0) ? chunks - 1 - i : i;
+          uint32_t r[32];
+          ptx::tmem_ld_32x32b_x32(taddr + 32 * c, r);
+          ptx::tmem_ld_wait();
+          if (PAIR ? i == 0 : i + 2 >= chunks) release();
+          if (!PAIR && p.split > 1) {
+            // this CTA's part of the sum, [token][channel], in the ring that nothing uses any more
+            float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) part[(32 * c + j) * FP8G_BM + row] = __uint_as_float(r[j]);
-          continue;
-        }
-        const int left = t.rows - 32 * c;
-        if constexpr (sizeof(TOut) == 4) {
-          if (ch < p.N) {
+            for (int j = 0; j < 32; ++j) part[(32 * c + j) * FP8G_BM + row] = __uint_as_float(r[j]);
+            continue;
+          }
+          const int left = t.rows - 32 * c;
+          if constexpr (sizeof(TOut) == 4) {
             TOut* out = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
+            if (c0 == step0) {
+              if (ch < p.N) {
+                if (left >= 32) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (j < left) out[static_cast<long>(j) * p.N] = __uint_as_float(r[j]) + bias;
-          }
-        } else {
-          // neighbouring lanes swap halves of a token pair: either then holds two adjacent channels of one token
-          const int odd = lane & 1;
-          const int ch2 = ch & ~1;
-          TOut* out = y + static_cast<long>(t.row0 + 32 * c + odd) * p.N + ch2;
+                  for (int j = 0; j < 32; ++j, out += p.N) *out = __uint_as_float(r[j]) + bias;
+                } else {
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            const float v0 = __uint_as_float(r[j]) + bias, v1 = __uint_as_float(r[j + 1]) + bias;
-            const float other = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 1);
-            if (j + odd < left && ch2 < p.N)
-              fp8_store2(out + static_cast<long>(j) * p.N, odd ? other : v0, odd ? v1 : other, ch2 + 1 < p.N, vec);
+                  for (int j = 0; j < 32; ++j, out += p.N)
+                    if (j < left) *out = __uint_as_float(r[j]) + bias;
+                }
+              }
+            } else if (ch < p.N) {   // a later chunk of the sum: on top of this thread's own value of the chunks before
+              float before[32];
+#pragma unroll
+              for (int j = 0; j < 32; ++j) before[j] = j < left ? out[static_cast<long>(j) * p.N] : 0.f;
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (j < left) out[static_cast<long>(j) * p.N] = before[j] + __uint_as_float(r[j]);
+            }
+          } else {
+            // Neighbouring lanes swap halves of a token pair: either then holds two adjacent channels of one token, the even
+            // lane of the first, the odd lane of the second.
+            const int odd = lane & 1, ch2 = ch & ~1;
+            const uint32_t sel = odd ? 0x3276u : 0x5410u;
+            TOut* out = y + static_cast<long>(t.row0 + 32 * c + odd) * p.N + ch2;
+            uint32_t two[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[2 * j]) + bias, __uint_as_float(r[2 * j + 1]) + bias);
+              two[j] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) two[j] = __byte_perm(two[j], __shfl_xor_sync(0xffffffffu, two[j], 1), sel);
+            if (vec && left >= 32) {
+              if (ch2 < p.N) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j, out += 2 * static_cast<long>(p.N)) *reinterpret_cast<uint32_t*>(out) = two[j];
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j, out += 2 * static_cast<long>(p.N))
+                if (2 * j + odd < left && ch2 < p.N) {
+                  const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&two[j]);
+                  if (vec) {
+                    *reinterpret_cast<__nv_bfloat162*>(out) = v;
+                  } else {
+                    out[0] = v.x;
+                    if (ch2 + 1 < p.N) out[1] = v.y;
+                  }
+                }
+            }
           }
         }
+        if (!released) release();
       }
-      if (!released) release();
     }
     if (!ok) {
       *abort_word = 1;
@@ -522,26 +557,28 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
   if (!PAIR && p.split > 1) {
     // every CTA adds up every split-th token of the tile over the cluster's partial sums, in rank order
     if (tile0 < num_tiles && *abort_word == 0) {
-      const Fp8Tile t = fp8_tile<PAIR>(p, tile_start, row_start, p.E, tile0, ch_tiles, tok_tiles);
+      const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile0, ch_tiles, tok_tiles);
       const uint32_t part = ptx::smem_u32(smem);
       const bool vec = (reinterpret_cast<uintptr_t>(p.y) & (2 * sizeof(TOut) - 1)) == 0 && (p.N & 1) == 0;
-      for (int i = threadIdx.x; i < (t.rows - rank + p.split - 1) / p.split * 64; i += FP8G_THREADS) {
-        const int tok = rank + (i >> 6) * p.split, c2 = 2 * (i & 63);
-        const int ch = t.ch_tile * FP8G_BM + c2;
-        float2 sum = make_float2(0.f, 0.f);
-        for (int s = 0; s < p.split; ++s) {
-          const float2 v = ptx::ld_dsmem_f2(ptx::mapa(part, static_cast<uint32_t>(s)) + (tok * FP8G_BM + c2) * 4);
-          sum.x += v.x;
-          sum.y += v.y;
-        }
-        if (ch < p.N) {
-          if (p.bias) {
-            const float* b = p.bias + static_cast<long>(t.expert) * p.N + ch;
-            sum.x += __ldg(b);
-            if (ch + 1 < p.N) sum.y += __ldg(b + 1);
-          }
-          fp8_store2(static_cast<TOut*>(p.y) + static_cast<long>(t.row0 + tok) * p.N + ch, sum.x, sum.y, ch + 1 < p.N, vec);
-        }
+      uint32_t part_of[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s) part_of[s] = ptx::mapa(part, static_cast<uint32_t>(min(s, p.split - 1)));
+      const int c4 = 4 * lane, ch = t.ch_tile * FP8G_BM + c4;   // a warp takes a token, a lane four channels
+      float bias[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bias[i] = (p.bias && ch + i < p.N) ? __ldg(p.bias + static_cast<long>(t.expert) * p.N + ch + i) : 0.f;
+      for (int tok = rank + warp * p.split; tok < t.rows; tok += FP8G_THREADS / 32 * p.split) {
+        float4 v[8];   // all in flight at once
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+          if (s < p.split) v[s] = ptx::ld_dsmem_f4(part_of[s] + (tok * FP8G_BM + c4) * 4);
+        float4 sum = v[0];
+#pragma unroll
+        for (int s = 1; s < 8; ++s)
+          if (s < p.split) sum = make_float4(sum.x + v[s].x, sum.y + v[s].y, sum.z + v[s].z, sum.w + v[s].w);
+        TOut* out = static_cast<TOut*>(p.y) + static_cast<long>(t.row0 + tok) * p.N + ch;
+        if (ch < p.N) fp8_store2(out, sum.x + bias[0], sum.y + bias[1], ch + 1 < p.N, vec);
+        if (ch + 2 < p.N) fp8_store2(out + 2, sum.z + bias[2], sum.w + bias[3], ch + 3 < p.N, vec);
       }
     }
     ptx::cluster_sync();

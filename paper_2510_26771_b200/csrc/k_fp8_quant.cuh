@@ -9,6 +9,8 @@
 // block-scaled product reads.  A block of zeros has scale 1.  A block that holds an infinity or a NaN has scale NaN
 // (255) and NaN codes: what is computed from it is NaN instead of a finite number that hides it.
 #pragma once
+#include <type_traits>
+
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -33,88 +35,208 @@ __device__ __forceinline__ Fp8Scale fp8_scale(uint32_t amax_bits) {
   return r;
 }
 
-// Eight adjacent features of one row as floats.
-__device__ __forceinline__ void fp8_load8(const __nv_bfloat16* p, float (&v)[8]) {
-  const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+// Eight adjacent features of one row, as loaded and as floats.
+template <typename T>
+struct Fp8Raw;
+template <>
+struct Fp8Raw<__nv_bfloat16> {
+  uint4 u;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, bool live) {
+    u = live ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
   }
-}
-__device__ __forceinline__ void fp8_load8(const float* p, float (&v)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
+  // all magnitudes at most 80 (a NaN may say either)
+  __device__ __forceinline__ bool within80() const {
+    const uint32_t m = ptx::max_abs_bf16x2(ptx::max_abs_bf16x2(u.x, u.y), ptx::max_abs_bf16x2(u.z, u.w)) & 0x7FFF7FFFu;
+    return max(m & 0xFFFFu, m >> 16) <= 0x42A0u;
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+};
+template <>
+struct Fp8Raw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p, bool live) {
+    a = live ? __ldg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    b = live ? __ldg(reinterpret_cast<const float4*>(p) + 1) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ bool within80() const {
+    const float m = ptx::max_abs_nan(ptx::max_abs_nan(a.x, a.y, a.z), ptx::max_abs_nan(a.w, b.x, b.y), ptx::max_abs_nan(b.z, b.w, 0.f));
+    return m <= 80.f;
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+};
+
 __device__ __forceinline__ uint2 fp8_pack8(const float (&v)[8], float inverse) {
-  uint2 r;
-  r.x = ptx::cvt_e4m3x4(v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse);
-  r.y = ptx::cvt_e4m3x4(v[4] * inverse, v[5] * inverse, v[6] * inverse, v[7] * inverse);
-  return r;
+  const float2 i2 = make_float2(inverse, inverse);
+  float2 s[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = __fmul2_rn(make_float2(v[2 * i], v[2 * i + 1]), i2);
+  return make_uint2(ptx::cvt_e4m3x4(s[0].x, s[0].y, s[1].x, s[1].y), ptx::cvt_e4m3x4(s[2].x, s[2].y, s[3].x, s[3].y));
 }
 
-// silu(g) * u.  Every operation is the IEEE-rounded one (expf's error is the only one above half an ulp).
-__device__ __forceinline__ float gated_silu(float g, float u) { return __fmul_rn(__fdiv_rn(g, 1.0f + expf(-g)), u); }
+// silu(g) * u = g / (1 + exp(-g)) * u, for two neighbours at once in packed fp32 instructions, to about an ulp of the
+// IEEE operations in that order.  exp(-g) is 2^(-g log2 e), and what rounding that product would lose, the power would
+// multiply by g.  So it is split: a bf16 gate (8 significant bits) times the first 16 bits of log2 e is exact, the rest of
+// the constant, times ln 2, becomes a factor 1 + small; an fp32 gate's product is held as head and tail instead.  The
+// quotient is g times the approximate reciprocal, corrected once by its remainder.  SMALL: |g| <= 80.  Otherwise the power
+// is taken as 0 or infinite past +-90, and an infinite divisor takes no correction (inf * 0).  NaNs and infinities come
+// out non-finite, as they do of the formula.
+template <bool SMALL, bool BF16>
+__device__ __forceinline__ float2 gated_silu2(float2 g, float2 u) {
+  auto both = [](float v) { return make_float2(v, v); };
+  const float2 x = SMALL ? g : make_float2(fminf(fmaxf(g.x, -90.f), 90.f), fminf(fmaxf(g.y, -90.f), 90.f));
+  float2 head, more;   // exp(-x) = 2^head (1 + more)
+  if constexpr (BF16) {
+    head = __fmul2_rn(x, both(-47274.f / 32768.f));
+    more = __fmul2_rn(x, both(-4.88843e-6f));         // (log2 e - 47274 / 32768) ln 2
+  } else {
+    constexpr float LOG2E = 1.44269504f, LOG2E_TAIL = 1.92596299e-8f, LN2 = 0.693147181f;
+    head = __fmul2_rn(x, both(-LOG2E));
+    const float2 tail = __ffma2_rn(x, both(-LOG2E), __fmul2_rn(x, both(LOG2E)));
+    more = __fmul2_rn(__ffma2_rn(x, both(-LOG2E_TAIL), tail), both(LN2));
+  }
+  const float2 p = make_float2(ptx::ex2(head.x), ptx::ex2(head.y));
+  // (p * more + p would be inf - inf where p is infinite)
+  const float2 e = SMALL ? __ffma2_rn(p, more, p) : __fmul2_rn(p, __fadd2_rn(more, both(1.f)));
+  const float2 minus_d = __ffma2_rn(e, both(-1.f), both(-1.f));
+  const float2 r = make_float2(ptx::rcp(-minus_d.x), ptx::rcp(-minus_d.y));
+  float2 q = __fmul2_rn(g, r);
+  const float2 fixed = __ffma2_rn(__ffma2_rn(q, minus_d, g), r, q);
+  if constexpr (SMALL) {
+    q = fixed;
+  } else {
+    q.x = minus_d.x > -__int_as_float(0x7F800000) ? fixed.x : q.x;
+    q.y = minus_d.y > -__int_as_float(0x7F800000) ? fixed.y : q.y;
+  }
+  return __fmul2_rn(q, u);
+}
 
-// Activations.  Eight lanes own one block of a row: lane l holds features [8 l, 8 l + 8) and [64 + 8 l, 72 + 8 l), so
-// that the eight lanes' loads and stores are contiguous; the maximum takes three shuffles.
-//   X       [T, ld]  rows of K features (GATED: of 2 K, the gates first)
+// n / ks for n below 2^31: `magic` is 2^32 / ks rounded up, so the product's upper half is the quotient or one above it.
+__device__ __forceinline__ unsigned fp8_div(unsigned n, unsigned ks, unsigned magic) {
+  unsigned q = ks == 1u ? n : __umulhi(n, magic);
+  return static_cast<int>(n - q * ks) < 0 ? q - 1u : q;
+}
+
+// Both activation quantizers: eight lanes own one block of a row, lane l features [8 l, 8 l + 8) and [64 + 8 l, 72 + 8 l),
+// so that the eight lanes' loads and stores are contiguous; the maximum takes three shuffles.  Blocks are numbered row by
+// row, ks = ceil(K / 128) to a row, `groups` of them.  A lane without a block takes part in the shuffles only (col = K).
+struct Fp8Place {
+  unsigned row;
+  int col;   // first feature of the lane's part
+};
+__device__ __forceinline__ Fp8Place fp8_place(unsigned g, unsigned groups, int K, unsigned ks, unsigned magic) {
+  Fp8Place at{0u, K};
+  if (g < groups) {
+    at.row = fp8_div(g, ks, magic);
+    at.col = static_cast<int>(g - at.row * ks) * FP8_BLOCK + static_cast<int>(threadIdx.x & 7u) * 8;
+  }
+  return at;
+}
+__device__ __forceinline__ void fp8_quantize_block(const float (&v)[2][8], Fp8Place at, unsigned g, int K, uint8_t* codes, uint8_t* scale) {
+  float largest = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) largest = ptx::max_abs_nan(largest, v[i >> 3][i & 7], v[i >> 3][(i & 7) + 1]);
+  uint32_t amax = __float_as_uint(largest);
+#pragma unroll
+  for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+  const Fp8Scale s = fp8_scale(amax);
+  uint8_t* out = codes + static_cast<long>(at.row) * K + at.col;
+  if (at.col < K) *reinterpret_cast<uint2*>(out) = fp8_pack8(v[0], s.inverse);
+  if (at.col + 64 < K) *reinterpret_cast<uint2*>(out + 64) = fp8_pack8(v[1], s.inverse);
+  if ((threadIdx.x & 7u) == 0 && at.col < K) scale[g] = s.byte;
+}
+
+// Activations.
+//   X       [T, ld]  rows of K features
 //   rows    [M] source row of every output row, or nullptr for row m itself; an index outside [0, T) gives a row of
 //           zeros and raises the device status word
-//   codes   [M, K], scale [M, ks], ks = ceil(K / 128), groups = M * ks
-template <typename TIn, bool GATED>
+//   codes   [M, K], scale [M, ks]
+// A thread loads its part of U blocks, 128 bytes, before it uses the first.
+template <typename TIn>
 __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_quant(const TIn* __restrict__ X, long ld, const int* __restrict__ rows, int T,
-                                                            int K, unsigned ks, unsigned groups, uint8_t* __restrict__ codes,
-                                                            uint8_t* __restrict__ scale) {
+                                                            int K, unsigned ks, unsigned magic, unsigned groups,
+                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
+  constexpr int U = sizeof(TIn) == 2 ? 4 : 2;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const unsigned lane8 = threadIdx.x & 7u;
-  const unsigned stride = gridDim.x * (FP8Q_THREADS / 8);
-  // all four groups of a warp stay in the loop together: the shuffles are warp-wide
-  for (unsigned g = blockIdx.x * (FP8Q_THREADS / 8) + (threadIdx.x >> 3); g - ((threadIdx.x >> 3) & 3u) < groups; g += stride) {
-    const bool live = g < groups;
-    const unsigned row = live ? g / ks : 0u;
-    const int col = static_cast<int>(g - row * ks) * FP8_BLOCK + static_cast<int>(lane8) * 8;
-    long src = row;
-    bool valid = live;
-    if (rows) {
-      const int i = live ? __ldg(rows + row) : 0;
-      valid = live && i >= 0 && i < T;
-      if (live && !valid && lane8 == 0) raise_device_status(STAMP_ERR_INVALID_ARG);
-      src = valid ? i : 0;
+  const unsigned sub = (threadIdx.x >> 3) & 3u;
+  // a warp takes 4 U blocks in a row; all its lanes stay in the loop together, the shuffles are warp-wide
+  for (unsigned first = (blockIdx.x * (FP8Q_THREADS / 32) + (threadIdx.x >> 5)) * (4 * U); first < groups;
+       first += gridDim.x * (FP8Q_THREADS / 32) * (4 * U)) {
+    Fp8Raw<TIn> raw[U][2];
+    Fp8Place at[U];
+#pragma unroll
+    for (int b = 0; b < U; ++b) {
+      at[b] = fp8_place(first + 4 * b + sub, groups, K, ks, magic);
+      long src = at[b].row;
+      bool valid = at[b].col < K;
+      if (rows && valid) {
+        const int i = __ldg(rows + at[b].row);
+        valid = i >= 0 && i < T;
+        if (!valid) raise_device_status(STAMP_ERR_INVALID_ARG);
+        src = valid ? i : 0;
+      }
+      const TIn* p = X + src * ld + at[b].col;
+      raw[b][0].load(p, valid);
+      raw[b][1].load(p + 64, valid && at[b].col + 64 < K);
     }
-    float v[2][8];
-    uint32_t amax = 0;
+#pragma unroll
+    for (int b = 0; b < U; ++b) {
+      float v[2][8];
+      raw[b][0].values(v[0]);
+      raw[b][1].values(v[1]);
+      fp8_quantize_block(v, at[b], first + 4 * b + sub, K, codes, scale);
+    }
+  }
+}
+
+// Behind a gated activation: X [M, ld] rows of K gates and K ups -> codes [M, K], scale [M, ks] of silu(gate) * up.
+// The arithmetic (about 14 instructions per feature, two of them on the special function unit) takes two thirds of the
+// time that the memory traffic does, and many resident warps overlap the two best: copies through shared memory, three
+// blocks ahead, cost 3 % more than loads to registers (16384 x 4096), two sets of registers in turn 7 %.
+template <typename TIn>
+__global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_gated_quant(const TIn* __restrict__ X, long ld, int K, unsigned ks, unsigned magic,
+                                                                  unsigned groups, uint8_t* __restrict__ codes,
+                                                                  uint8_t* __restrict__ scale) {
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const unsigned stride = gridDim.x * (FP8Q_THREADS / 8), sub = (threadIdx.x >> 3) & 3u;
+  // a warp's four blocks stay in the loop together
+  for (unsigned g = blockIdx.x * (FP8Q_THREADS / 8) + (threadIdx.x >> 3); g - sub < groups; g += stride) {
+    const Fp8Place at = fp8_place(g, groups, K, ks, magic);
+    const TIn* p = X + static_cast<long>(at.row) * ld + at.col;
+    Fp8Raw<TIn> gate[2], up[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int c = col + 64 * h;
-      if (valid && c < K) {
-        fp8_load8(X + src * ld + c, v[h]);
-        if constexpr (GATED) {
-          float up[8];
-          fp8_load8(X + src * ld + K + c, up);
+      gate[h].load(p + 64 * h, at.col + 64 * h < K);
+      up[h].load(p + 64 * h + K, at.col + 64 * h < K);
+    }
+    float v[2][8];
+    auto activate = [&](auto small) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[h][i] = gated_silu(v[h][i], up[i]);
+      for (int h = 0; h < 2; ++h) {
+        float a[8], c[8];
+        gate[h].values(a);
+        up[h].values(c);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const float2 y = gated_silu2<decltype(small)::value, sizeof(TIn) == 2>(make_float2(a[i], a[i + 1]), make_float2(c[i], c[i + 1]));
+          v[h][i] = y.x;
+          v[h][i + 1] = y.y;
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[h][i] = 0.f;
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) amax = max(amax, absbits(v[h][i]));
-    }
-#pragma unroll
-    for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-    const Fp8Scale s = fp8_scale(amax);
-    if (live) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (col + 64 * h < K)
-          *reinterpret_cast<uint2*>(codes + static_cast<long>(row) * K + col + 64 * h) = fp8_pack8(v[h], s.inverse);
-      if (lane8 == 0) scale[g] = s.byte;
-    }
+    };
+    if (gate[0].within80() && gate[1].within80()) activate(std::true_type{}); else activate(std::false_type{});
+    fp8_quantize_block(v, at, g, K, codes, scale);
   }
 }
 
@@ -132,12 +254,9 @@ __global__ void __launch_bounds__(256) k_fp8_quant_weights(const TIn* __restrict
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
     const int row = row0 + 16 * r;
-    if (row < N && col < K) {
-      fp8_load8(W + base + static_cast<long>(row) * K, v[r]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[r][i] = 0.f;
-    }
+    Fp8Raw<TIn> raw;
+    raw.load(W + base + static_cast<long>(row) * K, row < N && col < K);
+    raw.values(v[r]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) amax = max(amax, absbits(v[r][i]));
   }

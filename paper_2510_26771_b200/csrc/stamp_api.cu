@@ -1244,17 +1244,43 @@ static int fused_quantize_tiled(const Problem& pb, const CqChoice& cc, const voi
 // ------------------------------------------------------------------------------------------
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-template <typename TIn, bool GATED>
+// The blocks of an activation quantizer: how many, and how many CTAs take them when one takes `per_cta` at a time and
+// `resident` CTAs fit an SM (the rest by striding; twice as many as fit, so that the tail is spread).
+struct Fp8Blocks {
+  long ks, groups;
+  unsigned magic, ctas;
+};
+static int fp8_blocks(int M, int K, int per_cta, int resident, Fp8Blocks* b) {
+  b->ks = ((long)K + FP8_BLOCK - 1) / FP8_BLOCK;
+  b->groups = M * b->ks;
+  if (b->groups > (1L << 31) - (1L << 24)) return STAMP_ERR_UNSUPPORTED;   // the kernels count blocks in 32 bits
+  b->magic = b->ks > 1 ? (unsigned)(((1ULL << 32) + b->ks - 1) / b->ks) : 0u;
+  const long ctas = (b->groups + per_cta - 1) / per_cta;
+  long most = 2L * resident * sm_count();
+  b->ctas = (unsigned)(ctas < most ? ctas : most);
+  return STAMP_OK;
+}
+
+template <typename TIn>
 static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale,
                             cudaStream_t st) {
-  const long ks = (K + FP8_BLOCK - 1) / FP8_BLOCK;
-  const long groups = M * ks;
-  if (groups > (1L << 31)) return STAMP_ERR_UNSUPPORTED;   // the kernel counts blocks in 32 bits
-  const long ctas = (groups + FP8Q_THREADS / 8 - 1) / (FP8Q_THREADS / 8);
-  const long most = 8L * sm_count();   // the threads that fit the machine; the rest by striding
-  if (launch_pdl(k_fp8_quant<TIn, GATED>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(FP8Q_THREADS), 0, st,
-                 static_cast<const TIn*>(X), ld, rows, T, K, (unsigned)ks, (unsigned)groups, static_cast<uint8_t*>(codes),
-                 static_cast<uint8_t*>(scale)) != cudaSuccess) {
+  Fp8Blocks b;
+  if (int rc = fp8_blocks(M, K, FP8Q_THREADS / 8 * (sizeof(TIn) == 2 ? 4 : 2), 4, &b)) return rc;
+  if (launch_pdl(k_fp8_quant<TIn>, dim3(b.ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, rows, T, K,
+                 (unsigned)b.ks, b.magic, (unsigned)b.groups, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
+    cudaGetLastError();
+    return STAMP_ERR_CUDA;
+  }
+  STAMP_CHECK_LAUNCH();
+  return STAMP_OK;
+}
+
+template <typename TIn>
+static int launch_fp8_gated_quant(const void* X, long ld, int M, int F, void* codes, void* scale, cudaStream_t st) {
+  Fp8Blocks b;
+  if (int rc = fp8_blocks(M, F, FP8Q_THREADS / 8, 12, &b)) return rc;
+  if (launch_pdl(k_fp8_gated_quant<TIn>, dim3(b.ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, F, (unsigned)b.ks,
+                 b.magic, (unsigned)b.groups, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
     cudaGetLastError();
     return STAMP_ERR_CUDA;
   }
@@ -1263,7 +1289,7 @@ static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int 
 }
 
 template <bool PAIR, typename TOut>
-static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const CUtensorMap& txs, const Fp8GemmParams& p, long tiles,
+static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const CUtensorMap& txt, const Fp8GemmParams& p, long tiles,
                            cudaStream_t st) {
   auto kern = k_fp8_gemm<PAIR, TOut>;
   constexpr int bytes = Fp8Smem<PAIR>::DYN_BYTES;
@@ -1286,7 +1312,7 @@ static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const C
   at[1].val.clusterDim.z = 1;
   lc.attrs = at;
   lc.numAttrs = per_tile > 1 ? 2 : 1;
-  if (cudaLaunchKernelEx(&lc, kern, tw, tx, txs, p) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&lc, kern, tw, tx, txt, p) != cudaSuccess) {
     cudaGetLastError();
     return STAMP_ERR_CUDA;
   }
@@ -1294,28 +1320,82 @@ static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const C
   return STAMP_OK;
 }
 
+// Which kernel, tile height and split: the candidate whose slowest CTA is estimated to be through first, in SM clocks.
+// What a CTA spends on 128 features is its shared-memory traffic at 128 bytes a clock: the stage is written by the copies
+// and read by the instructions once, so 2 x (128 channels + rows) x 128 bytes -- a pair's CTA stages and reads half of
+// the token rows, which is why pairs of 256 x 256 are the only tiles at the tensor cores' own 512 clocks.  (Measured: 537
+// clocks for pairs of 256 rows, 455 of 128; 550 for single CTAs of 128 rows, 446 of 64.)  The waves of tiles are
+// whole, so smaller tiles win where large ones leave SMs idle in the last wave, and splitting the sum of a tile over a
+// cluster wins where there are too few tiles at all.  Device times, in us, of the choice and of the other side:
+//   16 x 4096 x 4096    tiles of 16 rows, split 4:  8.0   unsplit: 11.0
+//   512 x 4096 x 4096   128 rows:                  13.1   pairs of 256: 15.1
+//   1024 x 4096 x 4096  pairs of 256:              19.0   128 rows: 23.3
+//   8192 x 1152 x 1152  pairs of 192:              17.4   128 rows: 18.2
+struct Fp8Plan {
+  bool pair;
+  int bn, split;
+};
+static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
+  const int steps = (p.ks + 3) / 4;
+  // runs that have rows, and their length: of the experts nothing is known here but how many rows they share
+  const double runs = p.offsets ? (p.E < p.M ? p.E : p.M) : 1, run = p.M / runs;
+  Fp8Plan best{false, 128, 1};
+  double best_cost = 1e300;
+  auto consider = [&](bool pair, int bn, int split) {
+    // tiles of a run: whole for a single matrix; runs of unknown lengths end in half a tile on average
+    const double per_run = !p.offsets ? (p.M + bn - 1) / bn : run <= bn / 2 ? 1.0 : run / bn + 0.5;
+    const double tiles = runs * per_run * ((p.N + (pair ? 255 : 127)) / (pair ? 256 : 128));
+    const double slots = sm_count() / (pair ? 2 : split);
+    if (split > 1 && tiles > slots) return;   // (a cluster that splits a sum takes one tile: a second round starts from nothing)
+    const double waves = !p.offsets ? (double)(((long)tiles + (long)slots - 1) / (long)slots) : tiles < slots ? 1.0 : tiles / slots + 0.5;
+    const double box = pair ? bn / 2 : bn, rows = run / per_run / (pair ? 2 : 1);
+    const double staged = p.offsets && box > 2 * FP8G_TAIL_BOX && rows <= box / 2 ? rows : box;   // run_fp8_gemm: p.tail
+    const double clocks = waves * ((steps + split - 1) / split * 4 * (256 + staged + rows) + (pair ? 1500 : 700)) +
+                          (pair ? 5000 : split > 1 ? 2500 : 0);
+    if (clocks < best_cost) best_cost = clocks, best = Fp8Plan{pair, bn, split};
+  };
+  for (int bn = 16; bn <= 128; bn *= 2) {
+    consider(false, bn, 1);
+    for (int split = 2; split <= 8 && split <= steps; split *= 2) consider(false, bn, split);
+    if (bn >= run) break;
+  }
+  for (int bn = 128; bn <= 256; bn += 32)
+    if (p.M > 64) consider(true, bn, 1);
+  return best;
+}
+
 static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
-  CUtensorMap tw, tx, txs;
-  if (int rc = make_tmap_i8(p.w, (long)p.E * p.N, p.K, FP8G_BM, &tw)) return rc;
-  if (int rc = make_tmap_i8(p.x, p.M, p.K, FP8G_X_ROWS, &tx)) return rc;
-  if (int rc = make_tmap_i8(p.x, p.M, p.K, FP8G_X_SMALL, &txs)) return rc;
-  p.x_words = (p.ks & 3) == 0 && (reinterpret_cast<uintptr_t>(p.x_scale) & 3) == 0;
-  p.split = 1;
+  const int steps = (p.ks + 3) / 4;
+  Fp8Plan plan = plan_fp8_gemm(p);
+  const bool pair = plan.pair;
+  p.bn = plan.bn;
+  p.split = plan.split;
   p.band = 16;
   // tiles at most: an expert's run ends in one part tile, and no more experts than rows have any
-  auto tiles_of = [&](int bn, int bch) {
-    const long tok = p.offsets ? (long)p.M / bn + (p.E < p.M ? p.E : p.M) : ((long)p.M + bn - 1) / bn;
-    return tok * ((p.N + bch - 1) / bch);
-  };
-  const long tiles = tiles_of(128, 128), pair_tiles = tiles_of(256, 256);
-  const bool pair = pair_tiles >= sm_count() / 2;
+  const long tok_tiles = p.offsets ? (long)p.M / p.bn + (p.E < p.M ? p.E : p.M) : ((long)p.M + p.bn - 1) / p.bn;
+  const long tiles = tok_tiles * ((p.N + (pair ? 255 : 127)) / (pair ? 256 : 128));
+  const int box = pair ? p.bn / 2 : p.bn;
+  p.stage_bytes = FP8G_W_BYTES + box * FP8G_BK;
+  p.stages = FP8G_RING_BYTES / p.stage_bytes < FP8G_MAX_STAGES ? FP8G_RING_BYTES / p.stage_bytes : FP8G_MAX_STAGES;
+  // The tensor cores cut the running sum off instead of rounding it, and the error grows with the number of additions:
+  // against 64 bits, 4e-7 of the result at 4096 features and 2.3e-6 at 14336.  An fp32 output is summed in chunks of
+  // 4096 features, the chunks added in fp32 by the epilogue; in a bf16 output (2e-3) none of it shows.
+  p.chunk = (y_dtype == STAMP_F32 && p.split == 1) ? 8 : steps;
+  p.x_words = (p.ks & 3) == 0 && (reinterpret_cast<uintptr_t>(p.x_scale) & 3) == 0;
+  CUtensorMap tw, tx, txt;
+  if (int rc = make_tmap_i8(p.w, (long)p.E * p.N, p.K, FP8G_BM, &tw)) return rc;
+  if (int rc = make_tmap_i8(p.x, p.M, p.K, box, &tx)) return rc;
+  // Runs end anywhere: where a tile's rows fill half a box or less, copies of 32 rows bring fewer that are not used.  (In
+  // place of whole boxes everywhere they cost: 8192 x 4096 x 4096 99 -> 105 us.)
+  p.tail = p.offsets && box > 2 * FP8G_TAIL_BOX ? box / 2 : 0;
+  txt = tx;
+  if (p.tail)
+    if (int rc = make_tmap_i8(p.x, p.M, p.K, FP8G_TAIL_BOX, &txt)) return rc;
   if (pair)
-    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16>(tw, tx, txs, p, pair_tiles, st)
-                                 : launch_fp8_gemm<true, float>(tw, tx, txs, p, pair_tiles, st);
-  const int steps = (p.ks + 3) / 4;
-  while (p.split < 8 && tiles * p.split * 2 <= sm_count() && p.split * 2 <= steps) p.split *= 2;
-  return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16>(tw, tx, txs, p, tiles, st)
-                               : launch_fp8_gemm<false, float>(tw, tx, txs, p, tiles, st);
+    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16>(tw, tx, txt, p, tiles, st)
+                                 : launch_fp8_gemm<true, float>(tw, tx, txt, p, tiles, st);
+  return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16>(tw, tx, txt, p, tiles, st)
+                               : launch_fp8_gemm<false, float>(tw, tx, txt, p, tiles, st);
 }
 
 // Arguments common to both products.
@@ -1810,8 +1890,8 @@ int stamp_fp8_quantize(const void* X, int x_dtype, long long ldx, const int32_t*
   if (!X || !codes || !scale || !aligned16(X) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
   if (ldx % (x_dtype == STAMP_BF16 ? 8 : 4) != 0) return STAMP_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (x_dtype == STAMP_BF16) return launch_fp8_quant<__nv_bfloat16, false>(X, ldx, rows, T, M, K, codes, scale, st);
-  return launch_fp8_quant<float, false>(X, ldx, rows, T, M, K, codes, scale, st);
+  if (x_dtype == STAMP_BF16) return launch_fp8_quant<__nv_bfloat16>(X, ldx, rows, T, M, K, codes, scale, st);
+  return launch_fp8_quant<float>(X, ldx, rows, T, M, K, codes, scale, st);
 }
 
 int stamp_fp8_gated_quantize(const void* X, int x_dtype, long long ldx, int M, int F, void* codes, void* scale,
@@ -1823,8 +1903,8 @@ int stamp_fp8_gated_quantize(const void* X, int x_dtype, long long ldx, int M, i
   if (!X || !codes || !scale || !aligned16(X) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
   if (ldx % (x_dtype == STAMP_BF16 ? 8 : 4) != 0) return STAMP_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (x_dtype == STAMP_BF16) return launch_fp8_quant<__nv_bfloat16, true>(X, ldx, nullptr, M, M, F, codes, scale, st);
-  return launch_fp8_quant<float, true>(X, ldx, nullptr, M, M, F, codes, scale, st);
+  if (x_dtype == STAMP_BF16) return launch_fp8_gated_quant<__nv_bfloat16>(X, ldx, M, F, codes, scale, st);
+  return launch_fp8_gated_quant<float>(X, ldx, M, F, codes, scale, st);
 }
 
 int stamp_fp8_quantize_weights(const void* W, int w_dtype, int E, int N, int K, void* codes, void* scale, void* stream) {
