@@ -5,12 +5,14 @@ call fails, an exception is raised."""
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 from typing import Optional
 
 import torch
 
-from .build import LIB_PATH
+from .build import CALLS_PATH, LIB_PATH
 
 STAMP_OK = 0
 F32, BF16 = 0, 1
@@ -70,12 +72,6 @@ def lib() -> ctypes.CDLL:
         _lib.stamp_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
             getattr(_lib, name)
-        p, i, n = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong
-        _lib.stamp_fp8_quantize.argtypes = (p, i, n, p, i, i, i, p, p, p)
-        _lib.stamp_fp8_gated_quantize.argtypes = (p, i, n, i, i, p, p, p)
-        _lib.stamp_fp8_quantize_weights.argtypes = (p, i, i, i, i, p, p, p)
-        _lib.stamp_fp8_linear.argtypes = (p, p, p, p, p, i, i, i, p, i, p)
-        _lib.stamp_fp8_linear_grouped.argtypes = (p, p, p, p, p, p, i, i, i, i, p, i, p)
     return _lib
 
 
@@ -226,74 +222,49 @@ def stamp_linear_fused(cfg: StampConfig, X: torch.Tensor, w: torch.Tensor, w_for
     return Y
 
 
-# The calls of the block-scaled layers are a few microseconds of device time for single tokens, so their marshalling is
-# kept short: argument types are declared once (lib()), addresses are passed as integers, new outputs are not checked.
+# The block-scaled layers' calls take a few microseconds for single tokens, so csrc/torch_calls.cpp does their marshalling
+# (checks, outputs, stream); everything else about them is as for the calls above.
+_calls = None
+
+
+def calls():
+    """Load the marshalling module (built in-tree by paper_2510_26771_b200.build)."""
+    global _calls
+    if _calls is None:
+        lib()
+        if not os.path.exists(CALLS_PATH):
+            raise RuntimeError(f"marshalling module not built: {CALLS_PATH} is missing "
+                               "(run `python -m paper_2510_26771_b200.build`); there is no fallback path")
+        loader = importlib.machinery.ExtensionFileLoader("_torch_calls", CALLS_PATH)
+        spec = importlib.util.spec_from_file_location("_torch_calls", CALLS_PATH, loader=loader)
+        module = importlib.util.module_from_spec(spec)
+        loader.exec_module(module)
+        _calls = module
+    return _calls
+
+
+def _outputs(result, what: str):
+    """What a call returned, unless that is a status."""
+    if type(result) is int:
+        raise StampError(result, what)
+    return result
+
 
 def _fp8_blocks(n: int) -> int:
     return (n + FP8_BLOCK - 1) // FP8_BLOCK
 
 
-def _fp8_stream(t: torch.Tensor) -> int:
-    """Handle of the current stream of the tensor's device (torch.cuda.current_stream() builds an object around it)."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
-
-
-def _fp8_arg(t: torch.Tensor, what: str, shape, dtype) -> int:
-    """Address of a dense CUDA tensor of this shape and type."""
-    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous CUDA tensor of shape {tuple(shape)} and type {dtype}, "
-                         f"got {tuple(t.shape)}, {t.dtype} on {t.device}")
-    return t.data_ptr()
-
-
-def _fp8_rows(X: torch.Tensor):
-    """Rows, features, and the distance of two rows, of a CUDA matrix whose rows are dense (a slice of columns of a wider
-    one is fine)."""
-    if X.dim() != 2 or not X.is_cuda:
-        raise ValueError("expected a two-dimensional CUDA tensor")
-    rows, features = X.shape
-    ld, step = X.stride()
-    if step != 1 and features > 1:
-        raise ValueError("expected dense rows")
-    return rows, features, ld if rows > 1 else features
-
-
-def _fp8_outputs(X: torch.Tensor, M: int, K: int, codes, scale):
-    """Codes and scales to write, and their addresses."""
-    if codes is None:
-        codes = X.new_empty((M, K), dtype=FP8_CODES)
-        cp = codes.data_ptr()
-    else:
-        cp = _fp8_arg(codes, "codes", (M, K), FP8_CODES)
-    if scale is None:
-        scale = X.new_empty((M, _fp8_blocks(K)), dtype=FP8_SCALE)
-        sp = scale.data_ptr()
-    else:
-        sp = _fp8_arg(scale, "scale", (M, _fp8_blocks(K)), FP8_SCALE)
-    return codes, cp, scale, sp
-
-
 def stamp_fp8_quantize(X: torch.Tensor, rows: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
                        scale: Optional[torch.Tensor] = None):
     """[T, K] activations -> (codes [M, K], scale [M, ceil(K / 128)]); rows [M] int32: which row of X each output row is
-    (M = T and every row itself without it).  codes, scale: buffers to write instead of new ones."""
-    T, K, ld = _fp8_rows(X)
-    M = T if rows is None else rows.numel()
-    codes, cp, scale, sp = _fp8_outputs(X, M, K, codes, scale)
-    rp = None if rows is None else _fp8_arg(rows, "rows", (M,), torch.int32)
-    _check(lib().stamp_fp8_quantize(X.data_ptr(), _dtype_code(X), ld, rp, T, M, K, cp, sp, _fp8_stream(X)), "stamp_fp8_quantize")
-    return codes, scale
+    (M = T and every row itself without it).  X may be a slice of columns of a wider matrix.  codes, scale: buffers to
+    write instead of new ones."""
+    return _outputs((_calls or calls()).fp8_quantize(X, rows, codes, scale), "stamp_fp8_quantize")
 
 
 def stamp_fp8_gated_quantize(X: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """[M, 2 F] gates and ups -> (codes [M, F], scale [M, ceil(F / 128)]) of silu(gate) * up."""
-    M, F2, ld = _fp8_rows(X)
-    F = F2 // 2
-    if F2 != 2 * F:
-        raise ValueError("expected as many gates as ups")
-    codes, cp, scale, sp = _fp8_outputs(X, M, F, codes, scale)
-    _check(lib().stamp_fp8_gated_quantize(X.data_ptr(), _dtype_code(X), ld, M, F, cp, sp, _fp8_stream(X)), "stamp_fp8_gated_quantize")
-    return codes, scale
+    return _outputs((_calls or calls()).fp8_gated_quantize(X, codes, scale), "stamp_fp8_gated_quantize")
 
 
 def stamp_fp8_quantize_weights(W: torch.Tensor):
@@ -308,28 +279,11 @@ def stamp_fp8_quantize_weights(W: torch.Tensor):
     return codes, scale
 
 
-def _fp8_product_out(x: torch.Tensor, M: int, N: int, out_dtype, out):
-    """The output, its address and its type code."""
-    if out is None:
-        out = x.new_empty((M, N), dtype=out_dtype)
-        return out, out.data_ptr(), _dtype_code(out)
-    return out, _fp8_arg(out, "out", (M, N), out.dtype), _dtype_code(out)
-
-
 def stamp_fp8_linear(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
                      bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Codes [M, K] times weight codes [N, K] -> [M, N]; bias [N] float32."""
-    M, K = x.shape
-    N = w.shape[0]
-    blocks = _fp8_blocks(K)
-    Y, yp, yd = _fp8_product_out(x, M, N, out_dtype, out)
-    _check(lib().stamp_fp8_linear(
-        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, blocks), FP8_SCALE),
-        _fp8_arg(w, "w", (N, K), FP8_CODES), _fp8_arg(w_scale, "w_scale", (_fp8_blocks(N), blocks), FP8_SCALE),
-        None if bias is None else _fp8_arg(bias, "bias", (N,), torch.float32), M, N, K, yp, yd, _fp8_stream(x)),
-        "stamp_fp8_linear")
-    return Y
+    return _outputs((_calls or calls()).fp8_linear(x, x_scale, w, w_scale, bias, out_dtype, out), "stamp_fp8_linear")
 
 
 def stamp_fp8_linear_grouped(x: torch.Tensor, x_scale: torch.Tensor, offsets: torch.Tensor, w: torch.Tensor,
@@ -338,17 +292,8 @@ def stamp_fp8_linear_grouped(x: torch.Tensor, x_scale: torch.Tensor, offsets: to
     """Codes [M, K] in expert order times the weight codes [E, N, K] of each row's expert -> [M, N].  offsets [E + 1]
     int32 on the device: expert e's rows are offsets[e] .. offsets[e + 1] - 1; rows from offsets[E] on are not written.
     bias [E, N] float32."""
-    M, K = x.shape
-    E, N = w.shape[0], w.shape[1]
-    blocks = _fp8_blocks(K)
-    Y, yp, yd = _fp8_product_out(x, M, N, out_dtype, out)
-    _check(lib().stamp_fp8_linear_grouped(
-        _fp8_arg(x, "x", (M, K), FP8_CODES), _fp8_arg(x_scale, "x_scale", (M, blocks), FP8_SCALE),
-        _fp8_arg(offsets, "offsets", (E + 1,), torch.int32), _fp8_arg(w, "w", (E, N, K), FP8_CODES),
-        _fp8_arg(w_scale, "w_scale", (E, _fp8_blocks(N), blocks), FP8_SCALE),
-        None if bias is None else _fp8_arg(bias, "bias", (E, N), torch.float32), M, E, N, K, yp, yd, _fp8_stream(x)),
-        "stamp_fp8_linear_grouped")
-    return Y
+    return _outputs((_calls or calls()).fp8_linear_grouped(x, x_scale, offsets, w, w_scale, bias, out_dtype, out),
+                    "stamp_fp8_linear_grouped")
 
 
 def stamp_workspace_bytes_host(cfg: StampConfig, B: int, L: int, K: int, N: int, x_dtype: int, y_dtype: int) -> int:

@@ -1,4 +1,5 @@
-"""Build the CUDA library in-tree: csrc/*.cu -> paper_2510_26771_b200/libstamp.so (sm_100a only)."""
+"""Build the CUDA library in-tree: csrc/*.cu -> paper_2510_26771_b200/libstamp.so (sm_100a only), and beside it the
+Python module that marshals the block-scaled layers' calls: csrc/torch_calls.cpp -> _torch_calls.so (host code only)."""
 from __future__ import annotations
 
 import os
@@ -9,24 +10,50 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 _CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libstamp.so")
+CALLS_PATH = os.path.join(_PKG, "_torch_calls.so")
 
 
 def _sources():
     srcs = [os.path.join(_CSRC, "stamp_api.cu")]
-    deps = [os.path.join(_CSRC, f) for f in sorted(os.listdir(_CSRC))] + [os.path.join(_ROOT, "include", "stamp.h")]
-    return srcs, deps
+    deps = [os.path.join(_CSRC, f) for f in sorted(os.listdir(_CSRC)) if not f.endswith(".cpp")]
+    return srcs, deps + [os.path.join(_ROOT, "include", "stamp.h")]
+
+
+def _older(path: str, deps) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps)
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB_PATH):
-        return True
-    t = os.path.getmtime(LIB_PATH)
-    return any(os.path.getmtime(d) > t for d in _sources()[1])
+    return _older(LIB_PATH, _sources()[1])
+
+
+def build_calls(force: bool = False) -> str:
+    """Compile the marshalling module against torch's headers and the library (built before)."""
+    import sysconfig
+
+    import torch
+    src = os.path.join(_CSRC, "torch_calls.cpp")
+    if not force and not _older(CALLS_PATH, [src, os.path.join(_ROOT, "include", "stamp.h")]):
+        return CALLS_PATH
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    tmp = CALLS_PATH + f".tmp{os.getpid()}"
+    subprocess.check_call(
+        [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         "-I", os.path.join(_ROOT, "include"), "-isystem", os.path.join(base, "include"),
+         "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+         "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(cuda, "include"), "-o", tmp, src,
+         "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+         "-L", _PKG, "-l:libstamp.so", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, CALLS_PATH)
+    return CALLS_PATH
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile with nvcc for sm_100a.  Returns the path of the shared library."""
     if not force and not needs_build():
+        build_calls()
         return LIB_PATH
     srcs, _ = _sources()
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
@@ -39,6 +66,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         cmd.insert(2, "-v")
     subprocess.check_call(cmd)
     os.replace(tmp, LIB_PATH)
+    build_calls(force)
     return LIB_PATH
 
 

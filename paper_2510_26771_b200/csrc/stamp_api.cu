@@ -1336,7 +1336,7 @@ struct Fp8Plan {
   int bn, split;
 };
 static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
-  const int steps = (p.ks + 3) / 4;
+  const int steps = (p.ks + 3) / 4, sms = sm_count();
   // runs that have rows, and their length: of the experts nothing is known here but how many rows they share
   const double runs = p.offsets ? (p.E < p.M ? p.E : p.M) : 1, run = p.M / runs;
   Fp8Plan best{false, 128, 1};
@@ -1345,7 +1345,7 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
     // tiles of a run: whole for a single matrix; runs of unknown lengths end in half a tile on average
     const double per_run = !p.offsets ? (p.M + bn - 1) / bn : run <= bn / 2 ? 1.0 : run / bn + 0.5;
     const double tiles = runs * per_run * ((p.N + (pair ? 255 : 127)) / (pair ? 256 : 128));
-    const double slots = sm_count() / (pair ? 2 : split);
+    const double slots = sms / (pair ? 2 : split);
     if (split > 1 && tiles > slots) return;   // (a cluster that splits a sum takes one tile: a second round starts from nothing)
     const double waves = !p.offsets ? (double)(((long)tiles + (long)slots - 1) / (long)slots) : tiles < slots ? 1.0 : tiles / slots + 0.5;
     const double box = pair ? bn / 2 : bn, rows = run / per_run / (pair ? 2 : 1);
