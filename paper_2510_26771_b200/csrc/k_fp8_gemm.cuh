@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
         const int pieces = mine <= p.tail ? (mine + FP8G_TAIL_BOX - 1) / FP8G_TAIL_BOX : 0;
         const uint32_t bytes = pieces ? FP8G_W_BYTES + pieces * (FP8G_TAIL_BOX * FP8G_BK) : p.stage_bytes;
         for (int kb = kb0; kb < kb1; ++kb) {
-          if (!ptx::mbar_wait_bounded(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT)) {
+          if (!ptx::mbar_wait_bounded_sleepy(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT)) {
             ok = false;
             break;
           }
@@ -378,8 +378,9 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       const uint8_t* wsc = p.w_scale + (static_cast<long>(t.expert) * ch_blocks + cb) * p.ks;
       const uint8_t* xsc = p.x_scale + static_cast<long>(t.row0) * p.ks;
       // Rows of scale bytes on word boundaries: one load per step.  Otherwise the two aligned words that hold the bytes,
-      // where both are sure to lie within the scales (four rows of this table before and after), or byte by byte.
-      const int mode = p.x_words ? 0 : (t.row0 >= 4 && t.row0 + t.rows + 4 <= p.M) ? 1 : 2;
+      // where both are sure to lie within the scales (their eight bytes start at most three bytes before the first one
+      // wanted: four rows of the table before the tile's and eight behind them are enough), or byte by byte.
+      const int mode = p.x_words ? 0 : (t.row0 >= 4 && t.row0 + t.rows + 8 <= p.M) ? 1 : 2;
       // All loads of a step are issued before the first is used; they are in flight while the step waits for its slot.
       uint32_t ww, xw[BN / 32];
       auto load = [&](int s) {
@@ -454,7 +455,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       if (p.bias && ch < p.N) bias = __ldg(p.bias + static_cast<long>(t.expert) * p.N + ch);
       for (int c0 = step0; c0 < step1; c0 += p.chunk, ++it) {
         const int a = it & 1;
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
           ok = false;
           break;
         }

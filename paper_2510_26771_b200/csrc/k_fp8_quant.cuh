@@ -160,7 +160,10 @@ __device__ __forceinline__ void fp8_quantize_block(const float (&v)[2][8], Fp8Pl
 //   rows    [M] source row of every output row, or nullptr for row m itself; an index outside [0, T) gives a row of
 //           zeros and raises the device status word
 //   codes   [M, K], scale [M, ks]
-// A thread loads its part of U blocks, 128 bytes, before it uses the first.
+// A thread loads its part of U blocks, 128 bytes, before it uses the first.  Bound by memory: 16384 x 14336 in 107 us, the
+// copy rate (64 bytes in flight: 118 us).  Where the rows come from L2 -- 16384 rows dispatched from 4096 tokens of 2048
+// features, 12.1 us -- the instructions count as well, 8.5 a feature; four lanes to a block and half the blocks take
+// fewer, but also fewer warps fit: 12.7 and 111 us.
 template <typename TIn>
 __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_quant(const TIn* __restrict__ X, long ld, const int* __restrict__ rows, int T,
                                                             int K, unsigned ks, unsigned magic, unsigned groups,
@@ -200,9 +203,11 @@ __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_quant(const TIn* __restric
 }
 
 // Behind a gated activation: X [M, ld] rows of K gates and K ups -> codes [M, K], scale [M, ks] of silu(gate) * up.
-// The arithmetic (about 14 instructions per feature, two of them on the special function unit) takes two thirds of the
-// time that the memory traffic does, and many resident warps overlap the two best: copies through shared memory, three
-// blocks ahead, cost 3 % more than loads to registers (16384 x 4096), two sets of registers in turn 7 %.
+// 16384 x 4096 in 61.5 us, 84 % of the copy rate: the arithmetic (17 instructions a feature, two on the special function
+// unit, which is busy 58 % of the time) and the loads overlap across resident warps only.  One block at a time, because
+// more warps fit then: two blocks 70 us.  Copies through shared memory three blocks ahead, or two sets of registers in
+// turn, cost more instructions or warps than they hide (3 % and 7 %); expf and the IEEE division in place of
+// gated_silu2: 92 us.
 template <typename TIn>
 __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_gated_quant(const TIn* __restrict__ X, long ld, int K, unsigned ks, unsigned magic,
                                                                   unsigned groups, uint8_t* __restrict__ codes,
