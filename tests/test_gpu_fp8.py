@@ -512,6 +512,50 @@ def test_offsets_past_32_bits(st):
     assert bool((y[:1000] == 0).all())
 
 
+def load_example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "fp8_expert_layer.py")
+    spec = importlib.util.spec_from_file_location("fp8_expert_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    return example
+
+
+@pytest.mark.parametrize("tokens", [1, 300])
+def test_the_example_layer_against_the_plain_chain(st, tokens):
+    """The calls in the order an expert layer makes them, against the same chain in 64 bits.  The first product is rounded
+    to bf16: its fp32 error, K 2^-23 sum |terms| at most (K = 400, the sum about ten times the result: 5e-4), moves at most
+    5e-4 / 2^-8 = 12 % of the values by one bf16 step, and one in sixteen of those moves a code by one step of 2^-3:
+    sqrt(0.12 / 16) 2^-3 = 1.1e-2 of the hidden values' norm, and as much of the output's, is the most that can be left."""
+    import torch
+    example = load_example()
+    layer = example.ExpertLayer(400, 640, 6, 2)
+    x = torch.randn(tokens, 400, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").bfloat16()
+    got = layer(x).double().cpu().numpy()
+    rows, place, offsets, share = layer.route(x)
+    ends = offsets.tolist()
+    c, s = plain_quantize(x.double().cpu().numpy()[rows.cpu().numpy()])
+    xv = c * np.repeat(s, BLOCK, axis=1)[:, :400]
+    up, down = values(layer.up_codes, layer.up_scale, True), values(layer.down_codes, layer.down_scale, True)
+    y = np.zeros((len(xv), 400))
+    for e in range(6):
+        run = slice(ends[e], ends[e + 1])
+        h = torch.from_numpy(xv[run] @ up[e].T).to(torch.bfloat16).double().numpy()
+        h = h[:, :640] / (1 + np.exp(-h[:, :640])) * h[:, 640:]
+        if len(h):
+            c, s = plain_quantize(h)
+            y[run] = (c * np.repeat(s, BLOCK, axis=1)[:, :640]) @ down[e].T
+    want = (y[place.cpu().numpy()].reshape(tokens, 2, 400) * share.double().cpu().numpy()[:, :, None]).sum(axis=1)
+    # (rounding the output to bf16: 2^-8 of a value at most, less than 2^-9 of the norm)
+    assert np.linalg.norm(got - want) <= (1.1e-2 + 2.0 ** -9) * np.linalg.norm(want)
+
+
+def test_the_example_runs():
+    r = load_example().main(["--tokens", "200", "--features", "272", "--hidden", "256", "--experts", "4", "--top", "2", "--steps", "2"])
+    assert np.isfinite(r["prompt_error"]) and len(r["step_errors"]) == 2
+
+
 # ------------------------------------------------------------------------------------------ refusals
 def test_arguments_are_checked(st):
     import torch
