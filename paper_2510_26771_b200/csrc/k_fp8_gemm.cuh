@@ -243,9 +243,11 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
     if (ptx::elect_one()) {
+      // barriers and stages by their shared-memory addresses; PAIR: all copies of the pair are counted on the even CTA's
+      const uint32_t full0 = PAIR ? ptx::mapa(ptx::smem_u32(full), 0u) : ptx::smem_u32(full), ring = ptx::smem_u32(smem);
+      uint32_t dst = ring, phase = 0, issued = 0;
       int stage = 0;
-      uint32_t phase = 0, armed = 0, armed_parity = 0;
-      bool ok = true;
+      bool ok = true, ready = false;   // ready: the next stage was seen to be free
       for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
         const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
         const int mine = PAIR ? t.n / 2 : t.n;   // token rows this CTA stages (copies bring whole boxes: more, not used)
@@ -254,58 +256,53 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
         const int pieces = mine <= p.tail ? (mine + FP8G_TAIL_BOX - 1) / FP8G_TAIL_BOX : 0;
         const uint32_t bytes = pieces ? FP8G_W_BYTES + pieces * (FP8G_TAIL_BOX * FP8G_BK) : p.stage_bytes;
         for (int kb = kb0; kb < kb1; ++kb) {
-          if (!ptx::mbar_wait_bounded_sleepy(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT)) {
+          if (!ready && !ptx::mbar_wait_bounded_sleepy(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT)) {
             ok = false;
             break;
           }
-          uint8_t* ws = smem + stage * p.stage_bytes;
-          uint8_t* xs = ws + FP8G_W_BYTES;
-          if constexpr (PAIR) {
-            // all copies of the pair are counted on the even CTA's barrier
-            const uint32_t bar0 = ptx::mapa(ptx::smem_u32(&full[stage]), 0u);
-            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * bytes);
-            ptx::tma_load_2d_pair(ws, &tmap_w, bar0, kb * FP8G_BK, wrow);
-            if (pieces == 0) ptx::tma_load_2d_pair(xs, &tmap_x, bar0, kb * FP8G_BK, xrow);
-            for (int i = 0; i < pieces; ++i)
-              ptx::tma_load_2d_pair(xs + i * (FP8G_TAIL_BOX * FP8G_BK), &tmap_x_tail, bar0, kb * FP8G_BK, xrow + i * FP8G_TAIL_BOX);
-          } else {
-            ptx::mbar_arrive_expect_tx(&full[stage], bytes);
-            ptx::tma_load_2d(ws, &tmap_w, &full[stage], kb * FP8G_BK, wrow);
-            if (pieces == 0) ptx::tma_load_2d(xs, &tmap_x, &full[stage], kb * FP8G_BK, xrow);
-            for (int i = 0; i < pieces; ++i)
-              ptx::tma_load_2d(xs + i * (FP8G_TAIL_BOX * FP8G_BK), &tmap_x_tail, &full[stage], kb * FP8G_BK, xrow + i * FP8G_TAIL_BOX);
-          }
-          armed |= 1u << stage;
-          armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
+          const uint32_t bar = full0 + 8u * stage, ws = dst, xs = dst + FP8G_W_BYTES;
+          if (!PAIR || rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], PAIR ? 2 * bytes : bytes);
+          ++issued;
+          dst += p.stage_bytes;
           if (++stage == p.stages) {
             stage = 0;
             phase ^= 1u;
+            dst = ring;
           }
+          ready = ptx::mbar_test_wait(&empty[stage], phase ^ 1u);   // answered while the copies are issued
+          ptx::tma_load_2d_at<PAIR>(ws, &tmap_w, bar, kb * FP8G_BK, wrow);
+          if (pieces == 0) ptx::tma_load_2d_at<PAIR>(xs, &tmap_x, bar, kb * FP8G_BK, xrow);
+          for (int i = 0; i < pieces; ++i)
+            ptx::tma_load_2d_at<PAIR>(xs + i * (FP8G_TAIL_BOX * FP8G_BK), &tmap_x_tail, bar, kb * FP8G_BK, xrow + i * FP8G_TAIL_BOX);
         }
       }
       if (!ok) {
         *abort_word = 1;
         raise_device_status(STAMP_ERR_TIMEOUT);
-        for (int s = 0; s < p.stages; ++s)   // let the copies in flight land before the shared memory goes away
-          if (armed & (1u << s)) {
-            const long long t0 = clock64();
-            // (the odd CTA of a pair has no barrier of its own to watch: it just gives its copies the time)
-            while (((PAIR && rank != 0) || !ptx::mbar_try_wait(&full[s], (armed_parity >> s) & 1u)) && clock64() - t0 < 2000000LL) {
-            }
+        // let the copies in flight land before the shared memory goes away: the last fill of every stage
+        for (uint32_t s = 0; s < static_cast<uint32_t>(p.stages) && s < issued; ++s) {
+          const uint32_t parity = (issued - 1 - s) / p.stages & 1u;
+          const long long t0 = clock64();
+          // (the odd CTA of a pair has no barrier of its own to watch: it just gives its copies the time)
+          while (((PAIR && rank != 0) || !ptx::mbar_try_wait(&full[s], parity)) && clock64() - t0 < 2000000LL) {
           }
+        }
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (PAIR: the even CTA's, for both)
     if ((!PAIR || rank == 0) && ptx::elect_one()) {
       constexpr uint32_t idesc0 = ptx::make_mxf8_idesc(PAIR ? 2 * FP8G_BM : FP8G_BM);
+      // the ring's stages by the lower words of their weight descriptors; the token rows lie FP8G_W_BYTES further
+      const uint32_t first_low = ptx::sw128_desc_low(ptx::smem_u32(smem)), low_step = static_cast<uint32_t>(p.stage_bytes) >> 4;
+      uint32_t low = first_low, phase = 0, scount = 0;
       int stage = 0, it = 0;
-      uint32_t phase = 0, scount = 0;
-      bool ok = true;
+      bool ok = true, ready = false;   // ready: the operands of the next 128 features were seen to have arrived
       for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
-        const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+        const int n = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles).n;
+        const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, n, 0);
+        int in_chunk = 0;   // steps that are in the accumulator already
         for (int s = step0; s < step1 && ok; ++s, ++scount) {
-          const int in_chunk = (s - step0) % p.chunk;   // steps that are in the accumulator already
           const int a = it & 1;
           // The scale words of this step, and their tensor-memory columns: two buffers, so the MMAs of the step before
           // the last have to be through (they are, long before the last one's are: the queue stays filled).
@@ -320,8 +317,8 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
           const uint32_t sfs = ptx::smem_u32(smem + SM::SF_OFFSET + slot * SM::SF_SLOT);
           const uint32_t sfa = tmem_base + SM::SF_COL + (scount & 1u) * SM::SF_COLS, sfb = sfa + 4;
           ptx::tmem_copy_scales<PAIR>(sfa, ptx::make_rows16_desc(sfs));
-          for (int h = 0; h * 128 < t.n; ++h)
-            ptx::tmem_copy_scales<PAIR>(sfb + 4 * h, ptx::make_rows16_desc(sfs + 512 + 512 * h));
+          ptx::tmem_copy_scales<PAIR>(sfb, ptx::make_rows16_desc(sfs + 512));
+          if (PAIR && n > 128) ptx::tmem_copy_scales<PAIR>(sfb + 4, ptx::make_rows16_desc(sfs + 1024));
           if (in_chunk == 0) {
             // PAIR: the columns shared with the previous accumulator are drained (which implies that everything of the
             // one before it is); otherwise this accumulator's previous contents are
@@ -331,30 +328,31 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
             ptx::tc_fence_after();
           }
           const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(a * SM::ACC1);
-          const int last = min(4 * s + 4, num_kb);
-          for (int kb = 4 * s; kb < last; ++kb) {
-            if (!ptx::mbar_wait_bounded(&full[stage], phase, abort_word, FP8G_WAIT_LIMIT)) {
+          const int blocks = min(4, num_kb - 4 * s);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            if (b >= blocks) break;
+            if (!ready && !ptx::mbar_wait_bounded(&full[stage], phase, abort_word, FP8G_WAIT_LIMIT)) {
               ok = false;
               break;
             }
             ptx::tc_fence_after();
-            const uint32_t wa = ptx::smem_u32(smem + stage * p.stage_bytes);
-            const uint32_t xa = wa + FP8G_W_BYTES;
-            const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, t.n, static_cast<uint32_t>(kb & 3));
-#pragma unroll
-            for (int k = 0; k < FP8G_BK / 32; ++k)
-              ptx::mma_mxf8_ss<PAIR>(tmem_d, ptx::make_kmajor_sw128_desc(wa + k * 32), ptx::make_kmajor_sw128_desc(xa + k * 32),
-                                     idesc, sfa, sfb, (in_chunk > 0 || kb > 4 * s || k > 0) ? 1u : 0u);
-            if constexpr (PAIR) ptx::tc_commit_pair(&empty[stage], 3); else ptx::tc_commit(&empty[stage]);
+            const uint32_t w_low = low, used = ptx::smem_u32(&empty[stage]);
+            low += low_step;
             if (++stage == p.stages) {
               stage = 0;
               phase ^= 1u;
+              low = first_low;
             }
+            ready = ptx::mbar_test_wait(&full[stage], phase);   // answered while the instructions are issued
+            ptx::mma_mxf8_128<PAIR>(tmem_d, w_low, w_low + (FP8G_W_BYTES >> 4), idesc | (static_cast<uint32_t>(b) << 4 | static_cast<uint32_t>(b) << 29),
+                                    sfa, sfb, (in_chunk > 0 || b > 0) ? 1u : 0u, used);
           }
           if (!ok) break;
           if constexpr (PAIR) ptx::tc_commit_pair(&sfempty[slot], 3); else ptx::tc_commit(&sfempty[slot]);
-          if (in_chunk + 1 == p.chunk || s + 1 == step1) {
+          if (++in_chunk == p.chunk || s + 1 == step1) {
             if constexpr (PAIR) ptx::tc_commit_pair(&tfull[a], 3); else ptx::tc_commit(&tfull[a]);
+            in_chunk = 0;
             ++it;
           }
         }

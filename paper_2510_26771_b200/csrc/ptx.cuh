@@ -103,6 +103,19 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 
+// Whether the phase has completed, without waiting at all (try_wait may suspend the thread).
+__device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Bounded wait: spins on try_wait until the phase with the given parity completes, the
 // shared abort word becomes non-zero, or `limit_cycles` SM clocks pass.  Returns false when
 // it gave up; the caller then records the failure and unwinds without touching the data.
@@ -334,6 +347,20 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorM
       ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar_cluster_addr), "r"(c0), "r"(c1)
       : "memory");
 }
+// Either load by shared-memory address (PAIR: with a barrier of the pair's even CTA).
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_2d_at(uint32_t smem_dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
+  if constexpr (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1)
+        : "memory");
+}
 // Arrive on an mbarrier of another CTA of the cluster (address from mapa).
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
@@ -349,23 +376,46 @@ __host__ __device__ constexpr uint32_t make_mxf8_idesc(int m) {
 __device__ __forceinline__ uint32_t mxf8_idesc_with(uint32_t idesc, int n, uint32_t scale_id) {
   return idesc | (static_cast<uint32_t>(n >> 3) << 17) | (scale_id << 4) | (scale_id << 29);
 }
-// D[tmem] (+)= (A[smem] * sA[tmem]) (B[smem] * sB[tmem]), one scale per row of A, per row of B and 32 features.
+// D[tmem] (+)= (A[smem] * sA[tmem]) (B[smem] * sB[tmem]) over 128 features, one scale per row of A and of B: four
+// instructions of 32, then a commit that hands the stage back (PAIR: in both CTAs).  A and B are given by the lower words of
+// their descriptors (make_kmajor_sw128_desc; 32 bytes further in a row is 2 more), the upper one is the same for all.
+// Operands of tensor instructions end up in registers the warp shares, at some ten clocks each for a thread on its own, so
+// what is made per instruction counts: with 64-bit descriptors put together for each, 128 features took 480 clocks to
+// issue, in this form 230.
+constexpr uint32_t SW128_DESC_HIGH = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t sw128_desc_low(uint32_t smem_addr_bytes) { return ((smem_addr_bytes >> 4) & 0x3FFFu) | (1u << 16); }
 template <bool PAIR>
-__device__ __forceinline__ void mma_mxf8_ss(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t tmem_sa,
-                                            uint32_t tmem_sb, uint32_t accumulate) {
+__device__ __forceinline__ void mma_mxf8_128(uint32_t tmem_d, uint32_t a_low, uint32_t b_low, uint32_t idesc, uint32_t tmem_sa,
+                                             uint32_t tmem_sb, uint32_t accumulate, uint32_t empty_bar) {
   if constexpr (PAIR)
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
-        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb)
+        "{\n\t.reg .pred first, more;\n\t.reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n\t.reg .b32 x1, x2, x3, y1, y2, y3;\n\t"
+        "setp.ne.b32 first, %4, 0;\n\tsetp.eq.b32 more, 0, 0;\n\t"
+        "add.u32 x1, %1, 2;\n\tadd.u32 x2, %1, 4;\n\tadd.u32 x3, %1, 6;\n\tadd.u32 y1, %2, 2;\n\tadd.u32 y2, %2, 4;\n\tadd.u32 y3, %2, 6;\n\t"
+        "mov.b64 a0, {%1, %8};\n\tmov.b64 a1, {x1, %8};\n\tmov.b64 a2, {x2, %8};\n\tmov.b64 a3, {x3, %8};\n\t"
+        "mov.b64 b0, {%2, %8};\n\tmov.b64 b1, {y1, %8};\n\tmov.b64 b2, {y2, %8};\n\tmov.b64 b3, {y3, %8};\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], a0, b0, %3, [%5], [%6], first;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], a1, b1, %3, [%5], [%6], more;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], a2, b2, %3, [%5], [%6], more;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], a3, b3, %3, [%5], [%6], more;\n\t"
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%7], %9;\n\t}"
+        ::"r"(tmem_d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb), "r"(empty_bar),
+        "n"(SW128_DESC_HIGH), "h"(static_cast<uint16_t>(3))
         : "memory");
   else
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
-        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb)
+        "{\n\t.reg .pred first, more;\n\t.reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n\t.reg .b32 x1, x2, x3, y1, y2, y3;\n\t"
+        "setp.ne.b32 first, %4, 0;\n\tsetp.eq.b32 more, 0, 0;\n\t"
+        "add.u32 x1, %1, 2;\n\tadd.u32 x2, %1, 4;\n\tadd.u32 x3, %1, 6;\n\tadd.u32 y1, %2, 2;\n\tadd.u32 y2, %2, 4;\n\tadd.u32 y3, %2, 6;\n\t"
+        "mov.b64 a0, {%1, %8};\n\tmov.b64 a1, {x1, %8};\n\tmov.b64 a2, {x2, %8};\n\tmov.b64 a3, {x3, %8};\n\t"
+        "mov.b64 b0, {%2, %8};\n\tmov.b64 b1, {y1, %8};\n\tmov.b64 b2, {y2, %8};\n\tmov.b64 b3, {y3, %8};\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], a0, b0, %3, [%5], [%6], first;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], a1, b1, %3, [%5], [%6], more;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], a2, b2, %3, [%5], [%6], more;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], a3, b3, %3, [%5], [%6], more;\n\t"
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n\t}"
+        ::"r"(tmem_d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb), "r"(empty_bar),
+        "n"(SW128_DESC_HIGH)
         : "memory");
 }
 // Shared-memory descriptor of 32 rows of 16 bytes that lie one after the other (groups of eight rows 128 bytes apart,

@@ -1321,16 +1321,18 @@ static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const C
 }
 
 // Which kernel, tile height and split: the candidate whose slowest CTA is estimated to be through first, in SM clocks.
-// What a CTA spends on 128 features is its shared-memory traffic at 128 bytes a clock: the stage is written by the copies
-// and read by the instructions once, so 2 x (128 channels + rows) x 128 bytes -- a pair's CTA stages and reads half of
-// the token rows, which is why pairs of 256 x 256 are the only tiles at the tensor cores' own 512 clocks.  (Measured: 537
-// clocks for pairs of 256 rows, 455 of 128; 550 for single CTAs of 128 rows, 446 of 64.)  The waves of tiles are
-// whole, so smaller tiles win where large ones leave SMs idle in the last wave, and splitting the sum of a tile over a
-// cluster wins where there are too few tiles at all.  Device times, in us, of the choice and of the other side:
-//   16 x 4096 x 4096    tiles of 16 rows, split 4:  8.0   unsplit: 11.0
-//   512 x 4096 x 4096   128 rows:                  13.1   pairs of 256: 15.1
-//   1024 x 4096 x 4096  pairs of 256:              19.0   128 rows: 23.3
-//   8192 x 1152 x 1152  pairs of 192:              17.4   128 rows: 18.2
+// What a CTA spends on 128 features is mostly its shared-memory traffic: a stage is written by the copies and read by the
+// instructions, 128 channels and the token rows each time.  A pair's CTA stages and reads half of its tile's rows, which
+// is why pairs of 256 x 256 are the only tiles at the tensor cores' own 512 clocks; a single CTA measures 507 clocks with
+// 128 rows, 354 with 64, and from 32 down the 330 of its issue and copy loops.  Around that: what a tile costs besides, a
+// pair's later start, the exchange of a split sum.  The waves of tiles are whole, so smaller tiles win where large ones
+// leave SMs idle in the last wave, and splitting the sum of a tile over a cluster wins where there are too few tiles at
+// all.  Device times, in us, of the choice and of the other side:
+//   16 x 4096 x 4096    tiles of 16 rows, split 4:   7.6   unsplit: 8.4
+//   128 x 4096 x 4096   64 rows, unsplit:            8.9   128 rows, split 4: 10.0
+//   512 x 4096 x 4096   128 rows:                   12.3   pairs of 256: 15.0
+//   1024 x 4096 x 4096  pairs of 256:               18.9   128 rows: 21.5
+//   8192 x 1152 x 1152  128 rows:                   16.5   pairs of 256: 17.6
 struct Fp8Plan {
   bool pair;
   int bn, split;
@@ -1340,7 +1342,7 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
   // runs that have rows, and their length: of the experts nothing is known here but how many rows they share
   const double runs = p.offsets ? (p.E < p.M ? p.E : p.M) : 1, run = p.M / runs;
   Fp8Plan best{false, 128, 1};
-  double best_cost = 1e300;
+  double best_clocks = 1e300;
   auto consider = [&](bool pair, int bn, int split) {
     // tiles of a run: whole for a single matrix; runs of unknown lengths end in half a tile on average
     const double per_run = !p.offsets ? (p.M + bn - 1) / bn : run <= bn / 2 ? 1.0 : run / bn + 0.5;
@@ -1350,14 +1352,16 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
     const double waves = !p.offsets ? (double)(((long)tiles + (long)slots - 1) / (long)slots) : tiles < slots ? 1.0 : tiles / slots + 0.5;
     const double box = pair ? bn / 2 : bn, rows = run / per_run / (pair ? 2 : 1);
     const double staged = p.offsets && box > 2 * FP8G_TAIL_BOX && rows <= box / 2 ? rows : box;   // run_fp8_gemm: p.tail
-    const double clocks = waves * ((steps + split - 1) / split * 4 * (256 + staged + rows) + (pair ? 1500 : 700)) +
-                          (pair ? 5000 : split > 1 ? 2500 : 0);
-    if (clocks < best_cost) best_cost = clocks, best = Fp8Plan{pair, bn, split};
+    const double traffic = pair ? 256 + staged + rows : 200 + 1.2 * (staged + rows);
+    const double blocks = split == 1 ? p.ks : (steps + split - 1) / split * 4;
+    const double clocks = waves * (blocks * (traffic > 330 ? traffic : 330) + (pair ? 1500 : 700)) +
+                          (pair ? 5000 : split > 1 ? 2000 + 1000 * split + 15 * bn : 0);
+    if (clocks < best_clocks) best_clocks = clocks, best = Fp8Plan{pair, bn, split};
   };
   for (int bn = 16; bn <= 128; bn *= 2) {
     consider(false, bn, 1);
     for (int split = 2; split <= 8 && split <= steps; split *= 2) consider(false, bn, split);
-    if (bn >= run) break;
+    if (!p.offsets && bn >= p.M) break;   // (runs of experts may be longer than most)
   }
   for (int bn = 128; bn <= 256; bn += 32)
     if (p.M > 64) consider(true, bn, 1);
