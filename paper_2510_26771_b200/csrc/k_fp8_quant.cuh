@@ -120,28 +120,22 @@ __device__ __forceinline__ float2 gated_silu2(float2 g, float2 u) {
   return __fmul2_rn(q, u);
 }
 
-// n / ks for n below 2^31: `magic` is 2^32 / ks rounded up, so the product's upper half is the quotient or one above it.
-__device__ __forceinline__ unsigned fp8_div(unsigned n, unsigned ks, unsigned magic) {
-  unsigned q = ks == 1u ? n : __umulhi(n, magic);
-  return static_cast<int>(n - q * ks) < 0 ? q - 1u : q;
+// n / d for n below 2^31: `magic` is 2^32 / d rounded up, so the product's upper half is the quotient or one above it.
+__device__ __forceinline__ unsigned fp8_div(unsigned n, unsigned d, unsigned magic) {
+  const unsigned q = d == 1u ? n : __umulhi(n, magic);
+  return static_cast<int>(n - q * d) < 0 ? q - 1u : q;
 }
 
-// Both activation quantizers: eight lanes own one block of a row, lane l features [8 l, 8 l + 8) and [64 + 8 l, 72 + 8 l),
-// so that the eight lanes' loads and stores are contiguous; the maximum takes three shuffles.  Blocks are numbered row by
-// row, ks = ceil(K / 128) to a row, `groups` of them.  A lane without a block takes part in the shuffles only (col = K).
-struct Fp8Place {
-  unsigned row;
-  int col;   // first feature of the lane's part
+// Both activation quantizers: a warp takes a chunk of a row, four blocks at a time.  Eight lanes own one block, lane l
+// features [8 l, 8 l + 8) and [64 + 8 l, 72 + 8 l), so that the eight lanes' loads and stores are contiguous; the maximum
+// takes three shuffles.  Where a lane's features lie follows from the row and the chunk, once for all blocks of a chunk.
+struct Fp8Rows {
+  int K, ks;                 // features of a row, blocks of a row
+  unsigned chunks, magic;    // chunks of a row; fp8_div's magic for them
+  unsigned items;            // rows x chunks
 };
-__device__ __forceinline__ Fp8Place fp8_place(unsigned g, unsigned groups, int K, unsigned ks, unsigned magic) {
-  Fp8Place at{0u, K};
-  if (g < groups) {
-    at.row = fp8_div(g, ks, magic);
-    at.col = static_cast<int>(g - at.row * ks) * FP8_BLOCK + static_cast<int>(threadIdx.x & 7u) * 8;
-  }
-  return at;
-}
-__device__ __forceinline__ void fp8_quantize_block(const float (&v)[2][8], Fp8Place at, unsigned g, int K, uint8_t* codes, uint8_t* scale) {
+// One block: its codes (out: this lane's first feature, `left` features of the row from there on) and its scale.
+__device__ __forceinline__ void fp8_quantize_block(const float (&v)[2][8], int left, uint8_t* out, uint8_t* scale) {
   float largest = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; i += 2) largest = ptx::max_abs_nan(largest, v[i >> 3][i & 7], v[i >> 3][(i & 7) + 1]);
@@ -149,10 +143,11 @@ __device__ __forceinline__ void fp8_quantize_block(const float (&v)[2][8], Fp8Pl
 #pragma unroll
   for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
   const Fp8Scale s = fp8_scale(amax);
-  uint8_t* out = codes + static_cast<long>(at.row) * K + at.col;
-  if (at.col < K) *reinterpret_cast<uint2*>(out) = fp8_pack8(v[0], s.inverse);
-  if (at.col + 64 < K) *reinterpret_cast<uint2*>(out + 64) = fp8_pack8(v[1], s.inverse);
-  if ((threadIdx.x & 7u) == 0 && at.col < K) scale[g] = s.byte;
+  if (left > 0) {
+    *reinterpret_cast<uint2*>(out) = fp8_pack8(v[0], s.inverse);
+    if (left > 64) *reinterpret_cast<uint2*>(out + 64) = fp8_pack8(v[1], s.inverse);
+    if ((threadIdx.x & 7u) == 0) *scale = s.byte;
+  }
 }
 
 // Activations.
@@ -160,88 +155,96 @@ __device__ __forceinline__ void fp8_quantize_block(const float (&v)[2][8], Fp8Pl
 //   rows    [M] source row of every output row, or nullptr for row m itself; an index outside [0, T) gives a row of
 //           zeros and raises the device status word
 //   codes   [M, K], scale [M, ks]
-// A thread loads its part of U blocks, 128 bytes, before it uses the first.  Bound by memory: 16384 x 14336 in 107 us, the
-// copy rate (64 bytes in flight: 118 us).  Where the rows come from L2 -- 16384 rows dispatched from 4096 tokens of 2048
-// features, 12.1 us -- the instructions count as well, 8.5 a feature; four lanes to a block and half the blocks take
-// fewer, but also fewer warps fit: 12.7 and 111 us.
-template <typename TIn>
+// A chunk is 4 U blocks, and a thread loads its part of all of them before it uses the first.  Bound by memory: 16384 x
+// 14336 in 107 to 110 us, 97 to 100 % of the copy rate.  Where the rows come from L2 the instructions count: 16384 rows
+// dispatched from 4096 tokens of 2048 features take 9.8 us; with the place of every block found by itself, without regard to
+// rows, 12.1 us at 8.5 instructions a feature.
+template <typename TIn, int U>
 __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_quant(const TIn* __restrict__ X, long ld, const int* __restrict__ rows, int T,
-                                                            int K, unsigned ks, unsigned magic, unsigned groups,
-                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
-  constexpr int U = sizeof(TIn) == 2 ? 4 : 2;
+                                                            Fp8Rows r, uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const unsigned sub = (threadIdx.x >> 3) & 3u;
-  // a warp takes 4 U blocks in a row; all its lanes stay in the loop together, the shuffles are warp-wide
-  for (unsigned first = (blockIdx.x * (FP8Q_THREADS / 32) + (threadIdx.x >> 5)) * (4 * U); first < groups;
-       first += gridDim.x * (FP8Q_THREADS / 32) * (4 * U)) {
-    Fp8Raw<TIn> raw[U][2];
-    Fp8Place at[U];
-#pragma unroll
-    for (int b = 0; b < U; ++b) {
-      at[b] = fp8_place(first + 4 * b + sub, groups, K, ks, magic);
-      long src = at[b].row;
-      bool valid = at[b].col < K;
-      if (rows && valid) {
-        const int i = __ldg(rows + at[b].row);
-        valid = i >= 0 && i < T;
-        if (!valid) raise_device_status(STAMP_ERR_INVALID_ARG);
-        src = valid ? i : 0;
-      }
-      const TIn* p = X + src * ld + at[b].col;
-      raw[b][0].load(p, valid);
-      raw[b][1].load(p + 64, valid && at[b].col + 64 < K);
+  const int sub = (threadIdx.x >> 3) & 3, lane8 = threadIdx.x & 7;
+  for (unsigned item = blockIdx.x * (FP8Q_THREADS / 32) + (threadIdx.x >> 5); item < r.items; item += gridDim.x * (FP8Q_THREADS / 32)) {
+    const unsigned row = fp8_div(item, r.chunks, r.magic);
+    const int block = static_cast<int>(item - row * r.chunks) * (4 * U) + sub, col = block * FP8_BLOCK + lane8 * 8;
+    long src = row;
+    bool valid = true;
+    if (rows) {
+      const int i = __ldg(rows + row);
+      valid = i >= 0 && i < T;
+      if (!valid) raise_device_status(STAMP_ERR_INVALID_ARG);
+      src = valid ? i : 0;
     }
+    const TIn* p = X + src * ld + col;
+    const int left = r.K - col, have = valid ? left : 0;
+    Fp8Raw<TIn> raw[U][2];
+#pragma unroll
+    for (int b = 0; b < U; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) raw[b][h].load(p + (4 * b) * FP8_BLOCK + 64 * h, have > (4 * b) * FP8_BLOCK + 64 * h);
+    uint8_t* out = codes + static_cast<long>(row) * r.K + col;
+    uint8_t* sc = scale + static_cast<long>(row) * r.ks + block;
 #pragma unroll
     for (int b = 0; b < U; ++b) {
       float v[2][8];
       raw[b][0].values(v[0]);
       raw[b][1].values(v[1]);
-      fp8_quantize_block(v, at[b], first + 4 * b + sub, K, codes, scale);
+      fp8_quantize_block(v, left - (4 * b) * FP8_BLOCK, out + (4 * b) * FP8_BLOCK, sc + 4 * b);
     }
   }
 }
 
 // Behind a gated activation: X [M, ld] rows of K gates and K ups -> codes [M, K], scale [M, ks] of silu(gate) * up.
-// 16384 x 4096 in 61.5 us, 84 % of the copy rate: the arithmetic (17 instructions a feature, two on the special function
-// unit, which is busy 58 % of the time) and the loads overlap across resident warps only.  One block at a time, because
-// more warps fit then: two blocks 70 us.  Copies through shared memory three blocks ahead, or two sets of registers in
-// turn, cost more instructions or warps than they hide (3 % and 7 %); expf and the IEEE division in place of
-// gated_silu2: 92 us.
+// A chunk is `quads` times four blocks, one after the other.  16384 x 4096 in 60 us, 86 % of the copy rate: the arithmetic
+// (15 instructions a feature, two of them on the special function unit, which is busy 58 % of the time) and the loads
+// overlap across resident warps only, so it is one block at a time and more warps (two: 70 us against 61.5).  Copies through
+// shared memory three blocks ahead, or two sets of registers in turn, cost more instructions or warps than they hide (3 %
+// and 7 %); expf and the IEEE division in place of gated_silu2: 92 us.
 template <typename TIn>
-__global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_gated_quant(const TIn* __restrict__ X, long ld, int K, unsigned ks, unsigned magic,
-                                                                  unsigned groups, uint8_t* __restrict__ codes,
-                                                                  uint8_t* __restrict__ scale) {
+__global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_gated_quant(const TIn* __restrict__ X, long ld, Fp8Rows r, int quads,
+                                                                  uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const unsigned stride = gridDim.x * (FP8Q_THREADS / 8), sub = (threadIdx.x >> 3) & 3u;
-  // a warp's four blocks stay in the loop together
-  for (unsigned g = blockIdx.x * (FP8Q_THREADS / 8) + (threadIdx.x >> 3); g - sub < groups; g += stride) {
-    const Fp8Place at = fp8_place(g, groups, K, ks, magic);
-    const TIn* p = X + static_cast<long>(at.row) * ld + at.col;
-    Fp8Raw<TIn> gate[2], up[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      gate[h].load(p + 64 * h, at.col + 64 * h < K);
-      up[h].load(p + 64 * h + K, at.col + 64 * h < K);
-    }
-    float v[2][8];
-    auto activate = [&](auto small) {
+  const int sub = (threadIdx.x >> 3) & 3, lane8 = threadIdx.x & 7;
+  for (unsigned item = blockIdx.x * (FP8Q_THREADS / 32) + (threadIdx.x >> 5); item < r.items; item += gridDim.x * (FP8Q_THREADS / 32)) {
+    const unsigned row = fp8_div(item, r.chunks, r.magic);
+    int quad = static_cast<int>(item - row * r.chunks) * quads;
+    const int block = quad * 4 + sub, col = block * FP8_BLOCK + lane8 * 8;
+    const TIn* p = X + static_cast<long>(row) * ld + col;
+    uint8_t* out = codes + static_cast<long>(row) * r.K + col;
+    uint8_t* sc = scale + static_cast<long>(row) * r.ks + block;
+    int left = r.K - col;
+    // (the warp's four blocks stay in the loop together: the shuffles are warp-wide)
+    for (const int end = min(quad + quads, (r.ks + 3) / 4); quad < end; ++quad) {
+      Fp8Raw<TIn> gate[2], up[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float a[8], c[8];
-        gate[h].values(a);
-        up[h].values(c);
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-          const float2 y = gated_silu2<decltype(small)::value, sizeof(TIn) == 2>(make_float2(a[i], a[i + 1]), make_float2(c[i], c[i + 1]));
-          v[h][i] = y.x;
-          v[h][i + 1] = y.y;
-        }
+        gate[h].load(p + 64 * h, left > 64 * h);
+        up[h].load(p + 64 * h + r.K, left > 64 * h);
       }
-    };
-    if (gate[0].within80() && gate[1].within80()) activate(std::true_type{}); else activate(std::false_type{});
-    fp8_quantize_block(v, at, g, K, codes, scale);
+      float v[2][8];
+      auto activate = [&](auto small) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float a[8], c[8];
+          gate[h].values(a);
+          up[h].values(c);
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const float2 y = gated_silu2<decltype(small)::value, sizeof(TIn) == 2>(make_float2(a[i], a[i + 1]), make_float2(c[i], c[i + 1]));
+            v[h][i] = y.x;
+            v[h][i + 1] = y.y;
+          }
+        }
+      };
+      if (gate[0].within80() && gate[1].within80()) activate(std::true_type{}); else activate(std::false_type{});
+      fp8_quantize_block(v, left, out, sc);
+      p += 4 * FP8_BLOCK;
+      out += 4 * FP8_BLOCK;
+      sc += 4;
+      left -= 4 * FP8_BLOCK;
+    }
   }
 }
 

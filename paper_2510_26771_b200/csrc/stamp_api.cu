@@ -1244,30 +1244,28 @@ static int fused_quantize_tiled(const Problem& pb, const CqChoice& cc, const voi
 // ------------------------------------------------------------------------------------------
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// The blocks of an activation quantizer: how many, and how many CTAs take them when one takes `per_cta` at a time and
-// `resident` CTAs fit an SM (the rest by striding; twice as many as fit, so that the tail is spread).
-struct Fp8Blocks {
-  long ks, groups;
-  unsigned magic, ctas;
-};
-static int fp8_blocks(int M, int K, int per_cta, int resident, Fp8Blocks* b) {
-  b->ks = ((long)K + FP8_BLOCK - 1) / FP8_BLOCK;
-  b->groups = M * b->ks;
-  if (b->groups > (1L << 31) - (1L << 24)) return STAMP_ERR_UNSUPPORTED;   // the kernels count blocks in 32 bits
-  b->magic = b->ks > 1 ? (unsigned)(((1ULL << 32) + b->ks - 1) / b->ks) : 0u;
-  const long ctas = (b->groups + per_cta - 1) / per_cta;
-  const long most = 2L * resident * sm_count();
-  b->ctas = (unsigned)(ctas < most ? ctas : most);
+// The rows of an activation quantizer in chunks of `quads` times four blocks, and the CTAs that take them: as many as keep
+// an SM's `resident` ones busy twice over, the rest by striding.
+static int fp8_rows(int M, int K, int quads, int resident, Fp8Rows* r, unsigned* ctas) {
+  r->K = K;
+  r->ks = (K + FP8_BLOCK - 1) / FP8_BLOCK;
+  r->chunks = (unsigned)((r->ks + 4 * quads - 1) / (4 * quads));
+  r->magic = r->chunks > 1 ? (unsigned)(((1ULL << 32) + r->chunks - 1) / r->chunks) : 0u;
+  const long items = (long)M * r->chunks;
+  if (items > (1L << 31) - (1L << 24)) return STAMP_ERR_UNSUPPORTED;   // the kernels count chunks in 32 bits
+  r->items = (unsigned)items;
+  const long all = (items + FP8Q_THREADS / 32 - 1) / (FP8Q_THREADS / 32), most = 2L * resident * sm_count();
+  *ctas = (unsigned)(all < most ? all : most);
   return STAMP_OK;
 }
 
-template <typename TIn>
-static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale,
-                            cudaStream_t st) {
-  Fp8Blocks b;
-  if (int rc = fp8_blocks(M, K, FP8Q_THREADS / 8 * (sizeof(TIn) == 2 ? 4 : 2), 4, &b)) return rc;
-  if (launch_pdl(k_fp8_quant<TIn>, dim3(b.ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, rows, T, K,
-                 (unsigned)b.ks, b.magic, (unsigned)b.groups, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
+template <typename TIn, int U>
+static int launch_fp8_quant_u(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale, cudaStream_t st) {
+  Fp8Rows r;
+  unsigned ctas;
+  if (int rc = fp8_rows(M, K, U, 4, &r, &ctas)) return rc;
+  if (launch_pdl(k_fp8_quant<TIn, U>, dim3(ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, rows, T, r,
+                 static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
     cudaGetLastError();
     return STAMP_ERR_CUDA;
   }
@@ -1275,12 +1273,33 @@ static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int 
   return STAMP_OK;
 }
 
+// Chunks of 16, 12 or 8 blocks (fp32: half of that): the one that leaves the fewest lanes without a block at the ends of
+// the rows, where one with less in flight counts for 3 % and 10 % more (16384 x 14336 with 16 and with 8: 107 and 118 us).
+template <typename TIn>
+static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale,
+                            cudaStream_t st) {
+  const long quads = ((long)K + 4 * FP8_BLOCK - 1) / (4 * FP8_BLOCK);
+  if constexpr (sizeof(TIn) == 2) {
+    const double c4 = (quads + 3) / 4 * 4, c3 = (quads + 2) / 3 * 3 * 1.03, c2 = (quads + 1) / 2 * 2 * 1.1;
+    if (c4 <= c3 && c4 <= c2) return launch_fp8_quant_u<TIn, 4>(X, ld, rows, T, M, K, codes, scale, st);
+    return c3 <= c2 ? launch_fp8_quant_u<TIn, 3>(X, ld, rows, T, M, K, codes, scale, st)
+                    : launch_fp8_quant_u<TIn, 2>(X, ld, rows, T, M, K, codes, scale, st);
+  } else {
+    return (quads + 1) / 2 * 2 <= quads * 1.1 ? launch_fp8_quant_u<TIn, 2>(X, ld, rows, T, M, K, codes, scale, st)
+                                              : launch_fp8_quant_u<TIn, 1>(X, ld, rows, T, M, K, codes, scale, st);
+  }
+}
+
 template <typename TIn>
 static int launch_fp8_gated_quant(const void* X, long ld, int M, int F, void* codes, void* scale, cudaStream_t st) {
-  Fp8Blocks b;
-  if (int rc = fp8_blocks(M, F, FP8Q_THREADS / 8, 12, &b)) return rc;
-  if (launch_pdl(k_fp8_gated_quant<TIn>, dim3(b.ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, F, (unsigned)b.ks,
-                 b.magic, (unsigned)b.groups, static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
+  // four quads in a row share what finding the row costs, unless that leaves warps of the machine without any
+  const long all_quads = ((long)F + 4 * FP8_BLOCK - 1) / (4 * FP8_BLOCK);
+  const int quads = M * all_quads >= 4L * 40 * sm_count() ? 4 : 1;
+  Fp8Rows r;
+  unsigned ctas;
+  if (int rc = fp8_rows(M, F, quads, 12, &r, &ctas)) return rc;
+  if (launch_pdl(k_fp8_gated_quant<TIn>, dim3(ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, r, quads,
+                 static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
     cudaGetLastError();
     return STAMP_ERR_CUDA;
   }
