@@ -11,7 +11,7 @@
 // (columns).  The extent in tokens is a field of the instruction, in steps of 16: a tile with few rows -- a decode
 // step, the end of an expert's run -- costs what its rows cost, and no expert's rows have to be padded.
 //
-//   warp 0     TMA producer: 128-byte-swizzled K-major tiles of both operands into a ring of FP8G_STAGES
+//   warp 0     TMA producer: 128-byte-swizzled K-major tiles of both operands into a ring of 6 to 10 stages
 //   warp 1     allocates TMEM; one elected thread copies the scale words to TMEM (tcgen05.cp) and issues the MMAs
 //   warps 2-3  scale producers: gather the scale words of 512 features of the tile's tokens and channels into the
 //              order tcgen05.cp wants (row i of 32: rows i, i + 32, i + 64, i + 96), up to FP8G_SF_SLOTS steps ahead
@@ -24,6 +24,11 @@
 // PAIR = true: CTA pairs (cta_group::2), tiles of 256 channels x up to 256 tokens.  Two accumulators of 256 columns and
 // the scales do not fit the 512 columns: the accumulators overlap in 32 columns, which the epilogue drains first; the
 // next tile starts when they are free.
+//
+// What bounds it: large products the power limit (16384 x 14336 x 4096: 754 us = 2552 TFLOP/s at 990 W and about 1.1 GHz;
+// without it, at 1.9 GHz, shared memory and the tensor pipe together, 537 clocks per 128 features of a 256 x 256 pair
+// against the pipe's 512); few rows the weights' way from memory (1 x 4096 x 11008: 10.0 us against 6.9 at the copy rate,
+// 3.2 of them a launch with nothing to do; 320 rows over 64 experts of 2048 x 4096: 76 against 71).
 #pragma once
 #include "common.cuh"
 #include "k_fp8_quant.cuh"

@@ -1356,7 +1356,8 @@ struct Fp8Plan {
   bool pair;
   int bn, split;
 };
-static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
+// `most`: steps of 512 features that one accumulator may sum (run_fp8_gemm).
+static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p, int most) {
   const int steps = (p.ks + 3) / 4, sms = sm_count();
   // runs that have rows, and their length: of the experts nothing is known here but how many rows they share
   const double runs = p.offsets ? (p.E < p.M ? p.E : p.M) : 1, run = p.M / runs;
@@ -1367,6 +1368,7 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
     const double per_run = !p.offsets ? (p.M + bn - 1) / bn : run <= bn / 2 ? 1.0 : run / bn + 0.5;
     const double tiles = runs * per_run * ((p.N + (pair ? 255 : 127)) / (pair ? 256 : 128));
     const double slots = sms / (pair ? 2 : split);
+    if (split > 1 && (steps + split - 1) / split > most) return;   // (a part of a split sum is one accumulator's)
     if (split > 1 && tiles > slots) return;   // (a cluster that splits a sum takes one tile: a second round starts from nothing)
     const double waves = !p.offsets ? (double)(((long)tiles + (long)slots - 1) / (long)slots) : tiles < slots ? 1.0 : tiles / slots + 0.5;
     const double box = pair ? bn / 2 : bn, rows = run / per_run / (pair ? 2 : 1);
@@ -1389,7 +1391,11 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p) {
 
 static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
   const int steps = (p.ks + 3) / 4;
-  Fp8Plan plan = plan_fp8_gemm(p);
+  // The tensor cores cut the running sum off instead of rounding it, and the error grows with the number of additions:
+  // against 64 bits, 4e-7 of the result at 4096 features and 2.3e-6 at 14336.  An fp32 output is summed in chunks of
+  // 4096 features at most, the chunks added in fp32; in a bf16 output (2e-3) none of it shows.
+  p.chunk = y_dtype == STAMP_F32 && steps > 8 ? 8 : steps;
+  const Fp8Plan plan = plan_fp8_gemm(p, p.chunk);
   const bool pair = plan.pair;
   p.bn = plan.bn;
   p.split = plan.split;
@@ -1400,10 +1406,6 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
   const int box = pair ? p.bn / 2 : p.bn;
   p.stage_bytes = FP8G_W_BYTES + box * FP8G_BK;
   p.stages = FP8G_RING_BYTES / p.stage_bytes < FP8G_MAX_STAGES ? FP8G_RING_BYTES / p.stage_bytes : FP8G_MAX_STAGES;
-  // The tensor cores cut the running sum off instead of rounding it, and the error grows with the number of additions:
-  // against 64 bits, 4e-7 of the result at 4096 features and 2.3e-6 at 14336.  An fp32 output is summed in chunks of
-  // 4096 features, the chunks added in fp32 by the epilogue; in a bf16 output (2e-3) none of it shows.
-  p.chunk = (y_dtype == STAMP_F32 && p.split == 1) ? 8 : steps;
   p.x_words = (p.ks & 3) == 0 && (reinterpret_cast<uintptr_t>(p.x_scale) & 3) == 0;
   CUtensorMap tw, tx, txt;
   if (int rc = make_tmap_i8(p.w, (long)p.E * p.N, p.K, FP8G_BM, &tw)) return rc;

@@ -297,6 +297,30 @@ def test_every_block_meets_its_own_scales(st, M):
     assert torch.equal(y.double(), xv @ wv.t())
 
 
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+@pytest.mark.parametrize("K", [128, 256, 384, 640, 896])
+def test_scale_rows_of_every_length_and_alignment(st, K, shift):
+    """x_scale rows of one, two, three, five and seven bytes that start anywhere: read as words, as pairs of aligned words in
+    the middle of the table, byte by byte at its ends.  Exact in fp32 again."""
+    import torch
+    M, N, nb = 700, 136, K // 128
+    g = torch.Generator(device="cuda").manual_seed(K + shift)
+    x = torch.randint(-3, 4, (M, K), device="cuda", generator=g).float()
+    w = torch.randint(-3, 4, (N, K), device="cuda", generator=g).float()
+    e = torch.randint(0, 4, (M, nb), device="cuda", generator=g)
+    raw = torch.zeros(M * nb + 8, dtype=torch.uint8, device="cuda")
+    scale = raw[shift:shift + M * nb].view(M, nb)
+    scale.copy_((e + 127).to(torch.uint8))
+    one = torch.full((_blocks(N), nb), 127, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+    want = (x.double() * torch.exp2(e.double()).repeat_interleave(128, 1)) @ w.double().t()
+    codes, wc, xs = x.to(torch.float8_e4m3fn), w.to(torch.float8_e4m3fn), scale.view(torch.float8_e8m0fnu)
+    assert torch.equal(st.stamp_fp8_linear(codes, xs, wc, one, out_dtype=torch.float32).double(), want)
+    offsets = torch.tensor([0, 1, 3, 300, 300, 695, 700], dtype=torch.int32, device="cuda")
+    y = st.stamp_fp8_linear_grouped(codes, xs, offsets, wc.view(torch.uint8).expand(6, N, K).contiguous().view(torch.float8_e4m3fn),
+                                    one.view(torch.uint8).expand(6, -1, -1).contiguous().view(torch.float8_e8m0fnu), out_dtype=torch.float32)
+    assert torch.equal(y.double(), want)
+
+
 @pytest.mark.parametrize("M", [4, 300])
 def test_non_finite_activations_show_in_their_rows_only(st, M):
     import torch
