@@ -1244,9 +1244,10 @@ static int fused_quantize_tiled(const Problem& pb, const CqChoice& cc, const voi
 // ------------------------------------------------------------------------------------------
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// The rows of an activation quantizer in chunks of `quads` times four blocks, and the CTAs that take them: as many as keep
-// an SM's `resident` ones busy twice over, the rest by striding.
-static int fp8_rows(int M, int K, int quads, int resident, Fp8Rows* r, unsigned* ctas) {
+// The rows of an activation quantizer in chunks of `quads` times four blocks, and the CTAs that take them: one chunk per
+// warp, in the order of memory, up to 64 CTAs per SM (the rest by striding).  Fewer that stride are the slower the larger
+// the tensor: 16384 x 14336 in 111 us with 8 per SM, 102 with 64; up to 4096 x 4096 all are alike.
+static int fp8_rows(int M, int K, int quads, Fp8Rows* r, unsigned* ctas) {
   r->K = K;
   r->ks = (K + FP8_BLOCK - 1) / FP8_BLOCK;
   r->chunks = (unsigned)((r->ks + 4 * quads - 1) / (4 * quads));
@@ -1254,7 +1255,7 @@ static int fp8_rows(int M, int K, int quads, int resident, Fp8Rows* r, unsigned*
   const long items = (long)M * r->chunks;
   if (items > (1L << 31) - (1L << 24)) return STAMP_ERR_UNSUPPORTED;   // the kernels count chunks in 32 bits
   r->items = (unsigned)items;
-  const long all = (items + FP8Q_THREADS / 32 - 1) / (FP8Q_THREADS / 32), most = 2L * resident * sm_count();
+  const long all = (items + FP8Q_THREADS / 32 - 1) / (FP8Q_THREADS / 32), most = 64L * sm_count();
   *ctas = (unsigned)(all < most ? all : most);
   return STAMP_OK;
 }
@@ -1263,7 +1264,7 @@ template <typename TIn, int U>
 static int launch_fp8_quant_u(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale, cudaStream_t st) {
   Fp8Rows r;
   unsigned ctas;
-  if (int rc = fp8_rows(M, K, U, 4, &r, &ctas)) return rc;
+  if (int rc = fp8_rows(M, K, U, &r, &ctas)) return rc;
   if (launch_pdl(k_fp8_quant<TIn, U>, dim3(ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, rows, T, r,
                  static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
     cudaGetLastError();
@@ -1274,7 +1275,7 @@ static int launch_fp8_quant_u(const void* X, long ld, const int* rows, int T, in
 }
 
 // Chunks of 16, 12 or 8 blocks (fp32: half of that): the one that leaves the fewest lanes without a block at the ends of
-// the rows, where one with less in flight counts for 3 % and 10 % more (16384 x 14336 with 16 and with 8: 107 and 118 us).
+// the rows, where one with less in flight counts for 3 % and 10 % more (16384 x 14336 with 16 and with 8, striding: 107 and 118 us).
 template <typename TIn>
 static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale,
                             cudaStream_t st) {
@@ -1297,7 +1298,7 @@ static int launch_fp8_gated_quant(const void* X, long ld, int M, int F, void* co
   const int quads = M * all_quads >= 4L * 40 * sm_count() ? 4 : 1;
   Fp8Rows r;
   unsigned ctas;
-  if (int rc = fp8_rows(M, F, quads, 12, &r, &ctas)) return rc;
+  if (int rc = fp8_rows(M, F, quads, &r, &ctas)) return rc;
   if (launch_pdl(k_fp8_gated_quant<TIn>, dim3(ctas), dim3(FP8Q_THREADS), 0, st, static_cast<const TIn*>(X), ld, r, quads,
                  static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scale)) != cudaSuccess) {
     cudaGetLastError();
