@@ -360,6 +360,12 @@ int stamp_profile_gemm_events(void* start_event, void* stop_event);
  * stamp_last_device_status() reports it once.  Nothing faults or hangs.  No counterpart in the paper. */
 int stamp_debug_expire_wait(long long limit_cycles, void* stream);
 
+/* Which kernel a block-scaled product of these sizes runs on the current device: E = 0 for stamp_fp8_linear, else
+ * stamp_fp8_linear_grouped with E experts; sizes as there, M > 0.  *pair: 1 for CTA pairs with tiles of 256 channels, 0 for
+ * single CTAs with 128; *rows: token rows of a tile; *split: CTAs that share a tile's sum.  Launches nothing.  For tests,
+ * which state the kernel they mean. */
+int stamp_debug_fp8_plan(int M, int E, int N, int K, int y_dtype, int* pair, int* rows, int* split);
+
 /* Measurement: the rate of the tensor cores' int8 instruction alone.  Launches one CTA per SM; each issues
  * nbatch * 64 tcgen05.mma kind::i8 instructions (M128 x N256 x K32, int32 accumulators in tensor memory) on
  * operand tiles that stay in shared memory -- no loads in the loop, waits bounded -- and *ops_out receives the

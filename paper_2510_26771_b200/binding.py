@@ -29,7 +29,7 @@ EXPORTS = (
     "stamp_measure_i8_mma_issue", "stamp_debug_expire_wait",
     "stamp_dequantize", "stamp_prepare_weights_both",
     "stamp_fp8_quantize", "stamp_fp8_gated_quantize", "stamp_fp8_quantize_weights", "stamp_fp8_linear",
-    "stamp_fp8_linear_grouped",
+    "stamp_fp8_linear_grouped", "stamp_debug_fp8_plan",
 )
 
 FP8_BLOCK = 128                      # features per scale of the block-scaled 8-bit floating point layers
@@ -381,6 +381,14 @@ def stamp_measure_i8_mma_issue(nbatch: int) -> int:
 def stamp_debug_expire_wait(limit_cycles: int) -> None:
     """Launch the test kernel whose bounded wait runs out after limit_cycles SM clocks (device status: time-out)."""
     _check(lib().stamp_debug_expire_wait(ctypes.c_longlong(int(limit_cycles)), _stream()), "stamp_debug_expire_wait")
+
+
+def stamp_debug_fp8_plan(M: int, N: int, K: int, experts: int = 0, out_dtype=torch.bfloat16):
+    """(pair, rows, split): which kernel stamp_fp8_linear (experts = 0) or stamp_fp8_linear_grouped runs at these sizes."""
+    out = [ctypes.c_int() for _ in range(3)]
+    dtype = _dtype_code(torch.empty(0, dtype=out_dtype))
+    _check(lib().stamp_debug_fp8_plan(M, experts, N, K, dtype, *map(ctypes.byref, out)), "stamp_debug_fp8_plan")
+    return bool(out[0].value), out[1].value, out[2].value
 
 
 def stamp_last_launch_count() -> int:

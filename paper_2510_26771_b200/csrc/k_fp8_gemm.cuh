@@ -121,6 +121,33 @@ __device__ __forceinline__ uint32_t fp8_scale_word(const uint8_t* ptr, int n, bo
   return b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24);
 }
 
+// The order in which the two halves of the epilogue warps drain an accumulator: chunks of 32 columns, chunk c by half c & 1
+// whichever accumulator it is.  A sum in several parts is added up in the output, accumulator after accumulator, and
+// nothing orders the halves among each other: a chunk has to stay with one of them.  PAIR: the chunk whose columns the
+// accumulators share, the eighth of the first and the first of the second, comes first.
+__host__ __device__ constexpr int fp8_drain_chunk(bool descending, int half, int i, int count) {
+  return half + 2 * (descending ? count - 1 - i : i);
+}
+__host__ __device__ constexpr int fp8_overlap_half(int accumulator) { return accumulator == 0 ? 1 : 0; }
+constexpr bool fp8_drain_order_holds() {
+  for (int chunks = 1; chunks <= 8; ++chunks)
+    for (int a = 0; a < 2; ++a) {
+      unsigned taken = 0;
+      for (int half = 0; half < 2; ++half) {
+        const int count = (chunks - half + 1) / 2;
+        for (int i = 0; i < count; ++i) {
+          const int c = fp8_drain_chunk(a == 0, half, i, count);
+          if ((c & 1) != half || c < 0 || c >= chunks || (taken >> c & 1u) != 0u) return false;
+          if (c == (a == 0 ? 7 : 0) && (half != fp8_overlap_half(a) || i != 0)) return false;
+          taken |= 1u << c;
+        }
+      }
+      if (taken != (1u << chunks) - 1u) return false;
+    }
+  return true;
+}
+static_assert(fp8_drain_order_holds(), "every chunk once, by the same half in both accumulators, the shared columns first");
+
 // Two adjacent channels of one token.
 __device__ __forceinline__ void fp8_store2(float* y, float a, float b, bool both, bool vec) {
   if (vec && both) {
@@ -474,14 +501,15 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
           }
           released = true;
         };
-        if (PAIR && half != 0) release();   // the shared columns are in the other warps' first chunk
-        for (int i = half; i < chunks; i += 2) {
-          // the chunk that overlaps the other accumulator first: the last of the first one, the first of the second
-          const int c = (PAIR && a == 0) ? chunks - 1 - i : i;
+        // PAIR: the chunk that overlaps the other accumulator first; who has none of it hands back at once
+        if (PAIR && half != fp8_overlap_half(a)) release();
+        const int count = (chunks - half + 1) / 2;
+        for (int i = 0; i < count; ++i) {
+          const int c = fp8_drain_chunk(PAIR && a == 0, half, i, count);
           uint32_t r[32];
           ptx::tmem_ld_32x32b_x32(taddr + 32 * c, r);
           ptx::tmem_ld_wait();
-          if (PAIR ? i == 0 : i + 2 >= chunks) release();
+          if (!released && (PAIR || i + 1 == count)) release();
           if (!PAIR && p.split > 1) {
             // this CTA's part of the sum, [token][channel], in the ring that nothing uses any more
             float* part = reinterpret_cast<float*>(smem);
@@ -503,7 +531,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
                     if (j < left) *out = __uint_as_float(r[j]) + bias;
                 }
               }
-            } else if (ch < p.N) {   // a later chunk of the sum: on top of this thread's own value of the chunks before
+            } else if (ch < p.N) {   // a later part of the sum: on top of this thread's own value of the parts before
               float before[32];
 #pragma unroll
               for (int j = 0; j < 32; ++j) before[j] = j < left ? out[static_cast<long>(j) * p.N] : 0.f;

@@ -1357,7 +1357,7 @@ struct Fp8Plan {
   bool pair;
   int bn, split;
 };
-// `most`: steps of 512 features that one accumulator may sum (run_fp8_gemm).
+// `most`: steps of 512 features that one accumulator may sum (fp8_chunk).
 static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p, int most) {
   const int steps = (p.ks + 3) / 4, sms = sm_count();
   // runs that have rows, and their length: of the experts nothing is known here but how many rows they share
@@ -1390,12 +1390,17 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p, int most) {
   return best;
 }
 
+// Steps of 512 features that one accumulator sums.  The tensor cores cut the running sum off instead of rounding it, and
+// the error grows with the number of additions: against 64 bits, 4e-7 of the result at 4096 features and 2.3e-6 at 14336.
+// An fp32 output is summed in chunks of 4096 features at most, the chunks added in fp32; in a bf16 output (2e-3) none of it
+// shows.
+static int fp8_chunk(int ks, int y_dtype) {
+  const int steps = (ks + 3) / 4;
+  return y_dtype == STAMP_F32 && steps > 8 ? 8 : steps;
+}
+
 static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
-  const int steps = (p.ks + 3) / 4;
-  // The tensor cores cut the running sum off instead of rounding it, and the error grows with the number of additions:
-  // against 64 bits, 4e-7 of the result at 4096 features and 2.3e-6 at 14336.  An fp32 output is summed in chunks of
-  // 4096 features at most, the chunks added in fp32; in a bf16 output (2e-3) none of it shows.
-  p.chunk = y_dtype == STAMP_F32 && steps > 8 ? 8 : steps;
+  p.chunk = fp8_chunk(p.ks, y_dtype);
   const Fp8Plan plan = plan_fp8_gemm(p, p.chunk);
   const bool pair = plan.pair;
   p.bn = plan.bn;
@@ -1985,6 +1990,21 @@ int stamp_fp8_linear_grouped(const void* x, const void* x_scale, const int32_t* 
   if (int rc = check_fp8_product(p, y_dtype)) return rc;
   if (!offsets) return STAMP_ERR_INVALID_ARG;
   return M == 0 ? STAMP_OK : run_fp8_gemm(p, y_dtype, static_cast<cudaStream_t>(stream));
+}
+
+int stamp_debug_fp8_plan(int M, int E, int N, int K, int y_dtype, int* pair, int* rows, int* split) {
+  t_launches = 0;
+  if (!pair || !rows || !split || E < 0 || M <= 0) return STAMP_ERR_INVALID_ARG;
+  // (neither the plan nor the checks look behind the pointers; offsets only say whether there are experts)
+  alignas(16) static const int anything[4] = {};
+  const Fp8GemmParams p = fp8_params(anything, anything, E > 0 ? anything : nullptr, anything, anything, nullptr, M, E > 0 ? E : 1, N, K,
+                                     const_cast<int*>(anything));
+  if (int rc = check_fp8_product(p, y_dtype)) return rc;
+  const Fp8Plan plan = plan_fp8_gemm(p, fp8_chunk(p.ks, y_dtype));
+  *pair = plan.pair ? 1 : 0;
+  *rows = plan.bn;
+  *split = plan.split;
+  return STAMP_OK;
 }
 
 int stamp_last_launch_count(void) { return t_launches; }
