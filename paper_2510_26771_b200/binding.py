@@ -272,10 +272,12 @@ def stamp_fp8_quantize_weights(W: torch.Tensor):
     if W.dim() not in (2, 3):
         raise ValueError("expected a matrix, or one for each expert")
     E, (N, K) = W.shape[0] if W.dim() == 3 else 1, W.shape[-2:]
+    w = _ptr(W)
     codes = torch.empty(W.shape, dtype=FP8_CODES, device=W.device)
     scale = torch.empty((*W.shape[:-2], _fp8_blocks(N), _fp8_blocks(K)), dtype=FP8_SCALE, device=W.device)
-    _check(lib().stamp_fp8_quantize_weights(_ptr(W), _dtype_code(W), E, N, K, _ptr(codes), _ptr(scale), _stream()),
-           "stamp_fp8_quantize_weights")
+    with torch.cuda.device(W.device):
+        _check(lib().stamp_fp8_quantize_weights(w, _dtype_code(W), E, N, K, _ptr(codes), _ptr(scale), _stream()),
+               "stamp_fp8_quantize_weights")
     return codes, scale
 
 
