@@ -272,6 +272,8 @@ def stamp_fp8_quantize_weights(W: torch.Tensor):
     if W.dim() not in (2, 3):
         raise ValueError("expected a matrix, or one for each expert")
     E, (N, K) = W.shape[0] if W.dim() == 3 else 1, W.shape[-2:]
+    if max(E, N, K) > 0x7FFFFFFF:
+        raise ValueError("a size does not fit 32 bits")
     w = _ptr(W)
     codes = torch.empty(W.shape, dtype=FP8_CODES, device=W.device)
     scale = torch.empty((*W.shape[:-2], _fp8_blocks(N), _fp8_blocks(K)), dtype=FP8_SCALE, device=W.device)

@@ -1242,6 +1242,9 @@ static int fused_quantize_tiled(const Problem& pb, const CqChoice& cc, const voi
 // ------------------------------------------------------------------------------------------
 // Block-scaled 8-bit floating point layers
 // ------------------------------------------------------------------------------------------
+// The kernels index the features of a row, and what a chunk or a tile hangs over its end, in 32 bits.
+constexpr int FP8_MAX_FEATURES = 0x7FFFFFFF - 4095;
+
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // The rows of an activation quantizer in chunks of `quads` times four blocks, and the CTAs that take them: one chunk per
@@ -1432,7 +1435,7 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
 // Arguments common to both products.
 static int check_fp8_product(const Fp8GemmParams& p, int y_dtype) {
   if (p.M < 0 || p.E <= 0 || p.N <= 0 || p.K <= 0 || !dtype_ok(y_dtype)) return STAMP_ERR_INVALID_ARG;
-  if (p.K % 16 != 0 || p.E > FP8_MAX_EXPERTS || (long)p.E * p.N > (1L << 31) - 512 || p.M > (1 << 30)) return STAMP_ERR_UNSUPPORTED;
+  if (p.K % 16 != 0 || p.K > FP8_MAX_FEATURES || p.E > FP8_MAX_EXPERTS || (long)p.E * p.N > (1L << 31) - 512 || p.M > (1 << 30)) return STAMP_ERR_UNSUPPORTED;
   if (!p.w || !p.w_scale || !aligned16(p.w)) return STAMP_ERR_INVALID_ARG;
   if (p.M > 0 && (!p.x || !p.x_scale || !p.y || !aligned16(p.x))) return STAMP_ERR_INVALID_ARG;
   if (p.M > 0 && (reinterpret_cast<uintptr_t>(p.y) & (y_dtype == STAMP_BF16 ? 1 : 3)) != 0) return STAMP_ERR_INVALID_ARG;
@@ -1916,7 +1919,7 @@ int stamp_fp8_quantize(const void* X, int x_dtype, long long ldx, const int32_t*
   t_launches = 0;
   if (T < 0 || M < 0 || K <= 0 || ldx < K || !dtype_ok(x_dtype)) return STAMP_ERR_INVALID_ARG;
   if (!rows && M > T) return STAMP_ERR_INVALID_ARG;
-  if (K % 16 != 0) return STAMP_ERR_UNSUPPORTED;
+  if (K % 16 != 0 || K > FP8_MAX_FEATURES) return STAMP_ERR_UNSUPPORTED;
   if (M == 0) return STAMP_OK;
   if (!X || !codes || !scale || !aligned16(X) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
   if (ldx % (x_dtype == STAMP_BF16 ? 8 : 4) != 0) return STAMP_ERR_INVALID_ARG;
@@ -1929,7 +1932,7 @@ int stamp_fp8_gated_quantize(const void* X, int x_dtype, long long ldx, int M, i
                              void* stream) {
   t_launches = 0;
   if (M < 0 || F <= 0 || ldx < 2LL * F || !dtype_ok(x_dtype)) return STAMP_ERR_INVALID_ARG;
-  if (F % 16 != 0) return STAMP_ERR_UNSUPPORTED;
+  if (F % 16 != 0 || F > FP8_MAX_FEATURES) return STAMP_ERR_UNSUPPORTED;
   if (M == 0) return STAMP_OK;
   if (!X || !codes || !scale || !aligned16(X) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
   if (ldx % (x_dtype == STAMP_BF16 ? 8 : 4) != 0) return STAMP_ERR_INVALID_ARG;
@@ -1942,7 +1945,7 @@ int stamp_fp8_quantize_weights(const void* W, int w_dtype, int E, int N, int K, 
   t_launches = 0;
   if (!W || !codes || !scale || E <= 0 || N <= 0 || K <= 0 || !dtype_ok(w_dtype)) return STAMP_ERR_INVALID_ARG;
   const long nb = ((long)N + FP8_BLOCK - 1) / FP8_BLOCK;
-  if (K % 16 != 0 || nb > 65535 || E > 65535) return STAMP_ERR_UNSUPPORTED;
+  if (K % 16 != 0 || K > FP8_MAX_FEATURES || nb > 65535 || E > 65535) return STAMP_ERR_UNSUPPORTED;
   if (!aligned16(W) || !aligned16(codes)) return STAMP_ERR_INVALID_ARG;
   const dim3 grid((unsigned)((K + FP8_BLOCK - 1) / FP8_BLOCK), (unsigned)nb, (unsigned)E);
   cudaStream_t st = static_cast<cudaStream_t>(stream);

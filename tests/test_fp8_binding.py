@@ -53,3 +53,15 @@ def test_weights_off_the_devices_are_refused():
         binding.stamp_fp8_quantize_weights(torch.zeros(64, 256))
     with pytest.raises(ValueError):
         binding.stamp_fp8_quantize_weights(torch.zeros(256))
+
+
+@pytest.mark.parametrize("shape", [(16, 1 << 32), (1 << 32, 16), (1 << 31, 2, 16)])
+def test_sizes_past_32_bits_are_refused(monkeypatch, shape):
+    class Large(Weights):
+        def dim(self):
+            return len(self.shape)
+    Large.shape = torch.Size(shape)
+    monkeypatch.setattr(binding, "lib", lambda: pytest.fail("the library was called"))
+    monkeypatch.setattr(binding.torch, "empty", lambda *a, **k: pytest.fail("outputs were allocated"))
+    with pytest.raises(ValueError):
+        binding.stamp_fp8_quantize_weights(Large())
