@@ -12,7 +12,7 @@ from typing import Optional
 
 import torch
 
-from .build import CALLS_PATH, LIB_PATH
+from .build import LIB_PATH, calls_path
 
 STAMP_OK = 0
 F32, BF16 = 0, 1
@@ -232,11 +232,12 @@ def calls():
     global _calls
     if _calls is None:
         lib()
-        if not os.path.exists(CALLS_PATH):
-            raise RuntimeError(f"marshalling module not built: {CALLS_PATH} is missing "
+        path = calls_path()
+        if not os.path.exists(path):
+            raise RuntimeError(f"marshalling module not built: {path} is missing "
                                "(run `python -m paper_2510_26771_b200.build`); there is no fallback path")
-        loader = importlib.machinery.ExtensionFileLoader("_torch_calls", CALLS_PATH)
-        spec = importlib.util.spec_from_file_location("_torch_calls", CALLS_PATH, loader=loader)
+        loader = importlib.machinery.ExtensionFileLoader("_torch_calls", path)
+        spec = importlib.util.spec_from_file_location("_torch_calls", path, loader=loader)
         module = importlib.util.module_from_spec(spec)
         loader.exec_module(module)
         _calls = module
