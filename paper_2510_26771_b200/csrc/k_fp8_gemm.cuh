@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       bool ok = true, ready = false;   // ready: the operands of the next 128 features were seen to have arrived
       for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
         const int n = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles).n;
-        const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, n, 0);
+        const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, n);
         int in_chunk = 0;   // steps that are in the accumulator already
         for (int s = step0; s < step1 && ok; ++s, ++scount) {
           const int a = it & 1;

@@ -192,11 +192,6 @@ __device__ __forceinline__ void tma_load_2d(void* smem_dst, const CUtensorMap* m
       ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
       : "memory");
 }
-// Hint: bring a tile into L2; nothing waits on it.
-__device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* m, int c0, int c1) {
-  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1)
-               : "memory");
-}
 // Plain (untiled) bulk copy global -> shared; both addresses 16-byte aligned, bytes % 16 == 0.
 __device__ __forceinline__ void bulk_load(void* smem_dst, const void* gsrc, uint32_t bytes, uint64_t* bar) {
   asm volatile(
@@ -372,10 +367,8 @@ __host__ __device__ constexpr uint32_t make_mxf8_idesc(int m) {
   return (1u << 23)                          // scale format: e8m0
          | (static_cast<uint32_t>(m >> 4) << 24);
 }
-// N extent, and which byte of the 32-bit scale words in tensor memory this instruction takes for A and for B.
-__device__ __forceinline__ uint32_t mxf8_idesc_with(uint32_t idesc, int n, uint32_t scale_id) {
-  return idesc | (static_cast<uint32_t>(n >> 3) << 17) | (scale_id << 4) | (scale_id << 29);
-}
+// With the N extent.  (Which byte of the 32-bit scale words an instruction takes is bits 4-5 for B and 29-30 for A.)
+__device__ __forceinline__ uint32_t mxf8_idesc_with(uint32_t idesc, int n) { return idesc | (static_cast<uint32_t>(n >> 3) << 17); }
 // D[tmem] (+)= (A[smem] * sA[tmem]) (B[smem] * sB[tmem]) over 128 features, one scale per row of A and of B: four
 // instructions of 32, then a commit that hands the stage back (PAIR: in both CTAs).  A and B are given by the lower words of
 // their descriptors (make_kmajor_sw128_desc; 32 bytes further in a row is 2 more), the upper one is the same for all.
