@@ -88,10 +88,9 @@ __device__ __forceinline__ uint2 fp8_pack8(const float (&v)[8], float inverse) {
 // multiply by g.  So it is split: a bf16 gate (8 significant bits) times the first 16 bits of log2 e is exact, the rest of
 // the constant, times ln 2, becomes a factor 1 + small; an fp32 gate's product is held as head and tail instead.  The
 // quotient is g times the approximate reciprocal, corrected once by its remainder.  SMALL: |g| <= 80.  Otherwise the power
-// is taken as 0 or infinite past +-90, and an infinite divisor takes no correction (inf * 0); a quarter of the divisor is
-// what a negative gate is divided by, and the quotient is multiplied by the quarter: from 2^126 on (g = -87.34) the
-// reciprocal of the divisor itself is subnormal, which the approximation returns as zero.  NaNs and infinities come out
-// non-finite, as they do of the formula.
+// is taken as 0 or infinite past +-90, an infinite divisor takes no correction (inf * 0), and gate and divisor are both
+// divided by four: from 2^126 on (g = -87.34) the reciprocal of the divisor itself is subnormal, which the approximation
+// returns as zero.  NaNs and infinities come out non-finite, as they do of the formula.
 template <bool SMALL, bool BF16>
 __device__ __forceinline__ float2 gated_silu2(float2 g, float2 u) {
   auto both = [](float v) { return make_float2(v, v); };
@@ -109,19 +108,17 @@ __device__ __forceinline__ float2 gated_silu2(float2 g, float2 u) {
   const float2 p = make_float2(ptx::ex2(head.x), ptx::ex2(head.y));
   // (p * more + p would be inf - inf where p is infinite)
   const float2 e = SMALL ? __ffma2_rn(p, more, p) : __fmul2_rn(p, __fadd2_rn(more, both(1.f)));
-  // (c and the products by it: none where SMALL)
-  const float2 c = SMALL ? both(1.f) : make_float2(g.x < 0.f ? 0.25f : 1.f, g.y < 0.f ? 0.25f : 1.f);
-  const float2 minus_c = make_float2(-c.x, -c.y);
-  const float2 minus_d = __ffma2_rn(e, minus_c, minus_c);   // - c (1 + e)
+  // SMALL: g / (1 + e), otherwise both divided by four
+  const float2 n = SMALL ? g : __fmul2_rn(g, both(0.25f));
+  const float2 minus_d = SMALL ? __ffma2_rn(e, both(-1.f), both(-1.f)) : __ffma2_rn(e, both(-0.25f), both(-0.25f));
   const float2 r = make_float2(ptx::rcp(-minus_d.x), ptx::rcp(-minus_d.y));
-  float2 q = __fmul2_rn(g, r);
-  const float2 fixed = __ffma2_rn(__ffma2_rn(q, minus_d, g), r, q);
+  float2 q = __fmul2_rn(n, r);
+  const float2 fixed = __ffma2_rn(__ffma2_rn(q, minus_d, n), r, q);
   if constexpr (SMALL) {
     q = fixed;
   } else {
     q.x = minus_d.x > -__int_as_float(0x7F800000) ? fixed.x : q.x;
     q.y = minus_d.y > -__int_as_float(0x7F800000) ? fixed.y : q.y;
-    q = __fmul2_rn(q, c);
   }
   return __fmul2_rn(q, u);
 }
