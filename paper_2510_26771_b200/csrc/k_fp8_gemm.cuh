@@ -27,8 +27,11 @@
 //
 // What bounds it: large products the power limit (16384 x 14336 x 4096: 754 us = 2552 TFLOP/s at 990 W and about 1.1 GHz;
 // without it, at 1.9 GHz, shared memory and the tensor pipe together, 537 clocks per 128 features of a 256 x 256 pair
-// against the pipe's 512); few rows the weights' way from memory (1 x 4096 x 11008: 10.0 us against 6.9 at the copy rate,
-// 3.2 of them a launch with nothing to do; 320 rows over 64 experts of 2048 x 4096: 76 against 71).
+// against the pipe's 512); few rows the issue and copy loops of the CTAs that have a tile, where tiles are fewer than SMs (1 x 4096 x
+// 11008: 86 tiles of 32 steps at 330 clocks, 5.6 us, behind 3.2 of a launch with nothing to do: 10.0 us against 6.9 at the
+// copy rate, with 62 SMs idle), else the weights' way from memory (320 rows over 64 experts of 2048 x 4096: 75 against 71).
+// An fp32 output of more than 4096 features is read and written again for every further 4096: 16384 x 14336 x 4096 in 803 to
+// 867 us where one accumulator would take 735.
 #pragma once
 #include "common.cuh"
 #include "k_fp8_quant.cuh"

@@ -159,9 +159,11 @@ __device__ __forceinline__ void fp8_quantize_block(const float (&v)[2][8], int l
 //           zeros and raises the device status word
 //   codes   [M, K], scale [M, ks]
 // A chunk is 4 U blocks, and a thread loads its part of all of them before it uses the first.  Bound by memory: 16384 x
-// 14336 in 102 us, a little above the copy rate (a third of the traffic is writes, not half).  Where the rows come from L2 the instructions count: 16384 rows
-// dispatched from 4096 tokens of 2048 features take 9.8 us; with the place of every block found by itself, without regard to
-// rows, 12.1 us at 8.5 instructions a feature.
+// 14336 in 102 us, a little above the copy rate (a third of the traffic is writes, not half); fp32 rows in 165 us, likewise.
+// A dispatch loads, reduces and converts a token once for each of its experts: 16384 rows of 4096 tokens of 2048 features
+// take 12.1 us a call where a pass over memory would take 7.8 (fp32 17.2 and 10.3), 60 % of the issue slots and 40 % of the
+// warps busy.  Where tokens and codes stay in L2 it is 9.8; there, with the place of every block found by itself, without
+// regard to rows, 12.1 at 8.5 instructions a feature.
 template <typename TIn, int U>
 __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_quant(const TIn* __restrict__ X, long ld, const int* __restrict__ rows, int T,
                                                             Fp8Rows r, uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
@@ -199,7 +201,8 @@ __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_quant(const TIn* __restric
 }
 
 // Behind a gated activation: X [M, ld] rows of K gates and K ups -> codes [M, K], scale [M, ks] of silu(gate) * up.
-// A chunk is `quads` times four blocks, one after the other.  16384 x 4096 in 60 us, 86 % of the copy rate: the arithmetic
+// A chunk is `quads` times four blocks, one after the other.  16384 x 4096 in 60 us, 86 % of the copy rate (56 without gates
+// above 80, 91 for fp32 rows, at the copy rate): the arithmetic
 // (15 instructions a feature, two of them on the special function unit, which is busy 58 % of the time) and the loads
 // overlap across resident warps only, so it is one block at a time and more warps (two: 70 us against 61.5).  Copies through
 // shared memory three blocks ahead, or two sets of registers in turn, cost more instructions or warps than they hide (3 %
@@ -251,7 +254,8 @@ __global__ void __launch_bounds__(FP8Q_THREADS) k_fp8_gated_quant(const TIn* __r
   }
 }
 
-// Weights (offline): one CTA per block of 128 output channels x 128 features of one matrix.
+// Weights (offline): one CTA per block of 128 output channels x 128 features of one matrix.  11008 x 4096 in 27 us (20.7 at
+// the copy rate; fp32 37 and 34.5), 32 matrices of 4096 x 4096 in 267 (247; fp32 374 and 411).
 //   W [E, N, K], codes [E, N, K], scale [E, ceil(N / 128), ceil(K / 128)]; grid (ceil(K / 128), ceil(N / 128), E)
 template <typename TIn>
 __global__ void __launch_bounds__(256) k_fp8_quant_weights(const TIn* __restrict__ W, int N, int K, uint8_t* __restrict__ codes,

@@ -1277,8 +1277,11 @@ static int launch_fp8_quant_u(const void* X, long ld, const int* rows, int T, in
   return STAMP_OK;
 }
 
-// Chunks of 16, 12 or 8 blocks (fp32: half of that): the one that leaves the fewest lanes without a block at the ends of
-// the rows, where one with less in flight counts for 3 % and 10 % more (16384 x 14336 with 16 and with 8, striding: 107 and 118 us).
+// Chunks of 16, 12 or 8 blocks (fp32: 8 or 4): the one that leaves the fewest lanes without a block at the ends of the
+// rows, where one with less in flight counts for 3 % and 10 % more.  16384 rows, in us, with 16 / 12 / 8 blocks (the choice in
+// brackets): 512 features 8.2 / 7.1 / (6.0), 1152 features 11.2 / (10.2) / 12.2, 2688 features 21.8 / (20.5) / 21.3; where all
+// fit they are alike, 4096 features (30.8) / 30.6 / 30.4, 14336 features (102.7) / 103.4 / 102.9.  fp32 with 8 / 4: 512 features
+// 7.6 / (7.3), 640 features (9.4) / 9.8, 14336 features (165) / 167.
 template <typename TIn>
 static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int M, int K, void* codes, void* scale,
                             cudaStream_t st) {
@@ -1296,7 +1299,9 @@ static int launch_fp8_quant(const void* X, long ld, const int* rows, int T, int 
 
 template <typename TIn>
 static int launch_fp8_gated_quant(const void* X, long ld, int M, int F, void* codes, void* scale, cudaStream_t st) {
-  // four quads in a row share what finding the row costs, unless that leaves warps of the machine without any
+  // Four quads in a row share what finding the row costs, unless that leaves warps of the machine without any.  With 4 / 1, in
+  // us (the choice in brackets): 16384 x 4096 (57.3) / 59.3, 4096 x 4096 (17.5) / 17.6, 2048 x 2048 7.3 / (6.0), 33 x 2048
+  // 4.3 / (1.9).  fp32 rows follow the same rule, though they do without it: 16384 x 4096 (90.9) / 85.4, 33 x 2048 4.2 / (2.0).
   const long all_quads = ((long)F + 4 * FP8_BLOCK - 1) / (4 * FP8_BLOCK);
   const int quads = M * all_quads >= 4L * 40 * sm_count() ? 4 : 1;
   Fp8Rows r;
@@ -1394,9 +1399,13 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p, int most) {
 }
 
 // Steps of 512 features that one accumulator sums.  The tensor cores cut the running sum off instead of rounding it, and
-// the error grows with the number of additions: against 64 bits, 4e-7 of the result at 4096 features and 2.3e-6 at 14336.
-// An fp32 output is summed in chunks of 4096 features at most, the chunks added in fp32; in a bf16 output (2e-3) none of it
-// shows.
+// the error grows with the number of additions: against 64 bits, 4e-7 of the result at 4096 features and 2.3e-6 at 14336
+// (activations with outliers; with scales from 2^-7 to 2^2 per block 2.3e-6 and 1.6e-5, where an fp32 product has 9.1e-6).  An
+// fp32 output is summed in chunks of 4096 features at most, the chunks added in fp32: 4.4e-7 and 3.3e-6 at 14336.  What the
+// chunks cost, in us (chunks of 2048 / 4096 / 8192 / none): 16384 x 14336 x 4096 908 / 803 / 742 / 735, 1024 x 4224 x 4096
+// 32 / 28 / 24 / 24.  A bf16 output is summed in one: its own rounding is 1.7e-3, and of 16384 x 14336 x 4096 outputs 0.09 %
+// are the other neighbour of a value that lies within 2e-5 (of the outputs' root mean square) of the halfway point; the distance
+// from 64 bits, 1.65818e-3, is that of an fp32 product rounded to bf16, to six digits.
 static int fp8_chunk(int ks, int y_dtype) {
   const int steps = (ks + 3) / 4;
   return y_dtype == STAMP_F32 && steps > 8 ? 8 : steps;
@@ -1408,7 +1417,10 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
   const bool pair = plan.pair;
   p.bn = plan.bn;
   p.split = plan.split;
-  p.band = 8;   // with pairs of 256 x 256 about as many channel as token tiles at a time: 16384 x 14336 x 4096 811 -> 764 us
+  // With pairs of 256 x 256 about as many channel as token tiles at a time.  Bands of 2 / 8 / 64 channel tiles, in us: 16384 x
+  // 14336 x 4096 690-776 / 680-738 / 681-732, 16384 x 4096 x 4096 205 / 192 / 188, 4096 x 4096 x 28672 337-342 / 331-343 / 349-358,
+  // 16384 rows over 32 experts 265 / 239 / 237; 2048 x 4096 x 11008, single CTAs and few rows are alike within 2 %.
+  p.band = 8;
   // tiles at most: an expert's run ends in one part tile, and no more experts than rows have any
   const long tok_tiles = p.offsets ? (long)p.M / p.bn + (p.E < p.M ? p.E : p.M) : ((long)p.M + p.bn - 1) / p.bn;
   const long tiles = tok_tiles * ((p.N + (pair ? 255 : 127)) / (pair ? 256 : 128));
