@@ -310,6 +310,24 @@ int stamp_fp8_linear_grouped(const void* x, const void* x_scale, const int32_t* 
                              const void* w_scale, const float* bias, int M, int E, int N, int K, void* Y, int y_dtype,
                              void* stream);
 
+/* The product with what follows it in the same kernel:  Y = act(x W^T + bias) + residual, all in fp32, rounded once to the
+ * output type.  Operands and sums as in stamp_fp8_linear.
+ *   activation  stamp_activation.  GELU is v * Phi(v); GELU_TANH v * (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2;
+ *               SILU v / (1 + exp(-v)).  A NaN stays one under all of them                                          in
+ *   residual    [M, N] r_dtype, rows ldr elements apart (ldr >= N), or NULL.  It may be Y itself (same type, ldr = N), which is
+ *               then updated in place -- but not where an fp32 Y of more than 4096 features K has an activation
+ *               (STAMP_ERR_INVALID_ARG); any other overlap with Y is refused likewise                               in */
+typedef enum { STAMP_ACT_NONE = 0, STAMP_ACT_RELU = 1, STAMP_ACT_GELU = 2, STAMP_ACT_GELU_TANH = 3, STAMP_ACT_SILU = 4 } stamp_activation;
+int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
+                           const void* residual, int r_dtype, long long ldr, int M, int N, int K, void* Y, int y_dtype, void* stream);
+
+/* The same, quantized without being stored: codes [M, N] e4m3 and scale [M, ceil(N / 128)] e8m0 of act(x W^T + bias), as
+ * stamp_fp8_quantize would write them for the fp32 values -- the operand of the next product.  N is a multiple of 16; codes
+ * start on a 16-byte boundary.  The sum is taken in one accumulator (2e-6 at 14336 features): a code differs from that of the
+ * exact sum only where its value lies that near a rounding boundary. */
+int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
+                               int M, int N, int K, void* codes, void* scale, void* stream);
+
 /* ---- parity / debug exports: the intermediate stages, judged separately against the oracle ---- */
 
 /* T = L X in fp32, logical token order.  T [B, L, K] float out. */

@@ -29,8 +29,10 @@ EXPORTS = (
     "stamp_measure_i8_mma_issue", "stamp_debug_expire_wait",
     "stamp_dequantize", "stamp_prepare_weights_both",
     "stamp_fp8_quantize", "stamp_fp8_gated_quantize", "stamp_fp8_quantize_weights", "stamp_fp8_linear",
-    "stamp_fp8_linear_grouped", "stamp_debug_fp8_plan",
+    "stamp_fp8_linear_grouped", "stamp_debug_fp8_plan", "stamp_fp8_linear_fused", "stamp_fp8_linear_quantized",
 )
+
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 
 FP8_BLOCK = 128                      # features per scale of the block-scaled 8-bit floating point layers
 FP8_CODES, FP8_SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
@@ -299,6 +301,25 @@ def stamp_fp8_linear_grouped(x: torch.Tensor, x_scale: torch.Tensor, offsets: to
     bias [E, N] float32."""
     return _outputs((_calls or calls()).fp8_linear_grouped(x, x_scale, offsets, w, w_scale, bias, out_dtype, out),
                     "stamp_fp8_linear_grouped")
+
+
+def stamp_fp8_linear_fused(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                           bias: Optional[torch.Tensor] = None, activation: int = ACT_NONE,
+                           residual: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(codes [M, K] times weight codes [N, K] + bias [N] float32) + residual [M, N] -> [M, N] in one kernel.  residual:
+    float32 or bfloat16, a slice of columns of a wider matrix if need be; out may be the residual itself (in place)."""
+    return _outputs((_calls or calls()).fp8_linear_fused(x, x_scale, w, w_scale, bias, activation, residual, out_dtype, out),
+                    "stamp_fp8_linear_fused")
+
+
+def stamp_fp8_linear_quantized(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                               bias: Optional[torch.Tensor] = None, activation: int = ACT_NONE,
+                               codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """act(codes [M, K] times weight codes [N, K] + bias) quantized in the same kernel -> (codes [M, N], scale
+    [M, ceil(N / 128)]), the operand of the next product.  codes, scale: buffers to write instead of new ones."""
+    return _outputs((_calls or calls()).fp8_linear_quantized(x, x_scale, w, w_scale, bias, activation, codes, scale),
+                    "stamp_fp8_linear_quantized")
 
 
 def stamp_workspace_bytes_host(cfg: StampConfig, B: int, L: int, K: int, N: int, x_dtype: int, y_dtype: int) -> int:

@@ -67,6 +67,12 @@ struct Fp8GemmParams {
   int split;               // CTAs that share a tile's sum (PAIR: 1)
   int chunk;               // steps of 512 features that one accumulator sums (fp32 output), else all of them
   int band;                // channel tiles per raster band
+  // FUSED only: what follows the sum
+  int act;                 // stamp_activation
+  const void* residual;    // [M, ldr] float or bf16, or nullptr
+  int r_bf16;              // residual is bf16
+  long ldr;
+  uint8_t* y_scale;        // quantized output: [M, ceil(N / 128)]
 };
 
 template <bool PAIR>
@@ -78,7 +84,12 @@ struct Fp8Smem {
   static constexpr int NUM_BARS = 2 * FP8G_MAX_STAGES + 2 * FP8G_SF_SLOTS + 4; // full, empty, sffull, sfempty, tfull[2], tempty[2]
   static constexpr int TAB_OFFSET = BAR_OFFSET + NUM_BARS * 8 + 16;
   static constexpr int DYN_BYTES = TAB_OFFSET + 2 * (FP8_MAX_EXPERTS + 1) * 4 + 1024;
-  static_assert(DYN_BYTES <= 227 * 1024, "shared memory of one CTA");
+  // FUSED, quantized output: one barrier for each half of the epilogue warps, their maxima [half][buffer][quarter][token] and
+  // the tokens' inverse scales [warp][token]
+  static constexpr int EX_OFFSET = (TAB_OFFSET + 2 * (FP8_MAX_EXPERTS + 1) * 4 + 15) / 16 * 16;
+  static constexpr int EX_BYTES = 16 + 2 * 2 * 4 * 32 * 4 + FP8G_EPI_WARPS * 32 * 4;
+  static constexpr int FUSED_DYN_BYTES = EX_OFFSET + EX_BYTES + 1024;
+  static_assert(DYN_BYTES <= 227 * 1024 && FUSED_DYN_BYTES <= 227 * 1024, "shared memory of one CTA");
   // tensor memory: second accumulator, then the two buffers of scale columns (4 for channels, BN / 32 for tokens)
   static constexpr int ACC1 = PAIR ? 224 : FP8G_ACC_COLS;
   static constexpr int SF_COL = PAIR ? 480 : 2 * FP8G_ACC_COLS;
@@ -169,7 +180,80 @@ __device__ __forceinline__ void fp8_store2(__nv_bfloat16* y, float a, float b, b
   }
 }
 
-template <bool PAIR, typename TOut>
+// ---- what follows the sum in the fused form: activation, residual, quantization
+// The activation of two sums at once, in fp32.  NONE and RELU are exact; SILU as in the gated quantizer, about an ulp.
+// GELU v Phi(v) by CUDA's normal distribution function (5 ulp, also where Phi is small: 1 + erf would cancel there).
+// GELU_TANH: (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)), which does not cancel either; 2 u is rounded three times, so that the
+// result is within about (8 + 2 |2 u|) 2^-24 of itself.
+__device__ __forceinline__ float2 fp8_activate2(float2 v, int act) {
+  switch (act) {
+    case STAMP_ACT_RELU: return make_float2(v.x < 0.f ? 0.f : v.x, v.y < 0.f ? 0.f : v.y);   // (a NaN stays one)
+    case STAMP_ACT_GELU: return make_float2(v.x * normcdff(v.x), v.y * normcdff(v.y));
+    case STAMP_ACT_GELU_TANH: {
+      constexpr float C = 1.5957691216f * 1.4426950409f;   // 2 sqrt(2 / pi) log2(e)
+      const float ax = v.x * fmaf(v.x * v.x, -0.044715f * C, -C), ay = v.y * fmaf(v.y * v.y, -0.044715f * C, -C);
+      return make_float2(__fdividef(v.x, 1.f + ptx::ex2(ax)), __fdividef(v.y, 1.f + ptx::ex2(ay)));
+    }
+    case STAMP_ACT_SILU: return gated_silu2<false, false>(v, make_float2(1.f, 1.f));
+    default: return v;
+  }
+}
+// 32 sums of a thread.  (One jump for all of them.)
+__device__ __forceinline__ void fp8_activate32(uint32_t (&r)[32], float bias, int act) {
+  auto each = [&](auto which) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+      const float2 v = fp8_activate2(make_float2(__uint_as_float(r[j]) + bias, __uint_as_float(r[j + 1]) + bias), decltype(which)::value);
+      r[j] = __float_as_uint(v.x);
+      r[j + 1] = __float_as_uint(v.y);
+    }
+  };
+  switch (act) {
+    case STAMP_ACT_RELU: each(std::integral_constant<int, STAMP_ACT_RELU>{}); break;
+    case STAMP_ACT_GELU: each(std::integral_constant<int, STAMP_ACT_GELU>{}); break;
+    case STAMP_ACT_GELU_TANH: each(std::integral_constant<int, STAMP_ACT_GELU_TANH>{}); break;
+    case STAMP_ACT_SILU: each(std::integral_constant<int, STAMP_ACT_SILU>{}); break;
+    default: each(std::integral_constant<int, STAMP_ACT_NONE>{});
+  }
+}
+__device__ __forceinline__ float fp8_residual(const Fp8GemmParams& p, long row, int ch) {
+  const long at = row * p.ldr + ch;
+  return p.r_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.residual)[at]) : static_cast<const float*>(p.residual)[at];
+}
+// The residual of 32 tokens at this lane's channel, in fp32, loaded before the sums are waited for; zero where there is none.
+// Plain loads: the output may be the same memory, and every element is read by the thread that writes it.
+// PAIRS: bf16 rows whose channels can be read two at a time: as in the store, the even lane takes the first token of two,
+// the odd lane the second, and they swap halves (the same step there and back).
+__device__ __forceinline__ void fp8_load_residual(const Fp8GemmParams& p, long row, int left, int ch, bool pairs, float (&out)[32]) {
+  if (pairs) {
+    const int odd = threadIdx.x & 1, ch2 = ch & ~1;
+    const uint32_t sel = odd ? 0x3276u : 0x5410u;
+    const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(p.residual) + (row + odd) * p.ldr + ch2;
+    uint32_t two[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j, at += 2 * p.ldr) two[j] = (2 * j + odd < left && ch2 < p.N) ? *reinterpret_cast<const uint32_t*>(at) : 0u;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const uint32_t t = __byte_perm(two[j], __shfl_xor_sync(0xffffffffu, two[j], 1), sel);
+      out[2 * j] = __uint_as_float(t << 16);
+      out[2 * j + 1] = __uint_as_float(t & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) out[j] = (j < left && ch < p.N) ? fp8_residual(p, row + j, ch) : 0.f;
+  }
+}
+// The bytes of four tokens at one channel -> the four channels of one token, over four neighbouring lanes: lane r gets token r.
+__device__ __forceinline__ uint32_t fp8_transpose_bytes(uint32_t w) {
+  const int lane = threadIdx.x;
+  w = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 2), lane & 2 ? 0x3276u : 0x5410u);
+  return __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), lane & 1 ? 0x3715u : 0x6240u);
+}
+
+// FUSED: y = act(sum + bias) + residual; TOut = uint8_t (FUSED only): the codes of act(sum + bias), the next product's
+// operand.  A tile's 128 channels are one block of that operand, so its scale comes from the tile alone: the maximum over
+// the lanes of a warp, then over the four warps that hold the block's channels, which exchange it in shared memory.
+template <bool PAIR, typename TOut, bool FUSED = false>
 __global__ void __launch_bounds__(FP8G_THREADS, 1)
     k_fp8_gemm(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
                const __grid_constant__ CUtensorMap tmap_x_tail, Fp8GemmParams p) {
@@ -214,6 +298,10 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
       ptx::mbar_init(&tempty[a], PAIR ? 2 * FP8G_EPI_WARPS : FP8G_EPI_WARPS);
+    }
+    if constexpr (FUSED && sizeof(TOut) == 1) {
+      ptx::mbar_init(reinterpret_cast<uint64_t*>(smem + SM::EX_OFFSET), 4);
+      ptx::mbar_init(reinterpret_cast<uint64_t*>(smem + SM::EX_OFFSET) + 1, 4);
     }
     *abort_word = 0;
     ptx::fence_mbar_init();
@@ -481,6 +569,8 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
     TOut* const y = static_cast<TOut*>(p.y);
     int it = 0;
     bool ok = true;
+    const bool r_pairs = FUSED && p.residual && p.r_bf16 && (p.N & 1) == 0 && (p.ldr & 1) == 0 && (reinterpret_cast<uintptr_t>(p.residual) & 3) == 0;
+    uint32_t exchanged = 0;   // maxima that this half has exchanged
     for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
       const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
       const int ch = (PAIR ? 2 * t.ch_tile + rank : t.ch_tile) * FP8G_BM + row;
@@ -509,6 +599,11 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
         const int count = (chunks - half + 1) / 2;
         for (int i = 0; i < count; ++i) {
           const int c = fp8_drain_chunk(PAIR && a == 0, half, i, count);
+          float res[FUSED ? 32 : 1];
+          if constexpr (FUSED && sizeof(TOut) != 1) {
+            if (p.residual && (PAIR || p.split == 1) && (p.act == STAMP_ACT_NONE ? c0 == step0 : c0 + p.chunk >= step1))
+              fp8_load_residual(p, t.row0 + 32 * c, t.rows - 32 * c, ch, r_pairs, res);
+          }
           uint32_t r[32];
           ptx::tmem_ld_32x32b_x32(taddr + 32 * c, r);
           ptx::tmem_ld_wait();
@@ -521,7 +616,72 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
             continue;
           }
           const int left = t.rows - 32 * c;
-          if constexpr (sizeof(TOut) == 4) {
+          if constexpr (FUSED) {
+            const bool first = c0 == step0, last = c0 + p.chunk >= step1;   // (parts of the sum: fp32 outputs only)
+            if constexpr (sizeof(TOut) == 4) {
+              if (!first && ch < p.N) {
+                const TOut* before = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
+                float b[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) b[j] = j < left ? before[static_cast<long>(j) * p.N] : 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(b[j] + __uint_as_float(r[j]));
+              }
+            }
+            // the bias goes in with the first part, the activation follows the last; without one the residual goes in with the
+            // first part too: the output, which holds the parts, may be the residual's own memory
+            const bool plain = p.act == STAMP_ACT_NONE;
+            fp8_activate32(r, first ? bias : 0.f, last ? p.act : STAMP_ACT_NONE);
+            if (p.residual && (plain ? first : last)) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + res[j]);
+            }
+          }
+          if constexpr (sizeof(TOut) == 1) {
+            // the largest magnitude of every token: over this warp's channels, then over the block's four warps
+            uint8_t* const ex = smem + SM::EX_OFFSET;
+            float* const maxima = reinterpret_cast<float*>(ex + 16) + (half * 2 + static_cast<int>(exchanged & 1u)) * 128;
+            float* const inverse = reinterpret_cast<float*>(ex + 16) + 512 + (warp - 4) * 32;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              float m[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) m[i] = ptx::warp_max_abs(ch < p.N ? __uint_as_float(r[j + i]) : 0.f);
+              if (lane == 0) *reinterpret_cast<float4*>(maxima + quarter * 32 + j) = make_float4(m[0], m[1], m[2], m[3]);
+            }
+            __syncwarp();
+            uint64_t* const bar = reinterpret_cast<uint64_t*>(ex) + half;
+            if (lane == 0) ptx::mbar_arrive(bar);
+            if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar, exchanged & 1u, abort_word, FP8G_WAIT_LIMIT))) {
+              ok = false;
+              break;
+            }
+            ++exchanged;
+            uint32_t amax = 0;   // of token `lane`; bits of magnitudes order like integers, NaNs above infinity
+#pragma unroll
+            for (int q = 0; q < 4; ++q) amax = max(amax, __float_as_uint(maxima[q * 32 + lane]));
+            const Fp8Scale s = fp8_scale(amax);
+            const int block = PAIR ? 2 * t.ch_tile + rank : t.ch_tile, ks_out = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
+            if (quarter == 0 && lane < left && block < ks_out) p.y_scale[static_cast<long>(t.row0 + 32 * c + lane) * ks_out + block] = s.byte;
+            inverse[lane] = s.inverse;
+            __syncwarp();
+            uint8_t* out = static_cast<uint8_t*>(p.y) + static_cast<long>(t.row0 + 32 * c + (lane & 3)) * p.N + (ch & ~3);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4, out += 4 * static_cast<long>(p.N)) {
+              const float4 i4 = *reinterpret_cast<const float4*>(inverse + j);
+              const uint32_t w = fp8_transpose_bytes(ptx::cvt_e4m3x4(__uint_as_float(r[j]) * i4.x, __uint_as_float(r[j + 1]) * i4.y,
+                                                                      __uint_as_float(r[j + 2]) * i4.z, __uint_as_float(r[j + 3]) * i4.w));
+              if (j + (lane & 3) < left && ch < p.N) *reinterpret_cast<uint32_t*>(out) = w;
+            }
+            __syncwarp();   // (the next chunk's inverse scales go to the same place)
+          } else if constexpr (FUSED && sizeof(TOut) == 4) {
+            TOut* out = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
+            if (ch < p.N) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j, out += p.N)
+                if (j < left) *out = __uint_as_float(r[j]);
+            }
+          } else if constexpr (sizeof(TOut) == 4) {
             TOut* out = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
             if (c0 == step0) {
               if (ch < p.N) {
@@ -551,7 +711,8 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
             uint32_t two[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[2 * j]) + bias, __uint_as_float(r[2 * j + 1]) + bias);
+              const __nv_bfloat162 v = FUSED ? __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]))
+                                             : __floats2bfloat162_rn(__uint_as_float(r[2 * j]) + bias, __uint_as_float(r[2 * j + 1]) + bias);
               two[j] = *reinterpret_cast<const uint32_t*>(&v);
             }
 #pragma unroll
@@ -577,6 +738,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
           }
         }
         if (!released) release();
+        if (!ok) break;
       }
     }
     if (!ok) {
@@ -612,8 +774,33 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
         for (int s = 1; s < 8; ++s)
           if (s < p.split) sum = make_float4(sum.x + v[s].x, sum.y + v[s].y, sum.z + v[s].z, sum.w + v[s].w);
         TOut* out = static_cast<TOut*>(p.y) + static_cast<long>(t.row0 + tok) * p.N + ch;
+        if constexpr (FUSED) {
+          const float2 a = fp8_activate2(make_float2(sum.x + bias[0], sum.y + bias[1]), p.act);
+          const float2 b = fp8_activate2(make_float2(sum.z + bias[2], sum.w + bias[3]), p.act);
+          float v[4] = {a.x, a.y, b.x, b.y};
+          if constexpr (sizeof(TOut) == 1) {
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) most = ptx::max_abs_nan(most, ch < p.N ? v[i] : 0.f, ch < p.N ? v[i + 1] : 0.f);
+            const Fp8Scale s = fp8_scale(__float_as_uint(ptx::warp_max_abs(most)));
+            const int ks_out = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
+            if (lane == 0) p.y_scale[static_cast<long>(t.row0 + tok) * ks_out + t.ch_tile] = s.byte;
+            if (ch < p.N)
+              *reinterpret_cast<uint32_t*>(out) = ptx::cvt_e4m3x4(v[0] * s.inverse, v[1] * s.inverse, v[2] * s.inverse, v[3] * s.inverse);
+          } else {
+            if (p.residual) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (ch + i < p.N) v[i] += fp8_residual(p, t.row0 + tok, ch + i);
+            }
+            if (ch < p.N) fp8_store2(out, v[0], v[1], ch + 1 < p.N, vec);
+            if (ch + 2 < p.N) fp8_store2(out + 2, v[2], v[3], ch + 3 < p.N, vec);
+          }
+          continue;
+        } else {
         if (ch < p.N) fp8_store2(out, sum.x + bias[0], sum.y + bias[1], ch + 1 < p.N, vec);
         if (ch + 2 < p.N) fp8_store2(out + 2, sum.z + bias[2], sum.w + bias[3], ch + 3 < p.N, vec);
+        }
       }
     }
     ptx::cluster_sync();

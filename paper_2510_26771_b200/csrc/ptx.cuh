@@ -60,6 +60,12 @@ __device__ __forceinline__ float max_abs_nan(float a, float b, float c) {
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+// The largest magnitude over the warp, in every lane; NaN if there is one.
+__device__ __forceinline__ float warp_max_abs(float v) {
+  float r;
+  asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
 // The larger magnitudes of two pairs of bf16, with some sign.
 __device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;

@@ -1316,11 +1316,11 @@ static int launch_fp8_gated_quant(const void* X, long ld, int M, int F, void* co
   return STAMP_OK;
 }
 
-template <bool PAIR, typename TOut>
+template <bool PAIR, typename TOut, bool FUSED = false>
 static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const CUtensorMap& txt, const Fp8GemmParams& p, long tiles,
                            cudaStream_t st) {
-  auto kern = k_fp8_gemm<PAIR, TOut>;
-  constexpr int bytes = Fp8Smem<PAIR>::DYN_BYTES;
+  auto kern = k_fp8_gemm<PAIR, TOut, FUSED>;
+  constexpr int bytes = FUSED ? Fp8Smem<PAIR>::FUSED_DYN_BYTES : Fp8Smem<PAIR>::DYN_BYTES;
   if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), bytes)) return rc;
   const int per_tile = PAIR ? 2 : p.split;
   const long slots = sm_count() / per_tile;
@@ -1406,11 +1406,15 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p, int most) {
 // 32 / 28 / 24 / 24.  A bf16 output is summed in one: its own rounding is 1.7e-3, and of 16384 x 14336 x 4096 outputs 0.09 %
 // are the other neighbour of a value that lies within 2e-5 (of the outputs' root mean square) of the halfway point; the distance
 // from 64 bits, 1.65818e-3, is that of an fp32 product rounded to bf16, to six digits.
+constexpr int FP8_PART = 4096;
 static int fp8_chunk(int ks, int y_dtype) {
   const int steps = (ks + 3) / 4;
-  return y_dtype == STAMP_F32 && steps > 8 ? 8 : steps;
+  return y_dtype == STAMP_F32 && steps > FP8_PART / 512 ? FP8_PART / 512 : steps;
 }
 
+constexpr int FP8_OUT_CODES = -1;   // output type of the quantized form, beside the public ones
+
+template <bool FUSED = false>
 static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
   p.chunk = fp8_chunk(p.ks, y_dtype);
   const Fp8Plan plan = plan_fp8_gemm(p, p.chunk);
@@ -1437,11 +1441,29 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
   txt = tx;
   if (p.tail)
     if (int rc = make_tmap_i8(p.x, p.M, p.K, FP8G_TAIL_BOX, &txt)) return rc;
+  if constexpr (FUSED) {
+    if (y_dtype == FP8_OUT_CODES)
+      return pair ? launch_fp8_gemm<true, uint8_t, true>(tw, tx, txt, p, tiles, st)
+                  : launch_fp8_gemm<false, uint8_t, true>(tw, tx, txt, p, tiles, st);
+  }
   if (pair)
-    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16>(tw, tx, txt, p, tiles, st)
-                                 : launch_fp8_gemm<true, float>(tw, tx, txt, p, tiles, st);
-  return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16>(tw, tx, txt, p, tiles, st)
-                               : launch_fp8_gemm<false, float>(tw, tx, txt, p, tiles, st);
+    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16, FUSED>(tw, tx, txt, p, tiles, st)
+                                 : launch_fp8_gemm<true, float, FUSED>(tw, tx, txt, p, tiles, st);
+  return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16, FUSED>(tw, tx, txt, p, tiles, st)
+                               : launch_fp8_gemm<false, float, FUSED>(tw, tx, txt, p, tiles, st);
+}
+
+// A residual [M, N] with rows ldr elements apart: aligned to its type, and apart from Y or Y itself.
+static int check_residual(const void* residual, int r_dtype, long long ldr, long M, long N, const void* Y, int y_dtype) {
+  if (!dtype_ok(r_dtype) || ldr < N) return STAMP_ERR_INVALID_ARG;
+  if (M == 0) return STAMP_OK;
+  if (ldr > (1LL << 60) / M) return STAMP_ERR_UNSUPPORTED;
+  const long size = r_dtype == STAMP_BF16 ? 2 : 4;
+  const uintptr_t r = reinterpret_cast<uintptr_t>(residual), y = reinterpret_cast<uintptr_t>(Y);
+  if (r % size != 0) return STAMP_ERR_INVALID_ARG;
+  if (r == y && r_dtype == y_dtype && (ldr == N || M == 1)) return STAMP_OK;
+  const uintptr_t r_end = r + ((M - 1) * ldr + N) * size, y_end = y + M * N * (y_dtype == STAMP_BF16 ? 2 : 4);
+  return r < y_end && y < r_end ? STAMP_ERR_INVALID_ARG : STAMP_OK;
 }
 
 // Arguments common to both products.
@@ -2005,6 +2027,37 @@ int stamp_fp8_linear_grouped(const void* x, const void* x_scale, const int32_t* 
   if (int rc = check_fp8_product(p, y_dtype)) return rc;
   if (!offsets) return STAMP_ERR_INVALID_ARG;
   return M == 0 ? STAMP_OK : run_fp8_gemm(p, y_dtype, static_cast<cudaStream_t>(stream));
+}
+
+int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
+                           const void* residual, int r_dtype, long long ldr, int M, int N, int K, void* Y, int y_dtype, void* stream) {
+  t_launches = 0;
+  Fp8GemmParams p = fp8_params(x, x_scale, nullptr, w, w_scale, bias, M, 1, N, K, Y);
+  if (int rc = check_fp8_product(p, y_dtype)) return rc;
+  if (activation < STAMP_ACT_NONE || activation > STAMP_ACT_SILU) return STAMP_ERR_INVALID_ARG;
+  if (residual) {
+    if (int rc = check_residual(residual, r_dtype, ldr, M, N, Y, y_dtype)) return rc;
+    // the parts of a long fp32 sum are kept in Y until the activation can follow the last: too late for a residual there
+    if (residual == Y && y_dtype == STAMP_F32 && activation != STAMP_ACT_NONE && K > FP8_PART) return STAMP_ERR_INVALID_ARG;
+  }
+  p.act = activation;
+  p.residual = residual;
+  p.r_bf16 = r_dtype == STAMP_BF16;
+  p.ldr = ldr;
+  return M == 0 ? STAMP_OK : run_fp8_gemm<true>(p, y_dtype, static_cast<cudaStream_t>(stream));
+}
+
+int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
+                               int M, int N, int K, void* codes, void* scale, void* stream) {
+  t_launches = 0;
+  Fp8GemmParams p = fp8_params(x, x_scale, nullptr, w, w_scale, bias, M, 1, N, K, codes);
+  if (int rc = check_fp8_product(p, STAMP_BF16)) return rc;
+  if (activation < STAMP_ACT_NONE || activation > STAMP_ACT_SILU) return STAMP_ERR_INVALID_ARG;
+  if (N % 16 != 0) return STAMP_ERR_UNSUPPORTED;
+  if (M > 0 && (!scale || !aligned16(codes))) return STAMP_ERR_INVALID_ARG;
+  p.act = activation;
+  p.y_scale = static_cast<uint8_t*>(scale);
+  return M == 0 ? STAMP_OK : run_fp8_gemm<true>(p, FP8_OUT_CODES, static_cast<cudaStream_t>(stream));
 }
 
 int stamp_debug_fp8_plan(int M, int E, int N, int K, int y_dtype, int* pair, int* rows, int* split) {

@@ -199,9 +199,99 @@ PyObject* fp8_linear_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) {
   STAMP_ENTRY_END
 }
 
+// One matrix and its operands, checked.
+struct Product {
+  const at::Tensor& x;
+  const void *xp, *xs, *wp, *ws;
+  const float* bias;
+  int64_t M, N, K;
+};
+Product product_of(PyObject* const* a) {   // x, x_scale, w, w_scale, bias | None
+  const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[2], "w");
+  if (!x.is_cuda() || x.dim() != 2) refuse("x: expected a two-dimensional CUDA tensor");
+  if (w.dim() != 2) refuse("w: expected a matrix");
+  const at::Device device = x.device();
+  const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
+  return Product{x,
+                 dense(x, "x", {M, K}, CODES, device),
+                 dense(tensor(a[1], "x_scale"), "x_scale", {M, blocks(K)}, SCALE, device),
+                 dense(w, "w", {N, K}, CODES, device),
+                 dense(tensor(a[3], "w_scale"), "w_scale", {blocks(N), blocks(K)}, SCALE, device),
+                 a[4] == Py_None ? nullptr : static_cast<const float*>(dense(tensor(a[4], "bias"), "bias", {N}, at::kFloat, device)),
+                 M, N, K};
+}
+
+int as_int(PyObject* o, const char* what) {
+  const long v = PyLong_Check(o) ? PyLong_AsLong(o) : -1;
+  if (v < 0 || v > INT32_MAX) {
+    PyErr_Clear();
+    char text[80];
+    snprintf(text, sizeof text, "%s: expected a small non-negative number", what);
+    refuse(text);
+  }
+  return static_cast<int>(v);
+}
+
+// A residual [rows, features]: dense rows any distance apart.
+struct Residual {
+  const void* p = nullptr;
+  int type = STAMP_F32;
+  int64_t ld = 0;
+};
+Residual residual_of(PyObject* o, int64_t rows, int64_t features, const at::Device& device) {
+  Residual r;
+  if (o == Py_None) return r;
+  const at::Tensor& t = tensor(o, "residual");
+  if (t.dim() != 2 || t.size(0) != rows || t.size(1) != features || t.device() != device) refuse("residual: expected the output's shape and device");
+  if (features > 1 && t.stride(1) != 1) refuse("residual: expected dense rows");
+  if (rows > 1 && t.stride(0) < features) refuse("residual: expected rows that do not overlap");
+  r.p = t.data_ptr();
+  r.type = dtype_code(t.scalar_type());
+  r.ld = rows > 1 ? t.stride(0) : features;
+  return r;
+}
+
+at::ScalarType out_type(PyObject* dtype, PyObject* out) {
+  if (out != Py_None) return tensor(out, "out").scalar_type();
+  if (!THPDtype_Check(dtype)) refuse("out_dtype: expected a torch.dtype");
+  return reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+}
+
+// (x, x_scale, w, w_scale, bias | None, activation, residual | None, out_dtype, out | None) -> out
+PyObject* fp8_linear_fused(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  STAMP_ENTRY
+  expect(n, 9);
+  const Product p = product_of(a);
+  const c10::cuda::CUDAGuard guard(p.x.device());
+  const int act = as_int(a[5], "activation");
+  const Residual r = residual_of(a[6], p.M, p.N, p.x.device());
+  const at::ScalarType type = out_type(a[7], a[8]);
+  const int code = dtype_code(type);
+  const at::Tensor y = output(a[8], "out", {p.M, p.N}, type, p.x);
+  return status_or(stamp_fp8_linear_fused(p.xp, p.xs, p.wp, p.ws, p.bias, act, r.p, r.type, r.ld, as_int(p.M), as_int(p.N), as_int(p.K),
+                                          y.data_ptr(), code, stream_of(p.x)),
+                   y);
+  STAMP_ENTRY_END
+}
+
+// (x, x_scale, w, w_scale, bias | None, activation, codes | None, scale | None) -> (codes, scale)
+PyObject* fp8_linear_quantized(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  STAMP_ENTRY
+  expect(n, 8);
+  const Product p = product_of(a);
+  const c10::cuda::CUDAGuard guard(p.x.device());
+  const int act = as_int(a[5], "activation");
+  const at::Tensor codes = output(a[6], "codes", {p.M, p.N}, CODES, p.x);
+  const at::Tensor scale = output(a[7], "scale", {p.M, blocks(p.N)}, SCALE, p.x);
+  return status_or(stamp_fp8_linear_quantized(p.xp, p.xs, p.wp, p.ws, p.bias, act, as_int(p.M), as_int(p.N), as_int(p.K), codes.data_ptr(),
+                                              scale.data_ptr(), stream_of(p.x)),
+                   codes, scale);
+  STAMP_ENTRY_END
+}
+
 #define STAMP_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {STAMP_METHOD(fp8_quantize), STAMP_METHOD(fp8_gated_quantize), STAMP_METHOD(fp8_linear),
-                         STAMP_METHOD(fp8_linear_grouped), {nullptr, nullptr, 0, nullptr}};
+                         STAMP_METHOD(fp8_linear_grouped), STAMP_METHOD(fp8_linear_fused), STAMP_METHOD(fp8_linear_quantized), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
