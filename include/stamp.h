@@ -328,6 +328,54 @@ int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, co
 int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
                                int M, int N, int K, void* codes, void* scale, void* stream);
 
+/* ---- expert layers: the router's choice, the way back, and the whole layer for a few tokens --------------
+ * The calls of an expert layer share one description of the routing: M rows in expert order, rows[m] the token of row m,
+ * offsets[e] the first row of expert e, place[t, j] the row that token t's choice j became.  stamp_expert_route makes it;
+ * stamp_fp8_quantize (rows), stamp_fp8_linear_grouped (offsets), stamp_expert_combine (place) and stamp_fp8_expert_layer read
+ * it.  Like the calls above, these only enqueue kernels and may be captured once they have run outside of a capture. */
+
+/* The router's choice: of every token's E logits the `top` largest, of equal ones the lower expert, in falling order.
+ *   logits    [T, E] l_dtype, rows ldl elements apart (ldl >= E)                                                    in
+ *   normalize 0: shares are the softmax over all experts; else the softmax over the chosen ones                     in
+ *             A NaN is chosen last, and its token's shares are NaN; a token whose logits are all -inf (padding) has shares 0.
+ *   chosen    [T, top] int32, share [T, top] float                                                                  out
+ *   rows      [T * top] int32: the rows (t, j) in the order of their experts, inside an expert in memory order: their t out
+ *   place     [T, top] int32: where row (t, j) went; offsets [E + 1] int32; row_share [T * top] float: share by row   out
+ *   ws        stamp_expert_route_workspace_bytes() bytes, 256-byte aligned (none up to 128 tokens: may be NULL)
+ * E <= 1024, top <= min(E, 32), T * top <= 2^30.  T = 0 writes offsets (zeros) only. */
+int stamp_expert_route_workspace_bytes(int T, int E, int top, size_t* out_bytes);
+int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, int E, int top, int normalize, int32_t* chosen,
+                       float* share, int32_t* rows, int32_t* place, int32_t* offsets, float* row_share, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* The way back: out[t] = sum_j share[t, j] y[place[t, j]] + residual[t], in fp32 in the order of j, rounded once.
+ *   y        [M, N] y_dtype; place [T, top] int32; share [T, top] float                                             in
+ *            A place outside [0, M) adds nothing and is reported by stamp_last_device_status() as STAMP_ERR_INVALID_ARG.
+ *   residual [T, N] r_dtype, rows ldr elements apart, or NULL; it may be out itself (same type, ldr = N)            in
+ *   out      [T, N] o_dtype                                                                                         out */
+int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const float* share, const void* residual, int r_dtype,
+                         long long ldr, int T, int top, int M, int N, void* out, int o_dtype, void* stream);
+
+/* The whole layer for a few tokens (a decode step), in two kernels and without quantizing the activations:
+ *   h[m, f] = silu(g) u, g = w_up[e, f] . X[rows[m]] + up_bias[e, f], u the same for channel F + f   (e: the expert of row m)
+ *   Y[t]    = residual[t] + sum over the rows m of token t, in their order, of share[m] (w_down[e] h[m] + down_bias[e])
+ *   X        [T, K] x_dtype, rows ldx elements apart, as for stamp_fp8_quantize                                     in
+ *   rows     [M] int32, share [M] float (row_share of stamp_expert_route), offsets [E + 1] int32                    in
+ *            Rows from offsets[E] on belong to nobody; tokens without a row get the residual alone.  An index outside [0, T)
+ *            adds nothing; offsets out of order write nothing; either is reported by stamp_last_device_status() as
+ *            STAMP_ERR_INVALID_ARG.
+ *   w_up     [E, 2 F, K] codes (gates, then ups) with up_scale [E, ceil(2 F / 128), ceil(K / 128)], up_bias [E, 2 F] or NULL;
+ *   w_down   [E, N, F] codes with down_scale [E, ceil(N / 128), ceil(F / 128)], down_bias [E, N] or NULL            in
+ *   residual [T, N] r_dtype, rows ldr elements apart, or NULL; it may be Y itself (same type, ldr = N)              in
+ *   Y        [T, N] y_dtype                                                                                         out
+ *   ws       stamp_fp8_expert_workspace_bytes() bytes, 256-byte aligned
+ * T <= 64, M <= 2048, E <= 1024, K and F multiples of 16.  A token that holds an infinity or a NaN gets NaN. */
+int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes);
+int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int32_t* rows, const float* share, const int32_t* offsets,
+                           const void* w_up, const void* up_scale, const float* up_bias, const void* w_down, const void* down_scale,
+                           const float* down_bias, const void* residual, int r_dtype, long long ldr, int T, int M, int E, int K, int F,
+                           int N, void* Y, int y_dtype, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- parity / debug exports: the intermediate stages, judged separately against the oracle ---- */
 
 /* T = L X in fp32, logical token order.  T [B, L, K] float out. */

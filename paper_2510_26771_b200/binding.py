@@ -30,6 +30,8 @@ EXPORTS = (
     "stamp_dequantize", "stamp_prepare_weights_both",
     "stamp_fp8_quantize", "stamp_fp8_gated_quantize", "stamp_fp8_quantize_weights", "stamp_fp8_linear",
     "stamp_fp8_linear_grouped", "stamp_debug_fp8_plan", "stamp_fp8_linear_fused", "stamp_fp8_linear_quantized",
+    "stamp_expert_route_workspace_bytes", "stamp_expert_route", "stamp_expert_combine", "stamp_fp8_expert_workspace_bytes",
+    "stamp_fp8_expert_layer",
 )
 
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
@@ -320,6 +322,34 @@ def stamp_fp8_linear_quantized(x: torch.Tensor, x_scale: torch.Tensor, w: torch.
     [M, ceil(N / 128)]), the operand of the next product.  codes, scale: buffers to write instead of new ones."""
     return _outputs((_calls or calls()).fp8_linear_quantized(x, x_scale, w, w_scale, bias, activation, codes, scale),
                     "stamp_fp8_linear_quantized")
+
+
+def stamp_expert_route(logits: torch.Tensor, top: int, normalize: bool = True, out=None):
+    """[T, E] router logits -> (chosen [T, top] int32, share [T, top] float32, rows [T * top] int32, place [T, top] int32,
+    offsets [E + 1] int32, row_share [T * top] float32): every token's `top` experts, the rows in expert order as the products
+    take them, and where each row went.  normalize: shares are a softmax over the chosen experts, else over all.  out: the six
+    buffers to write instead of new ones."""
+    return _outputs((_calls or calls()).expert_route(logits, top, bool(normalize), out), "stamp_expert_route")
+
+
+def stamp_expert_combine(y: torch.Tensor, place: torch.Tensor, share: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                         out_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows [M, N] in expert order -> tokens [T, N]: the sum of each token's rows place [T, top] weighted with share [T, top],
+    plus residual.  out may be the residual itself (in place)."""
+    return _outputs((_calls or calls()).expert_combine(y, place, share, residual, out_dtype, out), "stamp_expert_combine")
+
+
+def stamp_fp8_expert_layer(x: torch.Tensor, rows: torch.Tensor, row_share: torch.Tensor, offsets: torch.Tensor, up: torch.Tensor,
+                           up_scale: torch.Tensor, down: torch.Tensor, down_scale: torch.Tensor,
+                           up_bias: Optional[torch.Tensor] = None, down_bias: Optional[torch.Tensor] = None,
+                           residual: Optional[torch.Tensor] = None, out_dtype=None, out: Optional[torch.Tensor] = None,
+                           ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A whole expert layer for up to 64 tokens [T, K] in two kernels, activations as they are -> [T, N].  rows, row_share,
+    offsets: as stamp_expert_route returns them; up [E, 2 F, K] and down [E, N, F] weight codes with their scales.  out_dtype:
+    x's own without it; out may be the residual itself (in place); ws: scratch to use instead of new memory."""
+    return _outputs((_calls or calls()).fp8_expert_layer(x, rows, row_share, offsets, up, up_scale, up_bias, down, down_scale,
+                                                         down_bias, residual, x.dtype if out_dtype is None else out_dtype, out, ws),
+                    "stamp_fp8_expert_layer")
 
 
 def stamp_workspace_bytes_host(cfg: StampConfig, B: int, L: int, K: int, N: int, x_dtype: int, y_dtype: int) -> int:

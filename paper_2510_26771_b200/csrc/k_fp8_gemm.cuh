@@ -738,7 +738,9 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
           }
         }
         if (!released) release();
-        if (!ok) break;
+        if constexpr (sizeof(TOut) == 1) {
+          if (!ok) break;
+        }
       }
     }
     if (!ok) {

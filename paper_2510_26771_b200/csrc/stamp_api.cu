@@ -10,6 +10,8 @@
 #include "k_dct.cuh"
 #include "k_dct_tc.cuh"
 #include "k_debug.cuh"
+#include "k_expert_layer.cuh"
+#include "k_expert_route.cuh"
 #include "k_fp8_gemm.cuh"
 #include "k_fp8_quant.cuh"
 #include "k_gemm.cuh"
@@ -1476,6 +1478,74 @@ static int check_fp8_product(const Fp8GemmParams& p, int y_dtype) {
   return STAMP_OK;
 }
 
+// ------------------------------------------------------------------------------------------
+// Expert layers: the router's choice, the way back, the whole layer for a few tokens
+// ------------------------------------------------------------------------------------------
+static int route_ctas(int T) {
+  if (T <= ROUTE_ONE_CTA_TOKENS) return 1;
+  const int most = (T + ROUTE_WARPS - 1) / ROUTE_WARPS, sms = sm_count();
+  return most < sms ? most : sms;
+}
+
+template <typename TIn>
+static int launch_route(const RouteParams& p, int ctas, cudaStream_t st) {
+  const int per = (p.E + 31) / 32;
+  auto kern = per <= 1   ? k_expert_choose<TIn, 1>
+              : per <= 2 ? k_expert_choose<TIn, 2>
+              : per <= 4 ? k_expert_choose<TIn, 4>
+              : per <= 8 ? k_expert_choose<TIn, 8>
+                         : k_expert_choose<TIn, 32>;
+  const size_t bytes = (size_t)(ROUTE_WARPS + 1) * p.E * 4;
+  if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), (size_t)(ROUTE_WARPS + 1) * ROUTE_MAX_EXPERTS * 4)) return rc;
+  if (launch_pdl(kern, dim3((unsigned)ctas), dim3(ROUTE_THREADS), bytes, st, p) != cudaSuccess) {
+    cudaGetLastError();
+    return STAMP_ERR_CUDA;
+  }
+  STAMP_CHECK_LAUNCH();
+  if (ctas == 1) return STAMP_OK;
+  if (launch_pdl(k_expert_place, dim3((unsigned)ctas), dim3(ROUTE_THREADS), (size_t)(p.E + 2 * ROUTE_THREADS) * 4, st, p) != cudaSuccess) {
+    cudaGetLastError();
+    return STAMP_ERR_CUDA;
+  }
+  STAMP_CHECK_LAUNCH();
+  return STAMP_OK;
+}
+
+static int check_route(int T, int E, int top) {
+  if (T < 0 || E <= 0 || top <= 0 || top > E) return STAMP_ERR_INVALID_ARG;
+  return E > ROUTE_MAX_EXPERTS || top > ROUTE_MAX_TOP || (long)T * top > (1L << 30) ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
+}
+
+static int run_expert_layer(const ExpertParams& p, int y_dtype, cudaStream_t st) {
+  if (p.M > 0) {
+    k_expert_up_plain<<<dim3((unsigned)((p.F + 7) / 8), (unsigned)p.M), 256, 0, st>>>(p);
+    STAMP_CHECK_LAUNCH();
+  }
+  const dim3 grid((unsigned)((p.N + 7) / 8), (unsigned)p.T);
+  if (y_dtype == STAMP_BF16)
+    k_expert_down_plain<__nv_bfloat16><<<grid, 256, 0, st>>>(p);
+  else
+    k_expert_down_plain<float><<<grid, 256, 0, st>>>(p);
+  STAMP_CHECK_LAUNCH();
+  return STAMP_OK;
+}
+
+template <typename TIn, typename TOut>
+static int launch_combine(const CombineParams& p, int r_bf16, cudaStream_t st) {
+  const auto vector = [](const void* q, size_t element) { return (reinterpret_cast<uintptr_t>(q) & (4 * element - 1)) == 0; };
+  const bool four = p.N % 4 == 0 && vector(p.y, sizeof(TIn)) && vector(p.out, sizeof(TOut)) &&
+                    (!p.residual || (p.ldr % 4 == 0 && vector(p.residual, r_bf16 ? 2 : 4)));
+  const int per = COMBINE_THREADS * (four ? 4 : 1);
+  const dim3 grid((unsigned)p.T, (unsigned)((p.N + (long)per - 1) / per));
+  auto kern = four ? k_expert_combine<TIn, TOut, 4> : k_expert_combine<TIn, TOut, 1>;
+  if (launch_pdl(kern, grid, dim3(COMBINE_THREADS), 0, st, p, r_bf16) != cudaSuccess) {
+    cudaGetLastError();
+    return STAMP_ERR_CUDA;
+  }
+  STAMP_CHECK_LAUNCH();
+  return STAMP_OK;
+}
+
 }  // namespace stamp
 
 // ============================================================================================
@@ -2058,6 +2128,116 @@ int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w
   p.act = activation;
   p.y_scale = static_cast<uint8_t*>(scale);
   return M == 0 ? STAMP_OK : run_fp8_gemm<true>(p, FP8_OUT_CODES, static_cast<cudaStream_t>(stream));
+}
+
+int stamp_expert_route_workspace_bytes(int T, int E, int top, size_t* out_bytes) {
+  if (!out_bytes) return STAMP_ERR_INVALID_ARG;
+  if (int rc = check_route(T, E, top)) return rc;
+  const int ctas = route_ctas(T);
+  *out_bytes = ctas > 1 ? align256((size_t)ctas * E * 4) : 0;
+  return STAMP_OK;
+}
+
+int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, int E, int top, int normalize, int32_t* chosen,
+                       float* share, int32_t* rows, int32_t* place, int32_t* offsets, float* row_share, void* ws, size_t ws_bytes,
+                       void* stream) {
+  t_launches = 0;
+  if (int rc = check_route(T, E, top)) return rc;
+  if (ldl < E || !dtype_ok(l_dtype) || !offsets) return STAMP_ERR_INVALID_ARG;
+  if (T > 0 && (!logits || !chosen || !share || !rows || !place || !row_share)) return STAMP_ERR_INVALID_ARG;
+  if (ldl > (1LL << 60) / (T > 0 ? T : 1)) return STAMP_ERR_UNSUPPORTED;
+  const int ctas = route_ctas(T);
+  if (ctas > 1 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < (size_t)ctas * E * 4)) return STAMP_ERR_WORKSPACE;
+  RouteParams p{};
+  p.logits = logits;
+  p.ldl = ldl;
+  p.T = T;
+  p.E = E;
+  p.top = top;
+  p.normalize = normalize != 0;
+  p.per_cta = (T + ctas - 1) / ctas;
+  p.per_warp = (p.per_cta + ROUTE_WARPS - 1) / ROUTE_WARPS;
+  p.chosen = chosen;
+  p.share = share;
+  p.rows = rows;
+  p.place = place;
+  p.offsets = offsets;
+  p.row_share = row_share;
+  p.counts = static_cast<int*>(ws);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return l_dtype == STAMP_BF16 ? launch_route<__nv_bfloat16>(p, ctas, st) : launch_route<float>(p, ctas, st);
+}
+
+int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const float* share, const void* residual, int r_dtype,
+                         long long ldr, int T, int top, int M, int N, void* out, int o_dtype, void* stream) {
+  t_launches = 0;
+  if (T < 0 || top <= 0 || M < 0 || N <= 0 || !dtype_ok(y_dtype) || !dtype_ok(o_dtype)) return STAMP_ERR_INVALID_ARG;
+  if (N > 65535 * COMBINE_THREADS || (long)T * top > (1L << 40)) return STAMP_ERR_UNSUPPORTED;
+  if (T == 0) return STAMP_OK;
+  if (!place || !share || !out || (M > 0 && !y)) return STAMP_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(y) & (y_dtype == STAMP_BF16 ? 1 : 3)) != 0 || (reinterpret_cast<uintptr_t>(out) & (o_dtype == STAMP_BF16 ? 1 : 3)) != 0)
+    return STAMP_ERR_INVALID_ARG;
+  if (residual)
+    if (int rc = check_residual(residual, r_dtype, ldr, T, N, out, o_dtype)) return rc;
+  const CombineParams p{y, place, share, residual, (long)ldr, T, top, M, N, out};
+  const int r_bf16 = r_dtype == STAMP_BF16;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (y_dtype == STAMP_BF16)
+    return o_dtype == STAMP_BF16 ? launch_combine<__nv_bfloat16, __nv_bfloat16>(p, r_bf16, st) : launch_combine<__nv_bfloat16, float>(p, r_bf16, st);
+  return o_dtype == STAMP_BF16 ? launch_combine<float, __nv_bfloat16>(p, r_bf16, st) : launch_combine<float, float>(p, r_bf16, st);
+}
+
+static int check_expert_layer(int T, int M, int E, int K, int F, int N) {
+  if (T < 0 || M < 0 || E <= 0 || K <= 0 || F <= 0 || N <= 0) return STAMP_ERR_INVALID_ARG;
+  if (T > EXPERT_FEW_TOKENS || M > EXPERT_FEW_ROWS || E > EXPERT_MAX || K % 16 != 0 || F % 16 != 0 || K > FP8_MAX_FEATURES || F > FP8_MAX_FEATURES / 2)
+    return STAMP_ERR_UNSUPPORTED;
+  return (long)E * 2 * F > (1L << 31) - 512 || (long)E * N > (1L << 31) - 512 ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
+}
+
+int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes) {
+  if (!out_bytes || M < 0 || F <= 0) return STAMP_ERR_INVALID_ARG;
+  if (M > EXPERT_FEW_ROWS || F > FP8_MAX_FEATURES / 2) return STAMP_ERR_UNSUPPORTED;
+  *out_bytes = align256((size_t)M * F * 4);
+  return STAMP_OK;
+}
+
+int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int32_t* rows, const float* share, const int32_t* offsets,
+                           const void* w_up, const void* up_scale, const float* up_bias, const void* w_down, const void* down_scale,
+                           const float* down_bias, const void* residual, int r_dtype, long long ldr, int T, int M, int E, int K, int F,
+                           int N, void* Y, int y_dtype, void* ws, size_t ws_bytes, void* stream) {
+  t_launches = 0;
+  if (int rc = check_expert_layer(T, M, E, K, F, N)) return rc;
+  if (ldx < K || !dtype_ok(x_dtype) || !dtype_ok(y_dtype) || !w_up || !up_scale || !w_down || !down_scale || !aligned16(w_up) ||
+      !aligned16(w_down))
+    return STAMP_ERR_INVALID_ARG;
+  if (T == 0) return STAMP_OK;
+  if (!X || !Y || !aligned16(X) || ldx % (x_dtype == STAMP_BF16 ? 8 : 4) != 0 || (reinterpret_cast<uintptr_t>(Y) & (y_dtype == STAMP_BF16 ? 1 : 3)) != 0)
+    return STAMP_ERR_INVALID_ARG;
+  if (!offsets || (M > 0 && (!rows || !share))) return STAMP_ERR_INVALID_ARG;
+  if (ldx > (1LL << 60) / T) return STAMP_ERR_UNSUPPORTED;
+  if (residual)
+    if (int rc = check_residual(residual, r_dtype, ldr, T, N, Y, y_dtype)) return rc;
+  if (M > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < (size_t)M * F * 4)) return STAMP_ERR_WORKSPACE;
+  ExpertParams p{};
+  p.x = X;
+  p.ldx = ldx;
+  p.x_bf16 = x_dtype == STAMP_BF16;
+  p.rows = rows;
+  p.share = share;
+  p.offsets = offsets;
+  p.w_up = static_cast<const uint8_t*>(w_up);
+  p.up_scale = static_cast<const uint8_t*>(up_scale);
+  p.w_down = static_cast<const uint8_t*>(w_down);
+  p.down_scale = static_cast<const uint8_t*>(down_scale);
+  p.up_bias = up_bias;
+  p.down_bias = down_bias;
+  p.residual = residual;
+  p.ldr = ldr;
+  p.r_bf16 = r_dtype == STAMP_BF16;
+  p.T = T, p.M = M, p.E = E, p.K = K, p.F = F, p.N = N;
+  p.h = static_cast<float*>(ws);
+  p.y = Y;
+  return run_expert_layer(p, y_dtype, static_cast<cudaStream_t>(stream));
 }
 
 int stamp_debug_fp8_plan(int M, int E, int N, int K, int y_dtype, int* pair, int* rows, int* split) {

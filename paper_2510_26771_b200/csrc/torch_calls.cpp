@@ -289,9 +289,107 @@ PyObject* fp8_linear_quantized(PyObject*, PyObject* const* a, Py_ssize_t n) {
   STAMP_ENTRY_END
 }
 
+// Scratch of at least `bytes`: `o` if it is given, else new memory of x's device (ordered, like the outputs, by its stream).
+at::Tensor scratch(PyObject* o, size_t bytes, const at::Tensor& x) {
+  if (o == Py_None) return at::empty({static_cast<int64_t>(bytes)}, x.options().dtype(at::kByte));
+  const at::Tensor& t = tensor(o, "ws");
+  if (t.device() != x.device() || !t.is_contiguous()) refuse("ws: expected a contiguous tensor on the inputs' device");
+  return t;
+}
+
+// (logits, top, normalize, out | None) -> (chosen, share, rows, place, offsets, row_share)
+PyObject* expert_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  STAMP_ENTRY
+  expect(n, 4);
+  const Rows l = rows_of(a[0]);
+  const c10::cuda::CUDAGuard guard(l.t.device());
+  const int64_t T = l.rows, E = l.features;
+  const int top = as_int(a[1], "top"), type = dtype_code(l.t.scalar_type());
+  PyObject* given[6] = {Py_None, Py_None, Py_None, Py_None, Py_None, Py_None};
+  if (a[3] != Py_None) {
+    if (!PyTuple_Check(a[3]) || PyTuple_GET_SIZE(a[3]) != 6) refuse("out: expected a tuple of six tensors");
+    for (int i = 0; i < 6; ++i) given[i] = PyTuple_GET_ITEM(a[3], i);
+  }
+  size_t bytes = 0;
+  if (const int rc = stamp_expert_route_workspace_bytes(as_int(T), as_int(E), top, &bytes)) return PyLong_FromLong(rc);
+  const at::Tensor t[6] = {output(given[0], "chosen", {T, top}, at::kInt, l.t), output(given[1], "share", {T, top}, at::kFloat, l.t),
+                           output(given[2], "rows", {T * top}, at::kInt, l.t),  output(given[3], "place", {T, top}, at::kInt, l.t),
+                           output(given[4], "offsets", {E + 1}, at::kInt, l.t), output(given[5], "row_share", {T * top}, at::kFloat, l.t)};
+  at::Tensor ws;
+  if (bytes > 0) ws = scratch(Py_None, bytes, l.t);
+  const int status = stamp_expert_route(l.t.data_ptr(), type, l.ld, as_int(T), as_int(E), top, a[2] == Py_True, static_cast<int32_t*>(t[0].data_ptr()),
+                                        static_cast<float*>(t[1].data_ptr()), static_cast<int32_t*>(t[2].data_ptr()),
+                                        static_cast<int32_t*>(t[3].data_ptr()), static_cast<int32_t*>(t[4].data_ptr()),
+                                        static_cast<float*>(t[5].data_ptr()), bytes > 0 ? ws.data_ptr() : nullptr, bytes, stream_of(l.t));
+  if (status != STAMP_OK) return PyLong_FromLong(status);
+  PyObject* all = PyTuple_New(6);
+  if (!all) return nullptr;
+  for (int i = 0; i < 6; ++i) PyTuple_SET_ITEM(all, i, THPVariable_Wrap(t[i]));
+  return all;
+  STAMP_ENTRY_END
+}
+
+// (y, place, share, residual | None, out_dtype, out | None) -> out
+PyObject* expert_combine(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  STAMP_ENTRY
+  expect(n, 6);
+  const at::Tensor &y = tensor(a[0], "y"), &place = tensor(a[1], "place"), &share = tensor(a[2], "share");
+  if (!y.is_cuda() || y.dim() != 2 || !y.is_contiguous()) refuse("y: expected a contiguous two-dimensional CUDA tensor");
+  if (place.dim() != 2) refuse("place: expected a matrix");
+  const c10::cuda::CUDAGuard guard(y.device());
+  const int64_t M = y.size(0), N = y.size(1), T = place.size(0), top = place.size(1);
+  const void* pp = dense(place, "place", {T, top}, at::kInt, y.device());
+  const void* sp = dense(share, "share", {T, top}, at::kFloat, y.device());
+  const Residual r = residual_of(a[3], T, N, y.device());
+  const at::ScalarType type = out_type(a[4], a[5]);
+  const int code = dtype_code(type), y_code = dtype_code(y.scalar_type());
+  const at::Tensor out = output(a[5], "out", {T, N}, type, y);
+  return status_or(stamp_expert_combine(y.data_ptr(), y_code, static_cast<const int32_t*>(pp), static_cast<const float*>(sp), r.p, r.type, r.ld,
+                                        as_int(T), as_int(top), as_int(M), as_int(N), out.data_ptr(), code, stream_of(y)),
+                   out);
+  STAMP_ENTRY_END
+}
+
+// (x, rows, share, offsets, up, up_scale, up_bias | None, down, down_scale, down_bias | None, residual | None, out_dtype, out | None,
+//  ws | None) -> out
+PyObject* fp8_expert_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  STAMP_ENTRY
+  expect(n, 14);
+  const Rows x = rows_of(a[0]);
+  const at::Device device = x.t.device();
+  const c10::cuda::CUDAGuard guard(device);
+  const at::Tensor &rows = tensor(a[1], "rows"), &up = tensor(a[4], "up"), &down = tensor(a[7], "down");
+  if (up.dim() != 3 || down.dim() != 3) refuse("up, down: expected a matrix for each expert");
+  const int64_t T = x.rows, K = x.features, M = rows.numel(), E = up.size(0), F = down.size(2), N = down.size(1);
+  const void* rp = dense(rows, "rows", {M}, at::kInt, device);
+  const void* sp = dense(tensor(a[2], "row_share"), "row_share", {M}, at::kFloat, device);
+  const void* op = dense(tensor(a[3], "offsets"), "offsets", {E + 1}, at::kInt, device);
+  const void* wu = dense(up, "up", {E, 2 * F, K}, CODES, device);
+  const void* su = dense(tensor(a[5], "up_scale"), "up_scale", {E, blocks(2 * F), blocks(K)}, SCALE, device);
+  const void* bu = a[6] == Py_None ? nullptr : dense(tensor(a[6], "up_bias"), "up_bias", {E, 2 * F}, at::kFloat, device);
+  const void* wd = dense(down, "down", {E, N, F}, CODES, device);
+  const void* sd = dense(tensor(a[8], "down_scale"), "down_scale", {E, blocks(N), blocks(F)}, SCALE, device);
+  const void* bd = a[9] == Py_None ? nullptr : dense(tensor(a[9], "down_bias"), "down_bias", {E, N}, at::kFloat, device);
+  const Residual r = residual_of(a[10], T, N, device);
+  const at::ScalarType type = out_type(a[11], a[12]);
+  const int code = dtype_code(type), x_code = dtype_code(x.t.scalar_type());
+  size_t bytes = 0;
+  if (const int rc = stamp_fp8_expert_workspace_bytes(as_int(M), as_int(F), &bytes)) return PyLong_FromLong(rc);
+  const at::Tensor y = output(a[12], "out", {T, N}, type, x.t);
+  const at::Tensor ws = scratch(a[13], bytes, x.t);
+  return status_or(stamp_fp8_expert_layer(x.t.data_ptr(), x_code, x.ld, static_cast<const int32_t*>(rp), static_cast<const float*>(sp),
+                                          static_cast<const int32_t*>(op), wu, su, static_cast<const float*>(bu), wd, sd,
+                                          static_cast<const float*>(bd), r.p, r.type, r.ld, as_int(T), as_int(M), as_int(E), as_int(K), as_int(F),
+                                          as_int(N), y.data_ptr(), code, ws.data_ptr(), static_cast<size_t>(ws.numel() * ws.element_size()),
+                                          stream_of(x.t)),
+                   y);
+  STAMP_ENTRY_END
+}
+
 #define STAMP_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {STAMP_METHOD(fp8_quantize), STAMP_METHOD(fp8_gated_quantize), STAMP_METHOD(fp8_linear),
-                         STAMP_METHOD(fp8_linear_grouped), STAMP_METHOD(fp8_linear_fused), STAMP_METHOD(fp8_linear_quantized), {nullptr, nullptr, 0, nullptr}};
+                         STAMP_METHOD(fp8_linear_grouped), STAMP_METHOD(fp8_linear_fused), STAMP_METHOD(fp8_linear_quantized),
+                         STAMP_METHOD(expert_route), STAMP_METHOD(expert_combine), STAMP_METHOD(fp8_expert_layer), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

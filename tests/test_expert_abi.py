@@ -1,0 +1,91 @@
+"""The expert layer's calls refuse bad arguments on the host, before anything is launched (no GPU needed)."""
+import ctypes
+
+import pytest
+
+from .test_fp8_abi import A, B, BF16, F32, INVALID, ODD, OK, UNSUPPORTED, p, st  # noqa: F401
+
+WORKSPACE = 3
+R = 1 << 30
+size = ctypes.c_size_t
+long_long = ctypes.c_longlong
+
+
+def route(st, logits=A, dtype=F32, ldl=64, T=4, E=64, top=8, normalize=1, chosen=B, share=B, rows=B, place=B, offsets=B, row_share=B, ws=0, ws_bytes=0):  # noqa: F811
+    return st.lib().stamp_expert_route(p(logits), dtype, long_long(ldl), T, E, top, normalize, p(chosen), p(share), p(rows), p(place), p(offsets), p(row_share),
+                                       p(ws), size(ws_bytes), p(0))
+
+
+def combine(st, y=A, dtype=F32, place=A, share=A, residual=0, r_dtype=F32, ldr=64, T=4, top=2, M=8, N=64, out=B, o_dtype=F32):  # noqa: F811
+    return st.lib().stamp_expert_combine(p(y), dtype, p(place), p(share), p(residual), r_dtype, long_long(ldr), T, top, M, N, p(out), o_dtype, p(0))
+
+
+def layer(st, X=A, dtype=BF16, ldx=256, rows=A, share=A, offsets=A, up=A, up_s=A, up_b=0, down=A, down_s=A, down_b=0, residual=0, r_dtype=BF16, ldr=64,  # noqa: F811
+          T=4, M=8, E=3, K=256, F=128, N=64, Y=B, o_dtype=BF16, ws=A, ws_bytes=1 << 20):
+    return st.lib().stamp_fp8_expert_layer(p(X), dtype, long_long(ldx), p(rows), p(share), p(offsets), p(up), p(up_s), p(up_b), p(down), p(down_s), p(down_b),
+                                           p(residual), r_dtype, long_long(ldr), T, M, E, K, F, N, p(Y), o_dtype, p(ws), size(ws_bytes), p(0))
+
+
+@pytest.mark.parametrize("call,bad", [
+    (route, dict(logits=0)), (route, dict(dtype=2)), (route, dict(ldl=63)), (route, dict(T=-1)), (route, dict(E=0)), (route, dict(top=0)), (route, dict(top=65)),
+    (route, dict(chosen=0)), (route, dict(share=0)), (route, dict(rows=0)), (route, dict(place=0)), (route, dict(offsets=0)), (route, dict(row_share=0)),
+    (combine, dict(y=0)), (combine, dict(dtype=3)), (combine, dict(place=0)), (combine, dict(share=0)), (combine, dict(T=-1)), (combine, dict(top=0)),
+    (combine, dict(M=-1)), (combine, dict(N=0)), (combine, dict(out=0)), (combine, dict(o_dtype=-1)), (combine, dict(out=B + 2)), (combine, dict(y=A + 1, dtype=BF16)),
+    (combine, dict(residual=R, ldr=63)), (combine, dict(residual=R, r_dtype=7)), (combine, dict(residual=B + 4)), (combine, dict(residual=B, ldr=68)),
+    (layer, dict(X=0)), (layer, dict(X=ODD)), (layer, dict(dtype=5)), (layer, dict(ldx=255)), (layer, dict(ldx=260)), (layer, dict(rows=0)), (layer, dict(share=0)),
+    (layer, dict(offsets=0)), (layer, dict(up=0)), (layer, dict(up=ODD)), (layer, dict(up_s=0)), (layer, dict(down=0)), (layer, dict(down=ODD)), (layer, dict(down_s=0)),
+    (layer, dict(residual=R, ldr=63)), (layer, dict(residual=B + 2)), (layer, dict(T=-1)), (layer, dict(M=-1)), (layer, dict(E=0)), (layer, dict(K=0)), (layer, dict(F=0)),
+    (layer, dict(N=0)), (layer, dict(Y=0)), (layer, dict(Y=B + 1)), (layer, dict(o_dtype=2)),
+])
+def test_invalid_arguments(st, call, bad):  # noqa: F811
+    assert call(st, **bad) == INVALID
+    assert st.stamp_last_launch_count() == 0
+
+
+@pytest.mark.parametrize("call,bad", [
+    (route, dict(E=1025, ldl=1025)), (route, dict(top=33)), (route, dict(T=1 << 28)), (route, dict(ldl=1 << 60)),
+    (combine, dict(N=1 << 24, ldr=1 << 24)), (combine, dict(residual=R, ldr=1 << 60)),
+    (layer, dict(T=65)), (layer, dict(M=2049)), (layer, dict(E=1025)), (layer, dict(K=100)), (layer, dict(F=24)), (layer, dict(E=1024, F=1 << 20)),
+    (layer, dict(E=1024, N=1 << 21)), (layer, dict(K=(1 << 31) - 16)), (layer, dict(ldx=1 << 60)), (layer, dict(residual=R, ldr=1 << 60)),
+])
+def test_unsupported_sizes(st, call, bad):  # noqa: F811
+    assert call(st, **bad) == UNSUPPORTED
+    assert st.stamp_last_launch_count() == 0
+
+
+@pytest.mark.parametrize("call,bad", [
+    (route, dict(T=129)), (route, dict(T=4096, ws=A, ws_bytes=100)), (route, dict(T=4096, ws=A + 16, ws_bytes=1 << 20)),
+    (layer, dict(ws=0)), (layer, dict(ws=A + 16)), (layer, dict(ws_bytes=8 * 128 * 4 - 1)),
+])
+def test_workspaces_are_checked(st, call, bad):  # noqa: F811
+    assert call(st, **bad) == WORKSPACE
+    assert st.stamp_last_launch_count() == 0
+
+
+def test_workspace_sizes(st):  # noqa: F811
+    out = size(7)
+    f = st.lib().stamp_expert_route_workspace_bytes
+    assert f(128, 64, 8, ctypes.byref(out)) == OK and out.value == 0
+    assert f(4096, 64, 8, ctypes.byref(out)) == OK and out.value >= 64 * 4 and out.value % 256 == 0
+    assert f(4, 64, 65, ctypes.byref(out)) == INVALID and f(4, 1025, 8, ctypes.byref(out)) == UNSUPPORTED and f(4, 64, 8, None) == INVALID
+    f = st.lib().stamp_fp8_expert_workspace_bytes
+    assert f(8, 128, ctypes.byref(out)) == OK and out.value >= 8 * 128 * 4 and out.value % 256 == 0
+    assert f(0, 128, ctypes.byref(out)) == OK
+    assert f(-1, 128, ctypes.byref(out)) == INVALID and f(2049, 128, ctypes.byref(out)) == UNSUPPORTED and f(8, 0, ctypes.byref(out)) == INVALID and f(8, 128, None) == INVALID
+
+
+def test_no_tokens_launch_nothing(st):  # noqa: F811
+    assert combine(st, T=0, place=0, share=0, out=0) == OK
+    assert layer(st, T=0, M=0, X=0, Y=0, rows=0, share=0, ws=0) == OK
+    assert st.stamp_last_launch_count() == 0
+
+
+def test_the_marshalling_module_refuses_what_is_not_a_cuda_tensor(st):  # noqa: F811
+    import torch
+    x, i = torch.zeros(4, 16), torch.zeros(4, 2, dtype=torch.int32)
+    c, s = torch.zeros(1, 16, 16).to(torch.float8_e4m3fn), torch.zeros(1, 1, 1, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    for bad in (lambda: st.stamp_expert_route(x, 2), lambda: st.stamp_expert_route(None, 2), lambda: st.stamp_expert_combine(x, i, i.float()),
+                lambda: st.stamp_expert_combine(3, i, i.float()), lambda: st.stamp_fp8_expert_layer(x, i[0], i[0].float(), i[0], c, s, c, s),
+                lambda: st.calls().expert_route(x), lambda: st.calls().expert_combine(x), lambda: st.calls().fp8_expert_layer(x)):
+        with pytest.raises(ValueError):
+            bad()
