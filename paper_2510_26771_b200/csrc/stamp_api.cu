@@ -1516,18 +1516,60 @@ static int check_route(int T, int E, int top) {
   return E > ROUTE_MAX_EXPERTS || top > ROUTE_MAX_TOP || (long)T * top > (1L << 30) ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
 }
 
-static int run_expert_layer(const ExpertParams& p, int y_dtype, cudaStream_t st) {
-  if (p.M > 0) {
-    k_expert_up_plain<<<dim3((unsigned)((p.F + 7) / 8), (unsigned)p.M), 256, 0, st>>>(p);
-    STAMP_CHECK_LAUNCH();
+template <bool UP, typename TOut>
+static int launch_expert(ExpertParams p, long units, cudaStream_t st) {
+  using SM = ExpertSmem<UP>;
+  auto kern = k_expert_layer<UP, TOut>;
+  if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), EXPERT_SMEM)) return rc;
+  const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T);
+  p.stage_bytes = (UP ? 2 : 1) * EXPERT_W_BYTES + (p.terms * p.cap + 15) / 16 * 16 * 128;
+  p.stages = (EXPERT_SMEM - fixed) / (p.stage_bytes + SM::SF_BYTES);
+  if (p.stages > EXPERT_MAX_STAGES) p.stages = EXPERT_MAX_STAGES;
+  CUtensorMap tm;
+  if (int rc = UP ? make_tmap_i8(p.w_up, (long)p.E * 2 * p.F, p.K, 128, &tm) : make_tmap_i8(p.w_down, (long)p.E * p.N, p.F, 128, &tm)) return rc;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3((unsigned)(units * p.split));
+  lc.blockDim = dim3(EXPERT_THREADS);
+  lc.dynamicSmemBytes = (size_t)(fixed + p.stages * (p.stage_bytes + SM::SF_BYTES));
+  lc.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)p.split;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = p.split > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&lc, kern, tm, p) != cudaSuccess) {
+    cudaGetLastError();
+    return STAMP_ERR_CUDA;
   }
-  const dim3 grid((unsigned)((p.N + 7) / 8), (unsigned)p.T);
-  if (y_dtype == STAMP_BF16)
-    k_expert_down_plain<__nv_bfloat16><<<grid, 256, 0, st>>>(p);
-  else
-    k_expert_down_plain<float><<<grid, 256, 0, st>>>(p);
   STAMP_CHECK_LAUNCH();
   return STAMP_OK;
+}
+
+static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
+  const int tokens = (p.T + 7) & ~7;
+  auto cap = [&](int columns) {   // rows of a run: as many as there are tokens, as far as their terms have columns
+    const int most = columns / p.terms & ~7;
+    return tokens < most ? tokens : most;
+  };
+  if (p.M > 0) {
+    p.terms = p.x_bf16 ? 2 : 4;
+    p.cap = cap(ExpertSmem<true>::COLUMNS);
+    p.split = 1;
+    const long tiles = (p.F + 127L) / 128, runs = p.E < p.M ? p.E : p.M;
+    const int blocks = (p.K + 127) / 128;
+    while (p.split < 8 && p.split * 4 <= blocks && tiles * runs * p.split < 4L * sm_count()) p.split *= 2;
+    if (int rc = launch_expert<true, float>(p, tiles * expert_max_runs(p.M, p.E, p.cap), st)) return rc;
+  }
+  p.terms = y_dtype == STAMP_BF16 ? 3 : 4;
+  p.cap = cap(ExpertSmem<false>::COLUMNS);
+  const long tiles = (p.N + 127L) / 128;
+  p.split = 1;
+  while (p.split < 8 && tiles * p.split < 2L * sm_count()) p.split *= 2;
+  return y_dtype == STAMP_BF16 ? launch_expert<false, __nv_bfloat16>(p, tiles, st) : launch_expert<false, float>(p, tiles, st);
 }
 
 template <typename TIn, typename TOut>
@@ -2191,7 +2233,9 @@ static int check_expert_layer(int T, int M, int E, int K, int F, int N) {
   if (T < 0 || M < 0 || E <= 0 || K <= 0 || F <= 0 || N <= 0) return STAMP_ERR_INVALID_ARG;
   if (T > EXPERT_FEW_TOKENS || M > EXPERT_FEW_ROWS || E > EXPERT_MAX || K % 16 != 0 || F % 16 != 0 || K > FP8_MAX_FEATURES || F > FP8_MAX_FEATURES / 2)
     return STAMP_ERR_UNSUPPORTED;
-  return (long)E * 2 * F > (1L << 31) - 512 || (long)E * N > (1L << 31) - 512 ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
+  if ((long)E * 2 * F > (1L << 31) - 512 || (long)E * N > (1L << 31) - 512) return STAMP_ERR_UNSUPPORTED;
+  // CTAs and steps are counted in 32 bits: runs of eight rows at least, a cluster of eight CTAs at most
+  return (long)expert_max_runs(M, E, 8) * ((F + 127L) / 128) * 8 > 0x7FFFFFFFL ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
 }
 
 int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes) {
