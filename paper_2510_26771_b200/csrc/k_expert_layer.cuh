@@ -13,23 +13,25 @@
 //   more than 2^14 below their block's largest keep an error of 2^-24 of that.
 // A term is a column of the product like any other row's, so the terms cost columns (16 at least in any case), not another
 // pass over the weights; the epilogue adds them up.  bf16 tokens take two terms, fp32 ones four, the hidden values three for a
-// bf16 output and four for an fp32 one.
+// bf16 output and four for an fp32 one.  UP leaves the hidden values as terms already, DOWN copies them like the weights.
 //
 //   warps 0-3   epilogue, one TMEM lane (output channel) a thread
-//   warp 4      TMA producer: 128 channels x 128 features of weights (UP: of gates and of ups) into a ring of stages
+//   warp 4      TMA producer: 128 channels x 128 features of weights (UP: of gates and of ups), DOWN: and of the rows' terms,
+//               into a ring of stages
 //   warp 5      allocates TMEM, copies the scale words to it and issues the MMAs
-//   warps 6-13  converters: the rows' terms and all scales.  As many warps for each stage of the ring as eight allow, always the
-//               same ones: who fills a stage has filled it the time before too, so that the parity it waits for is never
-//               an older one's, and it can load the stage's next rows as soon as it is through with the last
+//   warps 6-13  the scales, UP: and the tokens' terms.  Always the same warps for a stage of the ring: who fills it has filled
+//               it the time before too, so that the parity it waits for is never an older one's, and it can load the stage's
+//               next rows as soon as it is through with the last
 // Every wait is bounded; when one expires the CTA raises the device status word, unwinds and frees its TMEM.
 //
-// UP: a CTA takes one run (up to `cap` rows of one expert), 128 gates and the 128 ups that go with them, and, in a cluster of
-// `split`, a share of the features; the partial sums are added over distributed shared memory in rank order.
+// UP: a tile is one run (up to `cap` rows of one expert) times 128 gates and the 128 ups that go with them.  One CTA an SM takes
+// tile after tile, the epilogue of one beside the copies of the next.  Where there are few tiles a cluster of `split` CTAs
+// takes one, each a share of the features; the partial sums are added over distributed shared memory in rank order.
 // DOWN: a cluster takes 128 output channels and all runs; its CTAs share the sequence of all (run, 128 features).  A CTA adds
 // each run's rows, weighted, to its tokens in shared memory in the order of the rows; the CTAs' sums are added in rank order,
 // with the residual.  No atomics on results, nothing in memory but the hidden values, and every result repeats bit for bit.
-// DOWN is launched as a programmatic dependent of UP: it needs less than half of an SM's shared memory, as UP does, so its
-// first weights are on their way while UP's last CTAs run; only its converters wait for the hidden values.
+// DOWN is launched as a programmatic dependent of UP: its first weights are on their way while UP's last CTAs run; only its
+// copies of the hidden values and their scales wait.
 #pragma once
 #include "common.cuh"
 #include "k_fp8_gemm.cuh"
@@ -41,11 +43,10 @@ namespace stamp {
 constexpr int EXPERT_FEW_TOKENS = 64;
 constexpr int EXPERT_FEW_ROWS = 2048;
 constexpr int EXPERT_MAX = 1024;
-constexpr int EXPERT_CONVERTERS = 8;
-constexpr int EXPERT_THREADS = 32 * (6 + EXPERT_CONVERTERS);
 constexpr int EXPERT_MAX_STAGES = 8;
 constexpr int EXPERT_W_BYTES = 128 * 128;
-constexpr int EXPERT_SMEM = 112 * 1024;                 // of a CTA: two to an SM
+constexpr int EXPERT_MAX_SMEM = 224 * 1024;             // of a CTA that has an SM to itself; two of half of it fit one
+constexpr int EXPERT_H_BYTES = 2 * 8 * 128 * 4;         // UP: hidden values of eight rows on their way to terms, twice
 
 struct ExpertParams {
   const void* x;            // [T, ldx] bf16 or float
@@ -60,25 +61,31 @@ struct ExpertParams {
   long ldr;
   int r_bf16;
   int T, M, E, K, F, N;
-  float* h;                 // [M, F]
+  uint8_t* h;               // [terms][M, F] codes of the hidden values, terms of the DOWN kernel
+  uint8_t* h_scale;         // [M, ceil(F / 128)] scale of a row's first term
   void* y;                  // [T, N]
   // one kernel's plan
-  int terms, cap;           // terms of a row; rows of a run at most (a multiple of 8, terms * cap <= columns)
+  int terms, h_terms;       // terms of a row; of a hidden value
+  int cap;                  // rows of a run at most (a multiple of 8, terms * cap <= columns)
   int split;                // CTAs of a cluster
   int stages, stage_bytes;
 };
 
 template <bool UP>
 struct ExpertSmem {
-  static constexpr int COLUMNS = UP ? 64 : 96;          // of one accumulator
+  static constexpr int FILLERS = UP ? 10 : 8;           // warps that write scales (UP: and terms)
+  static constexpr int THREADS = 32 * (6 + FILLERS);
+  static constexpr int CTAS = UP ? 1 : 2;               // of an SM that the registers allow
+  static constexpr int COLUMNS = UP ? 32 : 64;          // of one sum
+  static constexpr int ACC = 64;                        // tensor memory: two accumulators (UP: gates, ups), then the stages' scales
+  static constexpr int SF_COL = 2 * ACC;
   static constexpr int SF_BYTES = UP ? 1536 : 1024;     // scale words of a stage: channels (UP: twice), then rows
   static constexpr int SF_COLS = SF_BYTES / 128;
-  static constexpr int SF_COL = 2 * COLUMNS;            // tensor memory: two accumulators (UP: gates, ups), then the stages' scales
   static_assert(SF_COL + EXPERT_MAX_STAGES * SF_COLS <= 256, "half of the tensor memory: two CTAs to an SM");
-  static constexpr int BARS = 2 * EXPERT_MAX_STAGES + 4;
-  // after the ring and the scale words: barriers, [tmem, abort, runs, bad], run tables, DOWN: sums [T][128]
+  static constexpr int BARS = 2 * EXPERT_MAX_STAGES + 6;
+  // after the ring and the scale words: barriers, [tmem, abort, runs, -], run table, UP: hidden values, tokens [M], DOWN: sums [T][128]
   __host__ __device__ static constexpr int tables(int max_runs) { return BARS * 8 + 16 + (max_runs * 8 + 15) / 16 * 16; }
-  __host__ __device__ static int fixed(int max_runs, int T) { return 1024 + tables(max_runs) + (UP ? 0 : T * 512); }
+  __host__ __device__ static int fixed(int max_runs, int T, int M) { return 1024 + tables(max_runs) + (UP ? EXPERT_H_BYTES + M * 4 : T * 512); }
 };
 
 // Runs at most: an expert's rows end in one part run, and no more experts than rows have any.
@@ -118,39 +125,42 @@ struct ExpertRaw {
   }
 };
 
-// One row's 128 features (four a lane) as terms: codes to row `row` of the operand tile (128-byte rows, 128-byte swizzle) and,
-// for each further term, `pitch` rows further; scale words to the order tmem_copy_scales wants.
-__device__ __forceinline__ void expert_convert(const float (&value)[4], int terms, int row, int pitch, uint8_t* tile, uint8_t* words) {
-  const int lane = threadIdx.x & 31;
+// The scale of term t, from the first term's (which stops at 2^-127; a NaN's terms are all NaN).
+__device__ __forceinline__ uint32_t expert_term_scale(uint32_t first, int t) {
+  const uint32_t down = t == 0 ? 0u : 5u * t - 1u;
+  return first == 255u ? 255u : first - min(first, down);
+}
+// 128 values of a row, four a lane, as terms: emit(t, codes) for each; returns the scale byte of the first.
+template <typename Emit>
+__device__ __forceinline__ uint32_t expert_terms(const float (&value)[4], int terms, Emit&& emit) {
   const float most = ptx::warp_max_abs(ptx::max_abs_nan(ptx::max_abs_nan(value[0], value[1], value[2]), value[3], 0.f));
   const Fp8Scale s = fp8_scale(__float_as_uint(most));
   float v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = value[i] * s.inverse;
-  uint32_t byte = s.byte, mine = 0u;
-  uint8_t* out = tile + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + ((lane & 3) << 2);   // (pitch is a multiple of 8)
   for (int t = 0;;) {
     const uint32_t c = ptx::cvt_e4m3x4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<uint32_t*>(out) = c;
-    if (lane == t) mine = byte;
+    emit(t, c);
     if (++t == terms) break;
-    out += pitch * 128;
-    // what is left, in units of the next term's scale (which stops at 2^-127; a NaN's terms are all NaN)
-    const uint32_t shift = min(t == 1 ? 4u : 5u, byte);
+    // what is left, in units of the next term's scale
+    const uint32_t shift = s.byte == 255 ? 0u : expert_term_scale(s.byte, t - 1) - expert_term_scale(s.byte, t);
     const float up = __uint_as_float((127u + shift) << 23);
     const float2 a = expert_e4m3x2(c), b = expert_e4m3x2(c >> 16);
     v[0] = (v[0] - a.x) * up, v[1] = (v[1] - a.y) * up, v[2] = (v[2] - b.x) * up, v[3] = (v[3] - b.y) * up;
-    if (byte != 255u) byte -= shift;
   }
-  if (lane < terms) {
-    const int r = row + lane * pitch;
-    *reinterpret_cast<uint32_t*>(words + ((r & 31) << 4) + ((r >> 5) << 2)) = mine * 0x01010101u;
-  }
+  return s.byte;
+}
+// Row i of a run, term t: its column.  Eight rows' first terms, then their second ones, and so on; then the next eight rows.
+__device__ __forceinline__ int expert_column(int i, int t, int terms) { return (i & ~7) * terms + t * 8 + (i & 7); }
+// The scale bytes of a row's terms, in the order that tmem_copy_scales wants.
+__device__ __forceinline__ void expert_scale_words(uint8_t* words, int i, int t, int terms, uint32_t first) {
+  const int r = expert_column(i, t, terms);
+  *reinterpret_cast<uint32_t*>(words + ((r & 31) << 4) + ((r >> 5) << 2)) = expert_term_scale(first, t) * 0x01010101u;
 }
 
 template <bool UP, typename TOut>
-__global__ void __launch_bounds__(EXPERT_THREADS, 2)
-    k_expert_layer(const __grid_constant__ CUtensorMap tmap, ExpertParams p) {
+__global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
+    k_expert_layer(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_h, ExpertParams p) {
   using SM = ExpertSmem<UP>;
   extern __shared__ uint8_t expert_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(expert_raw) + 1023) & ~uintptr_t(1023));
@@ -159,62 +169,80 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
   uint64_t* const empty = full + EXPERT_MAX_STAGES;
   uint64_t* const tfull = empty + EXPERT_MAX_STAGES;
   uint64_t* const tempty = tfull + 2;
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+  uint64_t* const exchange = tempty + 2;   // (and one word to spare)
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(exchange + 2);
   volatile uint32_t* const abort_word = tmem_slot + 1;
   int* const run_count = reinterpret_cast<int*>(tmem_slot + 2);   // -1: the offsets are out of order
   ExpertRun* const run_table = reinterpret_cast<ExpertRun*>(tmem_slot + 4);
   const int max_runs = expert_max_runs(p.M, p.E, p.cap);
   float* const sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(full) + SM::tables(max_runs));
+  float* const hidden = sums;
+  int* const tokens = reinterpret_cast<int*>(hidden + EXPERT_H_BYTES / 4);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.split > 1 ? static_cast<int>(ptx::cluster_ctarank()) : 0;
   const int unit = blockIdx.x / p.split;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      ptx::mbar_init(&full[s], 1 + EXPERT_CONVERTERS / p.stages);
+      ptx::mbar_init(&full[s], 1 + (UP ? SM::FILLERS / p.stages : 1));
       ptx::mbar_init(&empty[s], UP ? 2 : 1);
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
       ptx::mbar_init(&tempty[a], 4);
     }
+    ptx::mbar_init(exchange, 4);
     *abort_word = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&tmap);
+    if constexpr (!UP) ptx::prefetch_tensormap(&tmap_h);
   }
   if (warp == 5) {
     ptx::tmem_alloc(tmem_slot, 256);
     ptx::tmem_relinquish();
   }
   if constexpr (!UP) {
-    for (int i = threadIdx.x; i < p.T * 128; i += EXPERT_THREADS) sums[i] = 0.f;
+    for (int i = threadIdx.x; i < p.T * 128; i += SM::THREADS) sums[i] = 0.f;
   }
   // UP waits for what came before it.  DOWN starts when every CTA of UP has come past this point: what UP waited for is there
   // for DOWN too, and only the hidden values are to be waited for.  (Where no row exists, DOWN is alone and waits.)
   if (UP || p.M == 0) ptx::grid_dependency_wait();
-  if constexpr (UP) ptx::grid_launch_dependents();
+  if constexpr (UP) {
+    ptx::grid_launch_dependents();
+    for (int m = threadIdx.x; m < p.M; m += SM::THREADS) tokens[m] = __ldcg(p.rows + m);
+  }
   if (warp == 4) {
     bool bad = false;
     int runs = 0;
-    for (int e0 = 0; e0 < p.E; e0 += 32) {
-      const int e = e0 + lane;
-      const int first = e <= p.E ? __ldcg(p.offsets + e) : 0, last = e < p.E ? __ldcg(p.offsets + e + 1) : first;
-      bad |= e < p.E && (first < 0 || last > p.M || last < first || (e == 0 && first != 0));
-      if (__any_sync(0xffffffffu, bad)) {
-        bad = true;
-        break;
-      }
-      const int own = (last - first + p.cap - 1) / p.cap;
-      int before = own;
+    for (int e0 = 0; e0 < p.E && !bad; e0 += 128) {
+      int first[4], last[4];   // the loads of 128 experts at once
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, before, d);
-        if (lane >= d) before += v;
+      for (int i = 0; i < 4; ++i) {
+        const int e = e0 + 32 * i + lane;
+        first[i] = e < p.E ? __ldcg(p.offsets + e) : 0;
+        last[i] = e < p.E ? __ldcg(p.offsets + e + 1) : 0;
       }
-      const int at = runs + before - own;
-      for (int i = 0; i < own; ++i)
-        run_table[at + i] = ExpertRun{first + i * p.cap, static_cast<uint16_t>(e), static_cast<uint16_t>(min(p.cap, last - first - i * p.cap))};
-      runs += __shfl_sync(0xffffffffu, before, 31);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = e0 + 32 * i + lane;
+        bad |= first[i] < 0 || last[i] > p.M || last[i] < first[i] || (e == 0 && first[i] != 0);
+        if (__any_sync(0xffffffffu, bad)) {
+          bad = true;
+          break;
+        }
+        if (e0 + 32 * i >= p.E) break;
+        const int own = (last[i] - first[i] + p.cap - 1) / p.cap;
+        int before = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, before, d);
+          if (lane >= d) before += v;
+        }
+        const int at = runs + before - own;
+        for (int j = 0; j < own; ++j)
+          run_table[at + j] = ExpertRun{first[i] + j * p.cap, static_cast<uint16_t>(e), static_cast<uint16_t>(min(p.cap, last[i] - first[i] - j * p.cap))};
+        runs += __shfl_sync(0xffffffffu, before, 31);
+      }
     }
     if (lane == 0) {
       *run_count = bad ? -1 : runs;
@@ -227,46 +255,87 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
   const uint32_t tmem = *tmem_slot;
   const int runs = *run_count;
 
-  // What this CTA sums: UP one run's share of the features; DOWN its share of the sequence of (run, 128 features).
-  const int blocks = ((UP ? p.K : p.F) + 127) / 128;                       // of one run
+  // What this CTA sums.  UP: its share of the features, one tile (run, 128 channels) after the other; DOWN: its share of the
+  // sequence of (run, 128 features).
+  const int blocks = ((UP ? p.K : p.F) + 127) / 128;   // of one run
   const int tiles = UP ? (p.F + 127) / 128 : 1;
-  const int run0 = UP ? unit / tiles : 0, tile = UP ? unit - run0 * tiles : unit;
-  const bool idle = runs <= 0 || (UP && run0 >= runs);
-  const long all = UP ? blocks : static_cast<long>(runs) * blocks, base = UP ? static_cast<long>(run0) * blocks : 0;
-  const int u0 = idle ? 0 : static_cast<int>(base + all * rank / p.split), u1 = idle ? 0 : static_cast<int>(base + all * (rank + 1) / p.split);
+  int u0, u1, share0 = 0, share1 = blocks;
+  if constexpr (UP) {
+    u0 = unit;
+    u1 = runs > 0 ? runs * tiles : 0;
+    if (p.split > 1) share0 = blocks * rank / p.split, share1 = blocks * (rank + 1) / p.split;
+  } else {
+    const int all = runs > 0 ? runs * blocks : 0, each = all / p.split, more = all - each * p.split;
+    u0 = each * rank + min(rank, more);
+    u1 = u0 + each + (rank < more ? 1 : 0);
+  }
   struct Segment {
-    int kb0, kb1;
+    int kb0, kb1, tile, next;
     ExpertRun run;
   };
-  auto segment_at = [&](int u) {   // the part of one run that starts at u
-    const int r = u / blocks, kb0 = u - r * blocks;
-    return Segment{kb0, min(blocks, kb0 + u1 - u), run_table[r]};
+  auto segment_at = [&](int u) {   // one tile; the part of one run that starts at u
+    if constexpr (UP) {
+      const int r = u / tiles;
+      return Segment{share0, share1, u - r * tiles, u + static_cast<int>(gridDim.x) / p.split, run_table[r]};
+    } else {
+      const int r = u / blocks, kb0 = u - r * blocks, kb1 = min(blocks, kb0 + u1 - u);
+      return Segment{kb0, kb1, unit, u + kb1 - kb0, run_table[r]};
+    }
   };
-  const auto padded = [](int n) { return (n + 7) & ~7; };
+  const auto columns = [&](int n) { return p.terms * ((n + 7) & ~7); };
+
+  // UP: four hidden values a lane of one row's 128, as terms (F is a multiple of 16: a lane's channels are all there or none)
+  auto store_hidden = [&](float4 h, long row, int tile) {
+    const int f = tile * 128 + lane * 4;
+    const float v[4] = {h.x, h.y, h.z, h.w};
+    const uint32_t first = expert_terms(v, p.h_terms, [&](int t, uint32_t c) {
+      if (f < p.F) *reinterpret_cast<uint32_t*>(p.h + (static_cast<long>(t) * p.M + row) * p.F + f) = c;
+    });
+    if (lane == 0) p.h_scale[row * tiles + tile] = static_cast<uint8_t>(first);
+  };
 
   if (warp == 4) {
     // ------------------------------------------------------------------ TMA producer
     if (ptx::elect_one()) {
-      int stage = 0;
-      uint32_t phase = 0, issued = 0;
+      int stage = 0, issued = 0;
+      uint32_t phase = 0;
       bool ok = true;
+      // DOWN: the weights of the first round go ahead of the hidden values, whose kernel may still run
+      auto copy_hidden = [&](const Segment& g, int kb, int at) {
+        for (int r = 0; r < g.run.n; r += 8)
+          ptx::tma_load_3d(smem + at * p.stage_bytes + EXPERT_W_BYTES + r * p.terms * 128, &tmap_h, &full[at], kb * 128, g.run.row0 + r, 0);
+      };
+      auto first_hidden = [&]() {
+        ptx::grid_dependency_wait();
+        ptx::grid_launch_dependents();
+        int at = 0;
+        for (int u = u0; u < u1 && at < issued;) {
+          const Segment g = segment_at(u);
+          for (int kb = g.kb0; kb < g.kb1 && at < issued; ++kb) copy_hidden(g, kb, at++);
+          u = g.next;
+        }
+      };
       for (int u = u0; u < u1 && ok;) {
         const Segment g = segment_at(u);
-        const int row = g.run.expert * (UP ? 2 * p.F : p.N) + tile * 128;
+        const int row = g.run.expert * (UP ? 2 * p.F : p.N) + g.tile * 128;
+        const uint32_t bytes = UP ? 2 * EXPERT_W_BYTES : EXPERT_W_BYTES + columns(g.run.n) * 128;
         for (int kb = g.kb0; kb < g.kb1; ++kb) {
+          if (!UP && issued == p.stages) first_hidden();
           if (!ptx::mbar_wait_bounded_sleepy(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT)) {
             ok = false;
             break;
           }
           uint8_t* const dst = smem + stage * p.stage_bytes;
-          ptx::mbar_arrive_expect_tx(&full[stage], (UP ? 2 : 1) * EXPERT_W_BYTES);
-          ++issued;
+          ptx::mbar_arrive_expect_tx(&full[stage], bytes);
           ptx::tma_load_2d(dst, &tmap, &full[stage], kb * 128, row);
           if constexpr (UP) ptx::tma_load_2d(dst + EXPERT_W_BYTES, &tmap, &full[stage], kb * 128, row + p.F);
+          if (!UP && issued >= p.stages) copy_hidden(g, kb, stage);
+          ++issued;
           if (++stage == p.stages) stage = 0, phase ^= 1u;
         }
-        u += g.kb1 - g.kb0;
+        u = g.next;
       }
+      if (!UP && p.M > 0 && issued <= p.stages) first_hidden();
       if (!ok) {
         *abort_word = 1;
         raise_device_status(STAMP_ERR_TIMEOUT);
@@ -285,14 +354,14 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
       bool ok = true;
       for (int u = u0; u < u1 && ok; ++it) {
         const Segment g = segment_at(u);
-        const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, (p.terms * padded(g.run.n) + 15) & ~15);
-        const int a = UP ? 0 : it & 1;
-        if (!UP && !ptx::mbar_wait_bounded(&tempty[a], ((it >> 1) & 1) ^ 1, abort_word, FP8G_WAIT_LIMIT)) {
+        const uint32_t idesc = ptx::mxf8_idesc_with(idesc0, (columns(g.run.n) + 15) & ~15);
+        const int a = it & 1;
+        if (!ptx::mbar_wait_bounded(&tempty[a], ((it >> 1) & 1) ^ 1, abort_word, FP8G_WAIT_LIMIT)) {
           ok = false;
           break;
         }
         ptx::tc_fence_after();
-        const uint32_t acc = tmem + static_cast<uint32_t>(a * SM::COLUMNS);
+        const uint32_t acc = tmem + static_cast<uint32_t>(a * SM::ACC);
         for (int kb = g.kb0; kb < g.kb1; ++kb) {
           if (!ptx::mbar_wait_bounded(&full[stage], phase, abort_word, FP8G_WAIT_LIMIT)) {
             ok = false;
@@ -316,7 +385,7 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
         }
         if (!ok) break;
         ptx::tc_commit(&tfull[a]);
-        u += g.kb1 - g.kb0;
+        u = g.next;
       }
       if (!ok) {
         *abort_word = 1;
@@ -324,89 +393,91 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
       }
     }
   } else if (warp >= 6) {
-    // ------------------------------------------------------------------ converters
-    if (!UP && p.M > 0) {
-      ptx::grid_dependency_wait();
-      ptx::grid_launch_dependents();
-    }
-    const int features = UP ? p.K : p.F;
-    const bool bf16 = UP && p.x_bf16;
-    const void* const src = UP ? p.x : p.h;
-    const long ld = UP ? p.ldx : p.F;
+    // ------------------------------------------------------------------ scales, UP: and the tokens' terms
     const uint8_t* const scales = UP ? p.up_scale : p.down_scale;
     const int scale_rows = ((UP ? 2 * p.F : p.N) + 127) / 128;
-    const int up_first = UP ? (p.F + tile * 128) >> 7 : 0, up_rest = UP ? 128 - ((p.F + tile * 128) & 127) : 0;
-    const int each = EXPERT_CONVERTERS / p.stages;   // warps of a stage; they share its rows
+    const int each = UP ? SM::FILLERS / p.stages : 1;   // warps of a stage; they share its rows
     const int stage = (warp - 6) / each, part = (warp - 6) % each;
+    uint8_t* const xt = smem + stage * p.stage_bytes + 2 * EXPERT_W_BYTES;
+    uint8_t* const sf = words + stage * SM::SF_BYTES;
+    uint8_t* const rf = sf + SM::SF_BYTES - 512;
+    const bool bf16 = p.x_bf16;
     int i = 0, s = stage;   // steps before this segment; the next one that goes to this warp's stage
     uint32_t phase = 0;
-    bool ok = true;
+    bool ok = true, waited = UP;
     for (int u = u0; u < u1 && ok && stage < p.stages;) {
       const Segment g = segment_at(u);
-      const int n = g.run.n, pitch = padded(n);
-      int token = -1;   // lane r: where row r of the run is read
-      if (lane < n) {
-        token = UP ? __ldcg(p.rows + g.run.row0 + lane) : g.run.row0 + lane;
-        if (UP && (token < 0 || token >= p.T)) {
-          if (tile == 0 && rank == 0 && warp == 6) raise_device_status(STAMP_ERR_INVALID_ARG);
+      const int n = g.run.n, up_first = UP ? (p.F + g.tile * 128) >> 7 : 0, up_rest = UP ? 128 - ((p.F + g.tile * 128) & 127) : 0;
+      int token = -1;   // UP: lane r: the token of row r of the run
+      if (UP && lane < n) {
+        token = tokens[g.run.row0 + lane];
+        if (token < 0 || token >= p.T) {
+          if (g.tile == 0 && rank == 0 && warp == 6) raise_device_status(STAMP_ERR_INVALID_ARG);
           token = -1;
         }
       }
       const uint8_t* const sc = scales + static_cast<long>(g.run.expert) * scale_rows * blocks;
       for (; s < i + g.kb1 - g.kb0; s += p.stages, phase ^= 1u) {
         const int kb = g.kb0 + s - i;
-        const int col = kb * 128 + lane * 4;
-        // everything the stage needs is loaded before it is waited for, as far as eight rows for each warp
+        // everything the stage needs is loaded before it is waited for, UP: as far as eight rows for each warp
+        uint32_t w0 = __ldcg(sc + static_cast<long>(g.tile) * blocks + kb), w1 = 0, w2 = 0;
         ExpertRaw raw[8];
         auto load = [&](int r0) {
+          const int col = kb * 128 + lane * 4;
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
             const int t = __shfl_sync(0xffffffffu, token, (r0 + r * each) & 31);
-            raw[r].load(src, t * ld + col, bf16, r0 + r * each < n && t >= 0 && col < features);
+            raw[r].load(p.x, t * p.ldx + col, bf16, r0 + r * each < n && t >= 0 && col < p.K);
           }
         };
-        load(part);
-        uint32_t w0, w1 = 0, w2 = 0;
         if constexpr (UP) {
-          w0 = __ldcg(sc + static_cast<long>(tile) * blocks + kb);
+          load(part);
           w1 = __ldcg(sc + static_cast<long>(up_first) * blocks + kb);
           w2 = __ldcg(sc + static_cast<long>(min(up_first + 1, scale_rows - 1)) * blocks + kb);
         } else {
-          w0 = __ldcg(sc + static_cast<long>(tile) * blocks + kb);
+          if (!waited) ptx::grid_dependency_wait();
+          waited = true;
+          w1 = lane < n ? __ldcg(p.h_scale + static_cast<long>(g.run.row0 + lane) * blocks + kb) : 0u;
         }
         if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&empty[stage], phase ^ 1u, abort_word, FP8G_WAIT_LIMIT))) {
           ok = false;
           break;
         }
-        uint8_t* const xt = smem + stage * p.stage_bytes + (UP ? 2 : 1) * EXPERT_W_BYTES;
-        uint8_t* const sf = words + stage * SM::SF_BYTES;
-        if (part == 0) {
-          w0 *= 0x01010101u;
-          *reinterpret_cast<uint4*>(sf + lane * 16) = make_uint4(w0, w0, w0, w0);
-          if constexpr (UP) {
+        w0 *= 0x01010101u;
+        if (part == 0) *reinterpret_cast<uint4*>(sf + lane * 16) = make_uint4(w0, w0, w0, w0);
+        if constexpr (UP) {
+          if (part == 0) {
             // the ups may start inside a block of the scales
             w1 *= 0x01010101u, w2 *= 0x01010101u;
             *reinterpret_cast<uint4*>(sf + 512 + lane * 16) =
                 make_uint4(lane < up_rest ? w1 : w2, lane + 32 < up_rest ? w1 : w2, lane + 64 < up_rest ? w1 : w2, lane + 96 < up_rest ? w1 : w2);
           }
-        }
-        for (int r0 = part; r0 < n;) {
+          for (int r0 = part; r0 < n;) {
 #pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            if (r0 + r * each >= n) break;
-            float v[4];
-            raw[r].values(bf16, v);
-            expert_convert(v, p.terms, r0 + r * each, pitch, xt, sf + SM::SF_BYTES - 512);
+            for (int r = 0; r < 8; ++r) {
+              const int row = r0 + r * each;
+              if (row >= n) break;
+              float v[4];
+              raw[r].values(bf16, v);
+              // (rows of 128 bytes, 128-byte swizzle; a term's columns are eight further)
+              uint8_t* const out = xt + expert_column(row, 0, p.terms) * 128 + (((lane >> 2) ^ (row & 7)) << 4) + ((lane & 3) << 2);
+              const uint32_t first = expert_terms(v, p.terms, [&](int t, uint32_t c) { *reinterpret_cast<uint32_t*>(out + t * 1024) = c; });
+              if (lane < p.terms) expert_scale_words(rf, row, lane, p.terms, first);
+            }
+            r0 += 8 * each;
+            if (r0 < n) load(r0);
           }
-          r0 += 8 * each;
-          if (r0 < n) load(r0);
+        } else {
+          if (lane < n) {
+            for (int t = 0; t < p.terms; ++t) expert_scale_words(rf, lane, t, p.terms, w1);
+          }
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&full[stage]);
       }
       i += g.kb1 - g.kb0;
-      u += g.kb1 - g.kb0;
+      u = g.next;
     }
     if (!ok) {
       *abort_word = 1;
@@ -417,21 +488,26 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
     const int ch = warp * 32 + lane;
     bool ok = true;
     int it = 0;
-    // eight rows' sums at this thread's channel, their terms added up
-    auto eight = [&](uint32_t acc, int pitch, float (&v)[8]) {
+    // eight rows' sums at this thread's channel, their terms added up, the smallest first
+    auto eight = [&](uint32_t acc, int r0, float (&v)[8]) {
+      uint32_t c[4][8];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (t < p.terms) ptx::tmem_ld_32x32b_x8(acc + r0 * p.terms + t * 8, c[t]);
+      ptx::tmem_ld_wait();
 #pragma unroll
       for (int r = 0; r < 8; ++r) v[r] = 0.f;
-      for (int t = p.terms - 1; t >= 0; --t) {   // the smallest first
-        uint32_t c[8];
-        ptx::tmem_ld_32x32b_x8(acc + t * pitch, c);
-        ptx::tmem_ld_wait();
 #pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] += __uint_as_float(c[r]);
-      }
+      for (int t = 3; t >= 0; --t)
+        if (t < p.terms) {
+#pragma unroll
+          for (int r = 0; r < 8; ++r) v[r] += __uint_as_float(c[t][r]);
+        }
     };
-    for (int u = u0; u < u1; ++it) {
+    uint32_t exchanged = 0;
+    for (int u = u0; u < u1 && ok; ++it) {
       const Segment g = segment_at(u);
-      const int n = g.run.n, pitch = padded(n), a = UP ? 0 : it & 1;
+      const int n = g.run.n, a = it & 1, c = g.tile * 128 + ch;   // this thread's channel
       int token = -1;
       float share = 0.f;
       if (!UP && lane < n) {
@@ -440,43 +516,63 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
         if (token < 0 || token >= p.T) token = -1;
       }
       float bias = 0.f;   // (once for every row: with the run's first features)
-      if (!UP && p.down_bias && g.kb0 == 0 && tile * 128 + ch < p.N) bias = __ldcg(p.down_bias + static_cast<long>(g.run.expert) * p.N + tile * 128 + ch);
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&tfull[a], UP ? 0u : (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
+      float up_bias = 0.f;
+      if (!UP && p.down_bias && g.kb0 == 0 && c < p.N) bias = __ldcg(p.down_bias + static_cast<long>(g.run.expert) * p.N + c);
+      if (UP && p.up_bias && c < p.F && p.split == 1) {
+        bias = __ldcg(p.up_bias + static_cast<long>(g.run.expert) * 2 * p.F + c);
+        up_bias = __ldcg(p.up_bias + static_cast<long>(g.run.expert) * 2 * p.F + p.F + c);
+      }
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
         ok = false;
         break;
       }
       ptx::tc_fence_after();
-      const uint32_t acc = tmem + (static_cast<uint32_t>(warp * 32) << 16) + static_cast<uint32_t>(a * SM::COLUMNS);
+      const uint32_t acc = tmem + (static_cast<uint32_t>(warp * 32) << 16) + static_cast<uint32_t>(a * SM::ACC);
       for (int r0 = 0; r0 < n; r0 += 8) {
-        if constexpr (UP) {
-          // every CTA's part of the sums, [row][gates, ups], in the ring that nothing uses any more
-          float* const part = reinterpret_cast<float*>(smem);
-          float v[8], w[8];
-          eight(acc + r0, pitch, v);
-          eight(acc + SM::COLUMNS + r0, pitch, w);
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-            if (r0 + r < n) {
-              part[(r0 + r) * 256 + ch] = v[r];
-              part[(r0 + r) * 256 + 128 + ch] = w[r];
-            }
-        } else {
-          float v[8];
-          eight(acc + r0, pitch, v);
-          if (r0 + 8 >= n) {
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&tempty[a]);
-          }
+        float v[8], w[8];
+        eight(acc, r0, v);
+        if constexpr (UP) eight(acc + SM::COLUMNS, r0, w);
+        if (r0 + 8 >= n) {
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&tempty[a]);
+        }
+        if constexpr (!UP) {
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
             const int t = __shfl_sync(0xffffffffu, token, (r0 + r) & 31);
             const float s = __shfl_sync(0xffffffffu, share, (r0 + r) & 31);
             if (r0 + r < n && t >= 0) sums[t * 128 + ch] = fmaf(s, v[r] + bias, sums[t * 128 + ch]);
           }
+        } else if (p.split > 1) {
+          // this CTA's part of the sums, [row][gates, ups], in the ring that nothing uses any more
+          float* const part = reinterpret_cast<float*>(smem) + r0 * 256 + ch;
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            if (r0 + r < n) {
+              part[r * 256] = v[r];
+              part[r * 256 + 128] = w[r];
+            }
+        } else {
+          // hidden values by channel to hidden values by row: over shared memory, two buffers in turn
+          float* const at = hidden + (exchanged & 1u) * 1024;
+#pragma unroll
+          for (int r = 0; r < 8; r += 2) {
+            const float2 h = gated_silu2<false, false>(make_float2(v[r] + bias, v[r + 1] + bias), make_float2(w[r] + up_bias, w[r + 1] + up_bias));
+            at[r * 128 + ch] = c < p.F ? h.x : 0.f;
+            at[r * 128 + 128 + ch] = c < p.F ? h.y : 0.f;
+          }
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(exchange);
+          if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(exchange, exchanged & 1u, abort_word, FP8G_WAIT_LIMIT))) {
+            ok = false;
+            break;
+          }
+          ++exchanged;
+          for (int r = warp; r < 8 && r0 + r < n; r += 4) store_hidden(*reinterpret_cast<const float4*>(at + r * 128 + lane * 4), g.run.row0 + r0 + r, g.tile);
         }
       }
-      u += g.kb1 - g.kb0;
+      u = g.next;
     }
     if (!ok) {
       *abort_word = 1;
@@ -484,45 +580,72 @@ __global__ void __launch_bounds__(EXPERT_THREADS, 2)
     }
   }
 
+  // DOWN: the residual of the first token this warp writes is on its way while the cluster's CTAs wait for one another
+  auto residual = [&](int t, int c) {
+    const long at = t * p.ldr + c;
+    return !p.residual || c >= p.N || t >= p.T ? 0.f
+           : p.r_bf16                          ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.residual)[at])
+                                               : static_cast<const float*>(p.residual)[at];
+  };
+  float ahead[UP ? 1 : 4];
+  if constexpr (!UP) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ahead[i] = residual(rank + warp * p.split, unit * 128 + lane * 4 + i);
+  }
   ptx::tc_fence_before();
   __syncthreads();
   if (p.split > 1) ptx::cluster_sync();
   // (a CTA that gave up leaves its outputs as they were)
-  if (UP ? !idle && *abort_word == 0 : runs >= 0 && *abort_word == 0) {
+  if (UP ? p.split > 1 && u0 < u1 && *abort_word == 0 : runs >= 0 && *abort_word == 0) {
     // the sums of the cluster's CTAs in rank order; every CTA takes every split-th row (UP) or token (DOWN)
     const uint32_t part = ptx::smem_u32(UP ? reinterpret_cast<float*>(smem) : sums);
+    uint32_t part_of[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) part_of[s] = p.split > 1 ? ptx::mapa(part, static_cast<uint32_t>(min(s, p.split - 1))) : part;
+    // four channels of one row from every CTA, four loads in flight at once
+    auto total = [&](int at) {
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int s0 = 0; s0 < 8; s0 += 4) {
+        float4 v[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          if (s0 + s < p.split)
+            v[s] = p.split > 1 ? ptx::ld_dsmem_f4(part_of[s0 + s] + at * 4) : *reinterpret_cast<const float4*>((UP ? reinterpret_cast<const float*>(smem) : sums) + at);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          if (s0 + s < p.split) sum = make_float4(sum.x + v[s].x, sum.y + v[s].y, sum.z + v[s].z, sum.w + v[s].w);
+      }
+      return sum;
+    };
     if constexpr (UP) {
-      const ExpertRun run = run_table[run0];
-      for (int i = threadIdx.x; i < (run.n - rank + p.split - 1) / p.split * 128; i += EXPERT_THREADS) {
-        const int r = rank + (i >> 7) * p.split, ch = i & 127, f = tile * 128 + ch;
-        float g = 0.f, u = 0.f;
-        for (int s = 0; s < p.split; ++s) {
-          const uint32_t at = (p.split > 1 ? ptx::mapa(part, s) : part) + (r * 256 + ch) * 4;
-          g += p.split > 1 ? ptx::ld_dsmem_f1(at) : reinterpret_cast<const float*>(smem)[r * 256 + ch];
-          u += p.split > 1 ? ptx::ld_dsmem_f1(at + 512) : reinterpret_cast<const float*>(smem)[r * 256 + 128 + ch];
+      // a warp takes a row, a lane four channels
+      const Segment t = segment_at(u0);
+      const int f = t.tile * 128 + lane * 4;
+      for (int r = rank + warp * p.split; r < t.run.n; r += SM::THREADS / 32 * p.split) {
+        float4 g = total(r * 256 + lane * 4), u = total(r * 256 + 128 + lane * 4);
+        if (p.up_bias && f < p.F) {
+          const float* const b = p.up_bias + static_cast<long>(t.run.expert) * 2 * p.F + f;
+          g = make_float4(g.x + __ldg(b), g.y + __ldg(b + 1), g.z + __ldg(b + 2), g.w + __ldg(b + 3));
+          u = make_float4(u.x + __ldg(b + p.F), u.y + __ldg(b + p.F + 1), u.z + __ldg(b + p.F + 2), u.w + __ldg(b + p.F + 3));
         }
-        if (f < p.F) {
-          if (p.up_bias) {
-            const float* const b = p.up_bias + static_cast<long>(run.expert) * 2 * p.F + f;
-            g += __ldg(b);
-            u += __ldg(b + p.F);
-          }
-          p.h[static_cast<long>(run.row0 + r) * p.F + f] = gated_silu2<false, false>(make_float2(g, g), make_float2(u, u)).x;
-        }
+        const float2 h0 = gated_silu2<false, false>(make_float2(g.x, g.y), make_float2(u.x, u.y));
+        const float2 h1 = gated_silu2<false, false>(make_float2(g.z, g.w), make_float2(u.z, u.w));
+        store_hidden(f < p.F ? make_float4(h0.x, h0.y, h1.x, h1.y) : make_float4(0.f, 0.f, 0.f, 0.f), t.run.row0 + r, t.tile);
       }
     } else {
       if (p.M > 0) ptx::grid_dependency_wait();   // (the tokens may be overwritten from here on)
-      for (int i = threadIdx.x; i < (p.T - rank + p.split - 1) / p.split * 128; i += EXPERT_THREADS) {
-        const int t = rank + (i >> 7) * p.split, ch = i & 127, c = tile * 128 + ch;
-        float y = 0.f;
-        for (int s = 0; s < p.split; ++s) y += p.split > 1 ? ptx::ld_dsmem_f1(ptx::mapa(part, s) + (t * 128 + ch) * 4) : sums[t * 128 + ch];
-        if (c < p.N) {
-          if (p.residual) {
-            const long at = t * p.ldr + c;
-            y += p.r_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.residual)[at]) : static_cast<const float*>(p.residual)[at];
-          }
-          TOut* const out = static_cast<TOut*>(p.y) + static_cast<long>(t) * p.N + c;
-          if constexpr (sizeof(TOut) == 2) *out = __float2bfloat16_rn(y); else *out = y;
+      // a warp takes a token, a lane four channels
+      const int c = unit * 128 + lane * 4;
+      for (int t = rank + warp * p.split; t < p.T; t += SM::THREADS / 32 * p.split) {
+        const float4 sum = total(t * 128 + lane * 4);
+        const float y[4] = {sum.x, sum.y, sum.z, sum.w};
+        TOut* const out = static_cast<TOut*>(p.y) + static_cast<long>(t) * p.N + c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (c + i >= p.N) break;
+          const float v = y[i] + (t == rank + warp * p.split ? ahead[i] : residual(t, c + i));
+          if constexpr (sizeof(TOut) == 2) out[i] = __float2bfloat16_rn(v); else out[i] = v;
         }
       }
     }

@@ -217,6 +217,20 @@ static int make_tmap_i8(const void* base, long rows, int K, int box_rows, CUtens
   return r == CUDA_SUCCESS ? STAMP_OK : STAMP_ERR_CUDA;
 }
 
+// `terms` byte matrices [rows, K], one after the other; box = 128 bytes of K x 8 rows of every one, 128-byte swizzle.
+static int make_tmap_terms(const void* base, long rows, int K, int terms, CUtensorMap* out) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return STAMP_ERR_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)K, (cuuint64_t)rows, (cuuint64_t)terms};
+  cuuint64_t strides[2] = {(cuuint64_t)K, (cuuint64_t)rows * K};
+  cuuint32_t box[3] = {128u, 8u, (cuuint32_t)terms};
+  cuuint32_t estr[3] = {1u, 1u, 1u};
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? STAMP_OK : STAMP_ERR_CUDA;
+}
+
 // bf16 matrix [rows, cols] row-major; box = 64 columns (128 bytes) x box_rows rows, 128-byte swizzle.
 static int make_tmap_bf16(const void* base, long rows, long cols, CUtensorMap* out, int box_rows = 256) {
   EncodeTiledFn enc = get_encode();
@@ -1517,19 +1531,22 @@ static int check_route(int T, int E, int top) {
 }
 
 template <bool UP, typename TOut>
-static int launch_expert(ExpertParams p, long units, cudaStream_t st) {
+static int launch_expert(ExpertParams p, long ctas, int smem, cudaStream_t st) {
   using SM = ExpertSmem<UP>;
   auto kern = k_expert_layer<UP, TOut>;
-  if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), EXPERT_SMEM)) return rc;
-  const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T);
+  if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), EXPERT_MAX_SMEM)) return rc;
+  const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T, p.M);
   p.stage_bytes = (UP ? 2 : 1) * EXPERT_W_BYTES + (p.terms * p.cap + 15) / 16 * 16 * 128;
-  p.stages = (EXPERT_SMEM - fixed) / (p.stage_bytes + SM::SF_BYTES);
+  p.stages = (smem - fixed) / (p.stage_bytes + SM::SF_BYTES);
   if (p.stages > EXPERT_MAX_STAGES) p.stages = EXPERT_MAX_STAGES;
-  CUtensorMap tm;
+  CUtensorMap tm, th;
   if (int rc = UP ? make_tmap_i8(p.w_up, (long)p.E * 2 * p.F, p.K, 128, &tm) : make_tmap_i8(p.w_down, (long)p.E * p.N, p.F, 128, &tm)) return rc;
+  th = tm;
+  if (!UP && p.M > 0)
+    if (int rc = make_tmap_terms(p.h, p.M, p.F, p.terms, &th)) return rc;
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3((unsigned)(units * p.split));
-  lc.blockDim = dim3(EXPERT_THREADS);
+  lc.gridDim = dim3((unsigned)ctas);
+  lc.blockDim = dim3(SM::THREADS);
   lc.dynamicSmemBytes = (size_t)(fixed + p.stages * (p.stage_bytes + SM::SF_BYTES));
   lc.stream = st;
   cudaLaunchAttribute at[2];
@@ -1541,7 +1558,7 @@ static int launch_expert(ExpertParams p, long units, cudaStream_t st) {
   at[1].val.clusterDim.z = 1;
   lc.attrs = at;
   lc.numAttrs = p.split > 1 ? 2 : 1;
-  if (cudaLaunchKernelEx(&lc, kern, tm, p) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&lc, kern, tm, th, p) != cudaSuccess) {
     cudaGetLastError();
     return STAMP_ERR_CUDA;
   }
@@ -1555,21 +1572,31 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
     const int most = columns / p.terms & ~7;
     return tokens < most ? tokens : most;
   };
+  p.h_terms = y_dtype == STAMP_BF16 ? 3 : 4;
+  const long sms = sm_count();
   if (p.M > 0) {
     p.terms = p.x_bf16 ? 2 : 4;
     p.cap = cap(ExpertSmem<true>::COLUMNS);
-    p.split = 1;
-    const long tiles = (p.F + 127L) / 128, runs = p.E < p.M ? p.E : p.M;
+    const long tiles = (p.F + 127L) / 128, runs = p.E < p.M ? p.E : p.M, most = tiles * expert_max_runs(p.M, p.E, p.cap);
     const int blocks = (p.K + 127) / 128;
-    while (p.split < 8 && p.split * 4 <= blocks && tiles * runs * p.split < 4L * sm_count()) p.split *= 2;
-    if (int rc = launch_expert<true, float>(p, tiles * expert_max_runs(p.M, p.E, p.cap), st)) return rc;
+    // One CTA a tile, each SM one after the other, unless there are few tiles; then four or eight share one, where each has
+    // features enough to make up for the exchange and the clusters find their SMs at once.  One token, in us, with 1 / 2 / 4 / 8
+    // (the choice in brackets): 4 tiles of 1024 features 11.8 / 12.2 / 11.8 / (11.6), 8 of 2048 14.3 / 13.9 / 13.0 / (12.6), 16
+    // of 4096 19.2 / 23.6 / (18.5) / 24.2, 32 of 4096 27.7 / 23.6 / (21.5) / 34.2, 64 of 1152 (16.0) / 19.0 / 25.3 / 43.2.
+    p.split = tiles * runs <= 8 && blocks >= 8 ? 8 : tiles * runs <= 32 && blocks >= 16 ? 4 : 1;
+    const long ctas = p.split > 1 ? most * p.split : most < sms ? most : sms;
+    if (int rc = launch_expert<true, float>(p, ctas, EXPERT_MAX_SMEM, st)) return rc;
   }
-  p.terms = y_dtype == STAMP_BF16 ? 3 : 4;
+  p.terms = p.h_terms;
   p.cap = cap(ExpertSmem<false>::COLUMNS);
   const long tiles = (p.N + 127L) / 128;
+  // As many CTAs as SMs, or half of that at least.  With 4 / 8 to a tile, in us: 32 tiles, 13 tokens of 32 large experts (153) /
+  // 157, one token of two experts of 4096 x 4096 (27.3) / 30.6; 16 tiles, 64 tokens over 64 experts 191 / (149).
   p.split = 1;
-  while (p.split < 8 && tiles * p.split < 2L * sm_count()) p.split *= 2;
-  return y_dtype == STAMP_BF16 ? launch_expert<false, __nv_bfloat16>(p, tiles, st) : launch_expert<false, float>(p, tiles, st);
+  while (p.split < 8 && tiles * p.split * 2 <= sms) p.split *= 2;
+  // (two CTAs to an SM: with more than half of its shared memory a cluster of eight finds its SMs too late)
+  return y_dtype == STAMP_BF16 ? launch_expert<false, __nv_bfloat16>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st)
+                               : launch_expert<false, float>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st);
 }
 
 template <typename TIn, typename TOut>
@@ -2229,6 +2256,9 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
   return o_dtype == STAMP_BF16 ? launch_combine<float, __nv_bfloat16>(p, r_bf16, st) : launch_combine<float, float>(p, r_bf16, st);
 }
 
+// The hidden values' codes (four terms at most) and scales.
+static size_t expert_ws_bytes(int M, int F) { return align256((size_t)M * F * 4) + align256((size_t)M * ((F + 127L) / 128)); }
+
 static int check_expert_layer(int T, int M, int E, int K, int F, int N) {
   if (T < 0 || M < 0 || E <= 0 || K <= 0 || F <= 0 || N <= 0) return STAMP_ERR_INVALID_ARG;
   if (T > EXPERT_FEW_TOKENS || M > EXPERT_FEW_ROWS || E > EXPERT_MAX || K % 16 != 0 || F % 16 != 0 || K > FP8_MAX_FEATURES || F > FP8_MAX_FEATURES / 2)
@@ -2241,7 +2271,7 @@ static int check_expert_layer(int T, int M, int E, int K, int F, int N) {
 int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes) {
   if (!out_bytes || M < 0 || F <= 0) return STAMP_ERR_INVALID_ARG;
   if (M > EXPERT_FEW_ROWS || F > FP8_MAX_FEATURES / 2) return STAMP_ERR_UNSUPPORTED;
-  *out_bytes = align256((size_t)M * F * 4);
+  *out_bytes = expert_ws_bytes(M, F);
   return STAMP_OK;
 }
 
@@ -2261,7 +2291,7 @@ int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int3
   if (ldx > (1LL << 60) / T) return STAMP_ERR_UNSUPPORTED;
   if (residual)
     if (int rc = check_residual(residual, r_dtype, ldr, T, N, Y, y_dtype)) return rc;
-  if (M > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < (size_t)M * F * 4)) return STAMP_ERR_WORKSPACE;
+  if (M > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < expert_ws_bytes(M, F))) return STAMP_ERR_WORKSPACE;
   ExpertParams p{};
   p.x = X;
   p.ldx = ldx;
@@ -2279,7 +2309,8 @@ int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int3
   p.ldr = ldr;
   p.r_bf16 = r_dtype == STAMP_BF16;
   p.T = T, p.M = M, p.E = E, p.K = K, p.F = F, p.N = N;
-  p.h = static_cast<float*>(ws);
+  p.h = static_cast<uint8_t*>(ws);
+  p.h_scale = p.h + align256((size_t)M * F * 4);
   p.y = Y;
   return run_expert_layer(p, y_dtype, static_cast<cudaStream_t>(stream));
 }
