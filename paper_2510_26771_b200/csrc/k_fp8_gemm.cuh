@@ -49,6 +49,9 @@ constexpr int FP8G_SF_SLOTS = 4;                       // steps of 512 features 
 constexpr int FP8G_TAIL_BOX = 32;
 constexpr int FP8G_EPI_WARPS = 8;
 constexpr int FP8G_THREADS = 128 + 32 * FP8G_EPI_WARPS;
+constexpr int FP8G_FUSED_GROUPS = 2;                   // FUSED: epilogue warps in groups of four (the lanes' quarters)
+constexpr int FP8G_PART = FP8G_BM + 4;                 // FUSED: floats from one token to the next in a part of a split sum
+constexpr int FP8G_FUSED_THREADS = 128 + 128 * FP8G_FUSED_GROUPS;
 constexpr long long FP8G_WAIT_LIMIT = 4000000000LL;    // SM clocks (~2 s) before a wait gives up
 
 struct Fp8GemmParams {
@@ -84,10 +87,10 @@ struct Fp8Smem {
   static constexpr int NUM_BARS = 2 * FP8G_MAX_STAGES + 2 * FP8G_SF_SLOTS + 4; // full, empty, sffull, sfempty, tfull[2], tempty[2]
   static constexpr int TAB_OFFSET = BAR_OFFSET + NUM_BARS * 8 + 16;
   static constexpr int DYN_BYTES = TAB_OFFSET + 2 * (FP8_MAX_EXPERTS + 1) * 4 + 1024;
-  // FUSED, quantized output: one barrier for each half of the epilogue warps, their maxima [half][buffer][quarter][token] and
+  // FUSED, quantized output: a barrier for each group of four epilogue warps, their maxima [group][buffer][quarter][token] and
   // the tokens' inverse scales [warp][token]
-  static constexpr int EX_OFFSET = (TAB_OFFSET + 2 * (FP8_MAX_EXPERTS + 1) * 4 + 15) / 16 * 16;
-  static constexpr int EX_BYTES = 16 + 2 * 2 * 4 * 32 * 4 + FP8G_EPI_WARPS * 32 * 4;
+  static constexpr int EX_OFFSET = (TAB_OFFSET + 2 * 2 * 4 + 15) / 16 * 16;   // (one matrix: two entries of either table)
+  static constexpr int EX_BYTES = FP8G_FUSED_GROUPS * (8 + 2 * 4 * 32 * 4 + 4 * 32 * 4);
   static constexpr int FUSED_DYN_BYTES = EX_OFFSET + EX_BYTES + 1024;
   static_assert(DYN_BYTES <= 227 * 1024 && FUSED_DYN_BYTES <= 227 * 1024, "shared memory of one CTA");
   // tensor memory: second accumulator, then the two buffers of scale columns (4 for channels, BN / 32 for tokens)
@@ -126,6 +129,9 @@ __device__ __forceinline__ Fp8Tile fp8_tile(const Fp8GemmParams& p, const int* t
   return t;
 }
 
+// FUSED: whether the block of 128 channels from `first` on keeps its order: it ends inside a run of 32 channels.
+__device__ __forceinline__ bool fp8_plain_order(const Fp8GemmParams& p, int first) { return (p.N & 31) != 0 && first + FP8G_BM > p.N; }
+
 // The scale bytes of `n` (1..4) consecutive blocks as one word.  Where there is none -- blocks past K, rows past the
 // run, whose columns are not stored -- any finite scale does: 1.
 __device__ __forceinline__ uint32_t fp8_scale_word(const uint8_t* ptr, int n, bool live) {
@@ -143,6 +149,8 @@ __host__ __device__ constexpr int fp8_drain_chunk(bool descending, int half, int
   return half + 2 * (descending ? count - 1 - i : i);
 }
 __host__ __device__ constexpr int fp8_overlap_half(int accumulator) { return accumulator == 0 ? 1 : 0; }
+// The same with FP8G_FUSED_GROUPS groups of warps: chunk c by group c % 4, the last first in the first accumulator.
+__host__ __device__ constexpr int fp8_overlap_group(int accumulator) { return accumulator == 0 ? 7 % FP8G_FUSED_GROUPS : 0; }
 constexpr bool fp8_drain_order_holds() {
   for (int chunks = 1; chunks <= 8; ++chunks)
     for (int a = 0; a < 2; ++a) {
@@ -181,84 +189,152 @@ __device__ __forceinline__ void fp8_store2(__nv_bfloat16* y, float a, float b, b
 }
 
 // ---- what follows the sum in the fused form: activation, residual, quantization
-// The activation of two sums at once, in fp32.  NONE and RELU are exact; SILU as in the gated quantizer, about an ulp.
-// GELU v Phi(v) by CUDA's normal distribution function (5 ulp, also where Phi is small: 1 + erf would cancel there).
-// GELU_TANH: (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)), which does not cancel either; 2 u is rounded three times, so that the
-// result is within about (8 + 2 |2 u|) 2^-24 of itself.
-__device__ __forceinline__ float2 fp8_activate2(float2 v, int act) {
-  switch (act) {
-    case STAMP_ACT_RELU: return make_float2(v.x < 0.f ? 0.f : v.x, v.y < 0.f ? 0.f : v.y);   // (a NaN stays one)
-    case STAMP_ACT_GELU: return make_float2(v.x * normcdff(v.x), v.y * normcdff(v.y));
-    case STAMP_ACT_GELU_TANH: {
-      constexpr float C = 1.5957691216f * 1.4426950409f;   // 2 sqrt(2 / pi) log2(e)
-      const float ax = v.x * fmaf(v.x * v.x, -0.044715f * C, -C), ay = v.y * fmaf(v.y * v.y, -0.044715f * C, -C);
-      return make_float2(__fdividef(v.x, 1.f + ptx::ex2(ax)), __fdividef(v.y, 1.f + ptx::ex2(ay)));
-    }
-    case STAMP_ACT_SILU: return gated_silu2<false, false>(v, make_float2(1.f, 1.f));
-    default: return v;
+// The activation of two sums at once, in packed fp32; two values of the special function unit for each.
+//   LINEAR     none, or relu where `floor` is 0 instead of -inf (a NaN stays one).
+//   SILU       v / (1 + exp(-v)): the exponent's product is held as head and tail, as in the gated quantizer; divisor and v are
+//              both divided by four, since the reciprocal of a divisor from 2^126 on would be flushed to zero.  About 3 ulp.
+//   GELU_TANH  (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)), which does not cancel where tanh is near -1; 2 u is rounded three times, so
+//              that the result is within about (5 |2 u| + 18) 2^-24 of itself.
+//   GELU       v Phi(v), Phi(-x) = exp(-x^2 / 2) R(x) for x >= 0 (1 + erf would cancel in the lower tail).  R(x), half the scaled
+//              complementary error function of x / sqrt 2, is t P(1 - 2 t) with t = 1 / (1 + x / 3): a least-squares fit of
+//              degree 8, reweighted towards the smallest largest relative error (2^-24.4 for x <= 14, where exp(-x^2 / 2)
+//              vanishes).  In fp32, a reciprocal off by an ulp included, R is within 2^-21; all in all 2^-20.
+// An infinite sum comes out non-finite.
+enum Fp8Act { FP8_LINEAR, FP8_GELU, FP8_GELU_TANH, FP8_SILU };
+template <int ACT>
+__device__ __forceinline__ float2 fp8_activate2(float2 v, float floor) {
+  auto both = [](float x) { return make_float2(x, x); };
+  if constexpr (ACT == FP8_GELU) {
+    constexpr float P[9] = {0.243027896f, -0.169777423f, 0.0766731128f, -0.0157520343f, -0.00349331181f, 0.00230797403f, 0.000358678924f, -0.000301084074f, -8.89220537e-05f};
+    constexpr float C = -0.721347520f, C_TAIL = -9.62981495e-9f, LN2 = 0.693147181f;   // -log2(e) / 2 and the rest of it
+    const float2 x = make_float2(fminf(fabsf(v.x), 20.f), fminf(fabsf(v.y), 20.f));
+    const float2 d = __ffma2_rn(x, both(1.f / 3.f), both(1.f));
+    const float2 t = make_float2(ptx::rcp(d.x), ptx::rcp(d.y));
+    const float2 u = __ffma2_rn(t, both(-2.f), both(1.f));
+    float2 r = both(P[8]);
+#pragma unroll
+    for (int i = 7; i >= 0; --i) r = __ffma2_rn(r, u, both(P[i]));
+    // exp(-x^2 / 2) = 2^head (1 + more)
+    const float2 square = __fmul2_rn(x, x), rest = __ffma2_rn(x, x, __fmul2_rn(square, both(-1.f)));
+    const float2 head = __fmul2_rn(square, both(C));
+    float2 more = __ffma2_rn(square, both(C), __fmul2_rn(head, both(-1.f)));
+    more = __ffma2_rn(rest, both(C), __ffma2_rn(square, both(C_TAIL), more));
+    const float2 q = __fmul2_rn(__fmul2_rn(r, t), make_float2(ptx::ex2(head.x), ptx::ex2(head.y)));
+    const float2 w = __fmul2_rn(v, __ffma2_rn(q, __fmul2_rn(more, both(LN2)), q));
+    return make_float2(v.x > 0.f ? v.x - w.x : w.x, v.y > 0.f ? v.y - w.y : w.y);
+  } else if constexpr (ACT == FP8_GELU_TANH) {
+    constexpr float C = 1.5957691216f * 1.4426950409f;   // 2 sqrt(2 / pi) log2(e)
+    const float2 a = __fmul2_rn(v, __ffma2_rn(__fmul2_rn(v, v), both(-0.044715f * C), both(-C)));
+    const float2 d = __fadd2_rn(make_float2(ptx::ex2(a.x), ptx::ex2(a.y)), both(1.f));
+    return __fmul2_rn(v, make_float2(ptx::rcp(d.x), ptx::rcp(d.y)));
+  } else if constexpr (ACT == FP8_SILU) {
+    constexpr float LOG2E = 1.44269504f, LOG2E_TAIL = 1.92596299e-8f, LN2 = 0.693147181f;
+    const float2 x = make_float2(fminf(v.x, 90.f), fminf(v.y, 90.f));   // (inf would leave NaN below)
+    const float2 head = __fmul2_rn(x, both(-LOG2E));
+    const float2 tail = __ffma2_rn(x, both(-LOG2E), __fmul2_rn(head, both(-1.f)));
+    const float2 more = __fmul2_rn(__ffma2_rn(x, both(-LOG2E_TAIL), tail), both(0.25f * LN2));
+    const float2 p = make_float2(ptx::ex2(head.x), ptx::ex2(head.y));
+    const float2 d = __ffma2_rn(p, __fadd2_rn(more, both(0.25f)), both(0.25f));   // (1 + exp(-v)) / 4
+    return __fmul2_rn(__fmul2_rn(v, both(0.25f)), make_float2(ptx::rcp(d.x), ptx::rcp(d.y)));
+  } else {
+    return make_float2(ptx::max_nan(v.x, floor), ptx::max_nan(v.y, floor));
   }
 }
-// 32 sums of a thread.  (One jump for all of them.)
-__device__ __forceinline__ void fp8_activate32(uint32_t (&r)[32], float bias, int act) {
-  auto each = [&](auto which) {
-#pragma unroll
-    for (int j = 0; j < 32; j += 2) {
-      const float2 v = fp8_activate2(make_float2(__uint_as_float(r[j]) + bias, __uint_as_float(r[j + 1]) + bias), decltype(which)::value);
-      r[j] = __float_as_uint(v.x);
-      r[j + 1] = __float_as_uint(v.y);
-    }
-  };
+// f(variant, floor) for a stamp_activation: one jump around whatever f does.
+template <typename F>
+__device__ __forceinline__ void fp8_with_activation(int act, F&& f) {
+  const float none = -__int_as_float(0x7F800000);
   switch (act) {
-    case STAMP_ACT_RELU: each(std::integral_constant<int, STAMP_ACT_RELU>{}); break;
-    case STAMP_ACT_GELU: each(std::integral_constant<int, STAMP_ACT_GELU>{}); break;
-    case STAMP_ACT_GELU_TANH: each(std::integral_constant<int, STAMP_ACT_GELU_TANH>{}); break;
-    case STAMP_ACT_SILU: each(std::integral_constant<int, STAMP_ACT_SILU>{}); break;
-    default: each(std::integral_constant<int, STAMP_ACT_NONE>{});
+    case STAMP_ACT_GELU: f(std::integral_constant<int, FP8_GELU>{}, none); break;
+    case STAMP_ACT_GELU_TANH: f(std::integral_constant<int, FP8_GELU_TANH>{}, none); break;
+    case STAMP_ACT_SILU: f(std::integral_constant<int, FP8_SILU>{}, none); break;
+    default: f(std::integral_constant<int, FP8_LINEAR>{}, act == STAMP_ACT_RELU ? 0.f : none);
   }
 }
-__device__ __forceinline__ float fp8_residual(const Fp8GemmParams& p, long row, int ch) {
-  const long at = row * p.ldr + ch;
-  return p.r_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.residual)[at]) : static_cast<const float*>(p.residual)[at];
+// Four neighbouring channels of one token as one word, aligned to its size.
+__device__ __forceinline__ float4 fp8_load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 fp8_load4(const __nv_bfloat16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
 }
-// The residual of 32 tokens at this lane's channel, in fp32, loaded before the sums are waited for; zero where there is none.
-// Plain loads: the output may be the same memory, and every element is read by the thread that writes it.
-// PAIRS: bf16 rows whose channels can be read two at a time: as in the store, the even lane takes the first token of two,
-// the odd lane the second, and they swap halves (the same step there and back).
-__device__ __forceinline__ void fp8_load_residual(const Fp8GemmParams& p, long row, int left, int ch, bool pairs, float (&out)[32]) {
-  if (pairs) {
-    const int odd = threadIdx.x & 1, ch2 = ch & ~1;
-    const uint32_t sel = odd ? 0x3276u : 0x5410u;
-    const __nv_bfloat16* at = static_cast<const __nv_bfloat16*>(p.residual) + (row + odd) * p.ldr + ch2;
-    uint32_t two[16];
+__device__ __forceinline__ void fp8_store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void fp8_store4(__nv_bfloat16* p, float4 v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+// The same one by one, `step` elements apart, as many as there are.
+__device__ __forceinline__ float fp8_float(float v) { return v; }
+__device__ __forceinline__ float fp8_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ float4 fp8_load_some(const T* p, int step, int count) {
+  return make_float4(count > 0 ? fp8_float(p[0]) : 0.f, count > 1 ? fp8_float(p[step]) : 0.f, count > 2 ? fp8_float(p[2 * step]) : 0.f,
+                     count > 3 ? fp8_float(p[3 * step]) : 0.f);
+}
+__device__ __forceinline__ void fp8_store_some(float* p, float4 v, int step, int count) {
+  if (count > 0) p[0] = v.x;
+  if (count > 1) p[step] = v.y;
+  if (count > 2) p[2 * step] = v.z;
+  if (count > 3) p[3 * step] = v.w;
+}
+__device__ __forceinline__ void fp8_store_some(__nv_bfloat16* p, float4 v, int step, int count) {
+  if (count > 0) p[0] = __float2bfloat16_rn(v.x);
+  if (count > 1) p[step] = __float2bfloat16_rn(v.y);
+  if (count > 2) p[2 * step] = __float2bfloat16_rn(v.z);
+  if (count > 3) p[3 * step] = __float2bfloat16_rn(v.w);
+}
+// A thread's tokens of a chunk (8 k + e from its first on) at its four channels; rows `ld` elements apart, those below `left`
+// exist.  words: the channels are neighbours and every address is aligned: straight loads, all in flight at once.
+template <typename T>
+__device__ __forceinline__ void fp8_load_tokens(const T* p, long ld, int left, bool words, int step, int have, float4 (&out)[8]) {
+  if (words && left > 25) {
+    const T* q = p + ld;
 #pragma unroll
-    for (int j = 0; j < 16; ++j, at += 2 * p.ldr) two[j] = (2 * j + odd < left && ch2 < p.N) ? *reinterpret_cast<const uint32_t*>(at) : 0u;
+    for (int k = 0; k < 4; ++k, p += 8 * ld, q += 8 * ld) out[2 * k] = fp8_load4(p), out[2 * k + 1] = fp8_load4(q);
+  } else {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const uint32_t t = __byte_perm(two[j], __shfl_xor_sync(0xffffffffu, two[j], 1), sel);
-      out[2 * j] = __uint_as_float(t << 16);
-      out[2 * j + 1] = __uint_as_float(t & 0xFFFF0000u);
+    for (int j = 0; j < 8; ++j) {
+      const int tok = (j >> 1) * 8 + (j & 1);
+      out[j] = fp8_load_some(p + tok * ld, step, tok < left ? have : 0);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void fp8_store_tokens(T* p, long ld, int left, bool words, int step, int have, const float (&v)[4][8]) {
+  if (words && left > 25) {
+    T* q = p + ld;
+#pragma unroll
+    for (int k = 0; k < 4; ++k, p += 8 * ld, q += 8 * ld) {
+      fp8_store4(p, make_float4(v[0][2 * k], v[1][2 * k], v[2][2 * k], v[3][2 * k]));
+      fp8_store4(q, make_float4(v[0][2 * k + 1], v[1][2 * k + 1], v[2][2 * k + 1], v[3][2 * k + 1]));
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) out[j] = (j < left && ch < p.N) ? fp8_residual(p, row + j, ch) : 0.f;
+    for (int j = 0; j < 8; ++j) {
+      const int tok = (j >> 1) * 8 + (j & 1);
+      fp8_store_some(p + tok * ld, make_float4(v[0][j], v[1][j], v[2][j], v[3][j]), step, tok < left ? have : 0);
+    }
   }
-}
-// The bytes of four tokens at one channel -> the four channels of one token, over four neighbouring lanes: lane r gets token r.
-__device__ __forceinline__ uint32_t fp8_transpose_bytes(uint32_t w) {
-  const int lane = threadIdx.x;
-  w = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 2), lane & 2 ? 0x3276u : 0x5410u);
-  return __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), lane & 1 ? 0x3715u : 0x6240u);
 }
 
 // FUSED: y = act(sum + bias) + residual; TOut = uint8_t (FUSED only): the codes of act(sum + bias), the next product's
 // operand.  A tile's 128 channels are one block of that operand, so its scale comes from the tile alone: the maximum over
 // the lanes of a warp, then over the four warps that hold the block's channels, which exchange it in shared memory.
+//
+// FUSED reads the accumulator 16 lanes x 8 columns at a time (the 16x256b shape): a thread gets lanes l, l + 8, l + 16 and
+// l + 24 of a warp's 32, at eight columns.  The weights' rows are copied in an order that makes these four neighbouring channels
+// (a tensor map of four dimensions: channel 32 q + 4 g + c goes to row 32 q + 8 c + g of the tile), so that a thread stores whole
+// words -- four channels of a token as 16, 8 or 4 bytes -- with no exchange between lanes, loads the residual likewise, and
+// finds most of a token's maximum in its own registers.  With the plain epilogue's shape (a lane a channel, 32 columns), the
+// exchange and the predicates of its stores made 16 instructions an output, 24 with gelu and codes: 80 us for 8192 x 1152 x
+// 4608 with gelu to codes, two thirds of it the epilogue.
+// Where the channels are no multiple of 32 the last block keeps the plain order, and its outputs are stored one by one.
 template <bool PAIR, typename TOut, bool FUSED = false>
-__global__ void __launch_bounds__(FP8G_THREADS, 1)
+__global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
     k_fp8_gemm(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
                const __grid_constant__ CUtensorMap tmap_x_tail, Fp8GemmParams p) {
   using SM = Fp8Smem<PAIR>;
   constexpr int BN = SM::BN;
+  constexpr int THREADS = FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, EPI_WARPS = THREADS / 32 - 4;
   extern __shared__ uint8_t fp8g_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(fp8g_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + SM::BAR_OFFSET);
@@ -270,7 +346,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
   volatile uint32_t* abort_word = tmem_slot + 1;
   int* tile_start = reinterpret_cast<int*>(smem + SM::TAB_OFFSET);
-  int* row_start = tile_start + FP8_MAX_EXPERTS + 1;
+  int* row_start = tile_start + (FUSED ? 1 : FP8_MAX_EXPERTS) + 1;
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -297,17 +373,16 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
-      ptx::mbar_init(&tempty[a], PAIR ? 2 * FP8G_EPI_WARPS : FP8G_EPI_WARPS);
+      ptx::mbar_init(&tempty[a], PAIR ? 2 * EPI_WARPS : EPI_WARPS);
     }
-    if constexpr (FUSED && sizeof(TOut) == 1) {
-      ptx::mbar_init(reinterpret_cast<uint64_t*>(smem + SM::EX_OFFSET), 4);
-      ptx::mbar_init(reinterpret_cast<uint64_t*>(smem + SM::EX_OFFSET) + 1, 4);
+    if constexpr (sizeof(TOut) == 1) {
+      for (int g = 0; g < FP8G_FUSED_GROUPS; ++g) ptx::mbar_init(reinterpret_cast<uint64_t*>(smem + SM::EX_OFFSET) + g, 4);
     }
     *abort_word = 0;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&tmap_w);
     ptx::prefetch_tensormap(&tmap_x);
-    if (p.tail) ptx::prefetch_tensormap(&tmap_x_tail);
+    if (!FUSED && p.tail) ptx::prefetch_tensormap(&tmap_x_tail);
   }
   if (warp == 1) {
     if constexpr (PAIR) {
@@ -322,7 +397,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
   if (p.offsets) {
     ptx::grid_dependency_wait();
     bool bad = false;
-    for (int e = threadIdx.x; e <= p.E; e += FP8G_THREADS) {
+    for (int e = threadIdx.x; e <= p.E; e += THREADS) {
       const int o = __ldg(p.offsets + e);
       row_start[e] = o;
       bad |= o < 0 || o > p.M || (e == 0 ? o != 0 : o < __ldg(p.offsets + e - 1));
@@ -393,7 +468,12 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
             dst = ring;
           }
           ready = ptx::mbar_test_wait(&empty[stage], phase ^ 1u);   // answered while the copies are issued
-          ptx::tma_load_2d_at<PAIR>(ws, &tmap_w, bar, kb * FP8G_BK, wrow);
+          if constexpr (FUSED) {
+            if (fp8_plain_order(p, wrow)) ptx::tma_load_2d_at<PAIR>(ws, &tmap_x_tail, bar, kb * FP8G_BK, wrow);
+            else ptx::tma_load_4d_at<PAIR>(ws, &tmap_w, bar, kb * FP8G_BK, 0, 0, wrow >> 5);
+          } else {
+            ptx::tma_load_2d_at<PAIR>(ws, &tmap_w, bar, kb * FP8G_BK, wrow);
+          }
           if (pieces == 0) ptx::tma_load_2d_at<PAIR>(xs, &tmap_x, bar, kb * FP8G_BK, xrow);
           for (int i = 0; i < pieces; ++i)
             ptx::tma_load_2d_at<PAIR>(xs + i * (FP8G_TAIL_BOX * FP8G_BK), &tmap_x_tail, bar, kb * FP8G_BK, xrow + i * FP8G_TAIL_BOX);
@@ -559,6 +639,213 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       *abort_word = 1;
       if (lane == 0) raise_device_status(STAMP_ERR_TIMEOUT);
     }
+  } else if constexpr (FUSED) {
+    // ------------------------------------------------------------------ epilogue warps, with what follows the sum
+    constexpr int G = FP8G_FUSED_GROUPS;
+    const int quarter = warp & 3;          // TMEM lanes this warp may touch
+    const int group = (warp - 4) >> 2;     // which chunks of 32 columns it takes: every G-th
+    const int g4 = lane >> 2, col = 2 * (lane & 3);   // its channels; its tokens of a chunk: 8 k + col + e, k = 0..3, e = 0, 1
+    const uint32_t tempty_bar0 = PAIR ? ptx::mapa(ptx::smem_u32(&tempty[0]), 0u) : 0u;
+    const bool y_words = (p.N & 3) == 0 && (reinterpret_cast<uintptr_t>(p.y) & (4 * sizeof(TOut) - 1)) == 0;
+    const bool r_words = (p.ldr & 3) == 0 && (reinterpret_cast<uintptr_t>(p.residual) & (p.r_bf16 ? 7 : 15)) == 0;
+    TOut* const y = static_cast<TOut*>(p.y);
+    // Hints that bring a tile's residual to L2, a tile ahead: a chunk's loads are too few to hide the way from memory.
+    auto prefetch_residual = [&](int tile) {
+      if (sizeof(TOut) == 1 || !p.residual || !(PAIR || p.split == 1) || tile >= num_tiles) return;
+      const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+      const int size = p.r_bf16 ? 2 : 4, first = (PAIR ? 2 * t.ch_tile + rank : t.ch_tile) * FP8G_BM, end = min(first + FP8G_BM, p.N);
+      const char* const at = static_cast<const char*>(p.residual) + (static_cast<long>(t.row0) * p.ldr) * size;
+      for (int r = (warp - 4) * 32 + lane; r < t.rows; r += 128 * G)
+        for (int ch = first; ch < end; ch += 128 / size) ptx::prefetch_l2(at + (static_cast<long>(r) * p.ldr + ch) * size);
+    };
+    prefetch_residual(tile0);
+    uint32_t exchanged = 0;   // maxima that this group has exchanged
+    int it = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+      const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
+      const int block = PAIR ? 2 * t.ch_tile + rank : t.ch_tile;
+      const bool plain = fp8_plain_order(p, block * FP8G_BM);
+      // this thread's channels: ch, ch + step, ch + 2 step, ch + 3 step, `have` of which exist
+      const int ch = block * FP8G_BM + quarter * 32 + (plain ? g4 : 4 * g4), step = plain ? 8 : 1;
+      const int have = plain ? (ch < p.N) + (ch + 8 < p.N) + (ch + 16 < p.N) + (ch + 24 < p.N) : ch < p.N ? 4 : 0;
+      const bool all = !plain && have == 4;
+      float bias[4] = {0.f, 0.f, 0.f, 0.f};
+      if (p.bias) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) bias[c] = __ldg(p.bias + min(ch + c * step, p.N - 1));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) bias[c] = c < have ? bias[c] : 0.f;
+      }
+      for (int c0 = step0; c0 < step1; c0 += p.chunk, ++it) {
+        const int a = it & 1;
+        // (an fp32 output may be summed in parts, the others never are)
+        const bool first = sizeof(TOut) != 4 || c0 == step0, last = sizeof(TOut) != 4 || c0 + p.chunk >= step1;
+        // The bias goes in with the first part, the activation follows the last; without one the residual goes in with the
+        // first part too: the output, which holds the parts, may be the residual's own memory.
+        const bool whole = PAIR || p.split == 1;
+        const bool add = sizeof(TOut) != 1 && p.residual && whole && (p.act == STAMP_ACT_NONE ? first : last);
+        const int chunks = (t.n + 31) / 32, count = (chunks - group + G - 1) / G;
+        auto chunk_at = [&](int i) { return group + G * (PAIR && a == 0 ? count - 1 - i : i); };
+        // What a chunk adds to is loaded ahead: for the first chunk before the sums are waited for, then a chunk ahead.  Plain
+        // loads: every element is read by the thread that writes it.
+        float4 res[sizeof(TOut) == 1 ? 1 : 8], before[sizeof(TOut) == 4 ? 8 : 1];
+        auto fetch = [&](int c) {
+          const int tok = 32 * c + col, there = have > 0 ? t.rows - tok : 0;
+          if constexpr (sizeof(TOut) != 1) {
+            const long at = (t.row0 + static_cast<long>(tok)) * p.ldr + ch;
+            if (add) {
+              if (p.r_bf16) fp8_load_tokens(static_cast<const __nv_bfloat16*>(p.residual) + at, p.ldr, there, r_words && all, step, have, res);
+              else fp8_load_tokens(static_cast<const float*>(p.residual) + at, p.ldr, there, r_words && all, step, have, res);
+            }
+          }
+          if constexpr (sizeof(TOut) == 4) {
+            if (!first) fp8_load_tokens(y + (t.row0 + static_cast<long>(tok)) * p.N + ch, p.N, there, y_words && all, step, have, before);
+          }
+        };
+        if (first) prefetch_residual(tile + tile_step);
+        if (count > 0) fetch(chunk_at(0));
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
+          ok = false;
+          break;
+        }
+        ptx::tc_fence_after();
+        const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(a * SM::ACC1);
+        bool released = false;
+        auto release = [&]() {
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR) ptx::mbar_arrive_cluster_relaxed(tempty_bar0); else ptx::mbar_arrive(&tempty[a]);
+          }
+          released = true;
+        };
+        // PAIR: the chunk that overlaps the other accumulator first; who has none of it hands back at once
+        if (PAIR && group != fp8_overlap_group(a)) release();
+        auto drain = [&](auto variant, float floor) {
+          for (int i = 0; i < count; ++i) {
+            const int c = chunk_at(i), left = have > 0 ? t.rows - 32 * c - col : 0;   // tokens 8 k + e below `left` are stored
+            float v[4][8];
+            {
+              uint32_t lo[16], hi[16];
+              ptx::tmem_ld_16x256b_x4(taddr + 32 * c, lo);
+              ptx::tmem_ld_16x256b_x4(taddr + 32 * c + (16u << 16), hi);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  v[0][2 * k + e] = __uint_as_float(lo[4 * k + e]);
+                  v[1][2 * k + e] = __uint_as_float(lo[4 * k + 2 + e]);
+                  v[2][2 * k + e] = __uint_as_float(hi[4 * k + e]);
+                  v[3][2 * k + e] = __uint_as_float(hi[4 * k + 2 + e]);
+                }
+            }
+            if (!released && (PAIR || i + 1 == count)) release();
+            if (!whole) {
+              // this CTA's part of the sum, [token][channel], in the ring that nothing uses any more
+              float* const part = reinterpret_cast<float*>(smem) + (32 * c + col) * FP8G_PART + (ch - block * FP8G_BM);
+              fp8_store_tokens(part, FP8G_PART, 32, !plain, step, 4, v);
+              continue;
+            }
+            if constexpr (sizeof(TOut) == 4) {
+              if (!first) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[0][j] += before[j].x, v[1][j] += before[j].y, v[2][j] += before[j].z, v[3][j] += before[j].w;
+              }
+            }
+            // (a part that is not the first has its bias already, one that is not the last gets no activation: LINEAR, floor -inf)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int j = 0; j < 8; j += 2) {
+                float2 r = make_float2(v[k][j], v[k][j + 1]);
+                if (sizeof(TOut) != 4 || first) r = __fadd2_rn(r, make_float2(bias[k], bias[k]));
+                r = fp8_activate2<decltype(variant)::value>(r, floor);
+                v[k][j] = r.x;
+                v[k][j + 1] = r.y;
+              }
+            if constexpr (sizeof(TOut) != 1) {
+              if (add) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[0][j] += res[j].x, v[1][j] += res[j].y, v[2][j] += res[j].z, v[3][j] += res[j].w;
+              }
+              if (i + 1 < count) fetch(chunk_at(i + 1));
+              fp8_store_tokens(y + (t.row0 + 32L * c + col) * p.N + ch, p.N, left, y_words && all, step, have, v);
+            } else {
+              // the largest magnitude of every token: over this thread's channels, the lanes that have the same tokens (each
+              // step halves the tokens a lane looks after: lane -> one token), and the block's four warps
+              uint32_t m[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) m[j] = __float_as_uint(ptx::max_abs_nan(ptx::max_abs_nan(v[0][j], v[1][j], v[2][j]), v[3][j], 0.f));
+#pragma unroll
+              for (int d = 16, n = 4; d >= 4; d >>= 1, n >>= 1) {
+                const bool upper = (lane & d) != 0;
+#pragma unroll
+                for (int j = 0; j < n; ++j) {
+                  const uint32_t other = __shfl_xor_sync(0xffffffffu, upper ? m[j] : m[j + n], d);
+                  m[j] = max(upper ? m[j + n] : m[j], other);
+                }
+              }
+              const int mine = ((lane >> 3) & 3) * 8 + col + ((lane >> 2) & 1);   // the token that is left
+              uint8_t* const ex = smem + SM::EX_OFFSET;
+              uint64_t* const bar = reinterpret_cast<uint64_t*>(ex) + group;
+              uint32_t* const maxima = reinterpret_cast<uint32_t*>(ex + 8 * G) + (group * 2 + static_cast<int>(exchanged & 1u)) * 128;
+              float* const inverse = reinterpret_cast<float*>(ex + 8 * G) + G * 256 + (warp - 4) * 32;
+              maxima[quarter * 32 + mine] = m[0];
+              __syncwarp();
+              if (lane == 0) ptx::mbar_arrive(bar);
+              if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar, exchanged & 1u, abort_word, FP8G_WAIT_LIMIT))) {
+                ok = false;
+                break;
+              }
+              ++exchanged;
+              uint32_t amax = 0;   // bits of magnitudes order like integers, NaNs above infinity
+#pragma unroll
+              for (int q = 0; q < 4; ++q) amax = max(amax, maxima[q * 32 + mine]);
+              const Fp8Scale s = fp8_scale(amax);
+              const int ks_out = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
+              if (quarter == 0 && 32 * c + mine < t.rows && block < ks_out) p.y_scale[(t.row0 + 32L * c + mine) * ks_out + block] = s.byte;
+              inverse[mine] = s.inverse;
+              __syncwarp();
+              uint32_t codes[8];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 f = *reinterpret_cast<const float2*>(inverse + 8 * k + col);
+                const float2 a01 = __fmul2_rn(make_float2(v[0][2 * k], v[0][2 * k + 1]), f), b01 = __fmul2_rn(make_float2(v[1][2 * k], v[1][2 * k + 1]), f);
+                const float2 c01 = __fmul2_rn(make_float2(v[2][2 * k], v[2][2 * k + 1]), f), d01 = __fmul2_rn(make_float2(v[3][2 * k], v[3][2 * k + 1]), f);
+                codes[2 * k] = ptx::cvt_e4m3x4(a01.x, b01.x, c01.x, d01.x);
+                codes[2 * k + 1] = ptx::cvt_e4m3x4(a01.y, b01.y, c01.y, d01.y);
+              }
+              uint8_t* out = static_cast<uint8_t*>(p.y) + (t.row0 + 32L * c + col) * p.N + ch;
+              if (all && left > 25) {
+                uint8_t* next = out + p.N;
+#pragma unroll
+                for (int k = 0; k < 4; ++k, out += 8L * p.N, next += 8L * p.N) {
+                  *reinterpret_cast<uint32_t*>(out) = codes[2 * k];
+                  *reinterpret_cast<uint32_t*>(next) = codes[2 * k + 1];
+                }
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                  for (int i4 = 0; i4 < 4; ++i4)
+                    if ((j >> 1) * 8 + (j & 1) < left && i4 < have)
+                      out[static_cast<long>((j >> 1) * 8 + (j & 1)) * p.N + i4 * step] = static_cast<uint8_t>(codes[j] >> (8 * i4));
+              }
+              __syncwarp();   // (the next chunk's inverse scales go to the same place)
+            }
+          }
+        };
+        fp8_with_activation(last && whole ? p.act : STAMP_ACT_NONE, drain);
+        if (!released) release();
+        if (!ok) break;
+      }
+    }
+    if (!ok) {
+      *abort_word = 1;
+      if (lane == 0) raise_device_status(STAMP_ERR_TIMEOUT);
+    }
   } else if (warp >= 4) {
     // ------------------------------------------------------------------ epilogue warps
     const int quarter = warp & 3;          // TMEM lanes this warp may touch
@@ -569,8 +856,6 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
     TOut* const y = static_cast<TOut*>(p.y);
     int it = 0;
     bool ok = true;
-    const bool r_pairs = FUSED && p.residual && p.r_bf16 && (p.N & 1) == 0 && (p.ldr & 1) == 0 && (reinterpret_cast<uintptr_t>(p.residual) & 3) == 0;
-    uint32_t exchanged = 0;   // maxima that this half has exchanged
     for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
       const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
       const int ch = (PAIR ? 2 * t.ch_tile + rank : t.ch_tile) * FP8G_BM + row;
@@ -599,11 +884,6 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
         const int count = (chunks - half + 1) / 2;
         for (int i = 0; i < count; ++i) {
           const int c = fp8_drain_chunk(PAIR && a == 0, half, i, count);
-          float res[FUSED ? 32 : 1];
-          if constexpr (FUSED && sizeof(TOut) != 1) {
-            if (p.residual && (PAIR || p.split == 1) && (p.act == STAMP_ACT_NONE ? c0 == step0 : c0 + p.chunk >= step1))
-              fp8_load_residual(p, t.row0 + 32 * c, t.rows - 32 * c, ch, r_pairs, res);
-          }
           uint32_t r[32];
           ptx::tmem_ld_32x32b_x32(taddr + 32 * c, r);
           ptx::tmem_ld_wait();
@@ -616,72 +896,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
             continue;
           }
           const int left = t.rows - 32 * c;
-          if constexpr (FUSED) {
-            const bool first = c0 == step0, last = c0 + p.chunk >= step1;   // (parts of the sum: fp32 outputs only)
-            if constexpr (sizeof(TOut) == 4) {
-              if (!first && ch < p.N) {
-                const TOut* before = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
-                float b[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) b[j] = j < left ? before[static_cast<long>(j) * p.N] : 0.f;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(b[j] + __uint_as_float(r[j]));
-              }
-            }
-            // the bias goes in with the first part, the activation follows the last; without one the residual goes in with the
-            // first part too: the output, which holds the parts, may be the residual's own memory
-            const bool plain = p.act == STAMP_ACT_NONE;
-            fp8_activate32(r, first ? bias : 0.f, last ? p.act : STAMP_ACT_NONE);
-            if (p.residual && (plain ? first : last)) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + res[j]);
-            }
-          }
-          if constexpr (sizeof(TOut) == 1) {
-            // the largest magnitude of every token: over this warp's channels, then over the block's four warps
-            uint8_t* const ex = smem + SM::EX_OFFSET;
-            float* const maxima = reinterpret_cast<float*>(ex + 16) + (half * 2 + static_cast<int>(exchanged & 1u)) * 128;
-            float* const inverse = reinterpret_cast<float*>(ex + 16) + 512 + (warp - 4) * 32;
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              float m[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) m[i] = ptx::warp_max_abs(ch < p.N ? __uint_as_float(r[j + i]) : 0.f);
-              if (lane == 0) *reinterpret_cast<float4*>(maxima + quarter * 32 + j) = make_float4(m[0], m[1], m[2], m[3]);
-            }
-            __syncwarp();
-            uint64_t* const bar = reinterpret_cast<uint64_t*>(ex) + half;
-            if (lane == 0) ptx::mbar_arrive(bar);
-            if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar, exchanged & 1u, abort_word, FP8G_WAIT_LIMIT))) {
-              ok = false;
-              break;
-            }
-            ++exchanged;
-            uint32_t amax = 0;   // of token `lane`; bits of magnitudes order like integers, NaNs above infinity
-#pragma unroll
-            for (int q = 0; q < 4; ++q) amax = max(amax, __float_as_uint(maxima[q * 32 + lane]));
-            const Fp8Scale s = fp8_scale(amax);
-            const int block = PAIR ? 2 * t.ch_tile + rank : t.ch_tile, ks_out = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
-            if (quarter == 0 && lane < left && block < ks_out) p.y_scale[static_cast<long>(t.row0 + 32 * c + lane) * ks_out + block] = s.byte;
-            inverse[lane] = s.inverse;
-            __syncwarp();
-            uint8_t* out = static_cast<uint8_t*>(p.y) + static_cast<long>(t.row0 + 32 * c + (lane & 3)) * p.N + (ch & ~3);
-#pragma unroll
-            for (int j = 0; j < 32; j += 4, out += 4 * static_cast<long>(p.N)) {
-              const float4 i4 = *reinterpret_cast<const float4*>(inverse + j);
-              const uint32_t w = fp8_transpose_bytes(ptx::cvt_e4m3x4(__uint_as_float(r[j]) * i4.x, __uint_as_float(r[j + 1]) * i4.y,
-                                                                      __uint_as_float(r[j + 2]) * i4.z, __uint_as_float(r[j + 3]) * i4.w));
-              if (j + (lane & 3) < left && ch < p.N) *reinterpret_cast<uint32_t*>(out) = w;
-            }
-            __syncwarp();   // (the next chunk's inverse scales go to the same place)
-          } else if constexpr (FUSED && sizeof(TOut) == 4) {
-            TOut* out = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
-            if (ch < p.N) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j, out += p.N)
-                if (j < left) *out = __uint_as_float(r[j]);
-            }
-          } else if constexpr (sizeof(TOut) == 4) {
+          if constexpr (sizeof(TOut) == 4) {
             TOut* out = y + static_cast<long>(t.row0 + 32 * c) * p.N + ch;
             if (c0 == step0) {
               if (ch < p.N) {
@@ -711,8 +926,7 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
             uint32_t two[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-              const __nv_bfloat162 v = FUSED ? __floats2bfloat162_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]))
-                                             : __floats2bfloat162_rn(__uint_as_float(r[2 * j]) + bias, __uint_as_float(r[2 * j + 1]) + bias);
+              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[2 * j]) + bias, __uint_as_float(r[2 * j + 1]) + bias);
               two[j] = *reinterpret_cast<const uint32_t*>(&v);
             }
 #pragma unroll
@@ -738,9 +952,6 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
           }
         }
         if (!released) release();
-        if constexpr (sizeof(TOut) == 1) {
-          if (!ok) break;
-        }
       }
     }
     if (!ok) {
@@ -766,19 +977,22 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
       float bias[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) bias[i] = (p.bias && ch + i < p.N) ? __ldg(p.bias + static_cast<long>(t.expert) * p.N + ch + i) : 0.f;
-      for (int tok = rank + warp * p.split; tok < t.rows; tok += FP8G_THREADS / 32 * p.split) {
+      for (int tok = rank + warp * p.split; tok < t.rows; tok += THREADS / 32 * p.split) {
         float4 v[8];   // all in flight at once
 #pragma unroll
         for (int s = 0; s < 8; ++s)
-          if (s < p.split) v[s] = ptx::ld_dsmem_f4(part_of[s] + (tok * FP8G_BM + c4) * 4);
+          if (s < p.split) v[s] = ptx::ld_dsmem_f4(part_of[s] + (tok * (FUSED ? FP8G_PART : FP8G_BM) + c4) * 4);
         float4 sum = v[0];
 #pragma unroll
         for (int s = 1; s < 8; ++s)
           if (s < p.split) sum = make_float4(sum.x + v[s].x, sum.y + v[s].y, sum.z + v[s].z, sum.w + v[s].w);
         TOut* out = static_cast<TOut*>(p.y) + static_cast<long>(t.row0 + tok) * p.N + ch;
         if constexpr (FUSED) {
-          const float2 a = fp8_activate2(make_float2(sum.x + bias[0], sum.y + bias[1]), p.act);
-          const float2 b = fp8_activate2(make_float2(sum.z + bias[2], sum.w + bias[3]), p.act);
+          float2 a, b;
+          fp8_with_activation(p.act, [&](auto variant, float floor) {
+            a = fp8_activate2<decltype(variant)::value>(make_float2(sum.x + bias[0], sum.y + bias[1]), floor);
+            b = fp8_activate2<decltype(variant)::value>(make_float2(sum.z + bias[2], sum.w + bias[3]), floor);
+          });
           float v[4] = {a.x, a.y, b.x, b.y};
           if constexpr (sizeof(TOut) == 1) {
             float most = 0.f;
@@ -790,18 +1004,18 @@ __global__ void __launch_bounds__(FP8G_THREADS, 1)
             if (ch < p.N)
               *reinterpret_cast<uint32_t*>(out) = ptx::cvt_e4m3x4(v[0] * s.inverse, v[1] * s.inverse, v[2] * s.inverse, v[3] * s.inverse);
           } else {
-            if (p.residual) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (ch + i < p.N) v[i] += fp8_residual(p, t.row0 + tok, ch + i);
+            if (p.residual && ch < p.N) {
+              const long at = (t.row0 + static_cast<long>(tok)) * p.ldr + ch;
+              const float4 r = p.r_bf16 ? fp8_load_some(static_cast<const __nv_bfloat16*>(p.residual) + at, 1, p.N - ch)
+                                        : fp8_load_some(static_cast<const float*>(p.residual) + at, 1, p.N - ch);
+              v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
             }
             if (ch < p.N) fp8_store2(out, v[0], v[1], ch + 1 < p.N, vec);
             if (ch + 2 < p.N) fp8_store2(out + 2, v[2], v[3], ch + 3 < p.N, vec);
           }
-          continue;
         } else {
-        if (ch < p.N) fp8_store2(out, sum.x + bias[0], sum.y + bias[1], ch + 1 < p.N, vec);
-        if (ch + 2 < p.N) fp8_store2(out + 2, sum.z + bias[2], sum.w + bias[3], ch + 3 < p.N, vec);
+          if (ch < p.N) fp8_store2(out, sum.x + bias[0], sum.y + bias[1], ch + 1 < p.N, vec);
+          if (ch + 2 < p.N) fp8_store2(out + 2, sum.z + bias[2], sum.w + bias[3], ch + 3 < p.N, vec);
         }
       }
     }

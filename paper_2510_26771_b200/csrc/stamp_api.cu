@@ -217,6 +217,21 @@ static int make_tmap_i8(const void* base, long rows, int K, int box_rows, CUtens
   return r == CUDA_SUCCESS ? STAMP_OK : STAMP_ERR_CUDA;
 }
 
+// Byte matrix [rows, K], whole runs of 32 rows; box = 128 bytes of K x 128 rows, of every 32 the rows 0, 4, 8 .. 28, then 1, 5 .. 29
+// and so on (row 32 q + 4 g + c as dimensions q, c, g), 128-byte swizzle.
+static int make_tmap_by_fours(const void* base, long rows, int K, CUtensorMap* out) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return STAMP_ERR_CUDA;
+  cuuint64_t dims[4] = {(cuuint64_t)K, 8u, 4u, (cuuint64_t)(rows / 32)};
+  cuuint64_t strides[3] = {(cuuint64_t)4 * K, (cuuint64_t)K, (cuuint64_t)32 * K};
+  cuuint32_t box[4] = {128u, 8u, 4u, 4u};
+  cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? STAMP_OK : STAMP_ERR_CUDA;
+}
+
 // `terms` byte matrices [rows, K], one after the other; box = 128 bytes of K x 8 rows of every one, 128-byte swizzle.
 static int make_tmap_terms(const void* base, long rows, int K, int terms, CUtensorMap* out) {
   EncodeTiledFn enc = get_encode();
@@ -1344,7 +1359,7 @@ static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const C
   const long units = (p.split == 1 && tiles > slots) ? slots : tiles;
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3((unsigned)(units * per_tile));
-  lc.blockDim = dim3(FP8G_THREADS);
+  lc.blockDim = dim3(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS);
   lc.dynamicSmemBytes = bytes;
   lc.stream = st;
   cudaLaunchAttribute at[2];
@@ -1451,22 +1466,32 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
   CUtensorMap tw, tx, txt;
   if (int rc = make_tmap_i8(p.w, (long)p.E * p.N, p.K, FP8G_BM, &tw)) return rc;
   if (int rc = make_tmap_i8(p.x, p.M, p.K, box, &tx)) return rc;
+  if constexpr (FUSED) {
+    // the weights twice: with every 32 channels in the epilogue's order, and plain for a last block that is no multiple of 32
+    p.tail = 0;
+    txt = tw;
+    if (p.N >= 32)
+      if (int rc = make_tmap_by_fours(p.w, p.N, p.K, &tw)) return rc;
+    if (y_dtype == FP8_OUT_CODES)
+      return pair ? launch_fp8_gemm<true, uint8_t, true>(tw, tx, txt, p, tiles, st)
+                  : launch_fp8_gemm<false, uint8_t, true>(tw, tx, txt, p, tiles, st);
+    if (pair)
+      return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16, true>(tw, tx, txt, p, tiles, st)
+                                   : launch_fp8_gemm<true, float, true>(tw, tx, txt, p, tiles, st);
+    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16, true>(tw, tx, txt, p, tiles, st)
+                                 : launch_fp8_gemm<false, float, true>(tw, tx, txt, p, tiles, st);
+  }
   // Runs end anywhere: where a tile's rows fill half a box or less, copies of 32 rows bring fewer that are not used.  (In
   // place of whole boxes everywhere they cost: 8192 x 4096 x 4096 99 -> 105 us.)
   p.tail = p.offsets && box > 2 * FP8G_TAIL_BOX ? box / 2 : 0;
   txt = tx;
   if (p.tail)
     if (int rc = make_tmap_i8(p.x, p.M, p.K, FP8G_TAIL_BOX, &txt)) return rc;
-  if constexpr (FUSED) {
-    if (y_dtype == FP8_OUT_CODES)
-      return pair ? launch_fp8_gemm<true, uint8_t, true>(tw, tx, txt, p, tiles, st)
-                  : launch_fp8_gemm<false, uint8_t, true>(tw, tx, txt, p, tiles, st);
-  }
   if (pair)
-    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16, FUSED>(tw, tx, txt, p, tiles, st)
-                                 : launch_fp8_gemm<true, float, FUSED>(tw, tx, txt, p, tiles, st);
-  return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16, FUSED>(tw, tx, txt, p, tiles, st)
-                               : launch_fp8_gemm<false, float, FUSED>(tw, tx, txt, p, tiles, st);
+    return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16>(tw, tx, txt, p, tiles, st)
+                                 : launch_fp8_gemm<true, float>(tw, tx, txt, p, tiles, st);
+  return y_dtype == STAMP_BF16 ? launch_fp8_gemm<false, __nv_bfloat16>(tw, tx, txt, p, tiles, st)
+                               : launch_fp8_gemm<false, float>(tw, tx, txt, p, tiles, st);
 }
 
 // A residual [M, N] with rows ldr elements apart: aligned to its type, and apart from Y or Y itself.

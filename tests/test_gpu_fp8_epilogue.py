@@ -4,8 +4,8 @@ statements in 64 bits.
 Tolerances, derived before the first run:
   sum         as for the plain product: off = K * 2^-23 * sum_k |x_k w_k| (+ |bias| 2^-24).
   activation  its slope is at most 1.13 (gelu; silu 1.10, relu 1), so the sum's error comes out 1.13 times as large at most.
-              Its own error, relative to its value: silu 4 ulp = 2^-21; gelu: the normal distribution function within 5 ulp,
-              a product: 2^-20; gelu_tanh: 2 u is a product of three roundings and two rounded constants, at most 5 * 2^-24 of
+              Its own error, relative to its value: silu 4 ulp = 2^-21; gelu: the scaled complementary error function within
+              2^-21, the exponential within 2 ulp = 2^-22, three products of half an ulp: 2^-20; gelu_tanh: 2 u is a product of three roundings and two rounded constants, at most 5 * 2^-24 of
               itself, which the exponential turns into |2 u| times that; power, sum and quotient add at most 3 ulp each:
               (5 |2 u| + 18) * 2^-24.  Values below 1e-36 may be flushed.
   residual    one addition: 2^-24 of the result.
