@@ -328,7 +328,7 @@ def stamp_expert_route(logits: torch.Tensor, top: int, normalize: bool = True, o
     """[T, E] router logits -> (chosen [T, top] int32, share [T, top] float32, rows [T * top] int32, place [T, top] int32,
     offsets [E + 1] int32, row_share [T * top] float32): every token's `top` experts, the rows in expert order as the products
     take them, and where each row went.  normalize: shares are a softmax over the chosen experts, else over all.  out: the six
-    buffers to write instead of new ones."""
+    buffers to write instead of new ones (which share one allocation)."""
     return _outputs((_calls or calls()).expert_route(logits, top, bool(normalize), out), "stamp_expert_route")
 
 

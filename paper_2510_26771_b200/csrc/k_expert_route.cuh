@@ -17,10 +17,14 @@ constexpr int ROUTE_WARPS = 32;
 constexpr int ROUTE_THREADS = 32 * ROUTE_WARPS;
 constexpr int ROUTE_ONE_CTA_TOKENS = 128;   // up to here one CTA does it all in one launch
 
+// Experts of a row of counts: a multiple of four.
+__host__ __device__ constexpr int route_pitch(int E) { return (E + 3) & ~3; }
+
 struct RouteParams {
   const void* logits;   // [T, ldl]
   long ldl;
   int T, E, top, normalize;
+  int vector;           // logits can be read 16 bytes (a lane's, if that is less) at a time
   int per_cta, per_warp;   // tokens; each CTA and warp has a run of them
   int* chosen;          // [T, top]
   float* share;         // [T, top]
@@ -28,10 +32,10 @@ struct RouteParams {
   int* place;           // [T, top]
   int* offsets;         // [E + 1]
   float* row_share;     // [T * top]
-  int* counts;          // [CTAs, E] rows of every expert from a CTA's tokens (more than one CTA)
+  int* counts;          // [CTAs, route_pitch(E)] rows of every expert from a CTA's tokens (more than one CTA)
 };
 
-// A float's bits so that they order as it does; -0 as 0, NaN below everything, 0 and 1 left free.
+// A float's bits so that they order as it does; -0 as 0, NaN below everything, 0 left free.
 __device__ __forceinline__ uint32_t route_key(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);
   if ((b & 0x7FFFFFFFu) > 0x7F800000u) return 1u;
@@ -43,6 +47,113 @@ __device__ __forceinline__ float route_value(uint32_t key) {
 }
 __device__ __forceinline__ float route_load(const float* p) { return __ldg(p); }
 __device__ __forceinline__ float route_load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+
+// A logit and its expert, ordered: larger logits first, of equal ones the lower expert.  A bf16 logit has 16 bits, so both fit
+// one word (the lower half counts experts downwards); an fp32 one takes two.  `none` comes behind everything.  set_finite leaves
+// NaNs outside the infinities' range, where strange() finds them in a sorted list's ends; set gives them their place.
+template <typename TIn>
+struct RouteEntry;
+template <>
+struct RouteEntry<__nv_bfloat16> {
+  uint32_t word;
+  __device__ __forceinline__ void set(float logit, int e) { word = (route_key(logit) >> 16 << 16) | (0xFFFFu - e); }   // (a NaN: 0, with an expert)
+  __device__ __forceinline__ void set_finite(float logit, int e) {
+    const uint32_t b = __float_as_uint(logit + 0.f), flip = static_cast<uint32_t>(static_cast<int>(b) >> 31) | 0x80000000u;
+    word = ((b ^ flip) & 0xFFFF0000u) | (0xFFFFu - e);
+  }
+  __device__ __forceinline__ static bool strange(const RouteEntry& first, const RouteEntry& last) {
+    return first.word >= 0xFF810000u || last.word < 0x007F0000u;   // (infinity's upper half is 0xFF80, that of -infinity 0x007F)
+  }
+  __device__ __forceinline__ void none() { word = 0u; }
+  __device__ __forceinline__ static void order(RouteEntry& a, RouteEntry& b) {
+    const uint32_t hi = max(a.word, b.word);
+    b.word = min(a.word, b.word);
+    a.word = hi;
+  }
+  __device__ __forceinline__ RouteEntry best() const { return RouteEntry{__reduce_max_sync(0xffffffffu, word)}; }
+  __device__ __forceinline__ bool is(const RouteEntry& o) const { return word == o.word; }
+  __device__ __forceinline__ int expert() const { return 0xFFFF - (word & 0xFFFFu); }
+  __device__ __forceinline__ float logit() const {
+    const uint32_t key = word & 0xFFFF0000u;   // (the lower half of a negative float's key is all ones)
+    return key == 0u ? __int_as_float(0x7FC00000) : __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key & 0xFFFF0000u);
+  }
+};
+template <>
+struct RouteEntry<float> {
+  uint32_t key, e;
+  __device__ __forceinline__ void set(float logit, int expert) { key = route_key(logit), e = expert; }
+  __device__ __forceinline__ void set_finite(float logit, int expert) {
+    const uint32_t b = __float_as_uint(logit + 0.f);
+    key = b ^ (static_cast<uint32_t>(static_cast<int>(b) >> 31) | 0x80000000u), e = expert;
+  }
+  __device__ __forceinline__ static bool strange(const RouteEntry& first, const RouteEntry& last) {
+    return first.key > 0xFF800000u || last.key < 0x007FFFFFu;
+  }
+  __device__ __forceinline__ void none() { key = 0u, e = 0x7FFFFFFFu; }
+  __device__ __forceinline__ static void order(RouteEntry& a, RouteEntry& b) {
+    const bool swap = a.key < b.key || (a.key == b.key && a.e > b.e);
+    const RouteEntry c = a;
+    a.key = swap ? b.key : c.key, a.e = swap ? b.e : c.e;
+    b.key = swap ? c.key : b.key, b.e = swap ? c.e : b.e;
+  }
+  __device__ __forceinline__ RouteEntry best() const {
+    const uint32_t most = __reduce_max_sync(0xffffffffu, key);
+    return RouteEntry{most, __reduce_min_sync(0xffffffffu, key == most ? e : 0x7FFFFFFFu)};
+  }
+  __device__ __forceinline__ bool is(const RouteEntry& o) const { return e == o.e; }
+  __device__ __forceinline__ int expert() const { return static_cast<int>(e); }
+  __device__ __forceinline__ float logit() const { return route_value(key); }
+};
+// A lane's entries in order: sorting networks (of eight: two of four, then a merge).
+template <typename T, int PER>
+__device__ __forceinline__ void route_sort(RouteEntry<T> (&v)[PER]) {
+  auto at = [&](int a, int b) { RouteEntry<T>::order(v[a], v[b]); };
+  if constexpr (PER >= 2) {
+#pragma unroll
+    for (int i = 0; i < PER; i += 2) at(i, i + 1);
+  }
+  if constexpr (PER >= 4) {
+#pragma unroll
+    for (int i = 0; i < PER; i += 4) at(i, i + 2), at(i + 1, i + 3), at(i + 1, i + 2);
+  }
+  if constexpr (PER == 8) {
+    at(0, 4), at(1, 5), at(2, 6), at(3, 7);
+    at(2, 4), at(3, 5);
+    at(1, 2), at(3, 4), at(5, 6);
+  }
+}
+// PER neighbouring logits of a row as floats; beyond the row -inf.
+template <int PER>
+__device__ __forceinline__ void route_load_all(const float* p, int left, bool vector, float (&l)[PER]) {
+  if (PER >= 4 && vector && left >= PER) {
+#pragma unroll
+    for (int i = 0; i < PER; i += 4) {
+      const float4 u = __ldg(reinterpret_cast<const float4*>(p + i));
+      l[i] = u.x, l[(i + 1) % PER] = u.y, l[(i + 2) % PER] = u.z, l[(i + 3) % PER] = u.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) l[i] = i < left ? route_load(p + i) : -__int_as_float(0x7F800000);
+  }
+}
+template <int PER>
+__device__ __forceinline__ void route_load_all(const __nv_bfloat16* p, int left, bool vector, float (&l)[PER]) {
+  if (PER >= 4 && vector && left >= PER) {
+    uint32_t w[PER / 2 > 0 ? PER / 2 : 1];
+    if constexpr (PER == 8) {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    } else {
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+      w[0] = u.x, w[1 % (PER / 2 > 0 ? PER / 2 : 1)] = u.y;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) l[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) l[i] = i < left ? route_load(p + i) : -__int_as_float(0x7F800000);
+  }
+}
 
 // Exclusive sum over the CTA of one value per thread; `total` gets the sum.  scratch: 33 words.
 __device__ __forceinline__ int route_scan(int v, int* scratch, int& total) {
@@ -74,19 +185,37 @@ __device__ __forceinline__ int route_scan(int v, int* scratch, int& total) {
 
 // Where the rows of this CTA's tokens go, given its experts' first places (base, shared memory) and each row's rank among the
 // CTA's rows of the same expert (in place).
-__device__ __forceinline__ void route_store(const RouteParams& p, const int* base) {
+struct RouteRow {
+  long i, last;   // (token, choice) of this thread's next row, and the end of the CTA's
+  int expert, rank;
+  float share;
+  __device__ __forceinline__ void load(const RouteParams& p) {
+    if (i < last) expert = p.chosen[i], rank = p.place[i], share = p.share[i];
+  }
+};
+__device__ __forceinline__ RouteRow route_first(const RouteParams& p) {
   const long first = static_cast<long>(blockIdx.x) * p.per_cta * p.top;
-  const long last = min(first + static_cast<long>(p.per_cta) * p.top, static_cast<long>(p.T) * p.top);
-  for (long i = first + threadIdx.x; i < last; i += ROUTE_THREADS) {
-    const int at = base[p.chosen[i]] + p.place[i];
-    p.place[i] = at;
-    p.rows[at] = static_cast<int>(i / p.top);
-    p.row_share[at] = p.share[i];
+  RouteRow r{first + threadIdx.x, min(first + static_cast<long>(p.per_cta) * p.top, static_cast<long>(p.T) * p.top), 0, 0, 0.f};
+  r.load(p);
+  return r;
+}
+__device__ __forceinline__ void route_store(const RouteParams& p, const int* base, RouteRow r) {
+  while (r.i < r.last) {
+    const int at = base[r.expert] + r.rank;
+    p.place[r.i] = at;
+    p.rows[at] = static_cast<int>(static_cast<uint32_t>(r.i) / static_cast<uint32_t>(p.top));   // (T * top <= 2^30)
+    p.row_share[at] = r.share;
+    r.i += ROUTE_THREADS;
+    r.load(p);
   }
 }
 
-// A warp takes one token after the other: PER logits a lane, expert 32 i + lane in register i.  Each warp counts its rows by
-// expert in shared memory, and a row's rank is the count so far; the warps' counts are then summed in their order.
+// A warp takes one token after the other, a lane PER neighbouring experts: it sorts them once, then the lanes' first entries
+// are compared `top` times, and the lane that had the best one moves up.  (Searching all entries every time took three times the
+// instructions, which is what bounds it: 16384 tokens of 256 experts, top 8, 744 a token.)  Above 256 experts (PER = 32,
+// expert 32 i + lane in register i) sorting costs more than searching.
+// Each warp counts its rows by expert in shared memory, and a row's rank is the count so far; the warps' counts are then
+// summed in their order.
 template <typename TIn, int PER>
 __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) {
   extern __shared__ int route_counts[];   // [ROUTE_WARPS][E] rows by warp and expert, then base [E]
@@ -101,38 +230,71 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
   const long cta_end = min((static_cast<long>(blockIdx.x) + 1) * p.per_cta, static_cast<long>(p.T));
   const long t0 = static_cast<long>(blockIdx.x) * p.per_cta + static_cast<long>(warp) * p.per_warp;
   for (long t = t0; t < min(t0 + p.per_warp, cta_end); ++t) {
-    const TIn* at = static_cast<const TIn*>(p.logits) + t * p.ldl + lane;
-    uint32_t key[PER];
+    const TIn* row = static_cast<const TIn*>(p.logits) + t * p.ldl;
     float l[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) l[i] = 32 * i + lane < p.E ? route_load(at + 32 * i) : -__int_as_float(0x7F800000);
     bool nan = false;
+    int expert = 0;        // lane j: choice j and its logit
+    float best = 0.f;
+    if constexpr (PER <= 8) {
+      route_load_all<PER>(row + lane * PER, p.E - lane * PER, p.vector, l);
+      RouteEntry<TIn> entry[PER], mine_of{};
+      const bool full = p.E == 32 * PER;   // every lane has PER experts
+      if (full) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      key[i] = 32 * i + lane < p.E ? route_key(l[i]) : 0u;
-      nan |= key[i] == 1u;
+        for (int i = 0; i < PER; ++i) entry[i].set_finite(l[i], lane * PER + i);
+        route_sort<TIn, PER>(entry);
+        nan = __any_sync(0xffffffffu, RouteEntry<TIn>::strange(entry[0], entry[PER - 1]));
+      }
+      if (!full || nan) {
+        nan = false;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          entry[i].set(l[i], lane * PER + i);
+          if (lane * PER + i >= p.E) entry[i].none();
+          nan |= l[i] != l[i];
+        }
+        nan = __any_sync(0xffffffffu, nan);
+        route_sort<TIn, PER>(entry);
+      }
+      for (int j = 0; j < p.top; ++j) {
+        const RouteEntry<TIn> first = entry[0].best();
+        const bool up = entry[0].is(first);
+#pragma unroll
+        for (int i = 0; i + 1 < PER; ++i)
+          if (up) entry[i] = entry[i + 1];
+        if (up) entry[PER - 1].none();
+        if (lane == j) mine_of = first;
+      }
+      expert = mine_of.expert();
+      best = mine_of.logit();
+    } else {
+      uint32_t key[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        l[i] = 32 * i + lane < p.E ? route_load(row + 32 * i + lane) : -__int_as_float(0x7F800000);
+        key[i] = 32 * i + lane < p.E ? route_key(l[i]) : 0u;
+        nan |= l[i] != l[i];
+      }
+      for (int j = 0; j < p.top; ++j) {
+        uint32_t most = key[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) most = max(most, key[i]);
+        most = __reduce_max_sync(0xffffffffu, most);
+        int e = 0x7FFFFFFF;
+#pragma unroll
+        for (int i = PER - 1; i >= 0; --i)
+          if (key[i] == most) e = 32 * i + lane;
+        e = __reduce_min_sync(0xffffffffu, e);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (32 * i + lane == e) key[i] = 0u;
+        if (lane == j) expert = e, best = route_value(most);
+      }
+      nan = __any_sync(0xffffffffu, nan);
     }
-    nan = __any_sync(0xffffffffu, nan);
-    int expert = 0;        // lane j: choice j
-    uint32_t best = 0u;
-    for (int j = 0; j < p.top; ++j) {
-      uint32_t most = key[0];
-#pragma unroll
-      for (int i = 1; i < PER; ++i) most = max(most, key[i]);
-      most = __reduce_max_sync(0xffffffffu, most);
-      int e = 0x7FFFFFFF;
-#pragma unroll
-      for (int i = PER - 1; i >= 0; --i)
-        if (key[i] == most) e = 32 * i + lane;
-      e = __reduce_min_sync(0xffffffffu, e);
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (32 * i + lane == e) key[i] = 0u;
-      if (lane == j) expert = e, best = most;
-    }
-    const float largest = route_value(__shfl_sync(0xffffffffu, best, 0));
+    const float largest = __shfl_sync(0xffffffffu, best, 0);
     const bool dead = !nan && largest == -__int_as_float(0x7F800000);
-    const float weight = lane < p.top ? expf(route_value(best) - largest) : 0.f;
+    const float weight = lane < p.top ? expf(best - largest) : 0.f;
     float total = weight;
     if (!p.normalize) {
       total = 0.f;
@@ -161,8 +323,9 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
       sum += c;
     }
     base[e] = sum;
-    if (gridDim.x > 1) p.counts[static_cast<long>(blockIdx.x) * p.E + e] = sum;
+    if (gridDim.x > 1) p.counts[static_cast<long>(blockIdx.x) * route_pitch(p.E) + e] = sum;
   }
+  if (gridDim.x > 1 && threadIdx.x >= p.E && threadIdx.x < route_pitch(p.E)) p.counts[static_cast<long>(blockIdx.x) * route_pitch(p.E) + threadIdx.x] = 0;
   __syncthreads();
   for (long t = t0; t < min(t0 + p.per_warp, cta_end); ++t)
     if (lane < p.top) p.place[t * p.top + lane] += mine[p.chosen[t * p.top + lane]];
@@ -177,51 +340,49 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
   }
   if (e == 0) p.offsets[p.E] = total;
   __syncthreads();
-  route_store(p, base);
+  route_store(p, base, route_first(p));
 }
 
-// The second launch where several CTAs chose: every expert's first place, from the counts of all CTAs; then the rows.
+// The second launch where several CTAs chose: every expert's first place, from the counts of all CTAs; then the rows.  The
+// counts are padded to a multiple of four experts (`pitch`): a thread sums four experts over a share of the CTAs.
 __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_place(RouteParams p) {
-  extern __shared__ int route_counts[];   // base [E], then sums [ROUTE_THREADS] twice
+  extern __shared__ int4 route_sums[];   // [groups][pitch / 4] rows of the CTAs before this one, then of all
+  __shared__ int base[ROUTE_MAX_EXPERTS];
   __shared__ int scratch[33];
-  int* const base = route_counts;
-  int* const before_of = base + p.E;
-  int* const all_of = before_of + ROUTE_THREADS;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  // threads in groups of `width` >= E, each of which sums a share of the CTAs
-  int width = 32;
-  while (width < p.E) width *= 2;
-  const int groups = ROUTE_THREADS / width, g = threadIdx.x / width, e = threadIdx.x % width;
-  int before = 0, all = 0;   // rows of expert e from the CTAs before this one, and from all
-  if (e < p.E) {
-#pragma unroll 8
+  const int fours = route_pitch(p.E) / 4, groups = ROUTE_THREADS / fours, g = threadIdx.x / fours, i4 = threadIdx.x - g * fours;
+  const RouteRow row = route_first(p);   // (on its way with the counts)
+  int4 before = make_int4(0, 0, 0, 0), all = before;
+  if (g < groups) {
+#pragma unroll 4
     for (int b = g; b < static_cast<int>(gridDim.x); b += groups) {
-      const int c = __ldg(p.counts + static_cast<long>(b) * p.E + e);
-      all += c;
-      before += b < static_cast<int>(blockIdx.x) ? c : 0;
+      const int4 c = __ldg(reinterpret_cast<const int4*>(p.counts) + static_cast<long>(b) * fours + i4);
+      all.x += c.x, all.y += c.y, all.z += c.z, all.w += c.w;
+      if (b < static_cast<int>(blockIdx.x)) before.x += c.x, before.y += c.y, before.z += c.z, before.w += c.w;
     }
+    route_sums[g * fours + i4] = before;
+    route_sums[(groups + g) * fours + i4] = all;
   }
-  before_of[threadIdx.x] = before;
-  all_of[threadIdx.x] = all;
   __syncthreads();
-  if (g == 0) {
-    for (int o = 1; o < groups; ++o) {
-      before += before_of[o * width + e];
-      all += all_of[o * width + e];
+  const int e = threadIdx.x;
+  int mine = 0, sum = 0;
+  if (e < p.E) {
+    const int* const s = reinterpret_cast<const int*>(route_sums) + e;
+    for (int o = 0; o < groups; ++o) {
+      mine += s[o * fours * 4];
+      sum += s[(groups + o) * fours * 4];
     }
-  } else {
-    all = 0;
   }
   int total;
-  const int first = route_scan(all, scratch, total);   // (thread e < E: expert e; the others add nothing)
-  if (g == 0 && e < p.E) {
-    base[e] = first + before;
+  const int first = route_scan(sum, scratch, total);
+  if (e < p.E) {
+    base[e] = first + mine;
     if (blockIdx.x == 0) p.offsets[e] = first;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[p.E] = total;
+  if (blockIdx.x == 0 && e == 0) p.offsets[p.E] = total;
   __syncthreads();
-  route_store(p, base);
+  route_store(p, base, row);
 }
 
 // ---- the way back: out[t] = sum_j share[t, j] y[place[t, j]] + residual[t], in fp32 in the order of j, rounded once.

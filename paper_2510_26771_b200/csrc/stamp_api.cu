@@ -1542,7 +1542,8 @@ static int launch_route(const RouteParams& p, int ctas, cudaStream_t st) {
   }
   STAMP_CHECK_LAUNCH();
   if (ctas == 1) return STAMP_OK;
-  if (launch_pdl(k_expert_place, dim3((unsigned)ctas), dim3(ROUTE_THREADS), (size_t)(p.E + 2 * ROUTE_THREADS) * 4, st, p) != cudaSuccess) {
+  const size_t sums = (size_t)2 * ROUTE_THREADS * 16;
+  if (launch_pdl(k_expert_place, dim3((unsigned)ctas), dim3(ROUTE_THREADS), sums, st, p) != cudaSuccess) {
     cudaGetLastError();
     return STAMP_ERR_CUDA;
   }
@@ -2228,7 +2229,7 @@ int stamp_expert_route_workspace_bytes(int T, int E, int top, size_t* out_bytes)
   if (!out_bytes) return STAMP_ERR_INVALID_ARG;
   if (int rc = check_route(T, E, top)) return rc;
   const int ctas = route_ctas(T);
-  *out_bytes = ctas > 1 ? align256((size_t)ctas * E * 4) : 0;
+  *out_bytes = ctas > 1 ? align256((size_t)ctas * route_pitch(E) * 4) : 0;
   return STAMP_OK;
 }
 
@@ -2241,7 +2242,7 @@ int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, in
   if (T > 0 && (!logits || !chosen || !share || !rows || !place || !row_share)) return STAMP_ERR_INVALID_ARG;
   if (ldl > (1LL << 60) / (T > 0 ? T : 1)) return STAMP_ERR_UNSUPPORTED;
   const int ctas = route_ctas(T);
-  if (ctas > 1 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < (size_t)ctas * E * 4)) return STAMP_ERR_WORKSPACE;
+  if (ctas > 1 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < (size_t)ctas * route_pitch(E) * 4)) return STAMP_ERR_WORKSPACE;
   RouteParams p{};
   p.logits = logits;
   p.ldl = ldl;
@@ -2249,6 +2250,9 @@ int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, in
   p.E = E;
   p.top = top;
   p.normalize = normalize != 0;
+  // a lane's logits: 1, 2, 4 or 8 neighbours (launch_route)
+  const long size = l_dtype == STAMP_BF16 ? 2 : 4, lane = (E > 128 ? 8 : E > 64 ? 4 : 1) * size, word = lane < 16 ? lane : 16;
+  p.vector = reinterpret_cast<uintptr_t>(logits) % word == 0 && ldl * size % word == 0;
   p.per_cta = (T + ctas - 1) / ctas;
   p.per_warp = (p.per_cta + ROUTE_WARPS - 1) / ROUTE_WARPS;
   p.chosen = chosen;

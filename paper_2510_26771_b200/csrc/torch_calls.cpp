@@ -297,6 +297,14 @@ at::Tensor scratch(PyObject* o, size_t bytes, const at::Tensor& x) {
   return t;
 }
 
+// A contiguous tensor of this shape and type (four bytes wide) in `room`'s memory, `first` words in.
+at::Tensor part_of(const at::Tensor& room, int64_t first, at::IntArrayRef shape, at::ScalarType type) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(room.storage()), room.key_set(), c10::scalarTypeToTypeMeta(type));
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+  t.unsafeGetTensorImpl()->set_storage_offset(first);
+  return t;
+}
+
 // (logits, top, normalize, out | None) -> (chosen, share, rows, place, offsets, row_share)
 PyObject* expert_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
   STAMP_ENTRY
@@ -312,9 +320,24 @@ PyObject* expert_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   size_t bytes = 0;
   if (const int rc = stamp_expert_route_workspace_bytes(as_int(T), as_int(E), top, &bytes)) return PyLong_FromLong(rc);
-  const at::Tensor t[6] = {output(given[0], "chosen", {T, top}, at::kInt, l.t), output(given[1], "share", {T, top}, at::kFloat, l.t),
-                           output(given[2], "rows", {T * top}, at::kInt, l.t),  output(given[3], "place", {T, top}, at::kInt, l.t),
-                           output(given[4], "offsets", {E + 1}, at::kInt, l.t), output(given[5], "row_share", {T * top}, at::kFloat, l.t)};
+  // Six buffers of one allocation, with room for the counts: allocating each would take longer than the kernels do.
+  const int64_t rows = T * top, sizes[6] = {rows, rows, rows, rows, E + 1, rows};
+  const int64_t two[2] = {T, top}, one[1] = {rows}, ends[1] = {E + 1};
+  const at::IntArrayRef shapes[6] = {two, two, one, two, ends, one};
+  constexpr at::ScalarType types[6] = {at::kInt, at::kFloat, at::kInt, at::kInt, at::kInt, at::kFloat};
+  constexpr const char* names[6] = {"chosen", "share", "rows", "place", "offsets", "row_share"};
+  at::Tensor t[6], room;
+  if (a[3] == Py_None) {
+    int64_t at = 0, words = 0;
+    for (int64_t s : sizes) words += (s + 63) / 64 * 64;
+    room = at::empty({words}, l.t.options().dtype(at::kInt));
+    for (int i = 0; i < 6; ++i) {
+      t[i] = part_of(room, at, shapes[i], types[i]);
+      at += (sizes[i] + 63) / 64 * 64;
+    }
+  } else {
+    for (int i = 0; i < 6; ++i) t[i] = output(given[i], names[i], shapes[i], types[i], l.t);
+  }
   at::Tensor ws;
   if (bytes > 0) ws = scratch(Py_None, bytes, l.t);
   const int status = stamp_expert_route(l.t.data_ptr(), type, l.ld, as_int(T), as_int(E), top, a[2] == Py_True, static_cast<int32_t*>(t[0].data_ptr()),
