@@ -43,7 +43,7 @@ namespace stamp {
 constexpr int EXPERT_FEW_TOKENS = 64;
 constexpr int EXPERT_FEW_ROWS = 2048;
 constexpr int EXPERT_MAX = 1024;
-constexpr int EXPERT_MAX_STAGES = 8;
+constexpr int EXPERT_MAX_STAGES = 8, EXPERT_MAX_SPLIT = 16;
 constexpr int EXPERT_W_BYTES = 128 * 128;
 constexpr int EXPERT_MAX_SMEM = 224 * 1024;             // of a CTA that has an SM to itself; two of half of it fit one
 constexpr int EXPERT_H_BYTES = 2 * 8 * 128 * 4;         // UP: hidden values of eight rows on their way to terms, twice
@@ -78,10 +78,10 @@ struct ExpertSmem {
   static constexpr int CTAS = UP ? 1 : 2;               // of an SM that the registers allow
   static constexpr int COLUMNS = UP ? 32 : 64;          // of one sum
   static constexpr int ACC = 64;                        // tensor memory: two accumulators (UP: gates, ups), then the stages' scales
-  static constexpr int SF_COL = 2 * ACC;
+  static constexpr int SF_COL = 2 * ACC, TMEM = 256;
   static constexpr int SF_BYTES = UP ? 1536 : 1024;     // scale words of a stage: channels (UP: twice), then rows
   static constexpr int SF_COLS = SF_BYTES / 128;
-  static_assert(SF_COL + EXPERT_MAX_STAGES * SF_COLS <= 256, "half of the tensor memory: two CTAs to an SM");
+  static_assert(SF_COL + EXPERT_MAX_STAGES * SF_COLS <= TMEM && TMEM * CTAS <= 512, "tensor memory of an SM");
   static constexpr int BARS = 2 * EXPERT_MAX_STAGES + 6;
   // after the ring and the scale words: barriers, [tmem, abort, runs, -], run table, UP: hidden values, tokens [M], DOWN: sums [T][128]
   __host__ __device__ static constexpr int tables(int max_runs) { return BARS * 8 + 16 + (max_runs * 8 + 15) / 16 * 16; }
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
     if constexpr (!UP) ptx::prefetch_tensormap(&tmap_h);
   }
   if (warp == 5) {
-    ptx::tmem_alloc(tmem_slot, 256);
+    ptx::tmem_alloc(tmem_slot, SM::TMEM);
     ptx::tmem_relinquish();
   }
   if constexpr (!UP) {
@@ -599,14 +599,14 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
   if (UP ? p.split > 1 && u0 < u1 && *abort_word == 0 : runs >= 0 && *abort_word == 0) {
     // the sums of the cluster's CTAs in rank order; every CTA takes every split-th row (UP) or token (DOWN)
     const uint32_t part = ptx::smem_u32(UP ? reinterpret_cast<float*>(smem) : sums);
-    uint32_t part_of[8];
+    uint32_t part_of[EXPERT_MAX_SPLIT];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) part_of[s] = p.split > 1 ? ptx::mapa(part, static_cast<uint32_t>(min(s, p.split - 1))) : part;
+    for (int s = 0; s < EXPERT_MAX_SPLIT; ++s) part_of[s] = p.split > 1 ? ptx::mapa(part, static_cast<uint32_t>(min(s, p.split - 1))) : part;
     // four channels of one row from every CTA, four loads in flight at once
     auto total = [&](int at) {
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int s0 = 0; s0 < 8; s0 += 4) {
+      for (int s0 = 0; s0 < EXPERT_MAX_SPLIT; s0 += 4) {
         float4 v[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s)
@@ -654,7 +654,7 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
   if (p.split > 1) ptx::cluster_sync();
   if (warp == 5) {
     ptx::tc_fence_after();
-    ptx::tmem_dealloc(tmem, 256);
+    ptx::tmem_dealloc(tmem, SM::TMEM);
   }
 }
 

@@ -74,6 +74,7 @@ struct Fp8GemmParams {
   int act;                 // stamp_activation
   const void* residual;    // [M, ldr] float or bf16, or nullptr
   int r_bf16;              // residual is bf16
+  int words;               // four neighbouring channels of Y and of the residual are aligned words
   long ldr;
   uint8_t* y_scale;        // quantized output: [M, ceil(N / 128)]
 };
@@ -129,8 +130,9 @@ __device__ __forceinline__ Fp8Tile fp8_tile(const Fp8GemmParams& p, const int* t
   return t;
 }
 
-// FUSED: whether the block of 128 channels from `first` on keeps its order: it ends inside a run of 32 channels.
-__device__ __forceinline__ bool fp8_plain_order(const Fp8GemmParams& p, int first) { return (p.N & 31) != 0 && first + FP8G_BM > p.N; }
+// FUSED: whether the block of 128 channels from `first` on keeps its order: it ends inside a run of 32 channels, or four
+// channels of the output or the residual are no aligned word.
+__device__ __forceinline__ bool fp8_plain_order(const Fp8GemmParams& p, int first) { return !p.words || ((p.N & 31) != 0 && first + FP8G_BM > p.N); }
 
 // The scale bytes of `n` (1..4) consecutive blocks as one word.  Where there is none -- blocks past K, rows past the
 // run, whose columns are not stored -- any finite scale does: 1.
@@ -251,68 +253,69 @@ __device__ __forceinline__ void fp8_with_activation(int act, F&& f) {
     default: f(std::integral_constant<int, FP8_LINEAR>{}, act == STAMP_ACT_RELU ? 0.f : none);
   }
 }
-// Four neighbouring channels of one token as one word, aligned to its size.
-__device__ __forceinline__ float4 fp8_load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 fp8_load4(const __nv_bfloat16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
-}
+// Four neighbouring channels of one token, stored as one aligned word.
 __device__ __forceinline__ void fp8_store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void fp8_store4(__nv_bfloat16* p, float4 v) {
   const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
-// The same one by one, `step` elements apart, as many as there are.
-__device__ __forceinline__ float fp8_float(float v) { return v; }
-__device__ __forceinline__ float fp8_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <typename T>
-__device__ __forceinline__ float4 fp8_load_some(const T* p, int step, int count) {
-  return make_float4(count > 0 ? fp8_float(p[0]) : 0.f, count > 1 ? fp8_float(p[step]) : 0.f, count > 2 ? fp8_float(p[2 * step]) : 0.f,
-                     count > 3 ? fp8_float(p[3 * step]) : 0.f);
-}
-__device__ __forceinline__ void fp8_store_some(float* p, float4 v, int step, int count) {
-  if (count > 0) p[0] = v.x;
-  if (count > 1) p[step] = v.y;
-  if (count > 2) p[2 * step] = v.z;
-  if (count > 3) p[3 * step] = v.w;
-}
-__device__ __forceinline__ void fp8_store_some(__nv_bfloat16* p, float4 v, int step, int count) {
-  if (count > 0) p[0] = __float2bfloat16_rn(v.x);
-  if (count > 1) p[step] = __float2bfloat16_rn(v.y);
-  if (count > 2) p[2 * step] = __float2bfloat16_rn(v.z);
-  if (count > 3) p[3 * step] = __float2bfloat16_rn(v.w);
-}
-// A thread's tokens of a chunk (8 k + e from its first on) at its four channels; rows `ld` elements apart, those below `left`
-// exist.  words: the channels are neighbours and every address is aligned: straight loads, all in flight at once.
-template <typename T>
-__device__ __forceinline__ void fp8_load_tokens(const T* p, long ld, int left, bool words, int step, int have, float4 (&out)[8]) {
-  if (words && left > 25) {
-    const T* q = p + ld;
+__device__ __forceinline__ void fp8_put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void fp8_put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+// What a thread's columns are added to, as loaded: converted where it is used, so that no load waits for the one before.  A
+// thread's tokens of 8 KU columns are 8 k + e from its first on; rows are `ld` elements apart and those below `left` exist (of
+// the others the last one is loaded again; with none at all nothing is).
+template <int KU>
+__device__ __forceinline__ void fp8_load_tokens(const void* base, long at, long ld, bool bf16, int left, uint4 (&out)[2 * KU]) {
+  if (left <= 0) return;
+  const int most = left - 1;
+  if (bf16) {
+    const __nv_bfloat16* const p = static_cast<const __nv_bfloat16*>(base) + at;
 #pragma unroll
-    for (int k = 0; k < 4; ++k, p += 8 * ld, q += 8 * ld) out[2 * k] = fp8_load4(p), out[2 * k + 1] = fp8_load4(q);
+    for (int j = 0; j < 2 * KU; ++j) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p + min((j >> 1) * 8 + (j & 1), most) * ld);
+      out[j].x = u.x, out[j].y = u.y;
+    }
+  } else {
+    const float* const p = static_cast<const float*>(base) + at;
+#pragma unroll
+    for (int j = 0; j < 2 * KU; ++j) out[j] = *reinterpret_cast<const uint4*>(p + min((j >> 1) * 8 + (j & 1), most) * ld);
+  }
+}
+template <int KU>
+__device__ __forceinline__ void fp8_add_tokens(const uint4 (&raw)[2 * KU], bool bf16, float (&v)[4][2 * KU]) {
+  if (bf16) {
+#pragma unroll
+    for (int j = 0; j < 2 * KU; ++j) {
+      v[0][j] += __uint_as_float(raw[j].x << 16), v[1][j] += __uint_as_float(raw[j].x & 0xFFFF0000u);
+      v[2][j] += __uint_as_float(raw[j].y << 16), v[3][j] += __uint_as_float(raw[j].y & 0xFFFF0000u);
+    }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int tok = (j >> 1) * 8 + (j & 1);
-      out[j] = fp8_load_some(p + tok * ld, step, tok < left ? have : 0);
+    for (int j = 0; j < 2 * KU; ++j) {
+      v[0][j] += __uint_as_float(raw[j].x), v[1][j] += __uint_as_float(raw[j].y);
+      v[2][j] += __uint_as_float(raw[j].z), v[3][j] += __uint_as_float(raw[j].w);
     }
   }
 }
+template <int KU, typename T>
+__device__ __forceinline__ void fp8_store_tokens(T* p, long ld, int left, const float (&v)[4][2 * KU]) {
+  T* q = p + ld;
+#pragma unroll
+  for (int k = 0; k < KU; ++k, p += 8 * ld, q += 8 * ld) {
+    if (8 * k < left) fp8_store4(p, make_float4(v[0][2 * k], v[1][2 * k], v[2][2 * k], v[3][2 * k]));
+    if (8 * k + 1 < left) fp8_store4(q, make_float4(v[0][2 * k + 1], v[1][2 * k + 1], v[2][2 * k + 1], v[3][2 * k + 1]));
+  }
+}
+// 16 tokens at one channel, likewise; as loaded (bf16: in the upper half once it is used).
 template <typename T>
-__device__ __forceinline__ void fp8_store_tokens(T* p, long ld, int left, bool words, int step, int have, const float (&v)[4][8]) {
-  if (words && left > 25) {
-    T* q = p + ld;
+__device__ __forceinline__ void fp8_load_column(const T* p, long ld, int left, uint32_t (&out)[16]) {
+  if (left >= 16) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k, p += 8 * ld, q += 8 * ld) {
-      fp8_store4(p, make_float4(v[0][2 * k], v[1][2 * k], v[2][2 * k], v[3][2 * k]));
-      fp8_store4(q, make_float4(v[0][2 * k + 1], v[1][2 * k + 1], v[2][2 * k + 1], v[3][2 * k + 1]));
-    }
-  } else {
+    for (int j = 0; j < 16; ++j, p += ld) out[j] = *p;
+  } else if (left > 0) {
+    const int most = left - 1;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int tok = (j >> 1) * 8 + (j & 1);
-      fp8_store_some(p + tok * ld, make_float4(v[0][j], v[1][j], v[2][j], v[3][j]), step, tok < left ? have : 0);
-    }
+    for (int j = 0; j < 16; ++j) out[j] = p[min(j, most) * ld];
   }
 }
 
@@ -327,7 +330,9 @@ __device__ __forceinline__ void fp8_store_tokens(T* p, long ld, int left, bool w
 // finds most of a token's maximum in its own registers.  With the plain epilogue's shape (a lane a channel, 32 columns), the
 // exchange and the predicates of its stores made 16 instructions an output, 24 with gelu and codes: 80 us for 8192 x 1152 x
 // 4608 with gelu to codes, two thirds of it the epilogue.
-// Where the channels are no multiple of 32 the last block keeps the plain order, and its outputs are stored one by one.
+// A last block that ends inside a run of 32 channels, and all blocks where rows are not aligned, keep the plain order and shape:
+// a lane a channel, outputs one by one, 32 lanes side by side (1797 x 2688 x 4463 in fp32 with a residual 67 us with the words'
+// order and shape, whose four channels are then four stores 16 bytes apart).
 template <bool PAIR, typename TOut, bool FUSED = false>
 __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
     k_fp8_gemm(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
@@ -646,8 +651,6 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
     const int group = (warp - 4) >> 2;     // which chunks of 32 columns it takes: every G-th
     const int g4 = lane >> 2, col = 2 * (lane & 3);   // its channels; its tokens of a chunk: 8 k + col + e, k = 0..3, e = 0, 1
     const uint32_t tempty_bar0 = PAIR ? ptx::mapa(ptx::smem_u32(&tempty[0]), 0u) : 0u;
-    const bool y_words = (p.N & 3) == 0 && (reinterpret_cast<uintptr_t>(p.y) & (4 * sizeof(TOut) - 1)) == 0;
-    const bool r_words = (p.ldr & 3) == 0 && (reinterpret_cast<uintptr_t>(p.residual) & (p.r_bf16 ? 7 : 15)) == 0;
     TOut* const y = static_cast<TOut*>(p.y);
     // Hints that bring a tile's residual to L2, a tile ahead: a chunk's loads are too few to hide the way from memory.
     auto prefetch_residual = [&](int tile) {
@@ -666,16 +669,15 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
       const Fp8Tile t = fp8_tile(p, tile_start, row_start, p.E, tile, ch_tiles, tok_tiles);
       const int block = PAIR ? 2 * t.ch_tile + rank : t.ch_tile;
       const bool plain = fp8_plain_order(p, block * FP8G_BM);
-      // this thread's channels: ch, ch + step, ch + 2 step, ch + 3 step, `have` of which exist
-      const int ch = block * FP8G_BM + quarter * 32 + (plain ? g4 : 4 * g4), step = plain ? 8 : 1;
-      const int have = plain ? (ch < p.N) + (ch + 8 < p.N) + (ch + 16 < p.N) + (ch + 24 < p.N) : ch < p.N ? 4 : 0;
-      const bool all = !plain && have == 4;
+      // this thread's channels: four from ch on, or, in plain order, ch alone
+      const int ch = block * FP8G_BM + quarter * 32 + (plain ? lane : 4 * g4);
+      const bool have = ch < p.N;   // (all four or none)
       float bias[4] = {0.f, 0.f, 0.f, 0.f};
       if (p.bias) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) bias[c] = __ldg(p.bias + min(ch + c * step, p.N - 1));
+        for (int c = 0; c < 4; ++c) bias[c] = __ldg(p.bias + min(ch + c, p.N - 1));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) bias[c] = c < have ? bias[c] : 0.f;
+        for (int c = 0; c < 4; ++c) bias[c] = have ? bias[c] : 0.f;
       }
       for (int c0 = step0; c0 < step1; c0 += p.chunk, ++it) {
         const int a = it & 1;
@@ -687,29 +689,7 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
         const bool add = sizeof(TOut) != 1 && p.residual && whole && (p.act == STAMP_ACT_NONE ? first : last);
         const int chunks = (t.n + 31) / 32, count = (chunks - group + G - 1) / G;
         auto chunk_at = [&](int i) { return group + G * (PAIR && a == 0 ? count - 1 - i : i); };
-        // What a chunk adds to is loaded ahead: for the first chunk before the sums are waited for, then a chunk ahead.  Plain
-        // loads: every element is read by the thread that writes it.
-        float4 res[sizeof(TOut) == 1 ? 1 : 8], before[sizeof(TOut) == 4 ? 8 : 1];
-        auto fetch = [&](int c) {
-          const int tok = 32 * c + col, there = have > 0 ? t.rows - tok : 0;
-          if constexpr (sizeof(TOut) != 1) {
-            const long at = (t.row0 + static_cast<long>(tok)) * p.ldr + ch;
-            if (add) {
-              if (p.r_bf16) fp8_load_tokens(static_cast<const __nv_bfloat16*>(p.residual) + at, p.ldr, there, r_words && all, step, have, res);
-              else fp8_load_tokens(static_cast<const float*>(p.residual) + at, p.ldr, there, r_words && all, step, have, res);
-            }
-          }
-          if constexpr (sizeof(TOut) == 4) {
-            if (!first) fp8_load_tokens(y + (t.row0 + static_cast<long>(tok)) * p.N + ch, p.N, there, y_words && all, step, have, before);
-          }
-        };
         if (first) prefetch_residual(tile + tile_step);
-        if (count > 0) fetch(chunk_at(0));
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
-          ok = false;
-          break;
-        }
-        ptx::tc_fence_after();
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(a * SM::ACC1);
         bool released = false;
         auto release = [&]() {
@@ -720,19 +700,172 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
           }
           released = true;
         };
-        // PAIR: the chunk that overlaps the other accumulator first; who has none of it hands back at once
-        if (PAIR && group != fp8_overlap_group(a)) release();
+        // Waits for the sums.  PAIR: the chunk that overlaps the other accumulator is drained first; who has none of it hands back
+        // at once.
+        auto begin = [&]() {
+          if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded_sleepy(&tfull[a], (it >> 1) & 1, abort_word, FP8G_WAIT_LIMIT))) {
+            ok = false;
+            return false;
+          }
+          ptx::tc_fence_after();
+          if (PAIR && group != fp8_overlap_group(a)) release();
+          return true;
+        };
+        // The largest magnitudes of a chunk's tokens over this warp's channels, one a lane, to those over the block's four warps:
+        // scales to memory, inverse scales to this warp's shared memory.  False: the others have given up.
+        auto exchange = [&](int tok, int mine, uint32_t amax) {
+          uint8_t* const ex = smem + SM::EX_OFFSET;
+          uint64_t* const bar = reinterpret_cast<uint64_t*>(ex) + group;
+          uint32_t* const maxima = reinterpret_cast<uint32_t*>(ex + 8 * G) + (group * 2 + static_cast<int>(exchanged & 1u)) * 128;
+          float* const inverse = reinterpret_cast<float*>(ex + 8 * G) + G * 256 + (warp - 4) * 32;
+          maxima[quarter * 32 + mine] = amax;
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar);
+          if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar, exchanged & 1u, abort_word, FP8G_WAIT_LIMIT))) ok = false;
+          ++exchanged;
+          amax = 0;   // bits of magnitudes order like integers, NaNs above infinity
+#pragma unroll
+          for (int q = 0; q < 4; ++q) amax = max(amax, maxima[q * 32 + mine]);
+          const Fp8Scale s = fp8_scale(amax);
+          const int ks_out = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
+          if (ok && quarter == 0 && tok + mine < t.rows && block < ks_out) p.y_scale[(t.row0 + static_cast<long>(tok + mine)) * ks_out + block] = s.byte;
+          __syncwarp();   // (everyone has read the chunk's before)
+          inverse[mine] = s.inverse;
+          __syncwarp();
+          return static_cast<const float*>(inverse);
+        };
+        const int act = last && whole ? p.act : STAMP_ACT_NONE;
+        if (plain) {
+          // A lane a channel, 16 tokens at a time (codes: all 32 of a chunk, for their maxima), what they are added to loaded one
+          // step ahead.
+          constexpr int W = sizeof(TOut) == 1 ? 32 : 16, STEPS = 32 / W;
+          auto column_of = [&](int n) { return 32 * chunk_at(n / STEPS) + W * (n % STEPS); };
+          uint32_t more[sizeof(TOut) == 1 ? 1 : 16], old[sizeof(TOut) == 4 ? 16 : 1];
+          auto fetch = [&](int tok) {
+            const int left = have ? t.rows - tok : 0;
+            if constexpr (sizeof(TOut) != 1) {
+              const long at = (t.row0 + static_cast<long>(tok)) * p.ldr + ch;
+              if (add) {
+                if (p.r_bf16) fp8_load_column(static_cast<const uint16_t*>(p.residual) + at, p.ldr, left, more);
+                else fp8_load_column(static_cast<const uint32_t*>(p.residual) + at, p.ldr, left, more);
+              }
+            }
+            if constexpr (sizeof(TOut) == 4) {
+              if (!first) fp8_load_column(reinterpret_cast<const uint32_t*>(y) + (t.row0 + static_cast<long>(tok)) * p.N + ch, p.N, left, old);
+            }
+          };
+          if (count > 0) fetch(column_of(0));
+          auto drain = [&](auto variant, float floor) {
+            for (int n = 0; n < count * STEPS; ++n) {
+              const int tok = column_of(n), left = have ? t.rows - tok : 0;
+              const bool last_of = n + 1 == (PAIR ? STEPS : count * STEPS);
+              if (STEPS > 1 && tok >= t.rows) {   // (no such tokens, for anyone)
+                if (!released && last_of) release();
+                if (n + 1 < count * STEPS) fetch(column_of(n + 1));
+                continue;
+              }
+              uint32_t r[W];
+              float v[W];
+              if constexpr (W == 32) ptx::tmem_ld_32x32b_x32(taddr + tok, r); else ptx::tmem_ld_32x32b_x16(taddr + tok, r);
+              ptx::tmem_ld_wait();
+              if (!released && last_of) release();
+#pragma unroll
+              for (int j = 0; j < W; ++j) v[j] = __uint_as_float(r[j]);
+              if (!whole) {
+                float* const part = reinterpret_cast<float*>(smem) + tok * FP8G_PART + (ch - block * FP8G_BM);
+#pragma unroll
+                for (int j = 0; j < W; ++j) part[j * FP8G_PART] = v[j];
+                continue;
+              }
+              if constexpr (sizeof(TOut) == 4) {
+                if (!first) {
+#pragma unroll
+                  for (int j = 0; j < W; ++j) v[j] += __uint_as_float(old[j]);
+                }
+              }
+#pragma unroll
+              for (int j = 0; j < W; j += 2) {
+                float2 x = make_float2(v[j], v[j + 1]);
+                if (sizeof(TOut) != 4 || first) x = __fadd2_rn(x, make_float2(bias[0], bias[0]));
+                x = fp8_activate2<decltype(variant)::value>(x, floor);
+                v[j] = x.x;
+                v[j + 1] = x.y;
+              }
+              if constexpr (sizeof(TOut) != 1) {
+                if (add) {
+                  const int shift = p.r_bf16 ? 16 : 0;
+#pragma unroll
+                  for (int j = 0; j < W; ++j) v[j] += __uint_as_float(more[j] << shift);
+                }
+                if (n + 1 < count * STEPS) fetch(column_of(n + 1));
+                TOut* out = y + (t.row0 + static_cast<long>(tok)) * p.N + ch;
+                if (left >= W) {
+#pragma unroll
+                  for (int j = 0; j < W; ++j, out += p.N) fp8_put(out, v[j]);
+                } else {
+#pragma unroll
+                  for (int j = 0; j < W; ++j, out += p.N)
+                    if (j < left) fp8_put(out, v[j]);
+                }
+              } else {
+                uint32_t amax = 0;   // (channels that do not exist are zeros)
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                  const uint32_t m = __float_as_uint(ptx::warp_max_abs(v[j]));
+                  if (lane == j) amax = m;
+                }
+                const float* const inverse = exchange(tok, lane, amax);
+                if (!ok) return;
+                uint8_t* out = static_cast<uint8_t*>(p.y) + (t.row0 + static_cast<long>(tok)) * p.N + ch;
+#pragma unroll
+                for (int j = 0; j < W; j += 4, out += 4L * p.N) {
+                  const uint32_t codes = ptx::cvt_e4m3x4(v[j] * inverse[j], v[j + 1] * inverse[j + 1], v[j + 2] * inverse[j + 2], v[j + 3] * inverse[j + 3]);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+                    if (j + k < left) out[static_cast<long>(k) * p.N] = static_cast<uint8_t>(codes >> (8 * k));
+                }
+              }
+            }
+          };
+          if (begin()) fp8_with_activation(act, drain);
+          if (!released) release();
+          if (!ok) break;
+          continue;
+        }
+        // KU times eight columns at a time: codes all 32 of a chunk, for the tokens' maxima; bf16 pairs too, to have more loads in
+        // flight; single CTAs, which often have few rows, and fp32, which has more to hold, 16.
+        constexpr int KU = sizeof(TOut) == 1 || (PAIR && sizeof(TOut) == 2) ? 4 : 2, UNITS = 4 / KU;
+        auto column_of = [&](int n) { return 32 * chunk_at(n / UNITS) + 8 * KU * (n % UNITS); };
+        // What the columns add to is loaded ahead: for the first ones before the sums are waited for, then one step ahead.  Plain
+        // loads: every element is read by the thread that writes it.
+        uint4 res[sizeof(TOut) == 1 ? 1 : 2 * KU], before[sizeof(TOut) == 4 ? 2 * KU : 1];
+        auto fetch = [&](int c) {
+          const int tok = c + col, there = have ? t.rows - tok : 0;
+          if constexpr (sizeof(TOut) != 1) {
+            if (add) fp8_load_tokens<KU>(p.residual, (t.row0 + static_cast<long>(tok)) * p.ldr + ch, p.ldr, p.r_bf16, there, res);
+          }
+          if constexpr (sizeof(TOut) == 4) {
+            if (!first) fp8_load_tokens<KU>(y, (t.row0 + static_cast<long>(tok)) * p.N + ch, p.N, false, there, before);
+          }
+        };
+        if (count > 0) fetch(column_of(0));
         auto drain = [&](auto variant, float floor) {
-          for (int i = 0; i < count; ++i) {
-            const int c = chunk_at(i), left = have > 0 ? t.rows - 32 * c - col : 0;   // tokens 8 k + e below `left` are stored
-            float v[4][8];
+          for (int n = 0; n < count * UNITS; ++n) {
+            const int c = column_of(n), left = have ? t.rows - c - col : 0;   // tokens 8 k + e below `left` are stored
+            const bool last_of = n + 1 == (PAIR ? UNITS : count * UNITS);
+            if (UNITS > 1 && c >= t.rows) {   // (no such tokens, for anyone)
+              if (!released && last_of) release();
+              if (n + 1 < count * UNITS) fetch(column_of(n + 1));
+              continue;
+            }
+            float v[4][2 * KU];
             {
-              uint32_t lo[16], hi[16];
-              ptx::tmem_ld_16x256b_x4(taddr + 32 * c, lo);
-              ptx::tmem_ld_16x256b_x4(taddr + 32 * c + (16u << 16), hi);
+              uint32_t lo[4 * KU], hi[4 * KU];
+              ptx::tmem_ld_16x256b<KU>(taddr + c, lo);
+              ptx::tmem_ld_16x256b<KU>(taddr + c + (16u << 16), hi);
               ptx::tmem_ld_wait();
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
+              for (int k = 0; k < KU; ++k)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                   v[0][2 * k + e] = __uint_as_float(lo[4 * k + e]);
@@ -741,24 +874,21 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
                   v[3][2 * k + e] = __uint_as_float(hi[4 * k + 2 + e]);
                 }
             }
-            if (!released && (PAIR || i + 1 == count)) release();
+            if (!released && last_of) release();
             if (!whole) {
               // this CTA's part of the sum, [token][channel], in the ring that nothing uses any more
-              float* const part = reinterpret_cast<float*>(smem) + (32 * c + col) * FP8G_PART + (ch - block * FP8G_BM);
-              fp8_store_tokens(part, FP8G_PART, 32, !plain, step, 4, v);
+              float* const part = reinterpret_cast<float*>(smem) + (c + col) * FP8G_PART + (ch - block * FP8G_BM);
+              fp8_store_tokens<KU>(part, FP8G_PART, 8 * KU, v);
               continue;
             }
             if constexpr (sizeof(TOut) == 4) {
-              if (!first) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[0][j] += before[j].x, v[1][j] += before[j].y, v[2][j] += before[j].z, v[3][j] += before[j].w;
-              }
+              if (!first) fp8_add_tokens<KU>(before, false, v);
             }
             // (a part that is not the first has its bias already, one that is not the last gets no activation: LINEAR, floor -inf)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-              for (int j = 0; j < 8; j += 2) {
+              for (int j = 0; j < 2 * KU; j += 2) {
                 float2 r = make_float2(v[k][j], v[k][j + 1]);
                 if (sizeof(TOut) != 4 || first) r = __fadd2_rn(r, make_float2(bias[k], bias[k]));
                 r = fp8_activate2<decltype(variant)::value>(r, floor);
@@ -766,12 +896,9 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
                 v[k][j + 1] = r.y;
               }
             if constexpr (sizeof(TOut) != 1) {
-              if (add) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[0][j] += res[j].x, v[1][j] += res[j].y, v[2][j] += res[j].z, v[3][j] += res[j].w;
-              }
-              if (i + 1 < count) fetch(chunk_at(i + 1));
-              fp8_store_tokens(y + (t.row0 + 32L * c + col) * p.N + ch, p.N, left, y_words && all, step, have, v);
+              if (add) fp8_add_tokens<KU>(res, p.r_bf16, v);
+              if (n + 1 < count * UNITS) fetch(column_of(n + 1));
+              fp8_store_tokens<KU>(y + (t.row0 + static_cast<long>(c + col)) * p.N + ch, p.N, left, v);
             } else {
               // the largest magnitude of every token: over this thread's channels, the lanes that have the same tokens (each
               // step halves the tokens a lane looks after: lane -> one token), and the block's four warps
@@ -779,35 +906,17 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
 #pragma unroll
               for (int j = 0; j < 8; ++j) m[j] = __float_as_uint(ptx::max_abs_nan(ptx::max_abs_nan(v[0][j], v[1][j], v[2][j]), v[3][j], 0.f));
 #pragma unroll
-              for (int d = 16, n = 4; d >= 4; d >>= 1, n >>= 1) {
+              for (int d = 16, half = 4; d >= 4; d >>= 1, half >>= 1) {
                 const bool upper = (lane & d) != 0;
 #pragma unroll
-                for (int j = 0; j < n; ++j) {
-                  const uint32_t other = __shfl_xor_sync(0xffffffffu, upper ? m[j] : m[j + n], d);
-                  m[j] = max(upper ? m[j + n] : m[j], other);
+                for (int j = 0; j < half; ++j) {
+                  const uint32_t other = __shfl_xor_sync(0xffffffffu, upper ? m[j] : m[j + half], d);
+                  m[j] = max(upper ? m[j + half] : m[j], other);
                 }
               }
               const int mine = ((lane >> 3) & 3) * 8 + col + ((lane >> 2) & 1);   // the token that is left
-              uint8_t* const ex = smem + SM::EX_OFFSET;
-              uint64_t* const bar = reinterpret_cast<uint64_t*>(ex) + group;
-              uint32_t* const maxima = reinterpret_cast<uint32_t*>(ex + 8 * G) + (group * 2 + static_cast<int>(exchanged & 1u)) * 128;
-              float* const inverse = reinterpret_cast<float*>(ex + 8 * G) + G * 256 + (warp - 4) * 32;
-              maxima[quarter * 32 + mine] = m[0];
-              __syncwarp();
-              if (lane == 0) ptx::mbar_arrive(bar);
-              if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar, exchanged & 1u, abort_word, FP8G_WAIT_LIMIT))) {
-                ok = false;
-                break;
-              }
-              ++exchanged;
-              uint32_t amax = 0;   // bits of magnitudes order like integers, NaNs above infinity
-#pragma unroll
-              for (int q = 0; q < 4; ++q) amax = max(amax, maxima[q * 32 + mine]);
-              const Fp8Scale s = fp8_scale(amax);
-              const int ks_out = (p.N + FP8_BLOCK - 1) / FP8_BLOCK;
-              if (quarter == 0 && 32 * c + mine < t.rows && block < ks_out) p.y_scale[(t.row0 + 32L * c + mine) * ks_out + block] = s.byte;
-              inverse[mine] = s.inverse;
-              __syncwarp();
+              const float* const inverse = exchange(c, mine, m[0]);
+              if (!ok) return;
               uint32_t codes[8];
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
@@ -817,27 +926,17 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
                 codes[2 * k] = ptx::cvt_e4m3x4(a01.x, b01.x, c01.x, d01.x);
                 codes[2 * k + 1] = ptx::cvt_e4m3x4(a01.y, b01.y, c01.y, d01.y);
               }
-              uint8_t* out = static_cast<uint8_t*>(p.y) + (t.row0 + 32L * c + col) * p.N + ch;
-              if (all && left > 25) {
-                uint8_t* next = out + p.N;
+              uint8_t* out = static_cast<uint8_t*>(p.y) + (t.row0 + static_cast<long>(c + col)) * p.N + ch;
+              uint8_t* next = out + p.N;
 #pragma unroll
-                for (int k = 0; k < 4; ++k, out += 8L * p.N, next += 8L * p.N) {
-                  *reinterpret_cast<uint32_t*>(out) = codes[2 * k];
-                  *reinterpret_cast<uint32_t*>(next) = codes[2 * k + 1];
-                }
-              } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                  for (int i4 = 0; i4 < 4; ++i4)
-                    if ((j >> 1) * 8 + (j & 1) < left && i4 < have)
-                      out[static_cast<long>((j >> 1) * 8 + (j & 1)) * p.N + i4 * step] = static_cast<uint8_t>(codes[j] >> (8 * i4));
+              for (int k = 0; k < 4; ++k, out += 8L * p.N, next += 8L * p.N) {
+                if (8 * k < left) *reinterpret_cast<uint32_t*>(out) = codes[2 * k];
+                if (8 * k + 1 < left) *reinterpret_cast<uint32_t*>(next) = codes[2 * k + 1];
               }
-              __syncwarp();   // (the next chunk's inverse scales go to the same place)
             }
           }
         };
-        fp8_with_activation(last && whole ? p.act : STAMP_ACT_NONE, drain);
+        if (begin()) fp8_with_activation(act, drain);
         if (!released) release();
         if (!ok) break;
       }
@@ -1004,11 +1103,11 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
             if (ch < p.N)
               *reinterpret_cast<uint32_t*>(out) = ptx::cvt_e4m3x4(v[0] * s.inverse, v[1] * s.inverse, v[2] * s.inverse, v[3] * s.inverse);
           } else {
-            if (p.residual && ch < p.N) {
+            if (p.residual) {
               const long at = (t.row0 + static_cast<long>(tok)) * p.ldr + ch;
-              const float4 r = p.r_bf16 ? fp8_load_some(static_cast<const __nv_bfloat16*>(p.residual) + at, 1, p.N - ch)
-                                        : fp8_load_some(static_cast<const float*>(p.residual) + at, 1, p.N - ch);
-              v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (ch + i < p.N) v[i] += p.r_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.residual)[at + i]) : static_cast<const float*>(p.residual)[at + i];
             }
             if (ch < p.N) fp8_store2(out, v[0], v[1], ch + 1 < p.N, vec);
             if (ch + 2 < p.N) fp8_store2(out + 2, v[2], v[3], ch + 3 < p.N, vec);

@@ -1561,6 +1561,9 @@ static int launch_expert(ExpertParams p, long ctas, int smem, cudaStream_t st) {
   using SM = ExpertSmem<UP>;
   auto kern = k_expert_layer<UP, TOut>;
   if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), EXPERT_MAX_SMEM)) return rc;
+  // (clusters of 16, which DOWN takes, are not portable; B200 has them)
+  if (!UP && p.split > 8)
+    if (int rc = ensure_large_clusters(reinterpret_cast<const void*>(kern))) return rc;
   const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T, p.M);
   p.stage_bytes = (UP ? 2 : 1) * EXPERT_W_BYTES + (p.terms * p.cap + 15) / 16 * 16 * 128;
   p.stages = (smem - fixed) / (p.stage_bytes + SM::SF_BYTES);
@@ -1616,10 +1619,15 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
   p.terms = p.h_terms;
   p.cap = cap(ExpertSmem<false>::COLUMNS);
   const long tiles = (p.N + 127L) / 128;
-  // As many CTAs as SMs, or half of that at least.  With 4 / 8 to a tile, in us: 32 tiles, 13 tokens of 32 large experts (153) /
-  // 157, one token of two experts of 4096 x 4096 (27.3) / 30.6; 16 tiles, 64 tokens over 64 experts 191 / (149).
+  // As many CTAs as SMs, twice as many where each still has enough to do, sixteen to a tile where there are few tiles and enough
+  // to do.  With 4 / 8 / 16 to a tile, in us (the choice in brackets): 32 tiles, 13 tokens over 32 experts of 4096 x 4096 161.8 /
+  // (159.0) / 172.5, one token of two such experts (27.3) / 30.6; 28 tiles, 36 tokens over 60 experts of 656 43.2 / (38.5), one
+  // token of eight of 640 (21.3) / 23.8 / 33.8; 16 tiles, 64 tokens over 64 of 2048 191 / (149) / 168; 7 tiles, 55 tokens over 8 of
+  // 3456 - / 56.7 / (48.2), 5 tokens of four of 1856 33.0 / 27.5 / (26.0); 6 tiles, 3 tokens over 8 of 384 14.0 / (13.2) / 15.0.
+  const long steps = (long)(p.E < p.M ? p.E : p.M) * ((p.F + 127) / 128);   // (run, 128 features) of a tile, about
   p.split = 1;
-  while (p.split < 8 && tiles * p.split * 2 <= sms) p.split *= 2;
+  while (p.split < 8 && (tiles * p.split * 2 <= sms || (tiles * p.split * 2 <= 2 * sms && steps >= 16L * p.split * 2))) p.split *= 2;
+  if (p.split == 8 && tiles <= 7 && steps >= 16L * 8) p.split = 16;
   // (two CTAs to an SM: with more than half of its shared memory a cluster of eight finds its SMs too late)
   return y_dtype == STAMP_BF16 ? launch_expert<false, __nv_bfloat16>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st)
                                : launch_expert<false, float>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st);
@@ -2209,6 +2217,8 @@ int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, co
   p.residual = residual;
   p.r_bf16 = r_dtype == STAMP_BF16;
   p.ldr = ldr;
+  auto words = [](const void* q, int dtype) { return (reinterpret_cast<uintptr_t>(q) & (dtype == STAMP_BF16 ? 7 : 15)) == 0; };
+  p.words = N % 4 == 0 && words(Y, y_dtype) && (!residual || (ldr % 4 == 0 && words(residual, r_dtype)));
   return M == 0 ? STAMP_OK : run_fp8_gemm<true>(p, y_dtype, static_cast<cudaStream_t>(stream));
 }
 
@@ -2221,6 +2231,7 @@ int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w
   if (N % 16 != 0) return STAMP_ERR_UNSUPPORTED;
   if (M > 0 && (!scale || !aligned16(codes))) return STAMP_ERR_INVALID_ARG;
   p.act = activation;
+  p.words = 1;
   p.y_scale = static_cast<uint8_t*>(scale);
   return M == 0 ? STAMP_OK : run_fp8_gemm<true>(p, FP8_OUT_CODES, static_cast<cudaStream_t>(stream));
 }
