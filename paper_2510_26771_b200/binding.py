@@ -339,6 +339,13 @@ def stamp_expert_combine(y: torch.Tensor, place: torch.Tensor, share: torch.Tens
     return _outputs((_calls or calls()).expert_combine(y, place, share, residual, out_dtype, out), "stamp_expert_combine")
 
 
+def stamp_fp8_expert_workspace_bytes(rows: int, hidden: int) -> int:
+    """Bytes of scratch stamp_fp8_expert_layer takes for so many rows of so many hidden channels (its argument ws)."""
+    out = ctypes.c_size_t(0)
+    _check(lib().stamp_fp8_expert_workspace_bytes(rows, hidden, ctypes.byref(out)), "stamp_fp8_expert_workspace_bytes")
+    return int(out.value)
+
+
 def stamp_fp8_expert_layer(x: torch.Tensor, rows: torch.Tensor, row_share: torch.Tensor, offsets: torch.Tensor, up: torch.Tensor,
                            up_scale: torch.Tensor, down: torch.Tensor, down_scale: torch.Tensor,
                            up_bias: Optional[torch.Tensor] = None, down_bias: Optional[torch.Tensor] = None,

@@ -321,6 +321,23 @@ static int ensure_dyn_smem(const void* func, size_t bytes) {
   return STAMP_OK;
 }
 
+// Let `func` be launched in clusters of more than eight CTAs on the current device.
+static int ensure_large_clusters(const void* func) {
+  static std::unordered_map<unsigned long long, bool> granted;   // (device, function)
+  const int dev = current_device();
+  if (dev < 0) return STAMP_ERR_CUDA;
+  const unsigned long long key = (static_cast<unsigned long long>(dev) << 56) ^ reinterpret_cast<uintptr_t>(func);
+  std::lock_guard<std::mutex> lock(g_dev_mu);
+  if (!granted[key]) {
+    if (cudaFuncSetAttribute(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+      cudaGetLastError();
+      return STAMP_ERR_CUDA;
+    }
+    granted[key] = true;
+  }
+  return STAMP_OK;
+}
+
 // ------------------------------------------------------------------------------------------
 // Launchers
 // ------------------------------------------------------------------------------------------

@@ -303,7 +303,7 @@ def test_results_repeat_on_other_streams_and_with_given_scratch(st, T):  # noqa:
     rows, share, offsets = routing([1, 0, min(T, 9), 1, T, 0, 1, 1], T, seed=5)
     x = tokens(T, 512, "bfloat16")
     first = layer(st, x, rows, share, offsets, out_dtype=torch.float32)
-    ws = torch.full((len(rows) * 512 * 4 + 256,), 0xFF, dtype=torch.uint8, device="cuda")     # (NaN to begin with)
+    ws = torch.full((st.stamp_fp8_expert_workspace_bytes(len(rows), 512),), 0xFF, dtype=torch.uint8, device="cuda")     # (NaN to begin with)
     streams = [torch.cuda.Stream() for _ in range(2)]
     again = []
     for s in streams:
