@@ -2,10 +2,12 @@
 
     python examples/fp8_expert_layer.py [--tokens 2048] [--features 1152] [--hidden 2048] [--experts 16] [--top 4] [--steps 8]
 
-Each token goes to `top` of the experts; an expert is a gated layer, down(silu(gate(x)) * up(x)).  Per call: the router
-(torch), then four kernels -- the tokens are quantized in expert order (the dispatch), multiplied with their expert's
-gate and up weights, activated and quantized again, multiplied with its down weights -- and each token's rows are weighted
-and summed (torch).  Weights are random.  The printed error compares with the layer on the unquantized weights in fp32.
+Each token goes to `top` of the experts; an expert is a gated layer, down(silu(gate(x)) * up(x)).  A prompt: the router's
+logits (torch), the choice and the rows in expert order, then four kernels -- the tokens are quantized in expert order (the
+dispatch), multiplied with their expert's gate and up weights, activated and quantized again, multiplied with its down
+weights -- and each token's rows are weighted and summed.  A decode step of up to 64 tokens: logits, choice, and one call for
+all that follows, on activations that stay as they are.  Weights are random.  The printed errors compare with the layer on
+the unquantized weights in fp32.
 """
 import argparse
 import os
@@ -31,12 +33,8 @@ class ExpertLayer:
 
     def route(self, x: torch.Tensor):
         """For every row in expert order its token, where each (token, choice) went, every expert's first row, the weights."""
-        share, chosen = torch.softmax(x.float() @ self.router, dim=1).topk(self.top, dim=1)
-        chosen, order = torch.sort(chosen.reshape(-1), stable=True)
-        offsets = torch.searchsorted(chosen, torch.arange(self.experts + 1, device=x.device)).to(torch.int32)
-        place = torch.empty_like(order)
-        place[order] = torch.arange(order.numel(), device=x.device)
-        return (order // self.top).to(torch.int32), place, offsets, share / share.sum(dim=1, keepdim=True)
+        _, share, rows, place, offsets, _ = st.stamp_expert_route(x.float() @ self.router, self.top)
+        return rows, place, offsets, share
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
         rows, place, offsets, share = self.route(x)
@@ -44,7 +42,12 @@ class ExpertLayer:
         h = st.stamp_fp8_linear_grouped(codes, scale, offsets, self.up_codes, self.up_scale)
         codes, scale = st.stamp_fp8_gated_quantize(h)
         y = st.stamp_fp8_linear_grouped(codes, scale, offsets, self.down_codes, self.down_scale, out_dtype=torch.float32)
-        return (y[place].view(x.shape[0], self.top, -1) * share[:, :, None]).sum(dim=1).to(x.dtype)
+        return st.stamp_expert_combine(y, place, share, out_dtype=x.dtype)
+
+    def decode(self, x: torch.Tensor, residual=None) -> torch.Tensor:
+        """Up to 64 tokens, plus what goes round the layer."""
+        _, _, rows, _, offsets, row_share = st.stamp_expert_route(x.float() @ self.router, self.top)
+        return st.stamp_fp8_expert_layer(x, rows, row_share, offsets, self.up_codes, self.up_scale, self.down_codes, self.down_scale, residual=residual)
 
     def unquantized(self, x: torch.Tensor) -> torch.Tensor:
         rows, place, offsets, share = self.route(x)
@@ -70,7 +73,7 @@ def main(argv=None) -> dict:
     result = {"prompt_error": relative_error(layer(prompt), layer.unquantized(prompt)), "step_errors": []}
     for _ in range(a.steps):
         token = torch.randn(1, a.features, generator=g, device="cuda").bfloat16()
-        result["step_errors"].append(relative_error(layer(token), layer.unquantized(token)))
+        result["step_errors"].append(relative_error(layer.decode(token), layer.unquantized(token)))
     if st.stamp_last_device_status() != 0:
         raise RuntimeError("device status word raised")
     print(f"prompt of {a.tokens} tokens: relative error {result['prompt_error']:.4f}; "

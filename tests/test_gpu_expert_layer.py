@@ -119,6 +119,7 @@ CASES = {
     "many rows for each": (64, [64, 40, 33, 17, 16, 15], 384, 640, 384),
     "more rows than tokens": (7, [20, 50, 3], 128, 128, 128),
     "many experts": (16, [1, 0, 0, 2] * 40, 128, 144, 136),
+    "few features, many hidden channels": (9, [3, 0, 4, 1, 2], 256, 4096, 520),
     "no rows": (4, [0, 0, 0], 128, 128, 128),
 }
 
@@ -357,6 +358,26 @@ def test_a_decode_step_from_the_logits_on(st):  # noqa: F811
     a, b, r = (t.double().cpu().numpy() for t in (outs[0], outs[1], x))
     assert np.linalg.norm(a - b) <= 0.08 * np.linalg.norm(b - r)
     assert st.stamp_last_device_status() == 0
+
+
+def test_the_example_decodes(st):  # noqa: F811
+    """The example's step of a few tokens against the definition of the layer on its quantized weights."""
+    import importlib.util
+    import os
+
+    import torch
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "fp8_expert_layer.py")
+    spec = importlib.util.spec_from_file_location("fp8_expert_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    layer = example.ExpertLayer(272, 384, 6, 2)
+    x, residual = tokens(7, 272, "bfloat16"), tokens(7, 272, "bfloat16", seed=4)
+    y = layer.decode(x, residual)
+    rows, place, offsets, share = (t.cpu().numpy() for t in layer.route(x))
+    row_share = np.empty(14, dtype=np.float32)
+    row_share[place.reshape(-1)] = share.reshape(-1)
+    up, down = (values(c, s, True) for c, s in ((layer.up_codes, layer.up_scale), (layer.down_codes, layer.down_scale)))
+    check(y, *plain_layer(x.double().cpu().numpy(), rows, row_share, offsets, up, down, None, None, residual.double().cpu().numpy(), 7, 2.0 ** -20, 2.0 ** -13))
 
 
 def test_arguments_are_checked(st):  # noqa: F811
