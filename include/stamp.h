@@ -313,7 +313,8 @@ int stamp_fp8_linear_grouped(const void* x, const void* x_scale, const int32_t* 
 /* The product with what follows it in the same kernel:  Y = act(x W^T + bias) + residual, all in fp32, rounded once to the
  * output type.  Operands and sums as in stamp_fp8_linear.
  *   activation  stamp_activation.  GELU is v * Phi(v); GELU_TANH v * (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2;
- *               SILU v / (1 + exp(-v)).  A NaN stays one under all of them                                          in
+ *               SILU v / (1 + exp(-v)).  A NaN stays one under all of them, and what an infinite sum gives is that formula's
+ *               limit or a NaN                                                                              in
  *   residual    [M, N] r_dtype, rows ldr elements apart (ldr >= N), or NULL.  It may be Y itself (same type, ldr = N), which is
  *               then updated in place -- but not where an fp32 Y of more than 4096 features K has an activation
  *               (STAMP_ERR_INVALID_ARG); any other overlap with Y is refused likewise                               in */
@@ -323,7 +324,7 @@ int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, co
 
 /* The same, quantized without being stored: codes [M, N] e4m3 and scale [M, ceil(N / 128)] e8m0 of act(x W^T + bias), as
  * stamp_fp8_quantize would write them for the fp32 values -- the operand of the next product.  N is a multiple of 16; codes
- * start on a 16-byte boundary.  The sum is taken in one accumulator (2e-6 at 14336 features): a code differs from that of the
+ * start on a 16-byte boundary and do not overlap x.  The sum is taken in one accumulator (2e-6 at 14336 features): a code differs from that of the
  * exact sum only where its value lies that near a rounding boundary. */
 int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
                                int M, int N, int K, void* codes, void* scale, void* stream);
@@ -352,7 +353,7 @@ int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, in
  *   y        [M, N] y_dtype; place [T, top] int32; share [T, top] float                                             in
  *            A place outside [0, M) adds nothing and is reported by stamp_last_device_status() as STAMP_ERR_INVALID_ARG.
  *   residual [T, N] r_dtype, rows ldr elements apart, or NULL; it may be out itself (same type, ldr = N)            in
- *   out      [T, N] o_dtype                                                                                         out */
+ *   out      [T, N] o_dtype; it may not overlap y (STAMP_ERR_INVALID_ARG)                                           out */
 int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const float* share, const void* residual, int r_dtype,
                          long long ldr, int T, int top, int M, int N, void* out, int o_dtype, void* stream);
 

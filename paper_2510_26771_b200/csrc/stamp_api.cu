@@ -1512,6 +1512,10 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
 }
 
 // A residual [M, N] with rows ldr elements apart: aligned to its type, and apart from Y or Y itself.
+static bool overlap(const void* a, long a_bytes, const void* b, long b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
+}
 static int check_residual(const void* residual, int r_dtype, long long ldr, long M, long N, const void* Y, int y_dtype) {
   if (!dtype_ok(r_dtype) || ldr < N) return STAMP_ERR_INVALID_ARG;
   if (M == 0) return STAMP_OK;
@@ -1520,8 +1524,7 @@ static int check_residual(const void* residual, int r_dtype, long long ldr, long
   const uintptr_t r = reinterpret_cast<uintptr_t>(residual), y = reinterpret_cast<uintptr_t>(Y);
   if (r % size != 0) return STAMP_ERR_INVALID_ARG;
   if (r == y && r_dtype == y_dtype && (ldr == N || M == 1)) return STAMP_OK;
-  const uintptr_t r_end = r + ((M - 1) * ldr + N) * size, y_end = y + M * N * (y_dtype == STAMP_BF16 ? 2 : 4);
-  return r < y_end && y < r_end ? STAMP_ERR_INVALID_ARG : STAMP_OK;
+  return overlap(residual, ((M - 1) * ldr + N) * size, Y, M * N * (y_dtype == STAMP_BF16 ? 2 : 4)) ? STAMP_ERR_INVALID_ARG : STAMP_OK;
 }
 
 // Arguments common to both products.
@@ -2246,7 +2249,7 @@ int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w
   if (int rc = check_fp8_product(p, STAMP_BF16)) return rc;
   if (activation < STAMP_ACT_NONE || activation > STAMP_ACT_SILU) return STAMP_ERR_INVALID_ARG;
   if (N % 16 != 0) return STAMP_ERR_UNSUPPORTED;
-  if (M > 0 && (!scale || !aligned16(codes))) return STAMP_ERR_INVALID_ARG;
+  if (M > 0 && (!scale || !aligned16(codes) || overlap(codes, (long)M * N, x, (long)M * K))) return STAMP_ERR_INVALID_ARG;
   p.act = activation;
   p.words = 1;
   p.y_scale = static_cast<uint8_t*>(scale);
@@ -2305,6 +2308,7 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
     return STAMP_ERR_INVALID_ARG;
   if (residual)
     if (int rc = check_residual(residual, r_dtype, ldr, T, N, out, o_dtype)) return rc;
+  if (M > 0 && overlap(y, (long)M * N * (y_dtype == STAMP_BF16 ? 2 : 4), out, (long)T * N * (o_dtype == STAMP_BF16 ? 2 : 4))) return STAMP_ERR_INVALID_ARG;
   const CombineParams p{y, place, share, residual, (long)ldr, T, top, M, N, out};
   const int r_bf16 = r_dtype == STAMP_BF16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -2321,7 +2325,7 @@ static int check_expert_layer(int T, int M, int E, int K, int F, int N) {
   if (T > EXPERT_FEW_TOKENS || M > EXPERT_FEW_ROWS || E > EXPERT_MAX || K % 16 != 0 || F % 16 != 0 || K > FP8_MAX_FEATURES || F > FP8_MAX_FEATURES / 2)
     return STAMP_ERR_UNSUPPORTED;
   if ((long)E * 2 * F > (1L << 31) - 512 || (long)E * N > (1L << 31) - 512) return STAMP_ERR_UNSUPPORTED;
-  // CTAs and steps are counted in 32 bits: runs of eight rows at least, a cluster of eight CTAs at most
+  // CTAs and steps are counted in 32 bits: runs of eight rows at least, clusters of eight CTAs at most (of sixteen for a few tiles)
   return (long)expert_max_runs(M, E, 8) * ((F + 127L) / 128) * 8 > 0x7FFFFFFFL ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
 }
 

@@ -32,6 +32,7 @@ def layer(st, X=A, dtype=BF16, ldx=256, rows=A, share=A, offsets=A, up=A, up_s=A
     (combine, dict(y=0)), (combine, dict(dtype=3)), (combine, dict(place=0)), (combine, dict(share=0)), (combine, dict(T=-1)), (combine, dict(top=0)),
     (combine, dict(M=-1)), (combine, dict(N=0)), (combine, dict(out=0)), (combine, dict(o_dtype=-1)), (combine, dict(out=B + 2)), (combine, dict(y=A + 1, dtype=BF16)),
     (combine, dict(residual=R, ldr=63)), (combine, dict(residual=R, r_dtype=7)), (combine, dict(residual=B + 4)), (combine, dict(residual=B, ldr=68)),
+    (combine, dict(out=A, o_dtype=F32)), (combine, dict(y=B + 4 * 64 * 4 - 4)), (combine, dict(y=B - 8 * 64 * 4 + 4)),
     (layer, dict(X=0)), (layer, dict(X=ODD)), (layer, dict(dtype=5)), (layer, dict(ldx=255)), (layer, dict(ldx=260)), (layer, dict(rows=0)), (layer, dict(share=0)),
     (layer, dict(offsets=0)), (layer, dict(up=0)), (layer, dict(up=ODD)), (layer, dict(up_s=0)), (layer, dict(down=0)), (layer, dict(down=ODD)), (layer, dict(down_s=0)),
     (layer, dict(residual=R, ldr=63)), (layer, dict(residual=B + 2)), (layer, dict(T=-1)), (layer, dict(M=-1)), (layer, dict(E=0)), (layer, dict(K=0)), (layer, dict(F=0)),

@@ -24,6 +24,7 @@ def quantized(st, x=A, xs=A, w=A, ws=A, bias=0, act=0, M=4, N=64, K=256, codes=B
     (fused, dict(residual=B - 64 * 8 + 2)), (fused, dict(residual=B + 4 * 64 * 2 - 2)),
     (fused, dict(residual=B, r_dtype=F32, dtype=F32, act=1, K=4112)),
     (quantized, dict(x=0)), (quantized, dict(codes=0)), (quantized, dict(scale=0)), (quantized, dict(codes=ODD)), (quantized, dict(act=9)), (quantized, dict(K=0)),
+    (quantized, dict(N=256, codes=A)), (quantized, dict(codes=A + 4 * 256 - 16)), (quantized, dict(codes=A - 4 * 64 + 16)),
 ])
 def test_invalid_arguments(st, call, bad):  # noqa: F811
     assert call(st, **bad) == INVALID
