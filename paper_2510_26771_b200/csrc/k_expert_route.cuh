@@ -57,9 +57,15 @@ template <>
 struct RouteEntry<__nv_bfloat16> {
   uint32_t word;
   __device__ __forceinline__ void set(float logit, int e) { word = (route_key(logit) >> 16 << 16) | (0xFFFFu - e); }   // (a NaN: 0, with an expert)
-  __device__ __forceinline__ void set_finite(float logit, int e) {
-    const uint32_t b = __float_as_uint(logit + 0.f), flip = static_cast<uint32_t>(static_cast<int>(b) >> 31) | 0x80000000u;
-    word = ((b ^ flip) & 0xFFFF0000u) | (0xFFFFu - e);
+  // two neighbouring logits, as loaded
+  __device__ __forceinline__ static void set_finite(uint32_t two, int e, RouteEntry& a, RouteEntry& b) {
+    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f), sum = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&two), zero);
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(&sum);
+    uint32_t sign;   // of each half, over all of its bits
+    asm("prmt.b32 %0, %1, %1, 0xBB99;" : "=r"(sign) : "r"(v));
+    const uint32_t key = v ^ (sign | 0x80008000u);
+    a.word = __byte_perm(key, 0xFFFFu - e, 0x1054);
+    b.word = (key & 0xFFFF0000u) | (0xFFFFu - e - 1u);
   }
   __device__ __forceinline__ static bool strange(const RouteEntry& first, const RouteEntry& last) {
     return first.word >= 0xFF810000u || last.word < 0x007F0000u;   // (infinity's upper half is 0xFF80, that of -infinity 0x007F)
@@ -122,38 +128,57 @@ __device__ __forceinline__ void route_sort(RouteEntry<T> (&v)[PER]) {
     at(1, 2), at(3, 4), at(5, 6);
   }
 }
-// PER neighbouring logits of a row as floats; beyond the row -inf.
+// PER neighbouring logits of a row, as loaded; beyond the row -inf.
+template <typename T, int PER>
+struct RouteLogits;
 template <int PER>
-__device__ __forceinline__ void route_load_all(const float* p, int left, bool vector, float (&l)[PER]) {
-  if (PER >= 4 && vector && left >= PER) {
+struct RouteLogits<float, PER> {
+  float v[PER];
+  __device__ __forceinline__ void load(const float* p, int left, bool vector) {
+    if (PER >= 4 && vector && left >= PER) {
 #pragma unroll
-    for (int i = 0; i < PER; i += 4) {
-      const float4 u = __ldg(reinterpret_cast<const float4*>(p + i));
-      l[i] = u.x, l[(i + 1) % PER] = u.y, l[(i + 2) % PER] = u.z, l[(i + 3) % PER] = u.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) l[i] = i < left ? route_load(p + i) : -__int_as_float(0x7F800000);
-  }
-}
-template <int PER>
-__device__ __forceinline__ void route_load_all(const __nv_bfloat16* p, int left, bool vector, float (&l)[PER]) {
-  if (PER >= 4 && vector && left >= PER) {
-    uint32_t w[PER / 2 > 0 ? PER / 2 : 1];
-    if constexpr (PER == 8) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+      for (int i = 0; i < PER; i += 4) {
+        const float4 u = __ldg(reinterpret_cast<const float4*>(p + i));
+        v[i] = u.x, v[(i + 1) % PER] = u.y, v[(i + 2) % PER] = u.z, v[(i + 3) % PER] = u.w;
+      }
     } else {
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
-      w[0] = u.x, w[1 % (PER / 2 > 0 ? PER / 2 : 1)] = u.y;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) v[i] = i < left ? __ldg(p + i) : -__int_as_float(0x7F800000);
     }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) l[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) l[i] = i < left ? route_load(p + i) : -__int_as_float(0x7F800000);
   }
-}
+  __device__ __forceinline__ float value(int i) const { return v[i]; }
+  __device__ __forceinline__ void finite(RouteEntry<float> (&entry)[PER], int e) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) entry[i].set_finite(v[i], e + i);
+  }
+};
+template <int PER>
+struct RouteLogits<__nv_bfloat16, PER> {
+  uint32_t w[(PER + 1) / 2];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, bool vector) {
+    if (PER >= 4 && vector && left >= PER) {
+      if constexpr (PER == 8) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+      } else if constexpr (PER == 4) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+        w[0] = u.x, w[1] = u.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const uint32_t h = i < left ? *reinterpret_cast<const uint16_t*>(p + i) : 0xFF80u;
+        w[i / 2] = i & 1 ? w[i / 2] | h << 16 : h;
+      }
+    }
+  }
+  __device__ __forceinline__ float value(int i) const { return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); }
+  __device__ __forceinline__ void finite(RouteEntry<__nv_bfloat16> (&entry)[PER], int e) const {
+    RouteEntry<__nv_bfloat16> odd;
+#pragma unroll
+    for (int i = 0; i < PER; i += 2) RouteEntry<__nv_bfloat16>::set_finite(w[i / 2], e + i, entry[i], i + 1 < PER ? entry[(i + 1) % PER] : odd);
+  }
+};
 
 // Exclusive sum over the CTA of one value per thread; `total` gets the sum.  scratch: 33 words.
 __device__ __forceinline__ int route_scan(int v, int* scratch, int& total) {
@@ -210,10 +235,12 @@ __device__ __forceinline__ void route_store(const RouteParams& p, const int* bas
   }
 }
 
-// A warp takes one token after the other, a lane PER neighbouring experts: it sorts them once, then the lanes' first entries
-// are compared `top` times, and the lane that had the best one moves up.  (Searching all entries every time took three times the
-// instructions, which is what bounds it: 16384 tokens of 256 experts, top 8, 744 a token.)  Above 256 experts (PER = 32,
-// expert 32 i + lane in register i) sorting costs more than searching.
+// A warp takes one token after the other, the next one's logits on their way, a lane PER neighbouring experts: it sorts them
+// once, then the lanes' first entries are compared `top` times, and the lane that had the best one moves up.  (Searching all
+// entries every time took three times the instructions, which is what bounds it: 16384 tokens of 256 bf16 logits, top 8, both
+// launches 16.3 us where 8.4 MB have to be read, 1.7 us; fp32 logits, whose entries take two words, 20.1 us.)  Up to eight
+// choices are unrolled, so that only entries that can still be chosen move.  Above 256 experts (PER = 32, expert 32 i + lane in
+// register i) sorting costs more than searching.
 // Each warp counts its rows by expert in shared memory, and a row's rank is the count so far; the warps' counts are then
 // summed in their order.
 template <typename TIn, int PER>
@@ -229,19 +256,25 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
 
   const long cta_end = min((static_cast<long>(blockIdx.x) + 1) * p.per_cta, static_cast<long>(p.T));
   const long t0 = static_cast<long>(blockIdx.x) * p.per_cta + static_cast<long>(warp) * p.per_warp;
-  for (long t = t0; t < min(t0 + p.per_warp, cta_end); ++t) {
-    const TIn* row = static_cast<const TIn*>(p.logits) + t * p.ldl;
-    float l[PER];
+  const long t1 = min(t0 + p.per_warp, cta_end);
+  constexpr bool SORTED = PER <= 8;
+  RouteLogits<TIn, SORTED ? PER : 1> next;   // (a token ahead)
+  auto load = [&](long t) {
+    if (SORTED && t < t1) next.load(static_cast<const TIn*>(p.logits) + t * p.ldl + lane * PER, p.E - lane * PER, p.vector);
+  };
+  load(t0);
+  for (long t = t0; t < t1; ++t) {
+    float l[SORTED ? 1 : PER];
+    const auto now = next;
+    load(t + 1);
     bool nan = false;
     int expert = 0;        // lane j: choice j and its logit
     float best = 0.f;
-    if constexpr (PER <= 8) {
-      route_load_all<PER>(row + lane * PER, p.E - lane * PER, p.vector, l);
+    if constexpr (SORTED) {
       RouteEntry<TIn> entry[PER], mine_of{};
       const bool full = p.E == 32 * PER;   // every lane has PER experts
       if (full) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) entry[i].set_finite(l[i], lane * PER + i);
+        now.finite(entry, lane * PER);
         route_sort<TIn, PER>(entry);
         nan = __any_sync(0xffffffffu, RouteEntry<TIn>::strange(entry[0], entry[PER - 1]));
       }
@@ -249,25 +282,37 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
         nan = false;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          entry[i].set(l[i], lane * PER + i);
+          entry[i].set(now.value(i), lane * PER + i);
           if (lane * PER + i >= p.E) entry[i].none();
-          nan |= l[i] != l[i];
+          nan |= now.value(i) != now.value(i);
         }
         nan = __any_sync(0xffffffffu, nan);
         route_sort<TIn, PER>(entry);
       }
-      for (int j = 0; j < p.top; ++j) {
+      auto take = [&](int j, int left) {   // choice j, with `left` entries of a lane to come into question after it
         const RouteEntry<TIn> first = entry[0].best();
         const bool up = entry[0].is(first);
 #pragma unroll
-        for (int i = 0; i + 1 < PER; ++i)
-          if (up) entry[i] = entry[i + 1];
-        if (up) entry[PER - 1].none();
+        for (int i = 0; i < PER; ++i)
+          if (i < left && up) {
+            if (i + 1 < PER) entry[i] = entry[(i + 1) % PER];
+            else entry[i].none();
+          }
         if (lane == j) mine_of = first;
+      };
+      if (p.top <= 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (j >= p.top) break;
+          take(j, 7 - j);
+        }
+      } else {
+        for (int j = 0; j < p.top; ++j) take(j, PER);
       }
       expert = mine_of.expert();
       best = mine_of.logit();
     } else {
+      const TIn* row = static_cast<const TIn*>(p.logits) + t * p.ldl;
       uint32_t key[PER];
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -299,7 +344,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
     if (!p.normalize) {
       total = 0.f;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) total += expf(l[i] - largest);   // (lanes without an expert: exp(-inf))
+      for (int i = 0; i < PER; ++i) total += expf((SORTED ? now.value(SORTED ? i : 0) : l[SORTED ? 0 : i]) - largest);   // (lanes without an expert: exp(-inf))
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
@@ -327,8 +372,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
   }
   if (gridDim.x > 1 && threadIdx.x >= p.E && threadIdx.x < route_pitch(p.E)) p.counts[static_cast<long>(blockIdx.x) * route_pitch(p.E) + threadIdx.x] = 0;
   __syncthreads();
-  for (long t = t0; t < min(t0 + p.per_warp, cta_end); ++t)
-    if (lane < p.top) p.place[t * p.top + lane] += mine[p.chosen[t * p.top + lane]];
+  for (long i = t0 * p.top + lane; i < t1 * p.top; i += 32) p.place[i] += mine[p.chosen[i]];
   if (gridDim.x > 1) return;
   int total;
   const int e = threadIdx.x;
@@ -343,7 +387,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_choose(RouteParams p) 
   route_store(p, base, route_first(p));
 }
 
-// The second launch where several CTAs chose: every expert's first place, from the counts of all CTAs; then the rows.  The
+// The second launch where several CTAs chose (about 5 us of the 16 above: two trips to the L2, one for the counts, one for the
+// rows): every expert's first place, from the counts of all CTAs; then the rows.  The
 // counts are padded to a multiple of four experts (`pitch`): a thread sums four experts over a share of the CTAs.
 __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_place(RouteParams p) {
   extern __shared__ int4 route_sums[];   // [groups][pitch / 4] rows of the CTAs before this one, then of all
@@ -355,7 +400,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_expert_place(RouteParams p) {
   const RouteRow row = route_first(p);   // (on its way with the counts)
   int4 before = make_int4(0, 0, 0, 0), all = before;
   if (g < groups) {
-#pragma unroll 4
+#pragma unroll 10
     for (int b = g; b < static_cast<int>(gridDim.x); b += groups) {
       const int4 c = __ldg(reinterpret_cast<const int4*>(p.counts) + static_cast<long>(b) * fours + i4);
       all.x += c.x, all.y += c.y, all.z += c.z, all.w += c.w;
@@ -398,47 +443,80 @@ struct CombineParams {
 };
 constexpr int COMBINE_THREADS = 128;
 
+// V neighbouring channels as loaded and stored, 16 bytes at most a time.
 template <typename T, int V>
-struct Packed {};
-template <>
-struct Packed<float, 4> { using type = float4; };
-template <>
-struct Packed<__nv_bfloat16, 4> { using type = uint2; };
-template <>
-struct Packed<float, 1> { using type = float; };
-template <>
-struct Packed<__nv_bfloat16, 1> { using type = __nv_bfloat16; };
+struct Packed {
+  static constexpr int BYTES = sizeof(T) * V, WORDS = (BYTES + 3) / 4;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const void* base, long at) {
+    const char* const p = static_cast<const char*>(base) + at * sizeof(T);
+    if constexpr (BYTES % 16 == 0) {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 4) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p + i * 4);
+        w[i] = u.x, w[i + 1] = u.y, w[i + 2] = u.z, w[i + 3] = u.w;
+      }
+    } else if constexpr (BYTES == 8) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      w[0] = u.x, w[1] = u.y;
+    } else if constexpr (BYTES == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
+  }
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ static void store(void* base, long at, const float (&v)[V]) {
+    T* const p = static_cast<T*>(base) + at;
+    if constexpr (V == 1) {
+      if constexpr (sizeof(T) == 4) *p = v[0];
+      else *p = __float2bfloat16_rn(v[0]);
+    } else {
+      uint32_t u[WORDS];
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          u[i] = __float_as_uint(v[i]);
+        } else {
+          const __nv_bfloat162 two = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+          u[i] = *reinterpret_cast<const uint32_t*>(&two);
+        }
+      }
+      if constexpr (BYTES == 8) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(u[0], u[1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) reinterpret_cast<uint4*>(p)[i / 4] = make_uint4(u[i], u[(i + 1) % WORDS], u[(i + 2) % WORDS], u[(i + 3) % WORDS]);
+      }
+    }
+  }
+};
 
-__device__ __forceinline__ void unpack(const float4& u, float (&v)[4]) { v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w; }
-__device__ __forceinline__ void unpack(const uint2& u, float (&v)[4]) {
-  v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
-  v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
-}
-__device__ __forceinline__ void unpack(const float& u, float (&v)[1]) { v[0] = u; }
-__device__ __forceinline__ void unpack(const __nv_bfloat16& u, float (&v)[1]) { v[0] = __bfloat162float(u); }
-__device__ __forceinline__ void pack(const float (&v)[4], float4& u) { u = make_float4(v[0], v[1], v[2], v[3]); }
-__device__ __forceinline__ void pack(const float (&v)[4], uint2& u) {
-  const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
-  u = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-}
-__device__ __forceinline__ void pack(const float (&v)[1], float& u) { u = v[0]; }
-__device__ __forceinline__ void pack(const float (&v)[1], __nv_bfloat16& u) { u = __float2bfloat16_rn(v[0]); }
-
-// A thread takes V neighbouring channels of one token; four of the token's rows are in flight at a time.
-// grid (T, ceil(N / (COMBINE_THREADS V)))
-template <typename TIn, typename TOut, int V>
+// A thread takes V neighbouring channels of one token (rows off the words' alignment: V = 1 and U of them,
+// COMBINE_THREADS apart); four of the token's rows are in flight at a time.  grid (T, ceil(N / (COMBINE_THREADS V U)))
+template <typename TIn, typename TOut, int V, int U>
 __global__ void __launch_bounds__(COMBINE_THREADS) k_expert_combine(CombineParams p, int r_bf16) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const long t = blockIdx.x, c = (static_cast<long>(blockIdx.y) * COMBINE_THREADS + threadIdx.x) * V;
-  if (c >= p.N) return;
-  using In = typename Packed<TIn, V>::type;
-  using Out = typename Packed<TOut, V>::type;
-  float sum[V], v[V];
+  const long t = blockIdx.x, c0 = (static_cast<long>(blockIdx.y) * U * COMBINE_THREADS + threadIdx.x) * V;
+  auto channel = [&](int u) { return c0 + u * COMBINE_THREADS; };
+  // (the residual does not wait for the places)
+  Packed<float, V> wide[U];
+  Packed<__nv_bfloat16, V> narrow[U];
+  float sum[U][V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) sum[i] = 0.f;
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[u][i] = 0.f;
+    if (!p.residual || channel(u) >= p.N) continue;
+    if (r_bf16) narrow[u].load(p.residual, t * p.ldr + channel(u));
+    else wide[u].load(p.residual, t * p.ldr + channel(u));
+  }
   for (int j0 = 0; j0 < p.top; j0 += 4) {
-    In raw[4];
+    Packed<TIn, V> raw[4][U];
     float share[4];
     bool live[4];
 #pragma unroll
@@ -452,28 +530,28 @@ __global__ void __launch_bounds__(COMBINE_THREADS) k_expert_combine(CombineParam
         raise_device_status(STAMP_ERR_INVALID_ARG);
         continue;
       }
-      raw[j] = *reinterpret_cast<const In*>(static_cast<const TIn*>(p.y) + static_cast<long>(at) * p.N + c);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (channel(u) < p.N) raw[j][u].load(p.y, static_cast<long>(at) * p.N + channel(u));
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (!live[j]) continue;
-      unpack(raw[j], v);
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum[i] = fmaf(share[j], v[i], sum[i]);
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[u][i] = fmaf(share[j], raw[j][u].value(i), sum[u][i]);
     }
   }
-  if (p.residual) {
-    const long at = t * p.ldr + c;
-    if (r_bf16)
-      unpack(*reinterpret_cast<const typename Packed<__nv_bfloat16, V>::type*>(static_cast<const __nv_bfloat16*>(p.residual) + at), v);
-    else
-      unpack(*reinterpret_cast<const typename Packed<float, V>::type*>(static_cast<const float*>(p.residual) + at), v);
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum[i] += v[i];
+  for (int u = 0; u < U; ++u) {
+    if (channel(u) >= p.N) continue;
+    if (p.residual) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[u][i] += r_bf16 ? narrow[u].value(i) : wide[u].value(i);
+    }
+    Packed<TOut, V>::store(p.out, t * p.N + channel(u), sum[u]);
   }
-  Out o;
-  pack(sum, o);
-  *reinterpret_cast<Out*>(static_cast<TOut*>(p.out) + t * p.N + c) = o;
 }
 
 }  // namespace stamp

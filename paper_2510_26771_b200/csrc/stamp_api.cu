@@ -1655,12 +1655,27 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
 
 template <typename TIn, typename TOut>
 static int launch_combine(const CombineParams& p, int r_bf16, cudaStream_t st) {
-  const auto vector = [](const void* q, size_t element) { return (reinterpret_cast<uintptr_t>(q) & (4 * element - 1)) == 0; };
-  const bool four = p.N % 4 == 0 && vector(p.y, sizeof(TIn)) && vector(p.out, sizeof(TOut)) &&
-                    (!p.residual || (p.ldr % 4 == 0 && vector(p.residual, r_bf16 ? 2 : 4)));
-  const int per = COMBINE_THREADS * (four ? 4 : 1);
+  auto by = [&](int v) {   // every row of v channels starts on a whole word (of 16 bytes at most)
+    auto fits = [&](const void* q, long ld, size_t element) {
+      const size_t word = element * v < 16 ? element * v : 16;
+      return reinterpret_cast<uintptr_t>(q) % word == 0 && ld * element % word == 0;
+    };
+    return p.N % v == 0 && fits(p.y, p.N, sizeof(TIn)) && fits(p.out, p.N, sizeof(TOut)) && (!p.residual || fits(p.residual, p.ldr, r_bf16 ? 2 : 4));
+  };
+  // Channels of a thread: eight bf16 ones where a token has more than a CTA's fours of them (4096 tokens of four rows of 4096, us:
+  // 34.2, with four 37.1; 2632 of one of 768: 4.5, with four 6.2; 2120 of four of 1280: 9.6, with four 10.2); single ones four to a
+  // thread where that leaves enough CTAs (3342 of four of 1905: 26.7, one to a thread 52.6; 190 of eight of 1334: 4.6, one to
+  // a thread 4.1).
+  const bool eight = sizeof(TIn) == 2 && p.N > 4 * COMBINE_THREADS && by(8);
+  const bool spread = (long)p.T * p.N > 32L * sm_count() * COMBINE_THREADS;
+  int v = 1, u = 1;
+  auto kern = k_expert_combine<TIn, TOut, 1, 1>;
+  if (by(4)) kern = k_expert_combine<TIn, TOut, 4, 1>, v = 4;
+  else if (spread) kern = k_expert_combine<TIn, TOut, 1, 4>, u = 4;
+  if constexpr (sizeof(TIn) == 2)
+    if (eight) kern = k_expert_combine<TIn, TOut, 8, 1>, v = 8;
+  const int per = COMBINE_THREADS * v * u;
   const dim3 grid((unsigned)p.T, (unsigned)((p.N + (long)per - 1) / per));
-  auto kern = four ? k_expert_combine<TIn, TOut, 4> : k_expert_combine<TIn, TOut, 1>;
   if (launch_pdl(kern, grid, dim3(COMBINE_THREADS), 0, st, p, r_bf16) != cudaSuccess) {
     cudaGetLastError();
     return STAMP_ERR_CUDA;

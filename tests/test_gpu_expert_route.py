@@ -96,6 +96,26 @@ def test_masked_experts_padding_and_what_is_not_finite(st, T, normalize):  # noq
     assert bool(torch.isnan(got[1][8, 0]))
 
 
+@pytest.mark.parametrize("E", [32, 64, 128, 256, 512])
+@pytest.mark.parametrize("top", [8, 11])
+def test_ties_and_what_is_not_finite_where_every_lane_has_all_its_experts(st, E, top):  # noqa: F811
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(E + top)
+    x = torch.randint(-3, 1, (170, E), generator=g, device="cuda").float()
+    x[x == 0] *= torch.where(torch.rand(int((x == 0).sum()), generator=g, device="cuda") < 0.5, 1.0, -1.0)
+    tiny = torch.randint(-4, 5, (E,), generator=g, device="cuda").float() * 2.0 ** -130          # subnormal numbers of both types
+    nan = torch.full((2,), 0x7FC00000, dtype=torch.int32, device="cuda")
+    nan[1] = 0xFFC00000 - (1 << 32)
+    nan = nan.view(torch.float32)                                                              # NaNs of both signs
+    x[1], x[2, 3], x[3, E - 1], x[4, 1::2] = tiny, nan[0], nan[1], nan[1]
+    x[5], x[5, -2:] = nan[0], -1.0
+    x[6] = float("-inf")
+    x[7, 2:] = float("-inf")
+    x[8] = torch.finfo(torch.bfloat16).min
+    for v in (x, x.bfloat16()):
+        check_route(st.stamp_expert_route(v, top), plain_route(v, top, True))
+
+
 def test_logits_of_a_wider_matrix_and_given_buffers(st):  # noqa: F811
     import torch
     wide = torch.randn(200, 91, device="cuda")
