@@ -1639,15 +1639,20 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
   p.terms = p.h_terms;
   p.cap = cap(ExpertSmem<false>::COLUMNS);
   const long tiles = (p.N + 127L) / 128;
-  // As many CTAs as SMs, twice as many where each still has enough to do, sixteen to a tile where there are few tiles and enough
-  // to do.  With 4 / 8 / 16 to a tile, in us (the choice in brackets): 32 tiles, 13 tokens over 32 experts of 4096 x 4096 161.8 /
-  // (159.0) / 172.5, one token of two such experts (27.3) / 30.6; 28 tiles, 36 tokens over 60 experts of 656 43.2 / (38.5), one
-  // token of eight of 640 (21.3) / 23.8 / 33.8; 16 tiles, 64 tokens over 64 of 2048 191 / (149) / 168; 7 tiles, 55 tokens over 8 of
-  // 3456 - / 56.7 / (48.2), 5 tokens of four of 1856 33.0 / 27.5 / (26.0); 6 tiles, 3 tokens over 8 of 384 14.0 / (13.2) / 15.0.
+  // As many CTAs as SMs have room for at once, half as many again where each still has enough to do (more than that, and clusters
+  // find their SMs late), sixteen to a tile where there are few tiles and enough to do.  Us, by CTAs of a tile, the choice in
+  // brackets: 32 tiles, 13 tokens over 32 experts of 4096 x 4096, four: 160.2, six: 154.5, (seven: 152.5), eight: 163.4; one
+  // token of two such experts, (four: 27.3), eight: 30.6; 28 tiles, 24 tokens over 60 of 656, four: 65.2, (eight: 57.4), twelve:
+  // 68.4; 16 tiles, 64 tokens over 64 of 2048, six: 163.2, (eight: 151.0), ten: 146.2, twelve: 155.9, sixteen: 167.0; 12 tiles, 40
+  // tokens over 16 of 2048, eight: 42.2, (sixteen: 39.9); 9 tiles, one token of four of 2048, four: 17.4, (eight: 16.4), sixteen: 16.9;
+  // 7 tiles, 55 tokens over 8 of 3456, eight: 79.8, (sixteen: 67.4); fewer steps, one token of eight of 640, 28 tiles, (four: 21.2),
+  // five: 22.1, two tokens of eight of 1024, 11 tiles, (eight: 21.3), sixteen: 22.4.
   const long steps = (long)(p.E < p.M ? p.E : p.M) * ((p.F + 127) / 128);   // (run, 128 features) of a tile, about
   p.split = 1;
-  while (p.split < 8 && (tiles * p.split * 2 <= sms || (tiles * p.split * 2 <= 2 * sms && steps >= 16L * p.split * 2))) p.split *= 2;
-  if (p.split == 8 && tiles <= 7 && steps >= 16L * 8) p.split = 16;
+  while (p.split < 8 && tiles * p.split * 2 <= sms) p.split *= 2;
+  for (int split = p.split + 1; split <= 8; ++split)
+    if (tiles * split * 2 <= 3 * sms + 8 && steps >= 16L * split) p.split = split;
+  if (p.split == 8 && tiles <= 12 && steps >= 12L * 16) p.split = 16;
   // (two CTAs to an SM: with more than half of its shared memory a cluster of eight finds its SMs too late)
   return y_dtype == STAMP_BF16 ? launch_expert<false, __nv_bfloat16>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st)
                                : launch_expert<false, float>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st);

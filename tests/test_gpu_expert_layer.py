@@ -120,6 +120,7 @@ CASES = {
     "more rows than tokens": (7, [20, 50, 3], 128, 128, 128),
     "many experts": (16, [1, 0, 0, 2] * 40, 128, 144, 136),
     "few features, many hidden channels": (9, [3, 0, 4, 1, 2], 256, 4096, 520),
+    "many output channels": (9, [1] * 28, 128, 512, 3968),
     "no rows": (4, [0, 0, 0], 128, 128, 128),
 }
 
