@@ -33,11 +33,12 @@
 // DOWN is launched as a programmatic dependent of UP: its first weights are on their way while UP's last CTAs run; only its
 // copies of the hidden values and their scales wait.
 //
-// What bounds it.  Many experts: the weights' way from memory.  64 tokens, eight of 64 experts of 2048 x 2048 each: 805 MB, 125 us at
-// the copy rate, in 150 (UP 97, DOWN 53); 13 tokens, four of 32 experts of 4096 x 4096: the 26 to 28 experts that get rows, 196 to 211
-// us at 6.4 TB/s were all read, in 154 to 168 -- reads alone go faster than the copy that the rate is from.  Few tiles: the chain
-// launch, terms, sums, exchange, hidden values, sums, exchange.  One token, four experts of 1152 x 2048: 28 MB, 4.4 us at the copy
-// rate, in 15 to 16, of which 3.2 are the launch, 5 the first kernel's nine steps behind the first copy, and as much the second's.
+// What bounds it.  Many experts: the weights' way from memory.  64 tokens, eight of 64 experts of 2048 x 2048: 805 MB, 125 us at the
+// copy rate, in 150 (UP 5.3 TB/s, issue slots 42 % busy with the terms; DOWN's 128 CTAs leave 20 SMs without one); 13 tokens, four
+// of 32 experts of 4096 x 4096: 149 us, 202 at the copy rate if as many experts get rows as random choices reach -- reads alone go
+// faster than the copy that the rate is from.  Few tiles: one chain of launch, first copies, terms, sums, exchange, hidden values,
+// sums, exchange.  One token, four experts of 1152 x 2048: 28 MB, 4.4 us at the copy rate, in 15 to 16, where the two kernels alone
+// and cold take 11 and 13.
 // Measured and not kept, us for what is kept: tiles of 64 gates (171 for 150; one token 18.3 for 16); runs of 32 rows in UP (158 for
 // 152); one CTA an SM with 200 KB in DOWN (160 for 147: clusters of eight find their SMs late); two CTAs an SM in UP, one tile each
 // (187 for 150); hidden values in fp32, made into terms by DOWN (294 for 150).
