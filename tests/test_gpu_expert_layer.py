@@ -141,6 +141,23 @@ def test_against_the_definition(st, name, dtype):  # noqa: F811
     assert st.stamp_last_device_status() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("counts", [[2] * 1024, [0, 2048, 0], [1] * 64 + [0] * 955 + [300, 1, 0, 5, 6]], ids=["two for each", "all to one", "uneven"])
+def test_the_largest_tables(st, counts, dtype):  # noqa: F811
+    """As many tokens, rows and experts as the call takes; every token comes up many times, in one run too."""
+    import torch
+    T, K, F, N = 64, 32, 48, 72
+    layer = Layer(st, len(counts), K, F, N, seed=7)
+    rows, share, offsets = routing(counts, T, seed=7, spare=2048 - sum(counts))
+    x, residual = tokens(T, K, dtype), tokens(T, N, dtype, seed=8)
+    for out in (torch.bfloat16, torch.float32):
+        y = layer(st, x, rows, share, offsets, residual=residual, out_dtype=out)
+        want, off = layer.plain(x, rows, share, offsets, residual, out is torch.bfloat16, T)
+        # (a token's many rows are added one by one: each addition is rounded once more)
+        check(y, want, off + 2048 * 2.0 ** -24 * np.abs(want))
+    assert st.stamp_last_device_status() == 0
+
+
 def test_typical_errors_are_far_below_the_worst_case(st):  # noqa: F811
     """The bounds above grow with the lengths of the sums.  Errors of either sign grow with their roots: as a share of the
     output's norm an fp32 layer stays below 2e-5 and a bf16 one within the 2^-9 of its own rounding."""
