@@ -15,7 +15,7 @@
 //   warp 1     allocates TMEM; one elected thread copies the scale words to TMEM (tcgen05.cp) and issues the MMAs
 //   warps 2-3  scale producers: gather the scale words of 512 features of the tile's tokens and channels into the
 //              order tcgen05.cp wants (row i of 32: rows i, i + 32, i + 64, i + 96), up to FP8G_SF_SLOTS steps ahead
-//   warps 4-11 epilogue: drain the finished accumulator while the next tile fills the other
+//   warps 4-11 (GROUPS = 4: 4-19) epilogue: drain the finished accumulator while the next tile fills the other
 // Every wait is bounded; when one expires the CTA raises the device status word, unwinds and frees its TMEM.
 //
 // PAIR = false: tiles of 128 channels x up to 128 tokens, one CTA each.  For few tiles the sum can be split over a
@@ -47,11 +47,8 @@ constexpr int FP8G_ACC_COLS = 128;                     // tensor-memory columns 
 constexpr int FP8G_W_BYTES = FP8G_BM * FP8G_BK;
 constexpr int FP8G_SF_SLOTS = 4;                       // steps of 512 features whose scale words are staged
 constexpr int FP8G_TAIL_BOX = 32;
-constexpr int FP8G_EPI_WARPS = 8;
-constexpr int FP8G_THREADS = 128 + 32 * FP8G_EPI_WARPS;
-constexpr int FP8G_FUSED_GROUPS = 2;                   // FUSED: epilogue warps in groups of four (the lanes' quarters)
 constexpr int FP8G_PART = FP8G_BM + 4;                 // FUSED: floats from one token to the next in a part of a split sum
-constexpr int FP8G_FUSED_THREADS = 128 + 128 * FP8G_FUSED_GROUPS;
+constexpr int FP8G_MOST_GROUPS = 4;                    // epilogue warps come in groups of four, one for each quarter of the lanes
 constexpr long long FP8G_WAIT_LIMIT = 4000000000LL;    // SM clocks (~2 s) before a wait gives up
 
 struct Fp8GemmParams {
@@ -91,7 +88,7 @@ struct Fp8Smem {
   // FUSED, quantized output: a barrier for each group of four epilogue warps, their maxima [group][buffer][quarter][token] and
   // the tokens' inverse scales [warp][token]
   static constexpr int EX_OFFSET = (TAB_OFFSET + 2 * 2 * 4 + 15) / 16 * 16;   // (one matrix: two entries of either table)
-  static constexpr int EX_BYTES = FP8G_FUSED_GROUPS * (8 + 2 * 4 * 32 * 4 + 4 * 32 * 4);
+  static constexpr int EX_BYTES = FP8G_MOST_GROUPS * (8 + 2 * 4 * 32 * 4 + 4 * 32 * 4);
   static constexpr int FUSED_DYN_BYTES = EX_OFFSET + EX_BYTES + 1024;
   static_assert(DYN_BYTES <= 227 * 1024 && FUSED_DYN_BYTES <= 227 * 1024, "shared memory of one CTA");
   // tensor memory: second accumulator, then the two buffers of scale columns (4 for channels, BN / 32 for tokens)
@@ -151,8 +148,8 @@ __host__ __device__ constexpr int fp8_drain_chunk(bool descending, int half, int
   return half + 2 * (descending ? count - 1 - i : i);
 }
 __host__ __device__ constexpr int fp8_overlap_half(int accumulator) { return accumulator == 0 ? 1 : 0; }
-// The same with FP8G_FUSED_GROUPS groups of warps: chunk c by group c % 4, the last first in the first accumulator.
-__host__ __device__ constexpr int fp8_overlap_group(int accumulator) { return accumulator == 0 ? 7 % FP8G_FUSED_GROUPS : 0; }
+// FUSED, with two or four groups of warps: chunk c by group c % groups, the last first in the first accumulator.
+__host__ __device__ constexpr int fp8_overlap_group(int accumulator, int groups) { return accumulator == 0 ? 7 % groups : 0; }
 constexpr bool fp8_drain_order_holds() {
   for (int chunks = 1; chunks <= 8; ++chunks)
     for (int a = 0; a < 2; ++a) {
@@ -336,19 +333,20 @@ __device__ __forceinline__ void fp8_load_column(const T* p, long ld, int left, u
 //
 // Device times, in us, in brackets the plain product's to bf16 or fp32 on the same box: 1 x 4096 x 11008 with bias and silu 11.0
 // (10.2); 8192 x 4608 x 1152 with bias and a bf16 residual 42.7 (39.6), the residual's way from memory; 8192 x 1152 x 4608 with
-// bias and gelu_tanh to codes 54 (41.3): a tile's nine steps of 128 features are summed before its 256 columns are drained, 23
+// bias and gelu_tanh to codes 51 (41.3): a tile's nine steps of 128 features are summed before its 256 columns are drained, 23
 // warp instructions for 32 outputs, two values of the special function unit each, issue slots 38 % busy; 2048 x 4096 x 11008 with
-// silu to codes 73 (70); 16384 x 14336 x 4096 in fp32 with a residual 966 to 990 (930), 870 before the power limit sets in.
-// Tried: sixteen epilogue warps for codes (8192 x 1152 x 4608 50.7 with gelu_tanh, but 53.1 for 50.5 without an activation, and 74.7
-// for 72.7 at 4096 features); a long fp32 sum's parts added up in 128 registers a thread (960 for 966, but 84 for 76 where rows are
+// silu to codes 73 (70); 16384 x 14336 x 4096 in fp32 with a residual 966 to 990 (930), 870 before the power limit sets in.  In a
+// stream of such calls all of these are at that limit, 985 W, at 1.1 to 1.7 GHz.
+// Tried: a long fp32 sum's parts added up in 128 registers a thread (960 for 966, but 84 for 76 where rows are
 // not aligned: spills); tiles of 224 columns, whose accumulators share none (no difference).
-template <bool PAIR, typename TOut, bool FUSED = false>
-__global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
+template <bool PAIR, typename TOut, bool FUSED = false, int GROUPS = 2>
+__global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
     k_fp8_gemm(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
                const __grid_constant__ CUtensorMap tmap_x_tail, Fp8GemmParams p) {
   using SM = Fp8Smem<PAIR>;
   constexpr int BN = SM::BN;
-  constexpr int THREADS = FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, EPI_WARPS = THREADS / 32 - 4;
+  static_assert(GROUPS == 2 || (FUSED && GROUPS == FP8G_MOST_GROUPS), "groups of epilogue warps");
+  constexpr int THREADS = 128 + 128 * GROUPS, EPI_WARPS = THREADS / 32 - 4;
   extern __shared__ uint8_t fp8g_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(fp8g_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + SM::BAR_OFFSET);
@@ -390,7 +388,7 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
       ptx::mbar_init(&tempty[a], PAIR ? 2 * EPI_WARPS : EPI_WARPS);
     }
     if constexpr (sizeof(TOut) == 1) {
-      for (int g = 0; g < FP8G_FUSED_GROUPS; ++g) ptx::mbar_init(reinterpret_cast<uint64_t*>(smem + SM::EX_OFFSET) + g, 4);
+      for (int g = 0; g < GROUPS; ++g) ptx::mbar_init(reinterpret_cast<uint64_t*>(smem + SM::EX_OFFSET) + g, 4);
     }
     *abort_word = 0;
     ptx::fence_mbar_init();
@@ -655,7 +653,7 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
     }
   } else if constexpr (FUSED) {
     // ------------------------------------------------------------------ epilogue warps, with what follows the sum
-    constexpr int G = FP8G_FUSED_GROUPS;
+    constexpr int G = GROUPS;
     const int quarter = warp & 3;          // TMEM lanes this warp may touch
     const int group = (warp - 4) >> 2;     // which chunks of 32 columns it takes: every G-th
     const int g4 = lane >> 2, col = 2 * (lane & 3);   // its channels; its tokens of a chunk: 8 k + col + e, k = 0..3, e = 0, 1
@@ -717,7 +715,7 @@ __global__ void __launch_bounds__(FUSED ? FP8G_FUSED_THREADS : FP8G_THREADS, 1)
             return false;
           }
           ptx::tc_fence_after();
-          if (PAIR && group != fp8_overlap_group(a)) release();
+          if (PAIR && group != fp8_overlap_group(a, G)) release();
           return true;
         };
         // The largest magnitudes of a chunk's tokens over this warp's channels, one a lane, to those over the block's four warps:

@@ -119,6 +119,18 @@ def test_quantized_against_the_definition(st, M, K, N, act):  # noqa: F811
     assert st.stamp_last_device_status() == 0
 
 
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("M,K,N", [(3000, 640, 4112), (2300, 1024, 4112), (1700, 2048, 4096)])
+def test_quantized_pairs_against_the_definition(st, M, K, N, act):  # noqa: F811
+    assert st.stamp_debug_fp8_plan(M, N, K)[0]
+    x, xs, w, ws, bias = operands(st, M, K, N, seed=M + N)
+    want, off = expected(values(x, xs), values(w, ws, True), bias.double().cpu().numpy(), act)
+    for _ in range(2):
+        codes, scale = st.stamp_fp8_linear_quantized(x, xs, w, ws, bias=bias, activation=act_code(st, act))
+        check_quantized(codes, scale, want, off)
+    assert st.stamp_last_device_status() == 0
+
+
 # every kernel: single CTAs of each height, sums split by 2, 4 and 8, pairs of several heights; outputs that the tiles do not fill
 PLANS = [(1, 512, 128), (16, 4096, 512), (5, 2048, 130), (64, 4096, 384), (100, 1024, 2000), (512, 1024, 4096), (777, 2064, 4104), (1024, 640, 4096),
          (2048, 512, 4096), (1500, 1040, 11008), (4096, 256, 1152), (8, 8192, 64)]
