@@ -325,7 +325,8 @@ int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, co
 /* The same, quantized without being stored: codes [M, N] e4m3 and scale [M, ceil(N / 128)] e8m0 of act(x W^T + bias), as
  * stamp_fp8_quantize would write them for the fp32 values -- the operand of the next product.  N is a multiple of 16; codes
  * start on a 16-byte boundary and do not overlap x.  The sum is taken in one accumulator (2e-6 at 14336 features): a code differs from that of the
- * exact sum only where its value lies that near a rounding boundary. */
+ * exact sum only where its value lies that near a rounding boundary, and a block's scale (then twice the other, its codes half)
+ * only where the block's largest magnitude lies that near 448 times a power of two. */
 int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
                                int M, int N, int K, void* codes, void* scale, void* stream);
 
