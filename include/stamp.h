@@ -317,14 +317,16 @@ int stamp_fp8_linear_grouped(const void* x, const void* x_scale, const int32_t* 
  *               limit or a NaN                                                                              in
  *   residual    [M, N] r_dtype, rows ldr elements apart (ldr >= N), or NULL.  It may be Y itself (same type, ldr = N), which is
  *               then updated in place -- but not where an fp32 Y of more than 4096 features K has an activation
- *               (STAMP_ERR_INVALID_ARG); any other overlap with Y is refused likewise                               in */
+ *               (STAMP_ERR_INVALID_ARG); any other overlap with Y is refused likewise                               in
+ * Y may not share memory with x, the weights, their scales or the bias (STAMP_ERR_INVALID_ARG): other tiles still read them. */
 typedef enum { STAMP_ACT_NONE = 0, STAMP_ACT_RELU = 1, STAMP_ACT_GELU = 2, STAMP_ACT_GELU_TANH = 3, STAMP_ACT_SILU = 4 } stamp_activation;
 int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
                            const void* residual, int r_dtype, long long ldr, int M, int N, int K, void* Y, int y_dtype, void* stream);
 
 /* The same, quantized without being stored: codes [M, N] e4m3 and scale [M, ceil(N / 128)] e8m0 of act(x W^T + bias), as
  * stamp_fp8_quantize would write them for the fp32 values -- the operand of the next product.  N is a multiple of 16; codes
- * start on a 16-byte boundary and do not overlap x.  The sum is taken in one accumulator (2e-6 at 14336 features): a code differs from that of the
+ * start on a 16-byte boundary; neither codes nor scale may share memory with x, x_scale, the weights, their scales, the bias or each
+ * other (STAMP_ERR_INVALID_ARG).  The sum is taken in one accumulator (2e-6 at 14336 features): a code differs from that of the
  * exact sum only where its value lies that near a rounding boundary, and a block's scale (then twice the other, its codes half)
  * only where the block's largest magnitude lies that near 448 times a power of two. */
 int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,

@@ -3,6 +3,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <unordered_map>
 
@@ -1515,11 +1516,26 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
                                : launch_fp8_gemm<false, float>(tw, tx, txt, p, tiles, st);
 }
 
-// A residual [M, N] with rows ldr elements apart: aligned to its type, and apart from Y or Y itself.
 static bool overlap(const void* a, long a_bytes, const void* b, long b_bytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + b_bytes && y < x + a_bytes;
 }
+// Whether what is written shares memory with something that other CTAs may still read (nullptr: not given).
+struct Span {
+  const void* p;
+  long bytes;
+};
+static bool overlaps_any(const Span& out, std::initializer_list<Span> others) {
+  if (!out.p) return false;
+  for (const Span& s : others)
+    if (s.p && overlap(out.p, out.bytes, s.p, s.bytes)) return true;
+  return false;
+}
+static bool overlaps_operands(const Span& out, const Fp8GemmParams& p) {
+  const long M = p.M, N = p.N, K = p.K, ks = p.ks;
+  return overlaps_any(out, {{p.x, M * K}, {p.x_scale, M * ks}, {p.w, N * K}, {p.w_scale, (N + FP8_BLOCK - 1) / FP8_BLOCK * ks}, {p.bias, 4 * N}});
+}
+// A residual [M, N] with rows ldr elements apart: aligned to its type, and apart from Y or Y itself.
 static int check_residual(const void* residual, int r_dtype, long long ldr, long M, long N, const void* Y, int y_dtype) {
   if (!dtype_ok(r_dtype) || ldr < N) return STAMP_ERR_INVALID_ARG;
   if (M == 0) return STAMP_OK;
@@ -2257,6 +2273,7 @@ int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, co
     // the parts of a long fp32 sum are kept in Y until the activation can follow the last: too late for a residual there
     if (residual == Y && y_dtype == STAMP_F32 && activation != STAMP_ACT_NONE && K > FP8_PART) return STAMP_ERR_INVALID_ARG;
   }
+  if (M > 0 && overlaps_operands({Y, (long)M * N * (y_dtype == STAMP_BF16 ? 2 : 4)}, p)) return STAMP_ERR_INVALID_ARG;
   p.act = activation;
   p.residual = residual;
   p.r_bf16 = r_dtype == STAMP_BF16;
@@ -2273,7 +2290,10 @@ int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w
   if (int rc = check_fp8_product(p, STAMP_BF16)) return rc;
   if (activation < STAMP_ACT_NONE || activation > STAMP_ACT_SILU) return STAMP_ERR_INVALID_ARG;
   if (N % 16 != 0) return STAMP_ERR_UNSUPPORTED;
-  if (M > 0 && (!scale || !aligned16(codes) || overlap(codes, (long)M * N, x, (long)M * K))) return STAMP_ERR_INVALID_ARG;
+  if (M > 0) {
+    const Span out{codes, (long)M * N}, out_scale{scale, (long)M * ((N + FP8_BLOCK - 1L) / FP8_BLOCK)};
+    if (!scale || !aligned16(codes) || overlaps_operands(out, p) || overlaps_operands(out_scale, p) || overlaps_any(out, {out_scale})) return STAMP_ERR_INVALID_ARG;
+  }
   p.act = activation;
   p.words = 1;
   p.y_scale = static_cast<uint8_t*>(scale);

@@ -54,3 +54,20 @@ def test_the_marshalling_module_refuses_what_is_not_a_cuda_tensor(st):  # noqa: 
                 lambda: st.stamp_fp8_linear_quantized(1, s, c, s), lambda: st.calls().fp8_linear_fused(c), lambda: st.calls().fp8_linear_quantized(c)):
         with pytest.raises(ValueError):
             bad()
+
+
+FAR = 1 << 40
+
+
+# Another CTA may still read what one writes: an output shares no memory with an input, but for a residual updated in place.
+@pytest.mark.parametrize("call,bad", [
+    (fused, dict(x=FAR, Y=FAR)), (fused, dict(x=FAR, Y=FAR + 4 * 256 - 16)), (fused, dict(x=FAR + 4 * 64 * 2 - 16, Y=FAR)),
+    (fused, dict(xs=FAR, Y=FAR)), (fused, dict(xs=FAR + 4 * 64 * 2 - 1, Y=FAR)), (fused, dict(xs=FAR - 7, Y=FAR)),
+    (fused, dict(w=FAR, Y=FAR)), (fused, dict(ws=FAR + 2, Y=FAR)), (fused, dict(bias=FAR + 8, Y=FAR)),
+    (quantized, dict(xs=FAR, scale=FAR)), (quantized, dict(xs=FAR + 3, scale=FAR)), (quantized, dict(xs=FAR - 7, scale=FAR)), (quantized, dict(xs=FAR, codes=FAR)),
+    (quantized, dict(x=FAR, scale=FAR + 4 * 256 - 1)), (quantized, dict(codes=FAR, scale=FAR + 4 * 64 - 1)), (quantized, dict(codes=FAR, scale=FAR - 3)),
+    (quantized, dict(w=FAR, codes=FAR, scale=R)), (quantized, dict(ws=FAR, codes=FAR, scale=R)), (quantized, dict(bias=FAR, codes=FAR, scale=R)), (quantized, dict(w=FAR, scale=FAR)),
+])
+def test_outputs_over_inputs_are_refused(st, call, bad):  # noqa: F811
+    assert call(st, **{**(dict(codes=2 * FAR, scale=R) if call is quantized else {}), **bad}) == INVALID
+    assert st.stamp_last_launch_count() == 0
