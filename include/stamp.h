@@ -346,6 +346,7 @@ int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w
  *   rows      [T * top] int32: the rows (t, j) in the order of their experts, inside an expert in memory order: their t out
  *   place     [T, top] int32: where row (t, j) went; offsets [E + 1] int32; row_share [T * top] float: share by row   out
  *   ws        stamp_expert_route_workspace_bytes() bytes, 256-byte aligned (none up to 128 tokens: may be NULL)
+ * Outputs and scratch share no memory with the logits or each other (STAMP_ERR_INVALID_ARG).
  * E <= 1024, top <= min(E, 32), T * top <= 2^30.  T = 0 writes offsets (zeros) only. */
 int stamp_expert_route_workspace_bytes(int T, int E, int top, size_t* out_bytes);
 int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, int E, int top, int normalize, int32_t* chosen,
@@ -356,7 +357,7 @@ int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, in
  *   y        [M, N] y_dtype; place [T, top] int32; share [T, top] float                                             in
  *            A place outside [0, M) adds nothing and is reported by stamp_last_device_status() as STAMP_ERR_INVALID_ARG.
  *   residual [T, N] r_dtype, rows ldr elements apart, or NULL; it may be out itself (same type, ldr = N)            in
- *   out      [T, N] o_dtype; it may not overlap y (STAMP_ERR_INVALID_ARG)                                           out */
+ *   out      [T, N] o_dtype; it may not overlap y, place or share (STAMP_ERR_INVALID_ARG)                                           out */
 int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const float* share, const void* residual, int r_dtype,
                          long long ldr, int T, int top, int M, int N, void* out, int o_dtype, void* stream);
 
@@ -373,6 +374,8 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
  *   residual [T, N] r_dtype, rows ldr elements apart, or NULL; it may be Y itself (same type, ldr = N)              in
  *   Y        [T, N] y_dtype                                                                                         out
  *   ws       stamp_fp8_expert_workspace_bytes() bytes, 256-byte aligned
+ *            Y may be over X; it may not overlap rows, share, offsets, the way down's weights, scales and bias or ws, and ws nothing
+ *            at all (STAMP_ERR_INVALID_ARG).
  * T <= 64, M <= 2048, E <= 1024, K and F multiples of 16.  A token that holds an infinity or a NaN gets NaN. */
 int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes);
 int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int32_t* rows, const float* share, const int32_t* offsets,

@@ -1528,7 +1528,7 @@ struct Span {
 static bool overlaps_any(const Span& out, std::initializer_list<Span> others) {
   if (!out.p) return false;
   for (const Span& s : others)
-    if (s.p && overlap(out.p, out.bytes, s.p, s.bytes)) return true;
+    if (s.p && s.bytes > 0 && overlap(out.p, out.bytes, s.p, s.bytes)) return true;
   return false;
 }
 static bool overlaps_operands(const Span& out, const Fp8GemmParams& p) {
@@ -2318,6 +2318,17 @@ int stamp_expert_route(const void* logits, int l_dtype, long long ldl, int T, in
   if (ldl > (1LL << 60) / (T > 0 ? T : 1)) return STAMP_ERR_UNSUPPORTED;
   const int ctas = route_ctas(T);
   if (ctas > 1 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < (size_t)ctas * route_pitch(E) * 4)) return STAMP_ERR_WORKSPACE;
+  if (T > 0) {
+    const long rows_bytes = (long)T * top * 4;
+    const Span in{logits, ((T - 1) * (long)ldl + E) * (l_dtype == STAMP_BF16 ? 2 : 4)};
+    const Span out[7] = {{chosen, rows_bytes}, {share, rows_bytes}, {rows, rows_bytes}, {place, rows_bytes}, {offsets, (E + 1L) * 4}, {row_share, rows_bytes},
+                         {ctas > 1 ? ws : nullptr, (long)ctas * route_pitch(E) * 4}};
+    for (int i = 0; i < 7; ++i) {
+      if (overlaps_any(out[i], {in})) return STAMP_ERR_INVALID_ARG;
+      for (int j = 0; j < i; ++j)
+        if (overlaps_any(out[i], {out[j]})) return STAMP_ERR_INVALID_ARG;
+    }
+  }
   RouteParams p{};
   p.logits = logits;
   p.ldl = ldl;
@@ -2352,7 +2363,9 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
     return STAMP_ERR_INVALID_ARG;
   if (residual)
     if (int rc = check_residual(residual, r_dtype, ldr, T, N, out, o_dtype)) return rc;
-  if (M > 0 && overlap(y, (long)M * N * (y_dtype == STAMP_BF16 ? 2 : 4), out, (long)T * N * (o_dtype == STAMP_BF16 ? 2 : 4))) return STAMP_ERR_INVALID_ARG;
+  if (overlaps_any({out, (long)T * N * (o_dtype == STAMP_BF16 ? 2 : 4)},
+                   {{M > 0 ? y : nullptr, (long)M * N * (y_dtype == STAMP_BF16 ? 2 : 4)}, {place, (long)T * top * 4}, {share, (long)T * top * 4}}))
+    return STAMP_ERR_INVALID_ARG;
   const CombineParams p{y, place, share, residual, (long)ldr, T, top, M, N, out};
   const int r_bf16 = r_dtype == STAMP_BF16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -2397,6 +2410,16 @@ int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int3
   if (residual)
     if (int rc = check_residual(residual, r_dtype, ldr, T, N, Y, y_dtype)) return rc;
   if (M > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < expert_ws_bytes(M, F))) return STAMP_ERR_WORKSPACE;
+  // (the first kernel is through with the tokens when the second writes: Y may be over X)
+  const long x_size = x_dtype == STAMP_BF16 ? 2 : 4, k_blocks = (K + 127L) / 128, f_blocks = (F + 127L) / 128;
+  const Span out{Y, (long)T * N * (y_dtype == STAMP_BF16 ? 2 : 4)}, scratch{M > 0 ? ws : nullptr, (long)expert_ws_bytes(M, F)};
+  const Span rows_in{rows, M * 4L}, share_in{share, M * 4L}, offsets_in{offsets, (E + 1L) * 4}, down{w_down, (long)E * N * F},
+      down_s{down_scale, E * ((N + 127L) / 128) * f_blocks}, down_b{down_bias, (long)E * N * 4};
+  if (overlaps_any(out, {rows_in, share_in, offsets_in, down, down_s, down_b, scratch}) ||
+      overlaps_any(scratch, {rows_in, share_in, offsets_in, down, down_s, down_b, {X, ((T - 1) * (long)ldx + K) * x_size}, {w_up, (long)E * 2 * F * K},
+                             {up_scale, E * ((2L * F + 127) / 128) * k_blocks}, {up_bias, (long)E * 2 * F * 4},
+                             {residual, ((T - 1) * (long)ldr + N) * (r_dtype == STAMP_BF16 ? 2 : 4)}}))
+    return STAMP_ERR_INVALID_ARG;
   ExpertParams p{};
   p.x = X;
   p.ldx = ldx;

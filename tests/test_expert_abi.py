@@ -90,3 +90,21 @@ def test_the_marshalling_module_refuses_what_is_not_a_cuda_tensor(st):  # noqa: 
                 lambda: st.calls().expert_route(x), lambda: st.calls().expert_combine(x), lambda: st.calls().fp8_expert_layer(x)):
         with pytest.raises(ValueError):
             bad()
+
+
+FAR, Y = 1 << 40, 1 << 41
+SIX = dict(zip(("chosen", "share", "rows", "place", "offsets", "row_share"), (FAR + (i << 20) for i in range(6))))
+
+
+# Other CTAs, and the second kernel, may still read what one writes: outputs and scratch share no memory with each other nor with
+# what is read meanwhile.
+@pytest.mark.parametrize("call,bad", [
+    *((route, {a: SIX[b]}) for a in SIX for b in SIX if a < b), (route, dict(rows=SIX["place"] + 4 * 8 * 4 - 4)), (route, dict(offsets=SIX["share"] - 64 * 4)),
+    *((route, {a: A + 4 * 64 * 4 - 4}) for a in SIX), (route, dict(T=4096, ws=SIX["rows"], ws_bytes=1 << 20)), (route, dict(T=4096, ws=A, ws_bytes=1 << 20)),
+    (combine, dict(place=B)), (combine, dict(place=B - 4 * 2 * 4 + 4)), (combine, dict(share=B + 4 * 64 * 4 - 4)),
+    *((layer, {a: Y}) for a in ("rows", "share", "offsets", "down", "down_s", "down_b", "ws")), (layer, dict(offsets=Y - 12)), (layer, dict(ws=Y - 4096)),
+    *((layer, {a: FAR}) for a in ("X", "rows", "share", "offsets", "up", "up_s", "up_b", "down", "down_s", "down_b", "residual")),
+])
+def test_outputs_over_what_is_read_are_refused(st, call, bad):  # noqa: F811
+    assert call(st, **{**(SIX if call is route else dict(Y=Y, ws=FAR) if call is layer else {}), **bad}) == INVALID
+    assert st.stamp_last_launch_count() == 0

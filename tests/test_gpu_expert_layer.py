@@ -398,6 +398,27 @@ def test_the_example_decodes(st):  # noqa: F811
     check(y, *plain_layer(x.double().cpu().numpy(), rows, row_share, offsets, up, down, None, None, residual.double().cpu().numpy(), 7, 2.0 ** -20, 2.0 ** -13))
 
 
+@pytest.mark.parametrize("T", [1, 5, 64])
+def test_the_output_may_be_over_the_tokens(st, T):  # noqa: F811
+    """A step in place: tokens, residual and output are one matrix, or the output starts inside the tokens."""
+    import torch
+    for dtype in (torch.bfloat16, torch.float32):
+        layer = Layer(st, 6, 256, 384, 256, seed=T)
+        rows, share, offsets = routing([T, 1, 0, 1, T, 0], T, seed=T)
+        x = tokens(T, 256, str(dtype).split(".")[1], seed=T)
+        want, alone = layer(st, x, rows, share, offsets, residual=x), layer(st, x, rows, share, offsets)
+        for _ in range(4):
+            y = x.clone()
+            layer(st, y, rows, share, offsets, residual=y, out=y)
+            assert torch.equal(y, want)
+            room = torch.zeros(T * 256 + 128, dtype=dtype, device="cuda")
+            room[:T * 256] = x.view(-1)
+            y = room[128:].view(T, 256)
+            layer(st, room[:T * 256].view(T, 256), rows, share, offsets, out=y)
+            assert torch.equal(y, alone)
+    assert st.stamp_last_device_status() == 0
+
+
 def test_arguments_are_checked(st):  # noqa: F811
     import torch
     layer = Layer(st, 4, 128, 128, 128, seed=2)
