@@ -55,6 +55,7 @@ constexpr int EXPERT_FEW_ROWS = 2048;
 constexpr int EXPERT_MAX = 1024;
 constexpr int EXPERT_MAX_STAGES = 8, EXPERT_MAX_SPLIT = 16;
 constexpr int EXPERT_W_BYTES = 128 * 128;
+constexpr int EXPERT_PART = 32;                         // blocks of 128 features that one accumulator sums at most
 constexpr int EXPERT_MAX_SMEM = 224 * 1024;             // of a CTA that has an SM to itself; two of half of it fit one
 constexpr int EXPERT_H_BYTES = 2 * 8 * 128 * 4;         // UP: hidden values of eight rows on their way to terms, twice
 
@@ -93,9 +94,13 @@ struct ExpertSmem {
   static constexpr int SF_COLS = SF_BYTES / 128;
   static_assert(SF_COL + EXPERT_MAX_STAGES * SF_COLS <= TMEM && TMEM * CTAS <= 512, "tensor memory of an SM");
   static constexpr int BARS = 2 * EXPERT_MAX_STAGES + 6;
-  // after the ring and the scale words: barriers, [tmem, abort, runs, -], run table, UP: hidden values, tokens [M], DOWN: sums [T][128]
+  // after the ring and the scale words: barriers, [tmem, abort, runs, -], run table, UP: hidden values, tokens [M], sums of the parts
+  // before (PARTS) [row][gates, ups], DOWN: sums [T][128]
+  static constexpr int CARRIED_BYTES = COLUMNS / 2 * 256 * 4;   // (a row has two terms at least)
   __host__ __device__ static constexpr int tables(int max_runs) { return BARS * 8 + 16 + (max_runs * 8 + 15) / 16 * 16; }
-  __host__ __device__ static int fixed(int max_runs, int T, int M) { return 1024 + tables(max_runs) + (UP ? EXPERT_H_BYTES + M * 4 : T * 512); }
+  __host__ __device__ static int fixed(int max_runs, int T, int M, bool parts) {
+    return 1024 + tables(max_runs) + (UP ? EXPERT_H_BYTES + M * 4 + (parts ? CARRIED_BYTES : 0) : T * 512);
+  }
 };
 
 // Runs at most: an expert's rows end in one part run, and no more experts than rows have any.
@@ -168,7 +173,9 @@ __device__ __forceinline__ void expert_scale_words(uint8_t* words, int i, int t,
   *reinterpret_cast<uint32_t*>(words + ((r & 31) << 4) + ((r >> 5) << 2)) = expert_term_scale(first, t) * 0x01010101u;
 }
 
-template <bool UP, typename TOut>
+// PARTS (UP): a CTA's share of the features is more than one accumulator sums.  (A kernel of its own: with the parts' branches in it
+// the other takes 2 to 4 % longer, 55 tokens over 8 experts of 896 x 3456 70.5 us for 67.8.)
+template <bool UP, typename TOut, bool PARTS = false>
 __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
     k_expert_layer(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_h, ExpertParams p) {
   using SM = ExpertSmem<UP>;
@@ -188,6 +195,7 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
   float* const sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(full) + SM::tables(max_runs));
   float* const hidden = sums;
   int* const tokens = reinterpret_cast<int*>(hidden + EXPERT_H_BYTES / 4);
+  float* const carried = reinterpret_cast<float*>(tokens + p.M);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.split > 1 ? static_cast<int>(ptx::cluster_ctarank()) : 0;
@@ -266,14 +274,16 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
   const int runs = *run_count;
 
   // What this CTA sums.  UP: its share of the features, one tile (run, 128 channels) after the other; DOWN: its share of the
-  // sequence of (run, 128 features).
+  // sequence of (run, 128 features).  Either in parts of EXPERT_PART blocks: the tensor cores cut a running sum off instead of
+  // rounding it, and what that loses grows with the number of additions.
   const int blocks = ((UP ? p.K : p.F) + 127) / 128;   // of one run
   const int tiles = UP ? (p.F + 127) / 128 : 1;
-  int u0, u1, share0 = 0, share1 = blocks;
+  int u0, u1, share0 = 0, share1 = blocks, parts = 1;
   if constexpr (UP) {
-    u0 = unit;
-    u1 = runs > 0 ? runs * tiles : 0;
     if (p.split > 1) share0 = blocks * rank / p.split, share1 = blocks * (rank + 1) / p.split;
+    if constexpr (PARTS) parts = (share1 - share0 + EXPERT_PART - 1) / EXPERT_PART;
+    u0 = unit * parts;
+    u1 = runs > 0 ? runs * tiles * parts : 0;
   } else {
     const int all = runs > 0 ? runs * blocks : 0, each = all / p.split, more = all - each * p.split;
     u0 = each * rank + min(rank, more);
@@ -283,12 +293,18 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
     int kb0, kb1, tile, next;
     ExpertRun run;
   };
-  auto segment_at = [&](int u) {   // one tile; the part of one run that starts at u
+  auto segment_at = [&](int u) {   // one part of a tile; the part of one run that starts at u
     if constexpr (UP) {
-      const int r = u / tiles;
-      return Segment{share0, share1, u - r * tiles, u + static_cast<int>(gridDim.x) / p.split, run_table[r]};
+      const int step = static_cast<int>(gridDim.x) / p.split;
+      if constexpr (PARTS) {
+        const int t = u / parts, part = u - t * parts, r = t / tiles, kb0 = share0 + part * EXPERT_PART;
+        return Segment{kb0, min(share1, kb0 + EXPERT_PART), t - r * tiles, part + 1 < parts ? u + 1 : (t + step) * parts, run_table[r]};
+      } else {
+        const int r = u / tiles;
+        return Segment{share0, share1, u - r * tiles, u + step, run_table[r]};
+      }
     } else {
-      const int r = u / blocks, kb0 = u - r * blocks, kb1 = min(blocks, kb0 + u1 - u);
+      const int r = u / blocks, kb0 = u - r * blocks, kb1 = min(min(blocks, kb0 + EXPERT_PART), kb0 + u1 - u);
       return Segment{kb0, kb1, unit, u + kb1 - kb0, run_table[r]};
     }
   };
@@ -546,6 +562,19 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
           ptx::tc_fence_before();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&tempty[a]);
+        }
+        if constexpr (PARTS) {
+          // (every value of the parts before is this thread's own)
+          float* const before = carried + r0 * 256 + ch;
+          if (g.kb0 > share0) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] += before[r * 256], w[r] += before[r * 256 + 128];
+          }
+          if (g.kb1 < share1) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) before[r * 256] = v[r], before[r * 256 + 128] = w[r];
+            continue;
+          }
         }
         if constexpr (!UP) {
 #pragma unroll

@@ -1596,15 +1596,15 @@ static int check_route(int T, int E, int top) {
   return E > ROUTE_MAX_EXPERTS || top > ROUTE_MAX_TOP || (long)T * top > (1L << 30) ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
 }
 
-template <bool UP, typename TOut>
+template <bool UP, typename TOut, bool PARTS = false>
 static int launch_expert(ExpertParams p, long ctas, int smem, cudaStream_t st) {
   using SM = ExpertSmem<UP>;
-  auto kern = k_expert_layer<UP, TOut>;
+  auto kern = k_expert_layer<UP, TOut, PARTS>;
   if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), EXPERT_MAX_SMEM)) return rc;
   // (clusters of 16, which DOWN takes, are not portable; B200 has them)
   if (!UP && p.split > 8)
     if (int rc = ensure_large_clusters(reinterpret_cast<const void*>(kern))) return rc;
-  const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T, p.M);
+  const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T, p.M, PARTS);
   p.stage_bytes = (UP ? 2 : 1) * EXPERT_W_BYTES + (p.terms * p.cap + 15) / 16 * 16 * 128;
   p.stages = (smem - fixed) / (p.stage_bytes + SM::SF_BYTES);
   if (p.stages > EXPERT_MAX_STAGES) p.stages = EXPERT_MAX_STAGES;
@@ -1654,7 +1654,8 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
     // of 4096 19.2 / 23.6 / (18.5) / 24.2, 32 of 4096 27.7 / 23.6 / (21.5) / 34.2, 64 of 1152 (16.0) / 19.0 / 25.3 / 43.2.
     p.split = tiles * runs <= 8 && blocks >= 8 ? 8 : tiles * runs <= 32 && blocks >= 16 ? 4 : 1;
     const long ctas = p.split > 1 ? most * p.split : most < sms ? most : sms;
-    if (int rc = launch_expert<true, float>(p, ctas, EXPERT_MAX_SMEM, st)) return rc;
+    if (int rc = blocks > EXPERT_PART * p.split ? launch_expert<true, float, true>(p, ctas, EXPERT_MAX_SMEM, st) : launch_expert<true, float>(p, ctas, EXPERT_MAX_SMEM, st))
+      return rc;
   }
   p.terms = p.h_terms;
   p.cap = cap(ExpertSmem<false>::COLUMNS);
@@ -2382,8 +2383,10 @@ static int check_expert_layer(int T, int M, int E, int K, int F, int N) {
   if (T > EXPERT_FEW_TOKENS || M > EXPERT_FEW_ROWS || E > EXPERT_MAX || K % 16 != 0 || F % 16 != 0 || K > FP8_MAX_FEATURES || F > FP8_MAX_FEATURES / 2)
     return STAMP_ERR_UNSUPPORTED;
   if ((long)E * 2 * F > (1L << 31) - 512 || (long)E * N > (1L << 31) - 512) return STAMP_ERR_UNSUPPORTED;
-  // CTAs and steps are counted in 32 bits: runs of eight rows at least, clusters of eight CTAs at most (of sixteen for a few tiles)
-  return (long)expert_max_runs(M, E, 8) * ((F + 127L) / 128) * 8 > 0x7FFFFFFFL ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
+  // CTAs and steps are counted in 32 bits: runs of eight rows at least, clusters of eight CTAs at most (of sixteen for a few tiles); parts
+  // of tiles, as far as a round beyond the last
+  const long parts = 2 * ((K + 128L * EXPERT_PART - 1) / (128 * EXPERT_PART));
+  return (long)expert_max_runs(M, E, 8) * ((F + 127L) / 128) * (parts > 8 ? parts : 8) > 0x7FFFFFFFL ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
 }
 
 int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes) {

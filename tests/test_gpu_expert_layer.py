@@ -219,6 +219,35 @@ def test_integers_come_out_exact(st, T, counts, K, F, N):  # noqa: F811
     assert st.stamp_last_device_status() == 0
 
 
+@pytest.mark.parametrize("T,counts,K,F,N", [(1, [1, 0, 1], 34048, 128, 128), (3, [3, 0, 1, 2], 128, 8448, 257), (20, [1, 0, 4, 20] * 16, 8464, 144, 136),
+                                            (33, [33, 40], 4224, 4240, 136), (13, [13, 2, 5, 0, 1, 3], 12304, 784, 264)])
+def test_integers_come_out_exact_in_several_parts(st, T, counts, K, F, N):  # noqa: F811
+    """Sums of more than 4096 features, gates' and ups' as well as the way down's, in clusters and in one CTA."""
+    test_integers_come_out_exact(st, T, counts, K, F, N)
+
+
+@pytest.mark.parametrize("E,K,F", [(1, 262144, 128), (40, 65536, 16), (8, 16, 65536)], ids=["features, a cluster", "features, one CTA", "hidden channels"])
+def test_long_sums_are_taken_in_parts(st, E, K, F):  # noqa: F811
+    """The tensor cores cut a running sum off instead of rounding it: 4e-7 of a sum of 4096 features against 64 bits, as a share of
+    the norm, and more with every further feature of the same accumulator.  The errors of parts of 4096 add up like the parts
+    themselves, so that it is 4e-7 again, however long the sum.  Gates of 128 from their bias alone leave silu(g) = 128, bf16 tokens are held exactly, and fp32
+    hidden values' four terms are off by 2^-20 at most, 2^-20 / sqrt(3) as a root mean square: 6.8e-7 altogether, below 2^-20."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(E + K)
+    N = 256
+    x, up, down = torch.randn(E, K, generator=g, device="cuda").bfloat16(), torch.zeros(E, 2 * F, K, device="cuda"), torch.randn(E, N, F, generator=g, device="cuda")
+    up[:, F:] = torch.randn(E, F, K, generator=g, device="cuda")
+    (up, up_s), (down, down_s) = st.stamp_fp8_quantize_weights(up), st.stamp_fp8_quantize_weights(down)
+    up_bias = torch.zeros(E, 2 * F, device="cuda")
+    up_bias[:, :F] = 128.0
+    each = torch.arange(E + 1, dtype=torch.int32, device="cuda")
+    y = st.stamp_fp8_expert_layer(x, each[:-1].contiguous(), torch.ones(E, device="cuda"), each, up, up_s, down, down_s, up_bias=up_bias, out_dtype=torch.float32)
+    exact = lambda c, s: c.double() * s.double().repeat_interleave(BLOCK, 0)[:c.shape[0]].repeat_interleave(BLOCK, 1)[:, :c.shape[1]]  # noqa: E731
+    want = torch.stack([exact(down[e], down_s[e]) @ (128 * (exact(up[e], up_s[e])[F:] @ x[e].double())) for e in range(E)])
+    error = float((y.double() - want).norm() / want.norm())
+    assert error <= 2.0 ** -20, error
+
+
 def test_values_far_below_their_block_are_kept(st):  # noqa: F811
     """One large value in a block leaves the others 2^-20 of it: they still count to within 2^-20 of the large one."""
     import torch
