@@ -376,6 +376,9 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
  *   ws       stamp_fp8_expert_workspace_bytes() bytes, 256-byte aligned
  *            Y may be over X; it may not overlap rows, share, offsets, the way down's weights, scales and bias or ws, and ws nothing
  *            at all (STAMP_ERR_INVALID_ARG).
+ * Tokens and hidden values go into the 8-bit product as sums of e4m3 numbers: bf16 tokens exactly, but for values below 2^-14 of the
+ * largest of their block of 128 features, which are off by 2^-21 of that at most; fp32 tokens and hidden values to 2^-19 of the value or
+ * 2^-31 of their block's largest, whichever is more.
  * Sums of more than 4096 features (K or F) are taken in parts of 4096 at most, as the fp32 outputs of stamp_fp8_linear are.
  * T <= 64, M <= 2048, E <= 1024, K and F multiples of 16.  A token that holds an infinity or a NaN gets NaN. */
 int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes);

@@ -12,8 +12,8 @@
 //   further one by 2^-5 of what was left: two terms hold the 8 significant bits of a bf16 value, three 2^-14, four 2^-19.  Values
 //   more than 2^14 below their block's largest keep an error of 2^-24 of that.
 // A term is a column of the product like any other row's, so the terms cost columns (16 at least in any case), not another
-// pass over the weights; the epilogue adds them up.  bf16 tokens take two terms, fp32 ones four, the hidden values three for a
-// bf16 output and four for an fp32 one.  UP leaves the hidden values as terms already, DOWN copies them like the weights.
+// pass over the weights; the epilogue adds them up.  bf16 tokens take two terms, fp32 ones four, the hidden values four (three,
+// for a bf16 output, would do with 1 % less time and leave one output in a hundred at its other neighbour).  UP leaves the hidden values as terms already, DOWN copies them like the weights.
 //
 //   warps 0-3   epilogue, one TMEM lane (output channel) a thread
 //   warp 4      TMA producer: 128 channels x 128 features of weights (UP: of gates and of ups), DOWN: and of the rows' terms,
@@ -55,6 +55,7 @@ constexpr int EXPERT_FEW_ROWS = 2048;
 constexpr int EXPERT_MAX = 1024;
 constexpr int EXPERT_MAX_STAGES = 8, EXPERT_MAX_SPLIT = 16;
 constexpr int EXPERT_W_BYTES = 128 * 128;
+constexpr int EXPERT_H_TERMS = 4;                       // of a hidden value
 constexpr int EXPERT_PART = 32;                         // blocks of 128 features that one accumulator sums at most
 constexpr int EXPERT_MAX_SMEM = 224 * 1024;             // of a CTA that has an SM to itself; two of half of it fit one
 constexpr int EXPERT_H_BYTES = 2 * 8 * 128 * 4;         // UP: hidden values of eight rows on their way to terms, twice
@@ -76,7 +77,7 @@ struct ExpertParams {
   uint8_t* h_scale;         // [M, ceil(F / 128)] scale of a row's first term
   void* y;                  // [T, N]
   // one kernel's plan
-  int terms, h_terms;       // terms of a row; of a hidden value
+  int terms;                // of a row
   int cap;                  // rows of a run at most (a multiple of 8, terms * cap <= columns)
   int split;                // CTAs of a cluster
   int stages, stage_bytes;
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
   auto store_hidden = [&](float4 h, long row, int tile) {
     const int f = tile * 128 + lane * 4;
     const float v[4] = {h.x, h.y, h.z, h.w};
-    const uint32_t first = expert_terms(v, p.h_terms, [&](int t, uint32_t c) {
+    const uint32_t first = expert_terms(v, EXPERT_H_TERMS, [&](int t, uint32_t c) {
       if (f < p.F) *reinterpret_cast<uint32_t*>(p.h + (static_cast<long>(t) * p.M + row) * p.F + f) = c;
     });
     if (lane == 0) p.h_scale[row * tiles + tile] = static_cast<uint8_t>(first);

@@ -1641,7 +1641,6 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
     const int most = columns / p.terms & ~7;
     return tokens < most ? tokens : most;
   };
-  p.h_terms = y_dtype == STAMP_BF16 ? 3 : 4;
   const long sms = sm_count();
   if (p.M > 0) {
     p.terms = p.x_bf16 ? 2 : 4;
@@ -1657,7 +1656,7 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
     if (int rc = blocks > EXPERT_PART * p.split ? launch_expert<true, float, true>(p, ctas, EXPERT_MAX_SMEM, st) : launch_expert<true, float>(p, ctas, EXPERT_MAX_SMEM, st))
       return rc;
   }
-  p.terms = p.h_terms;
+  p.terms = EXPERT_H_TERMS;
   p.cap = cap(ExpertSmem<false>::COLUMNS);
   const long tiles = (p.N + 127L) / 128;
   // As many CTAs as SMs have room for at once, half as many again where each still has enough to do (more than that, and clusters
@@ -2375,8 +2374,8 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
   return o_dtype == STAMP_BF16 ? launch_combine<float, __nv_bfloat16>(p, r_bf16, st) : launch_combine<float, float>(p, r_bf16, st);
 }
 
-// The hidden values' codes (four terms at most) and scales.
-static size_t expert_ws_bytes(int M, int F) { return align256((size_t)M * F * 4) + align256((size_t)M * ((F + 127L) / 128)); }
+// The hidden values' codes and scales.
+static size_t expert_ws_bytes(int M, int F) { return align256((size_t)M * F * EXPERT_H_TERMS) + align256((size_t)M * ((F + 127L) / 128)); }
 
 static int check_expert_layer(int T, int M, int E, int K, int F, int N) {
   if (T < 0 || M < 0 || E <= 0 || K <= 0 || F <= 0 || N <= 0) return STAMP_ERR_INVALID_ARG;
@@ -2441,7 +2440,7 @@ int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int3
   p.r_bf16 = r_dtype == STAMP_BF16;
   p.T = T, p.M = M, p.E = E, p.K = K, p.F = F, p.N = N;
   p.h = static_cast<uint8_t*>(ws);
-  p.h_scale = p.h + align256((size_t)M * F * 4);
+  p.h_scale = p.h + align256((size_t)M * F * EXPERT_H_TERMS);
   p.y = Y;
   return run_expert_layer(p, y_dtype, static_cast<cudaStream_t>(stream));
 }

@@ -226,6 +226,18 @@ def test_integers_come_out_exact_in_several_parts(st, T, counts, K, F, N):  # no
     test_integers_come_out_exact(st, T, counts, K, F, N)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T,counts,K,F,N", [(1, [1, 0, 1], 1152, 2048, 1152), (13, [2, 0, 13, 1, 0, 5], 400, 272, 257), (64, [64, 33, 1, 16], 512, 640, 520)])
+def test_the_output_type_costs_its_own_rounding_only(st, T, counts, K, F, N, dtype):  # noqa: F811
+    """A bf16 output is the fp32 output rounded once: hidden values and sums do not depend on it."""
+    import torch
+    layer = Layer(st, len(counts), K, F, N, seed=K, bias=True)
+    rows, share, offsets = routing(counts, T, seed=T)
+    x, residual = tokens(T, K, dtype, seed=1), tokens(T, N, dtype, seed=2)
+    wide, narrow = (layer(st, x, rows, share, offsets, residual=residual, out_dtype=t) for t in (torch.float32, torch.bfloat16))
+    assert torch.equal(narrow, wide.bfloat16())
+
+
 @pytest.mark.parametrize("E,K,F", [(1, 262144, 128), (40, 65536, 16), (8, 16, 65536)], ids=["features, a cluster", "features, one CTA", "hidden channels"])
 def test_long_sums_are_taken_in_parts(st, E, K, F):  # noqa: F811
     """The tensor cores cut a running sum off instead of rounding it: 4e-7 of a sum of 4096 features against 64 bits, as a share of
