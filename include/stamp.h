@@ -446,6 +446,10 @@ int stamp_debug_expire_wait(long long limit_cycles, void* stream);
  * which state the kernel they mean. */
 int stamp_debug_fp8_plan(int M, int E, int N, int K, int y_dtype, int* pair, int* rows, int* split);
 
+/* The same for the two kernels of stamp_fp8_expert_layer: the CTAs that share a tile of the first (gates and ups) and of the second
+ * (the way down).  M > 0. */
+int stamp_debug_expert_plan(int T, int M, int E, int K, int F, int N, int x_dtype, int* up_split, int* down_split);
+
 /* Measurement: the rate of the tensor cores' int8 instruction alone.  Launches one CTA per SM; each issues
  * nbatch * 64 tcgen05.mma kind::i8 instructions (M128 x N256 x K32, int32 accumulators in tensor memory) on
  * operand tiles that stay in shared memory -- no loads in the loop, waits bounded -- and *ops_out receives the

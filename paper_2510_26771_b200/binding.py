@@ -31,7 +31,7 @@ EXPORTS = (
     "stamp_fp8_quantize", "stamp_fp8_gated_quantize", "stamp_fp8_quantize_weights", "stamp_fp8_linear",
     "stamp_fp8_linear_grouped", "stamp_debug_fp8_plan", "stamp_fp8_linear_fused", "stamp_fp8_linear_quantized",
     "stamp_expert_route_workspace_bytes", "stamp_expert_route", "stamp_expert_combine", "stamp_fp8_expert_workspace_bytes",
-    "stamp_fp8_expert_layer",
+    "stamp_fp8_expert_layer", "stamp_debug_expert_plan",
 )
 
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
@@ -452,6 +452,14 @@ def stamp_debug_fp8_plan(M: int, N: int, K: int, experts: int = 0, out_dtype=tor
     dtype = _dtype_code(torch.empty(0, dtype=out_dtype))
     _check(lib().stamp_debug_fp8_plan(M, experts, N, K, dtype, *map(ctypes.byref, out)), "stamp_debug_fp8_plan")
     return bool(out[0].value), out[1].value, out[2].value
+
+
+def stamp_debug_expert_plan(T: int, rows: int, experts: int, features: int, hidden: int, outputs: int, dtype=torch.bfloat16):
+    """(up, down): the CTAs that share a tile of stamp_fp8_expert_layer's first and second kernel at these sizes."""
+    out = [ctypes.c_int() for _ in range(2)]
+    code = _dtype_code(torch.empty(0, dtype=dtype))
+    _check(lib().stamp_debug_expert_plan(T, rows, experts, features, hidden, outputs, code, *map(ctypes.byref, out)), "stamp_debug_expert_plan")
+    return out[0].value, out[1].value
 
 
 def stamp_last_launch_count() -> int:

@@ -1635,30 +1635,39 @@ static int launch_expert(ExpertParams p, long ctas, int smem, cudaStream_t st) {
   return STAMP_OK;
 }
 
-static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
-  const int tokens = (p.T + 7) & ~7;
-  auto cap = [&](int columns) {   // rows of a run: as many as there are tokens, as far as their terms have columns
-    const int most = columns / p.terms & ~7;
-    return tokens < most ? tokens : most;
-  };
-  const long sms = sm_count();
-  if (p.M > 0) {
-    p.terms = p.x_bf16 ? 2 : 4;
-    p.cap = cap(ExpertSmem<true>::COLUMNS);
-    const long tiles = (p.F + 127L) / 128, runs = p.E < p.M ? p.E : p.M, most = tiles * expert_max_runs(p.M, p.E, p.cap);
-    const int blocks = (p.K + 127) / 128;
-    // One CTA a tile, each SM one after the other, unless there are few tiles; then four or eight share one, where each has
-    // features enough to make up for the exchange and the clusters find their SMs at once.  One token, in us, with 1 / 2 / 4 / 8
-    // (the choice in brackets): 4 tiles of 1024 features 11.8 / 12.2 / 11.8 / (11.6), 8 of 2048 14.3 / 13.9 / 13.0 / (12.6), 16
-    // of 4096 19.2 / 23.6 / (18.5) / 24.2, 32 of 4096 27.7 / 23.6 / (21.5) / 34.2, 64 of 1152 (16.0) / 19.0 / 25.3 / 43.2.
-    p.split = tiles * runs <= 8 && blocks >= 8 ? 8 : tiles * runs <= 32 && blocks >= 16 ? 4 : 1;
-    const long ctas = p.split > 1 ? most * p.split : most < sms ? most : sms;
-    if (int rc = blocks > EXPERT_PART * p.split ? launch_expert<true, float, true>(p, ctas, EXPERT_MAX_SMEM, st) : launch_expert<true, float>(p, ctas, EXPERT_MAX_SMEM, st))
-      return rc;
-  }
+// Runs there can well be: as many as experts have rows, or as it takes to hold them all.
+static long expert_runs(const ExpertParams& p) {
+  const long used = p.E < p.M ? p.E : p.M, full = ((long)p.M + p.cap - 1) / p.cap;
+  return used > full ? used : full;
+}
+// Rows of a run: as many as there are tokens, as far as their terms have columns.
+static int expert_cap(const ExpertParams& p, int columns) {
+  const int tokens = (p.T + 7) & ~7, most = columns / p.terms & ~7;
+  return tokens < most ? tokens : most;
+}
+
+// Terms, rows of a run and CTAs of a tile of the first kernel; the CTAs of its grid.
+static long plan_expert_up(ExpertParams& p) {
+  p.terms = p.x_bf16 ? 2 : 4;
+  p.cap = expert_cap(p, ExpertSmem<true>::COLUMNS);
+  const long tiles = (p.F + 127L) / 128, all = tiles * expert_runs(p), most = tiles * expert_max_runs(p.M, p.E, p.cap), sms = sm_count();
+  const int blocks = (p.K + 127) / 128;
+  // One CTA a tile, each SM one after the other, unless there are few tiles (of a run each); then four or eight share one, where
+  // each has features enough to make up for the exchange and the clusters find their SMs at once.  One token, in us, with 1 / 2 / 4 / 8
+  // (the choice in brackets): 4 tiles of 1024 features 11.8 / 12.2 / 11.8 / (11.6), 8 of 2048 14.3 / 13.9 / 13.0 / (12.6), 16
+  // of 4096 19.2 / 23.6 / (18.5) / 24.2, 32 of 4096 27.7 / 23.6 / (21.5) / 34.2, 64 of 1152 (16.0) / 19.0 / 25.3 / 43.2.  Many rows for
+  // each expert, the whole layer, with 1 / 4 / 8: 64 tokens to all of 8 experts of 4096 x 512, 128 tiles (57.2) / 89.8 / 136, fp32, 256
+  // tiles (66.4) / 131 / 216; of 2048 x 256, 64 tiles (34.4) / 43.1 / 66.8; to one of 4096 x 1024, 32 tiles 41.5 / (31.0) / 46.1; to both
+  // of two of 4096 x 128, 8 tiles 36.7 / 24.4 / (21.7).
+  p.split = all <= 8 && blocks >= 8 ? 8 : all <= 32 && blocks >= 16 ? 4 : 1;
+  return p.split > 1 ? most * p.split : most < sms ? most : sms;
+}
+
+// The same of the second kernel.
+static long plan_expert_down(ExpertParams& p) {
   p.terms = EXPERT_H_TERMS;
-  p.cap = cap(ExpertSmem<false>::COLUMNS);
-  const long tiles = (p.N + 127L) / 128;
+  p.cap = expert_cap(p, ExpertSmem<false>::COLUMNS);
+  const long tiles = (p.N + 127L) / 128, sms = sm_count();
   // As many CTAs as SMs have room for at once, half as many again where each still has enough to do (more than that, and clusters
   // find their SMs late), sixteen to a tile where there are few tiles and enough to do.  Us, by CTAs of a tile, the choice in
   // brackets: 32 tiles, 13 tokens over 32 experts of 4096 x 4096, four: 160.2, six: 154.5, (seven: 152.5), eight: 163.4; one
@@ -1667,15 +1676,25 @@ static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
   // tokens over 16 of 2048, eight: 42.2, (sixteen: 39.9); 9 tiles, one token of four of 2048, four: 17.4, (eight: 16.4), sixteen: 16.9;
   // 7 tiles, 55 tokens over 8 of 3456, eight: 79.8, (sixteen: 67.4); fewer steps, one token of eight of 640, 28 tiles, (four: 21.2),
   // five: 22.1, two tokens of eight of 1024, 11 tiles, (eight: 21.3), sixteen: 22.4.
-  const long steps = (long)(p.E < p.M ? p.E : p.M) * ((p.F + 127) / 128);   // (run, 128 features) of a tile, about
+  const long steps = expert_runs(p) * ((p.F + 127) / 128);   // (run, 128 features) of a tile, about
   p.split = 1;
   while (p.split < 8 && tiles * p.split * 2 <= sms) p.split *= 2;
   for (int split = p.split + 1; split <= 8; ++split)
     if (tiles * split * 2 <= 3 * sms + 8 && steps >= 16L * split) p.split = split;
   if (p.split == 8 && tiles <= 12 && steps >= 12L * 16) p.split = 16;
+  return tiles * p.split;
+}
+
+static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
+  if (p.M > 0) {
+    const long ctas = plan_expert_up(p);
+    const bool parts = (p.K + 127) / 128 > EXPERT_PART * p.split;
+    if (int rc = parts ? launch_expert<true, float, true>(p, ctas, EXPERT_MAX_SMEM, st) : launch_expert<true, float>(p, ctas, EXPERT_MAX_SMEM, st)) return rc;
+  }
+  const long ctas = plan_expert_down(p);
   // (two CTAs to an SM: with more than half of its shared memory a cluster of eight finds its SMs too late)
-  return y_dtype == STAMP_BF16 ? launch_expert<false, __nv_bfloat16>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st)
-                               : launch_expert<false, float>(p, tiles * p.split, EXPERT_MAX_SMEM / 2, st);
+  return y_dtype == STAMP_BF16 ? launch_expert<false, __nv_bfloat16>(p, ctas, EXPERT_MAX_SMEM / 2, st)
+                               : launch_expert<false, float>(p, ctas, EXPERT_MAX_SMEM / 2, st);
 }
 
 template <typename TIn, typename TOut>
@@ -2457,6 +2476,20 @@ int stamp_debug_fp8_plan(int M, int E, int N, int K, int y_dtype, int* pair, int
   *pair = plan.pair ? 1 : 0;
   *rows = plan.bn;
   *split = plan.split;
+  return STAMP_OK;
+}
+
+int stamp_debug_expert_plan(int T, int M, int E, int K, int F, int N, int x_dtype, int* up_split, int* down_split) {
+  t_launches = 0;
+  if (!up_split || !down_split || T <= 0 || M <= 0 || !dtype_ok(x_dtype)) return STAMP_ERR_INVALID_ARG;
+  if (int rc = check_expert_layer(T, M, E, K, F, N)) return rc;
+  ExpertParams p{};
+  p.x_bf16 = x_dtype == STAMP_BF16;
+  p.T = T, p.M = M, p.E = E, p.K = K, p.F = F, p.N = N;
+  plan_expert_up(p);
+  *up_split = p.split;
+  plan_expert_down(p);
+  *down_split = p.split;
   return STAMP_OK;
 }
 

@@ -108,3 +108,21 @@ SIX = dict(zip(("chosen", "share", "rows", "place", "offsets", "row_share"), (FA
 def test_outputs_over_what_is_read_are_refused(st, call, bad):  # noqa: F811
     assert call(st, **{**(SIX if call is route else dict(Y=Y, ws=FAR) if call is layer else {}), **bad}) == INVALID
     assert st.stamp_last_launch_count() == 0
+
+
+@pytest.mark.parametrize("T,M,E,K,F,dtype,up", [(1, 4, 16, 1152, 2048, "bfloat16", 1), (1, 4, 16, 4096, 512, "bfloat16", 4), (1, 1, 8, 1024, 512, "float32", 8),
+                                                (64, 512, 8, 4096, 512, "bfloat16", 1), (64, 512, 8, 4096, 512, "float32", 1), (64, 512, 8, 2048, 256, "bfloat16", 1),
+                                                (64, 64, 1, 4096, 1024, "bfloat16", 4), (64, 64, 1, 4096, 1024, "float32", 1), (64, 128, 2, 4096, 128, "bfloat16", 8),
+                                                (64, 128, 2, 4096, 128, "float32", 4), (64, 512, 64, 2048, 2048, "bfloat16", 1)])
+def test_tiles_of_the_first_kernel_are_shared_where_they_are_few(st, T, M, E, K, F, dtype, up):  # noqa: F811
+    """A tile is 128 channels of one run, and an expert's rows make a run for every 16 (fp32 tokens: 8) of them: a cluster takes one
+    tile only, so that many short rounds of whole SMs would come of counting experts instead (on 148 SMs)."""
+    import torch
+    assert st.stamp_debug_expert_plan(T, M, E, K, F, K, dtype=getattr(torch, dtype))[0] == up
+
+
+def test_plans_of_what_is_refused(st):  # noqa: F811
+    out = [ctypes.byref(ctypes.c_int()) for _ in range(2)]
+    f = st.lib().stamp_debug_expert_plan
+    assert f(4, 8, 3, 256, 128, 64, BF16, *out) == OK and f(4, 8, 3, 256, 128, 64, BF16, None, out[1]) == INVALID
+    assert f(4, 0, 3, 256, 128, 64, BF16, *out) == INVALID and f(4, 8, 3, 256, 128, 64, 2, *out) == INVALID and f(65, 8, 3, 256, 128, 64, BF16, *out) == UNSUPPORTED
