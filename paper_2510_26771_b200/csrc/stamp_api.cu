@@ -1668,20 +1668,23 @@ static long plan_expert_down(ExpertParams& p) {
   p.terms = EXPERT_H_TERMS;
   p.cap = expert_cap(p, ExpertSmem<false>::COLUMNS);
   const long tiles = (p.N + 127L) / 128, sms = sm_count();
-  // As many CTAs as SMs have room for at once, half as many again where each still has enough to do (more than that, and clusters
-  // find their SMs late), sixteen to a tile where there are few tiles and enough to do.  Us, by CTAs of a tile, the choice in
-  // brackets: 32 tiles, 13 tokens over 32 experts of 4096 x 4096, four: 160.2, six: 154.5, (seven: 152.5), eight: 163.4; one
-  // token of two such experts, (four: 27.3), eight: 30.6; 28 tiles, 24 tokens over 60 of 656, four: 65.2, (eight: 57.4), twelve:
-  // 68.4; 16 tiles, 64 tokens over 64 of 2048, six: 163.2, (eight: 151.0), ten: 146.2, twelve: 155.9, sixteen: 167.0; 12 tiles, 40
-  // tokens over 16 of 2048, eight: 42.2, (sixteen: 39.9); 9 tiles, one token of four of 2048, four: 17.4, (eight: 16.4), sixteen: 16.9;
-  // 7 tiles, 55 tokens over 8 of 3456, eight: 79.8, (sixteen: 67.4); fewer steps, one token of eight of 640, 28 tiles, (four: 21.2),
-  // five: 22.1, two tokens of eight of 1024, 11 tiles, (eight: 21.3), sixteen: 22.4.
+  // CTAs of a tile: a power of two with one CTA an SM; where each still has enough to do, as many as find their SMs at once, ten at
+  // most; sixteen where there are few tiles.  Two CTAs fit an SM, but a cluster's have to lie together: up to 1.6 CTAs an SM it still
+  // pays to add one (236 on 148 SMs), from 240 on clusters wait for others.  Layers of 13 tokens over 32 experts of 4096 hidden channels / 24
+  // over 60 of 656 / 64 over 64 of 2048, in us, by CTAs of a tile: 118 tiles, one 288.2 / 170.2 / 518.6, two (236) 240.8 / 121.2 / 350.4; 33 tiles, six 113.3 / 46.9 / 140.0, seven (231) 112.1 / 45.0 / 139.8,
+  // eight (264) 137.9 / 50.6 / 172.0; 32 tiles, six 119.6 / 50.3 / 139.2, seven (224) 118.4 / 48.4 / 138.7, eight (256) 123.4 / 50.3 / 153.6; 29
+  // tiles, seven 102.3 / 46.3 / 130.4, eight (232) 100.6 / 46.0 / 130.4, nine (261) 105.4 / 46.1 / 151.0; 24 tiles, eight 86.9 / 43.0 / 124.7, nine
+  // (216) 86.6 / 42.0 / 121.7, ten (240) 88.5 / 42.9 / 135.4; 16 tiles, eight 78.1 / 39.4 / 109.9, ten (160) 74.9 / 37.5 / 102.6.  Clusters of eleven
+  // and more find their SMs at some numbers of tiles and not at others (16 tiles, twelve 74.7 / 36.7 / 100.7, thirteen 76.2 / 36.4 / 114.8, fourteen 93.7 /
+  // 50.6 / 128.6); sixteen up to twelve tiles: 12 tiles, ten 75.6 / 38.5 / 99.9, sixteen 72.8 / 36.5 / 90.9.  Enough to do are sixteen steps for
+  // each (twelve for each of sixteen): with fewer, one token over four of 16 experts of 2048, 28 tiles, (four 19.3), five 18.8, eight 19.8; 9 tiles, four 17.8, (eight
+  // 16.6), sixteen 17.0.
   const long steps = expert_runs(p) * ((p.F + 127) / 128);   // (run, 128 features) of a tile, about
   p.split = 1;
   while (p.split < 8 && tiles * p.split * 2 <= sms) p.split *= 2;
-  for (int split = p.split + 1; split <= 8; ++split)
-    if (tiles * split * 2 <= 3 * sms + 8 && steps >= 16L * split) p.split = split;
-  if (p.split == 8 && tiles <= 12 && steps >= 12L * 16) p.split = 16;
+  for (int split = p.split + 1; split <= 10; ++split)
+    if (5 * tiles * split <= 8 * sms && steps >= 16L * split) p.split = split;
+  if (p.split >= 8 && tiles <= 12 && steps >= 12L * 16) p.split = 16;
   return tiles * p.split;
 }
 

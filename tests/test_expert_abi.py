@@ -121,6 +121,19 @@ def test_tiles_of_the_first_kernel_are_shared_where_they_are_few(st, T, M, E, K,
     assert st.stamp_debug_expert_plan(T, M, E, K, F, K, dtype=getattr(torch, dtype))[0] == up
 
 
+@pytest.mark.parametrize("tiles,down", [(5, 16), (12, 16), (13, 10), (16, 10), (23, 10), (24, 9), (26, 9), (27, 8), (28, 8), (29, 8), (30, 7), (32, 7), (33, 7), (34, 6),
+                                        (39, 6), (40, 5), (47, 5), (48, 4), (59, 4), (60, 3), (78, 3), (79, 2), (118, 2), (119, 1)])
+def test_ctas_of_the_second_kernels_tiles(st, tiles, down):  # noqa: F811
+    """The rule where every CTA has enough to do: as many to a tile as leave 1.6 CTAs an SM at most (on 148 SMs)."""
+    for T, M, E, F in ((13, 52, 32, 4096), (64, 512, 64, 2048), (55, 440, 8, 3456)):
+        assert st.stamp_debug_expert_plan(T, M, E, 1024, F, 128 * tiles)[1] == down
+    # little to do: one CTA an SM
+    split = 1
+    while split < 8 and tiles * split * 2 <= 148:
+        split *= 2
+    assert st.stamp_debug_expert_plan(1, 1, 16, 1024, 256, 128 * tiles)[1] == split
+
+
 def test_plans_of_what_is_refused(st):  # noqa: F811
     out = [ctypes.byref(ctypes.c_int()) for _ in range(2)]
     f = st.lib().stamp_debug_expert_plan
