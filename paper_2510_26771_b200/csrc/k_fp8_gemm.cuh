@@ -140,26 +140,26 @@ __device__ __forceinline__ uint32_t fp8_scale_word(const uint8_t* ptr, int n, bo
   return b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24);
 }
 
-// The order in which the two halves of the epilogue warps drain an accumulator: chunks of 32 columns, chunk c by half c & 1
-// whichever accumulator it is.  A sum in several parts is added up in the output, accumulator after accumulator, and
-// nothing orders the halves among each other: a chunk has to stay with one of them.  PAIR: the chunk whose columns the
-// accumulators share, the eighth of the first and the first of the second, comes first.
-__host__ __device__ constexpr int fp8_drain_chunk(bool descending, int half, int i, int count) {
-  return half + 2 * (descending ? count - 1 - i : i);
+// The order in which the groups of epilogue warps (two, the plain form's halves, or four) drain an accumulator: chunks of 32
+// columns, chunk c by group c % groups whichever accumulator it is.  A sum in several parts is added up in the output, accumulator
+// after accumulator, and nothing orders the groups among each other: a chunk has to stay with one of them.  PAIR: the chunk whose
+// columns the accumulators share, the eighth of the first and the first of the second, comes first; who has none of it hands the
+// accumulator back at once.
+__host__ __device__ constexpr int fp8_drain_chunks(int chunks, int group, int groups) { return (chunks - group + groups - 1) / groups; }
+__host__ __device__ constexpr int fp8_drain_chunk(bool descending, int group, int i, int count, int groups) {
+  return group + groups * (descending ? count - 1 - i : i);
 }
-__host__ __device__ constexpr int fp8_overlap_half(int accumulator) { return accumulator == 0 ? 1 : 0; }
-// FUSED, with two or four groups of warps: chunk c by group c % groups, the last first in the first accumulator.
 __host__ __device__ constexpr int fp8_overlap_group(int accumulator, int groups) { return accumulator == 0 ? 7 % groups : 0; }
-constexpr bool fp8_drain_order_holds() {
+constexpr bool fp8_drain_order_holds(int groups) {
   for (int chunks = 1; chunks <= 8; ++chunks)
     for (int a = 0; a < 2; ++a) {
       unsigned taken = 0;
-      for (int half = 0; half < 2; ++half) {
-        const int count = (chunks - half + 1) / 2;
+      for (int group = 0; group < groups; ++group) {
+        const int count = fp8_drain_chunks(chunks, group, groups);
         for (int i = 0; i < count; ++i) {
-          const int c = fp8_drain_chunk(a == 0, half, i, count);
-          if ((c & 1) != half || c < 0 || c >= chunks || (taken >> c & 1u) != 0u) return false;
-          if (c == (a == 0 ? 7 : 0) && (half != fp8_overlap_half(a) || i != 0)) return false;
+          const int c = fp8_drain_chunk(a == 0, group, i, count, groups);
+          if (c % groups != group || c < 0 || c >= chunks || (taken >> c & 1u) != 0u) return false;
+          if (c == (a == 0 ? 7 : 0) && (group != fp8_overlap_group(a, groups) || i != 0)) return false;
           taken |= 1u << c;
         }
       }
@@ -167,7 +167,7 @@ constexpr bool fp8_drain_order_holds() {
     }
   return true;
 }
-static_assert(fp8_drain_order_holds(), "every chunk once, by the same half in both accumulators, the shared columns first");
+static_assert(fp8_drain_order_holds(2) && fp8_drain_order_holds(4), "every chunk once, by the same group in both accumulators, the shared columns first");
 
 // Two adjacent channels of one token.
 __device__ __forceinline__ void fp8_store2(float* y, float a, float b, bool both, bool vec) {
@@ -694,8 +694,8 @@ __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
         // first part too: the output, which holds the parts, may be the residual's own memory.
         const bool whole = PAIR || p.split == 1;
         const bool add = sizeof(TOut) != 1 && p.residual && whole && (p.act == STAMP_ACT_NONE ? first : last);
-        const int chunks = (t.n + 31) / 32, count = (chunks - group + G - 1) / G;
-        auto chunk_at = [&](int i) { return group + G * (PAIR && a == 0 ? count - 1 - i : i); };
+        const int count = fp8_drain_chunks((t.n + 31) / 32, group, G);
+        auto chunk_at = [&](int i) { return fp8_drain_chunk(PAIR && a == 0, group, i, count, G); };
         if (first) prefetch_residual(tile + tile_step);
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(a * SM::ACC1);
         bool released = false;
@@ -975,7 +975,6 @@ __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
         }
         ptx::tc_fence_after();
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(a * SM::ACC1);
-        const int chunks = (t.n + 31) / 32;
         bool released = false;
         auto release = [&]() {
           ptx::tc_fence_before();
@@ -986,10 +985,10 @@ __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
           released = true;
         };
         // PAIR: the chunk that overlaps the other accumulator first; who has none of it hands back at once
-        if (PAIR && half != fp8_overlap_half(a)) release();
-        const int count = (chunks - half + 1) / 2;
+        if (PAIR && half != fp8_overlap_group(a, 2)) release();
+        const int count = fp8_drain_chunks((t.n + 31) / 32, half, 2);
         for (int i = 0; i < count; ++i) {
-          const int c = fp8_drain_chunk(PAIR && a == 0, half, i, count);
+          const int c = fp8_drain_chunk(PAIR && a == 0, half, i, count, 2);
           uint32_t r[32];
           ptx::tmem_ld_32x32b_x32(taddr + 32 * c, r);
           ptx::tmem_ld_wait();
