@@ -283,17 +283,12 @@ __device__ __forceinline__ void tmem_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)
 __device__ __forceinline__ void tmem_ld_32x32b_x1(uint32_t taddr, uint32_t& r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
 }
-// 16 lanes x 8 X columns (X = 1, 2 or 4), eight columns at a time: register 4 k + 2 h + e of thread i is lane
+// 16 lanes x 8 X columns (X = 2 or 4), eight columns at a time: register 4 k + 2 h + e of thread i is lane
 // (base + i / 4 + 8 h), column 8 k + 2 (i % 4) + e.
 template <int X>
 __device__ __forceinline__ void tmem_ld_16x256b(uint32_t taddr, uint32_t (&r)[4 * X]) {
-  static_assert(X == 1 || X == 2 || X == 4, "");
-  if constexpr (X == 1)
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(taddr)
-                 : "memory");
-  else if constexpr (X == 2)
+  static_assert(X == 2 || X == 4, "");
+  if constexpr (X == 2)
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(taddr)
