@@ -196,8 +196,8 @@ __device__ __forceinline__ void fp8_store2(__nv_bfloat16* y, float a, float b, b
 //              that the result is within about (5 |2 u| + 18) 2^-24 of itself.
 //   GELU       v Phi(v), Phi(-x) = exp(-x^2 / 2) R(x) for x >= 0 (1 + erf would cancel in the lower tail).  R(x), half the scaled
 //              complementary error function of x / sqrt 2, is t P(1 - 2 t) with t = 1 / (1 + x / 3): a least-squares fit of
-//              degree 8, reweighted towards the smallest largest relative error (2^-24.4 for x <= 14, where exp(-x^2 / 2)
-//              vanishes).  In fp32, a reciprocal off by an ulp included, R is within 2^-21; all in all 2^-20.
+//              degree 8, reweighted towards the smallest largest relative error (2^-23.3 for x <= 14, where exp(-x^2 / 2)
+//              vanishes, with the coefficients rounded to fp32).  In fp32, a reciprocal off by an ulp included, R is within 2^-21; all in all 2^-20.
 // An infinite sum comes out non-finite.
 enum Fp8Act { FP8_LINEAR, FP8_GELU, FP8_GELU_TANH, FP8_SILU };
 template <int ACT>
