@@ -168,6 +168,28 @@ def test_quantized_integers_come_out_exact(st, M, K, N):  # noqa: F811
     assert st.stamp_last_device_status() == 0
 
 
+@pytest.mark.parametrize("K,spread,error", [(4096, False, 4e-7), (14336, False, 2.3e-6), (4096, True, 2.3e-6), (14336, True, 1.6e-5)])
+@pytest.mark.parametrize("M,N", [(1024, 4096), (200, 528)])
+def test_long_quantized_sums_are_as_near_as_stated(st, M, N, K, spread, error):  # noqa: F811
+    """What the header says of the one accumulator, for the inputs it names, as a share of the outputs' root mean square; no single
+    sum is taken to be further off than eight times that."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(K + N)
+    x = torch.randn(M, K, generator=g, device="cuda")
+    x *= torch.where(torch.rand(K, generator=g, device="cuda") < 0.01, 30.0, 1.0)
+    w = 0.02 * torch.randn(N, K, generator=g, device="cuda")
+    x, xs = st.stamp_fp8_quantize(x)
+    w, ws = st.stamp_fp8_quantize_weights(w)
+    if spread:
+        xs = (torch.randint(-7, 3, xs.shape, generator=g, device="cuda") + 127).to(torch.uint8).view(torch.float8_e8m0fnu)
+    exact = lambda c, s, rows: c.double() * s.double().repeat_interleave(BLOCK, 1)[:, :K].repeat_interleave(rows, 0)[:c.shape[0]]  # noqa: E731
+    want = exact(x, xs, 1) @ exact(w, ws, BLOCK).t()
+    off = torch.full_like(want, 8 * error * float(want.square().mean().sqrt()))
+    codes, scale = st.stamp_fp8_linear_quantized(x, xs, w, ws)
+    check_quantized(codes, scale, want.cpu().numpy(), off.cpu().numpy())
+    assert st.stamp_last_device_status() == 0
+
+
 @pytest.mark.parametrize("K", [4096, 4224, 8704, 14336])
 @pytest.mark.parametrize("M,N", [(777, 4104), (1024, 4096), (140, 520)])
 def test_long_fp32_sums_are_activated_once(st, M, N, K):  # noqa: F811
