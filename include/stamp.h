@@ -381,10 +381,9 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
  *   ws       stamp_fp8_expert_workspace_bytes() bytes, 256-byte aligned
  *            Y may be over X; it may not overlap rows, share, offsets, the way down's weights, scales and bias or ws, and ws nothing
  *            at all (STAMP_ERR_INVALID_ARG).
- * Tokens and hidden values go into the 8-bit product as sums of e4m3 numbers: bf16 tokens exactly, but for values below 2^-14 of the
- * largest of their block of 128 features, which are off by 2^-21 of that at most; fp32 tokens and hidden values to 2^-19 of the value or
- * 2^-31 of their block's largest, whichever is more.
- * Sums of more than 4096 features (K or F) are taken in parts of 4096 at most, as the fp32 outputs of stamp_fp8_linear are.
+ * Tokens and hidden values go into the 8-bit product as sums of e4m3 numbers: bf16 tokens to their 8 significant bits or 2^-21 of
+ * the largest of their block of 128 features, whichever is more; fp32 tokens to 2^-24 of the value or 2^-36 of the largest; hidden values to 2^-19
+ * or 2^-31, for either output type.  Sums of more than 2048 features are taken in parts of 2048 at most.
  * T <= 64, M <= 2048, E <= 1024, K and F multiples of 16.  A token that holds an infinity or a NaN gets NaN. */
 int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes);
 int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int32_t* rows, const float* share, const int32_t* offsets,

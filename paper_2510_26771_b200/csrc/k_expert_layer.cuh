@@ -2,24 +2,27 @@
 //   h[m, f] = silu(g) u,  g = w_up[e, f] . x[rows[m]] + up_bias[e, f],  u the same for row F + f      (e: the expert of row m)
 //   y[t]    = residual[t] + sum over the rows m of token t of share[m] (w_down[e] h[m] + down_bias[e])
 //
-// With few tokens a layer is the way of its weights from memory: each byte is read once and meets a handful of rows.  The
+// With few tokens a layer is the way of its weights from memory: each byte meets a handful of rows.  (An expert's weights are read
+// once for every run of its rows: UP 16 of bf16 tokens or 8 of fp32 ones, DOWN 16; all but the first time mostly from L2.)  The
 // weights are e4m3 already, so they go by TMA to shared memory and from there into the block-scaled tensor instruction
 // (kind::mxf8f6f4, channels on the TMEM lanes, rows as columns) without passing a register.  The activations are not e4m3;
 // quantizing them would be the layer's largest error and saves nothing here.  They are written as a sum of e4m3 terms
 // instead, each with its own power-of-two scale for a block of 128:
-//   v = c0 s + c1 s 2^-4 + c2 s 2^-9 + c3 s 2^-14,   s the quantizer's scale of the block, c_i the nearest e4m3 number to
-//   what is left.  The first term is off by at most 2^-4 of v (16 s at the top of the range, hence the step to 2^-4), every
-//   further one by 2^-5 of what was left: two terms hold the 8 significant bits of a bf16 value, three 2^-14, four 2^-19.  Values
-//   more than 2^14 below their block's largest keep an error of 2^-24 of that.
+//   v = c0 s + c1 s 2^-4 + c2 s 2^-9 + c3 s 2^-14 + c4 s 2^-19,   s the quantizer's scale of the block, c_i the nearest e4m3 number
+//   to what is left.  The first term is off by at most 2^-4 of v (16 s at the top of the range, hence the step to 2^-4) and every further
+//   one by 2^-5 of that: two terms hold the 8 significant bits of a bf16 value, four 2^-19, five the 24 bits of an fp32 one.  e4m3
+//   numbers end in steps of 2^-9, so that two terms hold nothing below 2^-14 s (2^-21.8 of the block's largest value), four
+//   nothing below 2^-24 s (2^-31.8), five nothing below 2^-29 s (2^-36.8).
 // A term is a column of the product like any other row's, so the terms cost columns (16 at least in any case), not another
-// pass over the weights; the epilogue adds them up.  bf16 tokens take two terms, fp32 ones four, the hidden values four (three,
-// for a bf16 output, would do with 1 % less time and leave one output in a hundred at its other neighbour).  UP leaves the hidden values as terms already, DOWN copies them like the weights.
+// pass over the weights; the epilogue adds them up.  bf16 tokens take two terms, fp32 ones five, the hidden values four: three, for a bf16
+// output, would do with 1 % less time and leave one output in a hundred at its other neighbour.  UP leaves the hidden values as
+// terms already, DOWN copies them like the weights.
 //
 //   warps 0-3   epilogue, one TMEM lane (output channel) a thread
 //   warp 4      TMA producer: 128 channels x 128 features of weights (UP: of gates and of ups), DOWN: and of the rows' terms,
 //               into a ring of stages
 //   warp 5      allocates TMEM, copies the scale words to it and issues the MMAs
-//   warps 6-13  the scales, UP: and the tokens' terms.  Always the same warps for a stage of the ring: who fills it has filled
+//   warps 6-13  (UP: 6-15) the scales, UP: and the tokens' terms.  Always the same warps for a stage of the ring: who fills it has filled
 //               it the time before too, so that the parity it waits for is never an older one's, and it can load the stage's
 //               next rows as soon as it is through with the last
 // Every wait is bounded; when one expires the CTA raises the device status word, unwinds and frees its TMEM.
@@ -56,14 +59,16 @@ constexpr int EXPERT_MAX = 1024;
 constexpr int EXPERT_MAX_STAGES = 8, EXPERT_MAX_SPLIT = 16;
 constexpr int EXPERT_W_BYTES = 128 * 128;
 constexpr int EXPERT_H_TERMS = 4;                       // of a hidden value
-constexpr int EXPERT_PART = 32;                         // blocks of 128 features that one accumulator sums at most
+// Blocks of 128 features that one accumulator sums at most: half as many as for the products' fp32 outputs, since three sums one after
+// the other add up their errors.  13 tokens over 32 experts of 4096 x 4096 in bf16, fp32 output: 1.3e-6 of the result from 64 bits, with
+// parts of 32 blocks 1.75e-6 and 0.3 % less time, in one part 2.8e-6.
+constexpr int EXPERT_PART = 16;
 constexpr int EXPERT_MAX_SMEM = 224 * 1024;             // of a CTA that has an SM to itself; two of half of it fit one
 constexpr int EXPERT_H_BYTES = 2 * 8 * 128 * 4;         // UP: hidden values of eight rows on their way to terms, twice
 
 struct ExpertParams {
   const void* x;            // [T, ldx] bf16 or float
   long ldx;
-  int x_bf16;
   const int* rows;          // [M] token of every row
   const float* share;       // [M]
   const int* offsets;       // [E + 1]
@@ -77,30 +82,31 @@ struct ExpertParams {
   uint8_t* h_scale;         // [M, ceil(F / 128)] scale of a row's first term
   void* y;                  // [T, N]
   // one kernel's plan
-  int terms;                // of a row
-  int cap;                  // rows of a run at most (a multiple of 8, terms * cap <= columns)
+  int cap;                  // rows of a run at most (a multiple of 8)
   int split;                // CTAs of a cluster
   int stages, stage_bytes;
 };
 
-template <bool UP>
+// T: UP: the tokens' type, DOWN: the output's.
+template <bool UP, typename T>
 struct ExpertSmem {
+  static constexpr int TERMS = !UP ? EXPERT_H_TERMS : sizeof(T) == 2 ? 2 : 5;   // of a row
+  static constexpr int ROWS = UP && sizeof(T) == 4 ? 8 : 16;                    // of a run at most
   static constexpr int FILLERS = UP ? 10 : 8;           // warps that write scales (UP: and terms)
   static constexpr int THREADS = 32 * (6 + FILLERS);
   static constexpr int CTAS = UP ? 1 : 2;               // of an SM that the registers allow
-  static constexpr int COLUMNS = UP ? 32 : 64;          // of one sum
-  static constexpr int ACC = 64;                        // tensor memory: two accumulators (UP: gates, ups), then the stages' scales
-  static constexpr int SF_COL = 2 * ACC, TMEM = 256;
+  static constexpr int COLUMNS = (TERMS * ROWS + 15) / 16 * 16;   // of one sum
+  static constexpr int ACC = UP ? 2 * COLUMNS : COLUMNS;   // tensor memory: two accumulators (UP: gates, ups), then the stages' scales
   static constexpr int SF_BYTES = UP ? 1536 : 1024;     // scale words of a stage: channels (UP: twice), then rows
-  static constexpr int SF_COLS = SF_BYTES / 128;
+  static constexpr int SF_COLS = SF_BYTES / 128, SF_COL = 2 * ACC, TMEM = SF_COL + EXPERT_MAX_STAGES * SF_COLS <= 256 ? 256 : 512;
   static_assert(SF_COL + EXPERT_MAX_STAGES * SF_COLS <= TMEM && TMEM * CTAS <= 512, "tensor memory of an SM");
   static constexpr int BARS = 2 * EXPERT_MAX_STAGES + 6;
   // after the ring and the scale words: barriers, [tmem, abort, runs, -], run table, UP: hidden values, tokens [M], sums of the parts
   // before (PARTS) [row][gates, ups], DOWN: sums [T][128]
-  static constexpr int CARRIED_BYTES = COLUMNS / 2 * 256 * 4;   // (a row has two terms at least)
+  static constexpr int CARRIED_BYTES = ROWS * 256 * 4;
   __host__ __device__ static constexpr int tables(int max_runs) { return BARS * 8 + 16 + (max_runs * 8 + 15) / 16 * 16; }
-  __host__ __device__ static int fixed(int max_runs, int T, int M, bool parts) {
-    return 1024 + tables(max_runs) + (UP ? EXPERT_H_BYTES + M * 4 + (parts ? CARRIED_BYTES : 0) : T * 512);
+  __host__ __device__ static int fixed(int max_runs, int tokens, int M, bool parts) {
+    return 1024 + tables(max_runs) + (UP ? EXPERT_H_BYTES + M * 4 + (parts ? CARRIED_BYTES : 0) : tokens * 512);
   }
 };
 
@@ -119,26 +125,26 @@ __device__ __forceinline__ float2 expert_e4m3x2(uint32_t two) {
 }
 
 // Four neighbouring features of a row, as loaded.
-struct ExpertRaw {
-  uint4 u;
-  __device__ __forceinline__ void load(const void* base, long at, bool bf16, bool live) {
-    u = make_uint4(0u, 0u, 0u, 0u);
-    if (!live) return;
-    if (bf16) {
-      const uint2 v = __ldcg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(base) + at));
-      u.x = v.x, u.y = v.y;
-    } else {
-      u = __ldcg(reinterpret_cast<const uint4*>(static_cast<const float*>(base) + at));
-    }
+template <typename T>
+struct ExpertRaw;
+template <>
+struct ExpertRaw<__nv_bfloat16> {
+  uint2 u;
+  __device__ __forceinline__ void load(const void* base, long at, bool live) {
+    u = live ? __ldcg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(base) + at)) : make_uint2(0u, 0u);
   }
-  __device__ __forceinline__ void values(bool bf16, float (&v)[4]) const {
-    if (bf16) {
-      v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
-      v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
-    } else {
-      v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
-    }
+  __device__ __forceinline__ void values(float (&v)[4]) const {
+    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
   }
+};
+template <>
+struct ExpertRaw<float> {
+  float4 u;
+  __device__ __forceinline__ void load(const void* base, long at, bool live) {
+    u = live ? __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(base) + at)) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void values(float (&v)[4]) const { v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w; }
 };
 
 // The scale of term t, from the first term's (which stops at 2^-127; a NaN's terms are all NaN).
@@ -147,19 +153,20 @@ __device__ __forceinline__ uint32_t expert_term_scale(uint32_t first, int t) {
   return first == 255u ? 255u : first - min(first, down);
 }
 // 128 values of a row, four a lane, as terms: emit(t, codes) for each; returns the scale byte of the first.
-template <typename Emit>
-__device__ __forceinline__ uint32_t expert_terms(const float (&value)[4], int terms, Emit&& emit) {
+template <int TERMS, typename Emit>
+__device__ __forceinline__ uint32_t expert_terms(const float (&value)[4], Emit&& emit) {
   const float most = ptx::warp_max_abs(ptx::max_abs_nan(ptx::max_abs_nan(value[0], value[1], value[2]), value[3], 0.f));
   const Fp8Scale s = fp8_scale(__float_as_uint(most));
   float v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = value[i] * s.inverse;
-  for (int t = 0;;) {
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t) {
     const uint32_t c = ptx::cvt_e4m3x4(v[0], v[1], v[2], v[3]);
     emit(t, c);
-    if (++t == terms) break;
+    if (t + 1 == TERMS) break;
     // what is left, in units of the next term's scale
-    const uint32_t shift = s.byte == 255 ? 0u : expert_term_scale(s.byte, t - 1) - expert_term_scale(s.byte, t);
+    const uint32_t shift = s.byte == 255 ? 0u : expert_term_scale(s.byte, t) - expert_term_scale(s.byte, t + 1);
     const float up = __uint_as_float((127u + shift) << 23);
     const float2 a = expert_e4m3x2(c), b = expert_e4m3x2(c >> 16);
     v[0] = (v[0] - a.x) * up, v[1] = (v[1] - a.y) * up, v[2] = (v[2] - b.x) * up, v[3] = (v[3] - b.y) * up;
@@ -176,10 +183,11 @@ __device__ __forceinline__ void expert_scale_words(uint8_t* words, int i, int t,
 
 // PARTS (UP): a CTA's share of the features is more than one accumulator sums.  (A kernel of its own: with the parts' branches in it
 // the other takes 2 to 4 % longer, 55 tokens over 8 experts of 896 x 3456 70.5 us for 67.8.)
-template <bool UP, typename TOut, bool PARTS = false>
-__global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
+template <bool UP, typename T, bool PARTS = false>
+__global__ void __launch_bounds__(ExpertSmem<UP, T>::THREADS, ExpertSmem<UP, T>::CTAS)
     k_expert_layer(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_h, ExpertParams p) {
-  using SM = ExpertSmem<UP>;
+  using SM = ExpertSmem<UP, T>;
+  constexpr int TERMS = SM::TERMS;
   extern __shared__ uint8_t expert_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(expert_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* const words = smem + p.stages * p.stage_bytes;
@@ -309,13 +317,13 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
       return Segment{kb0, kb1, unit, u + kb1 - kb0, run_table[r]};
     }
   };
-  const auto columns = [&](int n) { return p.terms * ((n + 7) & ~7); };
+  const auto columns = [&](int n) { return TERMS * ((n + 7) & ~7); };
 
   // UP: four hidden values a lane of one row's 128, as terms (F is a multiple of 16: a lane's channels are all there or none)
   auto store_hidden = [&](float4 h, long row, int tile) {
     const int f = tile * 128 + lane * 4;
     const float v[4] = {h.x, h.y, h.z, h.w};
-    const uint32_t first = expert_terms(v, EXPERT_H_TERMS, [&](int t, uint32_t c) {
+    const uint32_t first = expert_terms<EXPERT_H_TERMS>(v, [&](int t, uint32_t c) {
       if (f < p.F) *reinterpret_cast<uint32_t*>(p.h + (static_cast<long>(t) * p.M + row) * p.F + f) = c;
     });
     if (lane == 0) p.h_scale[row * tiles + tile] = static_cast<uint8_t>(first);
@@ -330,7 +338,7 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
       // DOWN: the weights of the first round go ahead of the hidden values, whose kernel may still run
       auto copy_hidden = [&](const Segment& g, int kb, int at) {
         for (int r = 0; r < g.run.n; r += 8)
-          ptx::tma_load_3d(smem + at * p.stage_bytes + EXPERT_W_BYTES + r * p.terms * 128, &tmap_h, &full[at], kb * 128, g.run.row0 + r, 0);
+          ptx::tma_load_3d(smem + at * p.stage_bytes + EXPERT_W_BYTES + r * TERMS * 128, &tmap_h, &full[at], kb * 128, g.run.row0 + r, 0);
       };
       auto first_hidden = [&]() {
         ptx::grid_dependency_wait();
@@ -428,7 +436,6 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
     uint8_t* const xt = smem + stage * p.stage_bytes + 2 * EXPERT_W_BYTES;
     uint8_t* const sf = words + stage * SM::SF_BYTES;
     uint8_t* const rf = sf + SM::SF_BYTES - 512;
-    const bool bf16 = p.x_bf16;
     int i = 0, s = stage;   // steps before this segment; the next one that goes to this warp's stage
     uint32_t phase = 0;
     bool ok = true, waited = UP;
@@ -448,13 +455,13 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
         const int kb = g.kb0 + s - i;
         // everything the stage needs is loaded before it is waited for, UP: as far as eight rows for each warp
         uint32_t w0 = __ldcg(sc + static_cast<long>(g.tile) * blocks + kb), w1 = 0, w2 = 0;
-        ExpertRaw raw[8];
+        ExpertRaw<T> raw[8];
         auto load = [&](int r0) {
           const int col = kb * 128 + lane * 4;
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
             const int t = __shfl_sync(0xffffffffu, token, (r0 + r * each) & 31);
-            raw[r].load(p.x, t * p.ldx + col, bf16, r0 + r * each < n && t >= 0 && col < p.K);
+            raw[r].load(p.x, t * p.ldx + col, r0 + r * each < n && t >= 0 && col < p.K);
           }
         };
         if constexpr (UP) {
@@ -485,18 +492,18 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
               const int row = r0 + r * each;
               if (row >= n) break;
               float v[4];
-              raw[r].values(bf16, v);
+              raw[r].values(v);
               // (rows of 128 bytes, 128-byte swizzle; a term's columns are eight further)
-              uint8_t* const out = xt + expert_column(row, 0, p.terms) * 128 + (((lane >> 2) ^ (row & 7)) << 4) + ((lane & 3) << 2);
-              const uint32_t first = expert_terms(v, p.terms, [&](int t, uint32_t c) { *reinterpret_cast<uint32_t*>(out + t * 1024) = c; });
-              if (lane < p.terms) expert_scale_words(rf, row, lane, p.terms, first);
+              uint8_t* const out = xt + expert_column(row, 0, TERMS) * 128 + (((lane >> 2) ^ (row & 7)) << 4) + ((lane & 3) << 2);
+              const uint32_t first = expert_terms<TERMS>(v, [&](int t, uint32_t c) { *reinterpret_cast<uint32_t*>(out + t * 1024) = c; });
+              if (lane < TERMS) expert_scale_words(rf, row, lane, TERMS, first);
             }
             r0 += 8 * each;
             if (r0 < n) load(r0);
           }
         } else {
           if (lane < n) {
-            for (int t = 0; t < p.terms; ++t) expert_scale_words(rf, lane, t, p.terms, w1);
+            for (int t = 0; t < TERMS; ++t) expert_scale_words(rf, lane, t, TERMS, w1);
           }
         }
         ptx::fence_proxy_async_smem();
@@ -517,19 +524,16 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
     int it = 0;
     // eight rows' sums at this thread's channel, their terms added up, the smallest first
     auto eight = [&](uint32_t acc, int r0, float (&v)[8]) {
-      uint32_t c[4][8];
+      uint32_t c[TERMS][8];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (t < p.terms) ptx::tmem_ld_32x32b_x8(acc + r0 * p.terms + t * 8, c[t]);
+      for (int t = 0; t < TERMS; ++t) ptx::tmem_ld_32x32b_x8(acc + r0 * TERMS + t * 8, c[t]);
       ptx::tmem_ld_wait();
 #pragma unroll
       for (int r = 0; r < 8; ++r) v[r] = 0.f;
 #pragma unroll
-      for (int t = 3; t >= 0; --t)
-        if (t < p.terms) {
+      for (int t = TERMS - 1; t >= 0; --t)
 #pragma unroll
-          for (int r = 0; r < 8; ++r) v[r] += __uint_as_float(c[t][r]);
-        }
+        for (int r = 0; r < 8; ++r) v[r] += __uint_as_float(c[t][r]);
     };
     uint32_t exchanged = 0;
     for (int u = u0; u < u1 && ok; ++it) {
@@ -680,12 +684,12 @@ __global__ void __launch_bounds__(ExpertSmem<UP>::THREADS, ExpertSmem<UP>::CTAS)
       for (int t = rank + warp * p.split; t < p.T; t += SM::THREADS / 32 * p.split) {
         const float4 sum = total(t * 128 + lane * 4);
         const float y[4] = {sum.x, sum.y, sum.z, sum.w};
-        TOut* const out = static_cast<TOut*>(p.y) + static_cast<long>(t) * p.N + c;
+        T* const out = static_cast<T*>(p.y) + static_cast<long>(t) * p.N + c;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (c + i >= p.N) break;
           const float v = y[i] + (t == rank + warp * p.split ? ahead[i] : residual(t, c + i));
-          if constexpr (sizeof(TOut) == 2) out[i] = __float2bfloat16_rn(v); else out[i] = v;
+          if constexpr (sizeof(T) == 2) out[i] = __float2bfloat16_rn(v); else out[i] = v;
         }
       }
     }

@@ -1596,23 +1596,23 @@ static int check_route(int T, int E, int top) {
   return E > ROUTE_MAX_EXPERTS || top > ROUTE_MAX_TOP || (long)T * top > (1L << 30) ? STAMP_ERR_UNSUPPORTED : STAMP_OK;
 }
 
-template <bool UP, typename TOut, bool PARTS = false>
+template <bool UP, typename T, bool PARTS = false>
 static int launch_expert(ExpertParams p, long ctas, int smem, cudaStream_t st) {
-  using SM = ExpertSmem<UP>;
-  auto kern = k_expert_layer<UP, TOut, PARTS>;
+  using SM = ExpertSmem<UP, T>;
+  auto kern = k_expert_layer<UP, T, PARTS>;
   if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), EXPERT_MAX_SMEM)) return rc;
   // (clusters of 16, which DOWN takes, are not portable; B200 has them)
   if (!UP && p.split > 8)
     if (int rc = ensure_large_clusters(reinterpret_cast<const void*>(kern))) return rc;
   const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T, p.M, PARTS);
-  p.stage_bytes = (UP ? 2 : 1) * EXPERT_W_BYTES + (p.terms * p.cap + 15) / 16 * 16 * 128;
+  p.stage_bytes = (UP ? 2 : 1) * EXPERT_W_BYTES + (SM::TERMS * p.cap + 15) / 16 * 16 * 128;
   p.stages = (smem - fixed) / (p.stage_bytes + SM::SF_BYTES);
   if (p.stages > EXPERT_MAX_STAGES) p.stages = EXPERT_MAX_STAGES;
   CUtensorMap tm, th;
   if (int rc = UP ? make_tmap_i8(p.w_up, (long)p.E * 2 * p.F, p.K, 128, &tm) : make_tmap_i8(p.w_down, (long)p.E * p.N, p.F, 128, &tm)) return rc;
   th = tm;
   if (!UP && p.M > 0)
-    if (int rc = make_tmap_terms(p.h, p.M, p.F, p.terms, &th)) return rc;
+    if (int rc = make_tmap_terms(p.h, p.M, p.F, SM::TERMS, &th)) return rc;
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3((unsigned)ctas);
   lc.blockDim = dim3(SM::THREADS);
@@ -1640,16 +1640,15 @@ static long expert_runs(const ExpertParams& p) {
   const long used = p.E < p.M ? p.E : p.M, full = ((long)p.M + p.cap - 1) / p.cap;
   return used > full ? used : full;
 }
-// Rows of a run: as many as there are tokens, as far as their terms have columns.
-static int expert_cap(const ExpertParams& p, int columns) {
-  const int tokens = (p.T + 7) & ~7, most = columns / p.terms & ~7;
+// Rows of a run: as many as there are tokens, `most` at most.
+static int expert_cap(const ExpertParams& p, int most) {
+  const int tokens = (p.T + 7) & ~7;
   return tokens < most ? tokens : most;
 }
 
-// Terms, rows of a run and CTAs of a tile of the first kernel; the CTAs of its grid.
-static long plan_expert_up(ExpertParams& p) {
-  p.terms = p.x_bf16 ? 2 : 4;
-  p.cap = expert_cap(p, ExpertSmem<true>::COLUMNS);
+// Rows of a run and CTAs of a tile of the first kernel; the CTAs of its grid.
+static long plan_expert_up(ExpertParams& p, int x_dtype) {
+  p.cap = expert_cap(p, x_dtype == STAMP_BF16 ? ExpertSmem<true, __nv_bfloat16>::ROWS : ExpertSmem<true, float>::ROWS);
   const long tiles = (p.F + 127L) / 128, all = tiles * expert_runs(p), most = tiles * expert_max_runs(p.M, p.E, p.cap), sms = sm_count();
   const int blocks = (p.K + 127) / 128;
   // One CTA a tile, each SM one after the other, unless there are few tiles (of a run each); then four or eight share one, where
@@ -1665,8 +1664,7 @@ static long plan_expert_up(ExpertParams& p) {
 
 // The same of the second kernel.
 static long plan_expert_down(ExpertParams& p) {
-  p.terms = EXPERT_H_TERMS;
-  p.cap = expert_cap(p, ExpertSmem<false>::COLUMNS);
+  p.cap = expert_cap(p, ExpertSmem<false, float>::ROWS);
   const long tiles = (p.N + 127L) / 128, sms = sm_count();
   // CTAs of a tile: a power of two with one CTA an SM; where each still has enough to do, as many as find their SMs at once, ten at
   // most; sixteen where there are few tiles.  Two CTAs fit an SM, but a cluster's have to lie together: up to 1.6 CTAs an SM it still
@@ -1688,11 +1686,15 @@ static long plan_expert_down(ExpertParams& p) {
   return tiles * p.split;
 }
 
-static int run_expert_layer(ExpertParams p, int y_dtype, cudaStream_t st) {
+template <typename TIn>
+static int run_expert_up(const ExpertParams& p, long ctas, cudaStream_t st) {
+  return (p.K + 127) / 128 > EXPERT_PART * p.split ? launch_expert<true, TIn, true>(p, ctas, EXPERT_MAX_SMEM, st)
+                                                                  : launch_expert<true, TIn>(p, ctas, EXPERT_MAX_SMEM, st);
+}
+static int run_expert_layer(ExpertParams p, int x_dtype, int y_dtype, cudaStream_t st) {
   if (p.M > 0) {
-    const long ctas = plan_expert_up(p);
-    const bool parts = (p.K + 127) / 128 > EXPERT_PART * p.split;
-    if (int rc = parts ? launch_expert<true, float, true>(p, ctas, EXPERT_MAX_SMEM, st) : launch_expert<true, float>(p, ctas, EXPERT_MAX_SMEM, st)) return rc;
+    const long ctas = plan_expert_up(p, x_dtype);
+    if (int rc = x_dtype == STAMP_BF16 ? run_expert_up<__nv_bfloat16>(p, ctas, st) : run_expert_up<float>(p, ctas, st)) return rc;
   }
   const long ctas = plan_expert_down(p);
   // (two CTAs to an SM: with more than half of its shared memory a cluster of eight finds its SMs too late)
@@ -2447,7 +2449,6 @@ int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int3
   ExpertParams p{};
   p.x = X;
   p.ldx = ldx;
-  p.x_bf16 = x_dtype == STAMP_BF16;
   p.rows = rows;
   p.share = share;
   p.offsets = offsets;
@@ -2464,7 +2465,7 @@ int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int3
   p.h = static_cast<uint8_t*>(ws);
   p.h_scale = p.h + align256((size_t)M * F * EXPERT_H_TERMS);
   p.y = Y;
-  return run_expert_layer(p, y_dtype, static_cast<cudaStream_t>(stream));
+  return run_expert_layer(p, x_dtype, y_dtype, static_cast<cudaStream_t>(stream));
 }
 
 int stamp_debug_fp8_plan(int M, int E, int N, int K, int y_dtype, int* pair, int* rows, int* split) {
@@ -2487,9 +2488,8 @@ int stamp_debug_expert_plan(int T, int M, int E, int K, int F, int N, int x_dtyp
   if (!up_split || !down_split || T <= 0 || M <= 0 || !dtype_ok(x_dtype)) return STAMP_ERR_INVALID_ARG;
   if (int rc = check_expert_layer(T, M, E, K, F, N)) return rc;
   ExpertParams p{};
-  p.x_bf16 = x_dtype == STAMP_BF16;
   p.T = T, p.M = M, p.E = E, p.K = K, p.F = F, p.N = N;
-  plan_expert_up(p);
+  plan_expert_up(p, x_dtype);
   *up_split = p.split;
   plan_expert_down(p);
   *down_split = p.split;

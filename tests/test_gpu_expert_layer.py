@@ -241,8 +241,8 @@ def test_the_output_type_costs_its_own_rounding_only(st, T, counts, K, F, N, dty
 @pytest.mark.parametrize("E,K,F", [(1, 262144, 128), (40, 65536, 16), (8, 16, 65536)], ids=["features, a cluster", "features, one CTA", "hidden channels"])
 def test_long_sums_are_taken_in_parts(st, E, K, F):  # noqa: F811
     """The tensor cores cut a running sum off instead of rounding it: 4e-7 of a sum of 4096 features against 64 bits, as a share of
-    the norm, and more with every further feature of the same accumulator.  The errors of parts of 4096 add up like the parts
-    themselves, so that it is 4e-7 again, however long the sum.  Gates of 128 from their bias alone leave silu(g) = 128, bf16 tokens are held exactly, and fp32
+    the norm, and more with every further feature of the same accumulator.  The errors of parts add up like the parts
+    themselves, so that it is no more than 4e-7 again for parts of 4096 and fewer, however long the sum.  Gates of 128 from their bias alone leave silu(g) = 128, bf16 tokens are held exactly, and fp32
     hidden values' four terms are off by 2^-20 at most, 2^-20 / sqrt(3) as a root mean square: 6.8e-7 altogether, below 2^-20."""
     import torch
     g = torch.Generator(device="cuda").manual_seed(E + K)
@@ -257,6 +257,41 @@ def test_long_sums_are_taken_in_parts(st, E, K, F):  # noqa: F811
     exact = lambda c, s: c.double() * s.double().repeat_interleave(BLOCK, 0)[:c.shape[0]].repeat_interleave(BLOCK, 1)[:, :c.shape[1]]  # noqa: E731
     want = torch.stack([exact(down[e], down_s[e]) @ (128 * (exact(up[e], up_s[e])[F:] @ x[e].double())) for e in range(E)])
     error = float((y.double() - want).norm() / want.norm())
+    assert error <= 2.0 ** -20, error
+
+
+def test_fp32_tokens_keep_their_last_bits(st):  # noqa: F811
+    """A feature less its own first eight bits: 24 bits in five terms, so that what is left comes out to the hidden values' 2^-19."""
+    import torch
+    K, F = 256, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.zeros(40, K, device="cuda")
+    x[:, 3] = (1 + torch.rand(40, generator=g, device="cuda")) * torch.where(torch.rand(40, generator=g, device="cuda") < 0.5, 1.0, -1.0)
+    x[:, 77] = x[:, 3].bfloat16().float()
+    up = torch.zeros(1, 2 * F, K, device="cuda")
+    up[0, F:, 3], up[0, F:, 77] = 1.0, -1.0
+    up_bias = torch.zeros(1, 2 * F, device="cuda")
+    up_bias[0, :F] = 128.0                                   # silu(128) = 128
+    codes, scale = st.stamp_fp8_quantize_weights(up)
+    dc, ds = st.stamp_fp8_quantize_weights(torch.eye(F, device="cuda")[None])
+    rows, share, offsets = torch.arange(40, dtype=torch.int32, device="cuda"), torch.ones(40, device="cuda"), torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+    y = st.stamp_fp8_expert_layer(x, rows, share, offsets, codes, scale, dc, ds, up_bias=up_bias)
+    want = 128 * (x[:, 3:4].double() - x[:, 77:78].double())
+    assert bool(((y.double() - want).abs() <= 2.0 ** -18 * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T,counts,K,F,N", [(7, [2, 1, 0, 3, 2, 4, 1, 1], 4096, 1024, 512), (3, [1, 2, 3], 1024, 4096, 512), (20, [20, 7, 0, 13], 4096, 512, 264)])
+def test_fp32_outputs_are_as_near_as_a_product_in_fp32(st, T, counts, K, F, N, dtype):  # noqa: F811
+    """As a share of the norm.  Sums of 2048 features are off by 2e-7 (half of what those of 4096 are), gates and ups both count, the
+    hidden values' terms are off by 2^-20 / sqrt(3), the way down's sums by 2e-7 again: 6.5e-7 altogether, below 2^-20."""
+    import torch
+    layer = Layer(st, len(counts), K, F, N, seed=K + F)
+    rows, share, offsets = routing(counts, T, seed=T)
+    x = torch.randn(T, K, generator=torch.Generator(device="cuda").manual_seed(T), device="cuda").to(getattr(torch, dtype))
+    y = layer(st, x, rows, share, offsets, out_dtype=torch.float32).double().cpu().numpy()
+    want = layer.plain(x, rows, share, offsets, None, False, T)[0]
+    error = np.linalg.norm(y - want) / np.linalg.norm(want)
     assert error <= 2.0 ** -20, error
 
 
