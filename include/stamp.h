@@ -327,10 +327,9 @@ int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, co
  * stamp_fp8_quantize would write them for these values in fp32 -- the operand of the next product.  N is a multiple of 16; codes
  * start on a 16-byte boundary; neither codes nor scale may share memory with x, x_scale, the weights, their scales, the bias or each
  * other (STAMP_ERR_INVALID_ARG).
- *   The sum is taken in one accumulator whatever K is, like a bf16 output's; only an fp32 output of more than 4096 features is summed in
- * parts, and stamp_fp8_quantize of that one may differ.  Measured against 64 bits, as a share of the outputs' root mean square, it is off
- * by 4e-7 at 4096 features and 2.3e-6 at 14336 (activations with outliers, quantized by stamp_fp8_quantize), by 2.3e-6 and 1.6e-5 where
- * scales lie anywhere from 2^-7 to 2^2, block by block.  The activation adds 2^-21 of the value (SILU), 2^-20 (GELU) or (5 |2 u| + 18)
+ *   They are the values that stamp_fp8_linear_fused gives as fp32, bit for bit: sums of more than 4096 features in parts.  Measured
+ * against 64 bits, as a share of the outputs' root mean square, sums are off by 4.4e-7 (activations with outliers, quantized by
+ * stamp_fp8_quantize), by 3.3e-6 where scales lie anywhere from 2^-7 to 2^2, block by block.  The activation adds 2^-21 of the value (SILU), 2^-20 (GELU) or (5 |2 u| + 18)
  * 2^-24 (GELU_TANH, u the tanh's argument).  A code differs from that of the exact value only where this lies that near a rounding
  * boundary; a block's scale (then twice the other, its codes half) only where the block's largest magnitude lies that near 448
  * times a power of two. */

@@ -339,13 +339,18 @@ __device__ __forceinline__ void fp8_load_column(const T* p, long ld, int left, u
 // stream of such calls all of these are at that limit, 985 W, at 1.1 to 1.7 GHz.
 // Tried: a long fp32 sum's parts added up in 128 registers a thread (960 for 966, but 84 for 76 where rows are
 // not aligned: spills); tiles of 224 columns, whose accumulators share none (no difference).
-template <bool PAIR, typename TOut, bool FUSED = false, int GROUPS = 2>
+//
+// PARTS (codes): a sum of more than one accumulator's.  The fp32 form adds its parts up in the output; codes have no room for them, so a
+// thread keeps its own, up to 128 of them, in local memory (128 KB of a CTA, which stay in L2) and quantizes with the last.  2048 x 11008 x
+// 4096 102 us, in one accumulator 92; 16384 x 14336 x 4096 833 and 684 (fp32 output 927).
+template <bool PAIR, typename TOut, bool FUSED = false, int GROUPS = 2, bool PARTS = false>
 __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
     k_fp8_gemm(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
                const __grid_constant__ CUtensorMap tmap_x_tail, Fp8GemmParams p) {
   using SM = Fp8Smem<PAIR>;
   constexpr int BN = SM::BN;
   static_assert(GROUPS == 2 || (FUSED && GROUPS == FP8G_MOST_GROUPS), "groups of epilogue warps");
+  static_assert(!PARTS || (FUSED && sizeof(TOut) == 1 && GROUPS == 2), "parts kept by the thread: of codes");
   constexpr int THREADS = 128 + 128 * GROUPS, EPI_WARPS = THREADS / 32 - 4;
   extern __shared__ uint8_t fp8g_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(fp8g_raw) + 1023) & ~uintptr_t(1023));
@@ -669,6 +674,8 @@ __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
         for (int ch = first; ch < end; ch += 128 / size) ptx::prefetch_l2(at + (static_cast<long>(r) * p.ldr + ch) * size);
     };
     prefetch_residual(tile0);
+    constexpr bool SUMMED = sizeof(TOut) == 4 || PARTS;   // of several accumulators, if need be
+    float carried[PARTS ? BN / 32 / G : 1][32];           // PARTS: this thread's sums of the parts before, by chunk
     uint32_t exchanged = 0;   // maxima that this group has exchanged
     int it = 0;
     bool ok = true;
@@ -688,8 +695,7 @@ __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
       }
       for (int c0 = step0; c0 < step1; c0 += p.chunk, ++it) {
         const int a = it & 1;
-        // (an fp32 output may be summed in parts, the others never are)
-        const bool first = sizeof(TOut) != 4 || c0 == step0, last = sizeof(TOut) != 4 || c0 + p.chunk >= step1;
+        const bool first = !SUMMED || c0 == step0, last = !SUMMED || c0 + p.chunk >= step1;
         // The bias goes in with the first part, the activation follows the last; without one the residual goes in with the
         // first part too: the output, which holds the parts, may be the residual's own memory.
         const bool whole = PAIR || p.split == 1;
@@ -790,10 +796,22 @@ __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
                   for (int j = 0; j < W; ++j) v[j] += __uint_as_float(old[j]);
                 }
               }
+              if constexpr (PARTS) {
+                float (&kept)[32] = carried[chunk_at(n) / G];
+                if (!first) {
+#pragma unroll
+                  for (int j = 0; j < W; ++j) v[j] += kept[j];
+                }
+                if (!last) {
+#pragma unroll
+                  for (int j = 0; j < W; ++j) kept[j] = first ? v[j] + bias[0] : v[j];
+                  continue;
+                }
+              }
 #pragma unroll
               for (int j = 0; j < W; j += 2) {
                 float2 x = make_float2(v[j], v[j + 1]);
-                if (sizeof(TOut) != 4 || first) x = __fadd2_rn(x, make_float2(bias[0], bias[0]));
+                if (!SUMMED || first) x = __fadd2_rn(x, make_float2(bias[0], bias[0]));
                 x = fp8_activate2<decltype(variant)::value>(x, floor);
                 v[j] = x.x;
                 v[j + 1] = x.y;
@@ -891,13 +909,25 @@ __global__ void __launch_bounds__(128 + 128 * GROUPS, 1)
             if constexpr (sizeof(TOut) == 4) {
               if (!first) fp8_add_tokens<KU>(before, false, v);
             }
+            if constexpr (PARTS) {
+              float (&kept)[32] = carried[chunk_at(n) / G];
+              if (!first) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j >> 3][j & 7] += kept[j];
+              }
+              if (!last) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) kept[j] = first ? v[j >> 3][j & 7] + bias[j >> 3] : v[j >> 3][j & 7];
+                continue;
+              }
+            }
             // (a part that is not the first has its bias already, one that is not the last gets no activation: LINEAR, floor -inf)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
               for (int j = 0; j < 2 * KU; j += 2) {
                 float2 r = make_float2(v[k][j], v[k][j + 1]);
-                if (sizeof(TOut) != 4 || first) r = __fadd2_rn(r, make_float2(bias[k], bias[k]));
+                if (!SUMMED || first) r = __fadd2_rn(r, make_float2(bias[k], bias[k]));
                 r = fp8_activate2<decltype(variant)::value>(r, floor);
                 v[k][j] = r.x;
                 v[k][j + 1] = r.y;

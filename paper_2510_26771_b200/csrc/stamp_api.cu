@@ -1365,10 +1365,10 @@ static int launch_fp8_gated_quant(const void* X, long ld, int M, int F, void* co
   return STAMP_OK;
 }
 
-template <bool PAIR, typename TOut, bool FUSED = false, int GROUPS = 2>
+template <bool PAIR, typename TOut, bool FUSED = false, int GROUPS = 2, bool PARTS = false>
 static int launch_fp8_gemm(const CUtensorMap& tw, const CUtensorMap& tx, const CUtensorMap& txt, const Fp8GemmParams& p, long tiles,
                            cudaStream_t st) {
-  auto kern = k_fp8_gemm<PAIR, TOut, FUSED, GROUPS>;
+  auto kern = k_fp8_gemm<PAIR, TOut, FUSED, GROUPS, PARTS>;
   constexpr int bytes = FUSED ? Fp8Smem<PAIR>::FUSED_DYN_BYTES : Fp8Smem<PAIR>::DYN_BYTES;
   if (int rc = ensure_dyn_smem(reinterpret_cast<const void*>(kern), bytes)) return rc;
   const int per_tile = PAIR ? 2 : p.split;
@@ -1452,16 +1452,15 @@ static Fp8Plan plan_fp8_gemm(const Fp8GemmParams& p, int most) {
 // (activations with outliers; with scales from 2^-7 to 2^2 per block 2.3e-6 and 1.6e-5, where an fp32 product has 9.1e-6).  An
 // fp32 output is summed in chunks of 4096 features at most, the chunks added in fp32: 4.4e-7 and 3.3e-6 at 14336.  What the
 // chunks cost, in us (chunks of 2048 / 4096 / 8192 / none): 16384 x 14336 x 4096 908 / 803 / 742 / 735, 1024 x 4224 x 4096
-// 32 / 28 / 24 / 24.  A bf16 output is summed in one: its own rounding is 1.7e-3, and of 16384 x 14336 x 4096 outputs 0.09 %
+// 32 / 28 / 24 / 24.  Codes are those of the fp32 output and summed alike.  A bf16 output is summed in one: its own rounding is 1.7e-3, and of 16384 x 14336 x 4096 outputs 0.09 %
 // are the other neighbour of a value that lies within 2e-5 (of the outputs' root mean square) of the halfway point; the distance
 // from 64 bits, 1.65818e-3, is that of an fp32 product rounded to bf16, to six digits.
 constexpr int FP8_PART = 4096;
+constexpr int FP8_OUT_CODES = -1;   // output type of the quantized form, beside the public ones: summed like an fp32 output
 static int fp8_chunk(int ks, int y_dtype) {
   const int steps = (ks + 3) / 4;
-  return y_dtype == STAMP_F32 && steps > FP8_PART / 512 ? FP8_PART / 512 : steps;
+  return y_dtype != STAMP_BF16 && steps > FP8_PART / 512 ? FP8_PART / 512 : steps;
 }
-
-constexpr int FP8_OUT_CODES = -1;   // output type of the quantized form, beside the public ones
 
 template <bool FUSED = false>
 static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
@@ -1493,10 +1492,13 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
     // Codes of a short sum take longer to drain than to sum where every output goes through the special function unit: twice the
     // epilogue warps then, which take issue slots and start later elsewhere.  8192 rows, 4608 channels, us, 8 / 16 warps: gelu_tanh
     // at 512 features 50.9 / 45.5, at 1152 55.4 / 51.0, at 2048 67.0 / 67.1, at 3200 93.8 / 95.5; no activation at 1152 50.5 / 53.1.
-    if (y_dtype == FP8_OUT_CODES)
+    if (y_dtype == FP8_OUT_CODES) {
+      if ((p.ks + 3) / 4 > p.chunk && p.split == 1)
+        return pair ? launch_fp8_gemm<true, uint8_t, true, 2, true>(tw, tx, txt, p, tiles, st) : launch_fp8_gemm<false, uint8_t, true, 2, true>(tw, tx, txt, p, tiles, st);
       return !pair                                   ? launch_fp8_gemm<false, uint8_t, true>(tw, tx, txt, p, tiles, st)
              : p.ks <= 12 && p.act >= STAMP_ACT_GELU ? launch_fp8_gemm<true, uint8_t, true, FP8G_MOST_GROUPS>(tw, tx, txt, p, tiles, st)
                                                      : launch_fp8_gemm<true, uint8_t, true>(tw, tx, txt, p, tiles, st);
+    }
     if (pair)
       return y_dtype == STAMP_BF16 ? launch_fp8_gemm<true, __nv_bfloat16, true>(tw, tx, txt, p, tiles, st)
                                    : launch_fp8_gemm<true, float, true>(tw, tx, txt, p, tiles, st);
