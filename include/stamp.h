@@ -327,12 +327,12 @@ int stamp_fp8_linear_fused(const void* x, const void* x_scale, const void* w, co
  * stamp_fp8_quantize would write them for these values in fp32 -- the operand of the next product.  N is a multiple of 16; codes
  * start on a 16-byte boundary; neither codes nor scale may share memory with x, x_scale, the weights, their scales, the bias or each
  * other (STAMP_ERR_INVALID_ARG).
- *   They are the values that stamp_fp8_linear_fused gives as fp32, bit for bit: sums of more than 4096 features in parts.  Measured
+ *   These are the values that stamp_fp8_linear_fused gives as fp32, bit for bit: sums of more than 4096 features in parts.  Measured
  * against 64 bits, as a share of the outputs' root mean square, sums are off by 4.4e-7 (activations with outliers, quantized by
- * stamp_fp8_quantize), by 3.3e-6 where scales lie anywhere from 2^-7 to 2^2, block by block.  The activation adds 2^-21 of the value (SILU), 2^-20 (GELU) or (5 |2 u| + 18)
- * 2^-24 (GELU_TANH, u the tanh's argument).  A code differs from that of the exact value only where this lies that near a rounding
- * boundary; a block's scale (then twice the other, its codes half) only where the block's largest magnitude lies that near 448
- * times a power of two. */
+ * stamp_fp8_quantize), by 3.3e-6 where scales lie anywhere from 2^-7 to 2^2, block by block.  The activation adds 2^-21 of the value
+ * (SILU), 2^-20 (GELU) or (5 |2 u| + 18) 2^-24 (GELU_TANH, u the tanh's argument).  A code differs from that of the exact value
+ * only where this lies that near a rounding boundary; a block's scale (then twice the other, its codes half) only where the
+ * block's largest magnitude lies that near 448 times a power of two. */
 int stamp_fp8_linear_quantized(const void* x, const void* x_scale, const void* w, const void* w_scale, const float* bias, int activation,
                                int M, int N, int K, void* codes, void* scale, void* stream);
 
@@ -380,9 +380,9 @@ int stamp_expert_combine(const void* y, int y_dtype, const int32_t* place, const
  *   ws       stamp_fp8_expert_workspace_bytes() bytes, 256-byte aligned
  *            Y may be over X; it may not overlap rows, share, offsets, the way down's weights, scales and bias or ws, and ws nothing
  *            at all (STAMP_ERR_INVALID_ARG).
- * Tokens and hidden values go into the 8-bit product as sums of e4m3 numbers: bf16 tokens to their 8 significant bits or 2^-21 of
- * the largest of their block of 128 features, whichever is more; fp32 tokens to 2^-24 of the value or 2^-36 of the largest; hidden values to 2^-19
- * or 2^-31, for either output type.  Sums of more than 2048 features are taken in parts of 2048 at most.
+ * Tokens and hidden values go into the 8-bit product as sums of e4m3 numbers: bf16 tokens to their 8 significant bits or 2^-21
+ * of the largest of their block of 128 features, whichever is more; fp32 tokens to 2^-24 of the value or 2^-36 of the largest;
+ * hidden values to 2^-19 or 2^-31, for either output type.  Sums of more than 2048 features are taken in parts of 2048 at most.
  * T <= 64, M <= 2048, E <= 1024, K and F multiples of 16.  A token that holds an infinity or a NaN gets NaN. */
 int stamp_fp8_expert_workspace_bytes(int M, int F, size_t* out_bytes);
 int stamp_fp8_expert_layer(const void* X, int x_dtype, long long ldx, const int32_t* rows, const float* share, const int32_t* offsets,

@@ -37,14 +37,15 @@
 // copies of the hidden values and their scales wait.
 //
 // What bounds it.  Many experts: the weights' way from memory.  64 tokens, eight of 64 experts of 2048 x 2048: 805 MB, 125 us at the
-// copy rate, in 150 (UP 5.3 TB/s, issue slots 42 % busy with the terms; DOWN's 128 CTAs leave 20 SMs without one); 13 tokens, four
-// of 32 experts of 4096 x 4096: 149 us, 202 at the copy rate if as many experts get rows as random choices reach -- reads alone go
-// faster than the copy that the rate is from.  Few tiles: one chain of launch, first copies, terms, sums, exchange, hidden values,
-// sums, exchange.  One token, four experts of 1152 x 2048: 28 MB, 4.4 us at the copy rate, in 15 to 16, where the two kernels alone
-// and cold take 11 and 13.
-// Measured and not kept, us for what is kept: tiles of 64 gates (171 for 150; one token 18.3 for 16); runs of 32 rows in UP (158 for
+// copy rate, in 143 (fp32 tokens 157: 8 rows a run, five terms each; UP 5.6 TB/s cold); 13 tokens, four of 32 experts of 4096 x 4096: 189 us
+// where random choices reach some 26 of them (1.3 GB, 206 at the copy rate: reads alone go faster than the copy that the rate is from).  Few tiles:
+// one chain of launch, first copies, terms, sums, exchange, hidden values, sums, exchange.  One token, four experts of 1152 x 2048: 28 MB,
+// 4.4 us at the copy rate, in 16.4, where the two kernels alone and cold take 13 and 14.  Many rows for each of few experts: UP's runs, 55 tokens to
+// all of 8 experts of 896 x 3456 64 us where the weights alone would take 11.6.
+// Measured and not kept, us for what was kept then: tiles of 64 gates (171 for 150; one token 18.3 for 16); runs of 32 rows in UP (158 for
 // 152); one CTA an SM with 200 KB in DOWN (160 for 147: clusters of eight find their SMs late); two CTAs an SM in UP, one tile each
-// (187 for 150); hidden values in fp32, made into terms by DOWN (294 for 150).
+// (187 for 150); hidden values in fp32, made into terms by DOWN (294 for 150); one kernel for both token types, which counts its terms as it
+// runs (146 for 143; one token 16.9 for 16.4).
 #pragma once
 #include "common.cuh"
 #include "k_fp8_gemm.cuh"

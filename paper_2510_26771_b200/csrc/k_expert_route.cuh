@@ -237,10 +237,11 @@ __device__ __forceinline__ void route_store(const RouteParams& p, const int* bas
 
 // A warp takes one token after the other, the next one's logits on their way, a lane PER neighbouring experts: it sorts them
 // once, then the lanes' first entries are compared `top` times, and the lane that had the best one moves up.  (Searching all
-// entries every time took three times the instructions, which is what bounds it: 16384 tokens of 256 bf16 logits, top 8, both
-// launches 16.3 us where 8.4 MB have to be read, 1.7 us; fp32 logits, whose entries take two words, 20.1 us.)  Up to eight
+// entries every time took three times the instructions.  16384 tokens of 256 bf16 logits, top 8, both launches 16.3 us where 8.4 MB
+// have to be read, 1.7 us: 390 instructions a token, eight of them warp-wide maxima that wait for one another with eight warps a scheduler to
+// fill in, then the second launch; fp32 logits, whose entries take two words, 20.1 us.)  Up to eight
 // choices are unrolled, so that only entries that can still be chosen move.  Above 256 experts (PER = 32, expert 32 i + lane in
-// register i) sorting costs more than searching.
+// register i) sorting costs more than searching; that form spills, and takes 79 us for 16384 tokens of 384 experts, 107 of 1024.
 // Each warp counts its rows by expert in shared memory, and a row's rank is the count so far; the warps' counts are then
 // summed in their order.
 template <typename TIn, int PER>

@@ -331,12 +331,12 @@ __device__ __forceinline__ void fp8_load_column(const T* p, long ld, int left, u
 // a lane a channel, outputs one by one, 32 lanes side by side (1797 x 2688 x 4463 in fp32 with a residual 67 us with the words'
 // order and shape, whose four channels are then four stores 16 bytes apart).
 //
-// Device times, in us, in brackets the plain product's to bf16 or fp32 on the same box: 1 x 4096 x 11008 with bias and silu 11.0
-// (10.2); 8192 x 4608 x 1152 with bias and a bf16 residual 42.7 (39.6), the residual's way from memory; 8192 x 1152 x 4608 with
-// bias and gelu_tanh to codes 51 (41.3): a tile's nine steps of 128 features are summed before its 256 columns are drained, 23
-// warp instructions for 32 outputs, two values of the special function unit each, issue slots 38 % busy; 2048 x 4096 x 11008 with
-// silu to codes 73 (70); 16384 x 14336 x 4096 in fp32 with a residual 966 to 990 (930), 870 before the power limit sets in.  In a
-// stream of such calls all of these are at that limit, 985 W, at 1.1 to 1.7 GHz.
+// Device times, in us, in brackets the plain product's to bf16 or fp32 on the same box: 1 x 4096 x 11008 with bias and silu 11.3
+// (10.6), 64 rows 12.2 (11.5), 128 rows 14.5 (13.0); 8192 x 4608 x 1152 with bias and a bf16 residual 42.7 (39.6), the residual's way from memory;
+// 8192 x 1152 x 4608 with bias and gelu_tanh to codes 51 (41.3): a tile's nine steps of 128 features are summed before its 256 columns
+// are drained, 21 warp instructions for 32 outputs in all, two values of the special function unit each, issue slots 46 % busy;
+// 2048 x 4096 x 11008 with silu to codes 71 (69); 16384 x 14336 x 4096 in fp32 with a residual 966 to 990 (930), 870 before the power
+// limit sets in.  In a stream of such calls all of the large ones are at that limit, 985 W, at 1.1 to 1.7 GHz.
 // Tried: a long fp32 sum's parts added up in 128 registers a thread (960 for 966, but 84 for 76 where rows are
 // not aligned: spills); tiles of 224 columns, whose accumulators share none (no difference).
 //

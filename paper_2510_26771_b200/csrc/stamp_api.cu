@@ -1490,8 +1490,10 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
     if (p.N >= 32)
       if (int rc = make_tmap_by_fours(p.w, p.N, p.K, &tw)) return rc;
     // Codes of a short sum take longer to drain than to sum where every output goes through the special function unit: twice the
-    // epilogue warps then, which take issue slots and start later elsewhere.  8192 rows, 4608 channels, us, 8 / 16 warps: gelu_tanh
-    // at 512 features 50.9 / 45.5, at 1152 55.4 / 51.0, at 2048 67.0 / 67.1, at 3200 93.8 / 95.5; no activation at 1152 50.5 / 53.1.
+    // epilogue warps then, which take issue slots and start later elsewhere.  Us with 8 / 16 warps: 8192 rows, 4608 channels, gelu_tanh at 512
+    // features 49.1 / 45.7, at 1152 53.9 / 50.8, at 1536 60.1 / 58.2, at 2048 65.2 / 64.7; silu 49.9 / 47.6, 55.0 / 52.6, 60.2 / 58.7, 66.3 / 67.4; no activation
+    // 35.2 / 35.8, 41.9 / 43.0, 47.2 / 49.1, 58.8 / 61.1.  2048 rows, 11008 channels, gelu_tanh 32.6 / 31.3, 36.8 / 35.6, 36.7 / 36.5, 41.4 / 41.7; 16384 rows,
+    // 2048 channels 44.5 / 41.3, 48.4 / 45.8, 53.7 / 50.4, 59.9 / 58.4; 1024 rows, 4096 channels, one tile for a pair at most, at 1536 13.6 / 13.9.
     if (y_dtype == FP8_OUT_CODES) {
       if ((p.ks + 3) / 4 > p.chunk && p.split == 1)
         return pair ? launch_fp8_gemm<true, uint8_t, true, 2, true>(tw, tx, txt, p, tiles, st) : launch_fp8_gemm<false, uint8_t, true, 2, true>(tw, tx, txt, p, tiles, st);

@@ -193,7 +193,7 @@ def test_long_quantized_sums_are_as_near_as_stated(st, M, N, K, spread, error): 
 # one CTA, a split sum, single CTAs of 128 rows, pairs; last parts of 16, 128, 512 and 4096 features; last blocks of 16 and 64 channels
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
 @pytest.mark.parametrize("M,K,N", [(1, 4096, 144), (1, 14336, 256), (9, 4112, 4112), (40, 11008, 1040), (140, 4224, 528), (300, 4608, 12288), (513, 8192, 4160),
-                                   (777, 4112, 4112), (1024, 14336, 2048), (2048, 4608, 4096), (700, 8704, 272)])
+                                   (777, 4112, 4112), (1024, 14336, 2048), (2048, 4608, 4096), (700, 8704, 272), (64, 512, 640), (1700, 1152, 4608), (2300, 2048, 4112)])
 def test_quantized_outputs_are_those_of_the_fp32_product(st, M, K, N, act):  # noqa: F811
     """The quantizer's codes and scales of stamp_fp8_linear_fused's fp32 outputs, however long the sum, bit for bit."""
     import torch
