@@ -99,8 +99,10 @@ struct ExpertSmem {
   static constexpr int COLUMNS = (TERMS * ROWS + 15) / 16 * 16;   // of one sum
   static constexpr int ACC = UP ? 2 * COLUMNS : COLUMNS;   // tensor memory: two accumulators (UP: gates, ups), then the stages' scales
   static constexpr int SF_BYTES = UP ? 1536 : 1024;     // scale words of a stage: channels (UP: twice), then rows
-  static constexpr int SF_COLS = SF_BYTES / 128, SF_COL = 2 * ACC, TMEM = SF_COL + EXPERT_MAX_STAGES * SF_COLS <= 256 ? 256 : 512;
-  static_assert(SF_COL + EXPERT_MAX_STAGES * SF_COLS <= TMEM && TMEM * CTAS <= 512, "tensor memory of an SM");
+  static constexpr int SF_COLS = SF_BYTES / 128, SF_COL = 2 * ACC;
+  // Half of an SM's columns for every CTA, so that UP and DOWN, which waits for it, never wait for one another's.
+  static constexpr int TMEM = 256, MAX_STAGES = UP && sizeof(T) == 4 ? 5 : EXPERT_MAX_STAGES;
+  static_assert(SF_COL + MAX_STAGES * SF_COLS <= TMEM, "tensor memory of a CTA");
   static constexpr int BARS = 2 * EXPERT_MAX_STAGES + 6;
   // after the ring and the scale words: barriers, [tmem, abort, runs, -], run table, UP: hidden values, tokens [M], sums of the parts
   // before (PARTS) [row][gates, ups], DOWN: sums [T][128]

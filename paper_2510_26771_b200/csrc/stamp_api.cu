@@ -1611,7 +1611,7 @@ static int launch_expert(ExpertParams p, long ctas, int smem, cudaStream_t st) {
   const int fixed = SM::fixed(expert_max_runs(p.M, p.E, p.cap), p.T, p.M, PARTS);
   p.stage_bytes = (UP ? 2 : 1) * EXPERT_W_BYTES + (SM::TERMS * p.cap + 15) / 16 * 16 * 128;
   p.stages = (smem - fixed) / (p.stage_bytes + SM::SF_BYTES);
-  if (p.stages > EXPERT_MAX_STAGES) p.stages = EXPERT_MAX_STAGES;
+  if (p.stages > SM::MAX_STAGES) p.stages = SM::MAX_STAGES;
   CUtensorMap tm, th;
   if (int rc = UP ? make_tmap_i8(p.w_up, (long)p.E * 2 * p.F, p.K, 128, &tm) : make_tmap_i8(p.w_down, (long)p.E * p.N, p.F, 128, &tm)) return rc;
   th = tm;

@@ -226,6 +226,13 @@ def test_integers_come_out_exact_in_several_parts(st, T, counts, K, F, N):  # no
     test_integers_come_out_exact(st, T, counts, K, F, N)
 
 
+@pytest.mark.parametrize("T,counts,K,F,N,down", [(16, [1] * 32, 272, 640, 1664, 10), (20, [1, 0, 4, 2] * 16, 144, 784, 2560, 10), (9, [2, 1, 3] * 12, 128, 656, 3200, 9),
+                                                 (13, [1] * 40, 128, 528, 3584, 8), (40, [40, 9, 33, 17] * 3, 128, 1296, 1536, 16)])
+def test_integers_come_out_exact_in_clusters_of_every_size(st, T, counts, K, F, N, down):  # noqa: F811
+    assert st.stamp_debug_expert_plan(T, sum(counts), len(counts), K, F, N)[1] == down
+    test_integers_come_out_exact(st, T, counts, K, F, N)
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 @pytest.mark.parametrize("T,counts,K,F,N", [(1, [1, 0, 1], 1152, 2048, 1152), (13, [2, 0, 13, 1, 0, 5], 400, 272, 257), (64, [64, 33, 1, 16], 512, 640, 520)])
 def test_the_output_type_costs_its_own_rounding_only(st, T, counts, K, F, N, dtype):  # noqa: F811
