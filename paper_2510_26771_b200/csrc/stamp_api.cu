@@ -1489,11 +1489,12 @@ static int run_fp8_gemm(Fp8GemmParams p, int y_dtype, cudaStream_t st) {
     txt = tw;
     if (p.N >= 32)
       if (int rc = make_tmap_by_fours(p.w, p.N, p.K, &tw)) return rc;
-    // Codes of a short sum take longer to drain than to sum where every output goes through the special function unit: twice the
-    // epilogue warps then, which take issue slots and start later elsewhere.  Us with 8 / 16 warps: 8192 rows, 4608 channels, gelu_tanh at 512
-    // features 49.1 / 45.7, at 1152 53.9 / 50.8, at 1536 60.1 / 58.2, at 2048 65.2 / 64.7; silu 49.9 / 47.6, 55.0 / 52.6, 60.2 / 58.7, 66.3 / 67.4; no activation
-    // 35.2 / 35.8, 41.9 / 43.0, 47.2 / 49.1, 58.8 / 61.1.  2048 rows, 11008 channels, gelu_tanh 32.6 / 31.3, 36.8 / 35.6, 36.7 / 36.5, 41.4 / 41.7; 16384 rows,
-    // 2048 channels 44.5 / 41.3, 48.4 / 45.8, 53.7 / 50.4, 59.9 / 58.4; 1024 rows, 4096 channels, one tile for a pair at most, at 1536 13.6 / 13.9.
+    // Codes of a short sum take longer to drain than to sum where every output goes through the special function unit: twice
+    // the epilogue warps then, which take issue slots and start later elsewhere. Us with 8 / 16 warps: 8192 rows, 4608
+    // channels, gelu_tanh at 512 features 49.1 / 45.7, at 1152 53.9 / 50.8, at 1536 60.1 / 58.2, at 2048 65.2 / 64.7; silu 49.9
+    // / 47.6, 55.0 / 52.6, 60.2 / 58.7, 66.3 / 67.4; no activation 35.2 / 35.8, 41.9 / 43.0, 47.2 / 49.1, 58.8 / 61.1. 2048
+    // rows, 11008 channels, gelu_tanh 32.6 / 31.3, 36.8 / 35.6, 36.7 / 36.5, 41.4 / 41.7; 16384 rows, 2048 channels 44.5 /
+    // 41.3, 48.4 / 45.8, 53.7 / 50.4, 59.9 / 58.4; 1024 rows, 4096 channels, one tile for a pair at most, at 1536 13.6 / 13.9.
     if (y_dtype == FP8_OUT_CODES) {
       if ((p.ks + 3) / 4 > p.chunk && p.split == 1)
         return pair ? launch_fp8_gemm<true, uint8_t, true, 2, true>(tw, tx, txt, p, tiles, st) : launch_fp8_gemm<false, uint8_t, true, 2, true>(tw, tx, txt, p, tiles, st);
@@ -1655,13 +1656,13 @@ static long plan_expert_up(ExpertParams& p, int x_dtype) {
   p.cap = expert_cap(p, x_dtype == STAMP_BF16 ? ExpertSmem<true, __nv_bfloat16>::ROWS : ExpertSmem<true, float>::ROWS);
   const long tiles = (p.F + 127L) / 128, all = tiles * expert_runs(p), most = tiles * expert_max_runs(p.M, p.E, p.cap), sms = sm_count();
   const int blocks = (p.K + 127) / 128;
-  // One CTA a tile, each SM one after the other, unless there are few tiles (of a run each); then four or eight share one, where
-  // each has features enough to make up for the exchange and the clusters find their SMs at once.  One token, in us, with 1 / 2 / 4 / 8
-  // (the choice in brackets): 4 tiles of 1024 features 11.8 / 12.2 / 11.8 / (11.6), 8 of 2048 14.3 / 13.9 / 13.0 / (12.6), 16
-  // of 4096 19.2 / 23.6 / (18.5) / 24.2, 32 of 4096 27.7 / 23.6 / (21.5) / 34.2, 64 of 1152 (16.0) / 19.0 / 25.3 / 43.2.  Many rows for
-  // each expert, the whole layer, with 1 / 4 / 8: 64 tokens to all of 8 experts of 4096 x 512, 128 tiles (57.2) / 89.8 / 136, fp32, 256
-  // tiles (66.4) / 131 / 216; of 2048 x 256, 64 tiles (34.4) / 43.1 / 66.8; to one of 4096 x 1024, 32 tiles 41.5 / (31.0) / 46.1; to both
-  // of two of 4096 x 128, 8 tiles 36.7 / 24.4 / (21.7).
+  // One CTA a tile, each SM one after the other, unless there are few tiles (of a run each); then four or eight share one,
+  // where each has features enough to make up for the exchange and the clusters find their SMs at once. One token, in us, with
+  // 1 / 2 / 4 / 8 (the choice in brackets): 4 tiles of 1024 features 11.8 / 12.2 / 11.8 / (11.6), 8 of 2048 14.3 / 13.9 / 13.0
+  // / (12.6), 16 of 4096 19.2 / 23.6 / (18.5) / 24.2, 32 of 4096 27.7 / 23.6 / (21.5) / 34.2, 64 of 1152 (16.0) / 19.0 / 25.3 /
+  // 43.2. Many rows for each expert, the whole layer, with 1 / 4 / 8: 64 tokens to all of 8 experts of 4096 x 512, 128 tiles
+  // (57.2) / 89.8 / 136, fp32, 256 tiles (66.4) / 131 / 216; of 2048 x 256, 64 tiles (34.4) / 43.1 / 66.8; to one of 4096 x
+  // 1024, 32 tiles 41.5 / (31.0) / 46.1; to both of two of 4096 x 128, 8 tiles 36.7 / 24.4 / (21.7).
   p.split = all <= 8 && blocks >= 8 ? 8 : all <= 32 && blocks >= 16 ? 4 : 1;
   return p.split > 1 ? most * p.split : most < sms ? most : sms;
 }
@@ -1670,17 +1671,19 @@ static long plan_expert_up(ExpertParams& p, int x_dtype) {
 static long plan_expert_down(ExpertParams& p) {
   p.cap = expert_cap(p, ExpertSmem<false, float>::ROWS);
   const long tiles = (p.N + 127L) / 128, sms = sm_count();
-  // CTAs of a tile: a power of two with one CTA an SM; where each still has enough to do, as many as find their SMs at once, ten at
-  // most; sixteen where there are few tiles.  Two CTAs fit an SM, but a cluster's have to lie together: up to 1.6 CTAs an SM it still
-  // pays to add one (236 on 148 SMs), from 240 on clusters wait for others.  Layers of 13 tokens over 32 experts of 4096 hidden channels / 24
-  // over 60 of 656 / 64 over 64 of 2048, in us, by CTAs of a tile: 118 tiles, one 288.2 / 170.2 / 518.6, two (236) 240.8 / 121.2 / 350.4; 33 tiles, six 113.3 / 46.9 / 140.0, seven (231) 112.1 / 45.0 / 139.8,
-  // eight (264) 137.9 / 50.6 / 172.0; 32 tiles, six 119.6 / 50.3 / 139.2, seven (224) 118.4 / 48.4 / 138.7, eight (256) 123.4 / 50.3 / 153.6; 29
-  // tiles, seven 102.3 / 46.3 / 130.4, eight (232) 100.6 / 46.0 / 130.4, nine (261) 105.4 / 46.1 / 151.0; 24 tiles, eight 86.9 / 43.0 / 124.7, nine
-  // (216) 86.6 / 42.0 / 121.7, ten (240) 88.5 / 42.9 / 135.4; 16 tiles, eight 78.1 / 39.4 / 109.9, ten (160) 74.9 / 37.5 / 102.6.  Clusters of eleven
-  // and more find their SMs at some numbers of tiles and not at others (16 tiles, twelve 74.7 / 36.7 / 100.7, thirteen 76.2 / 36.4 / 114.8, fourteen 93.7 /
-  // 50.6 / 128.6); sixteen up to twelve tiles: 12 tiles, ten 75.6 / 38.5 / 99.9, sixteen 72.8 / 36.5 / 90.9.  Enough to do are sixteen steps for
-  // each (twelve for each of sixteen): with fewer, one token over four of 16 experts of 2048, 28 tiles, (four 19.3), five 18.8, eight 19.8; 9 tiles, four 17.8, (eight
-  // 16.6), sixteen 17.0.
+  // CTAs of a tile: a power of two with one CTA an SM; where each still has enough to do, as many as find their SMs at once,
+  // ten at most; sixteen where there are few tiles. Two CTAs fit an SM, but a cluster's have to lie together: up to 1.6 CTAs an
+  // SM it still pays to add one (236 on 148 SMs), from 240 on clusters wait for others. Layers of 13 tokens over 32 experts of
+  // 4096 hidden channels / 24 over 60 of 656 / 64 over 64 of 2048, in us, by CTAs of a tile: 118 tiles, one 288.2 / 170.2 /
+  // 518.6, two (236) 240.8 / 121.2 / 350.4; 33 tiles, six 113.3 / 46.9 / 140.0, seven (231) 112.1 / 45.0 / 139.8, eight (264)
+  // 137.9 / 50.6 / 172.0; 32 tiles, six 119.6 / 50.3 / 139.2, seven (224) 118.4 / 48.4 / 138.7, eight (256) 123.4 / 50.3 /
+  // 153.6; 29 tiles, seven 102.3 / 46.3 / 130.4, eight (232) 100.6 / 46.0 / 130.4, nine (261) 105.4 / 46.1 / 151.0; 24 tiles,
+  // eight 86.9 / 43.0 / 124.7, nine (216) 86.6 / 42.0 / 121.7, ten (240) 88.5 / 42.9 / 135.4; 16 tiles, eight 78.1 / 39.4 /
+  // 109.9, ten (160) 74.9 / 37.5 / 102.6. Clusters of eleven and more find their SMs at some numbers of tiles and not at others
+  // (16 tiles, twelve 74.7 / 36.7 / 100.7, thirteen 76.2 / 36.4 / 114.8, fourteen 93.7 / 50.6 / 128.6); sixteen up to twelve
+  // tiles: 12 tiles, ten 75.6 / 38.5 / 99.9, sixteen 72.8 / 36.5 / 90.9. Enough to do are sixteen steps for each (twelve for
+  // each of sixteen): with fewer, one token over four of 16 experts of 2048, 28 tiles, (four 19.3), five 18.8, eight 19.8; 9
+  // tiles, four 17.8, (eight 16.6), sixteen 17.0.
   const long steps = expert_runs(p) * ((p.F + 127) / 128);   // (run, 128 features) of a tile, about
   p.split = 1;
   while (p.split < 8 && tiles * p.split * 2 <= sms) p.split *= 2;
